@@ -54,6 +54,9 @@ typedef enum {
 
 typedef enum { GMB_F32 = 0, GMB_BF16 = 1 } gmb_dtype;
 
+/* Microscaled formats, by the bits of an element. */
+typedef enum { GMB_MXFP4 = 4, GMB_MXFP8 = 8 } gmb_mx_format;
+
 /* Bits of the device status word. */
 #define GMB_STATUS_ERANGE 1u
 #define GMB_STATUS_EDUP 2u
@@ -418,6 +421,182 @@ int gmb_sgd_update(const gmb_sage_weights* weights, const gmb_sage_grads* grads,
  * caller-owned, updated in place on `stream`. */
 int gmb_sgd_update_bf16(const gmb_sage_weights* weights, const gmb_sage_weights* master, const gmb_sage_grads* grads,
                         float lr, void* stream);
+
+/* ---- microscaled vertex store ------------------------------------------- */
+
+/* The feature (or embedding) rows of the key-value store (Section III-C) in
+ * 4 or 8 bits an element: a quarter to an eighth of the bytes that every
+ * pull and every mean moves.  A row of `dim` elements is a record of
+ * gmb_mx_row_bytes(dim, format) bytes:
+ *   - its elements in nb = ceil(dim / 32) blocks of 32.  GMB_MXFP4: 16 bytes
+ *     a block, element i in half i % 2 of byte i / 2 (0: the low half), sign
+ *     bit, then the magnitudes 0 .5 1 1.5 2 3 4 6; GMB_MXFP8: 32 bytes, e4m3
+ *     (bias 7, largest value 448, code 0x7F not a number).  Elements past dim
+ *     are 0;
+ *   - nb scale bytes c, the block's scale being 2^(c - 127), 255 not a number;
+ *   - zeros up to a multiple of 16 bytes.
+ * A table of records has an address and a row stride that are multiples of
+ * 16 (the stride at least a record; bytes between record and stride are not
+ * touched).  dim is 1 .. 65536, a table's rows 1 .. 2^31 - 1.
+ * Quantising takes c = max(e - s, 0) with e the fp32 exponent field of the
+ * block's largest magnitude and s = 2 (4 bits) or 8 (8 bits), and rounds
+ * x / 2^(c - 127) to the nearest element, ties to even; what lies past the
+ * largest element becomes it.  A block that holds an infinity or NaN gets
+ * c = 255 and reads back as NaN.  Values of 4 or 8 bits are exact in fp32,
+ * and in bf16 unless a bf16 denormal cannot hold them. */
+
+/* Bytes of a record (0 for a bad dim or format). */
+int64_t gmb_mx_row_bytes(int32_t dim, int32_t format);
+
+/* Quantises rows into a table: record r_i = x[i, :] for i < n, where n = *n_dev
+ * clamped to n_cap, or n_cap when n_dev is NULL; r_i = ids[i], or i when ids
+ * is NULL (n_cap at most num_rows then).
+ *   x       device, element (i, j) at i * row_stride + j * col_stride elements
+ *           of `dtype` (strides >= 0): rows, or the columns of a weight matrix
+ *           [d_in][d_out] (row_stride 1, col_stride d_out) that
+ *           gmb_mx_linear wants as rows.  Rows need no alignment.
+ *   ids     device int32[n_cap] or NULL.  An id outside [0, num_rows) sets
+ *           GMB_STATUS_ERANGE and its row is not written.
+ *   state   NULL: the ids are distinct (as a block's src_ids are); records of
+ *           an id that comes twice are unspecified.  Else the sampler state
+ *           of a graph of num_rows vertices: an id may come any number of
+ *           times and its last row is what the record holds.  The state's
+ *           table is left clear; calls that share it must be ordered on one
+ *           stream.
+ *   status  device status word or NULL (with a state: the state's). */
+int gmb_mx_quantise(const void* x, int32_t dtype, int64_t row_stride, int64_t col_stride, const int32_t* ids,
+                    const int32_t* n_dev, int64_t n_cap, int32_t dim, int32_t format, void* table, int64_t num_rows,
+                    int64_t table_stride, void* state, size_t state_bytes, uint32_t* status, void* stream);
+
+/* gmb_gather_features from a store: out[i, :] = the values of record ids[i]
+ * (record i when ids is NULL), i < n as above, as fp32 or bf16 (`dtype`).
+ *   out  device [n_cap, dim] row-major; rows at i >= n are not written; a row
+ *        whose id is outside [0, num_rows) is zero-filled and sets
+ *        GMB_STATUS_ERANGE in `status` (device word or NULL). */
+int gmb_mx_gather(const int32_t* ids, const int32_t* n_dev, int64_t n_cap, const void* table, int64_t num_rows,
+                  int64_t table_stride, int32_t dim, int32_t format, void* out, int32_t dtype, uint32_t* status,
+                  void* stream);
+
+/* The mean of Eq. (1) straight from a store: out[v, :] = (1 / k_v) times the
+ * sum over e in [indptr[v], indptr[v + 1]) of the values of record ids[e], 0
+ * for an empty range, fp32 sums.
+ *   indptr  device int32[n_cap + 1], rising (a block's row offsets)
+ *   ids     device int32, a record of the table for every e (a block's nbr);
+ *           one outside [0, num_rows) is read as record 0
+ *   n_dev   device int32 or NULL: destinations, clamped to n_cap (a block's
+ *           sizes[0])
+ *   out     device [n_cap, dim] of `dtype`. */
+int gmb_mx_mean(const int32_t* indptr, const int32_t* ids, const int32_t* n_dev, int64_t n_cap, const void* table,
+                int64_t num_rows, int64_t table_stride, int32_t dim, int32_t format, void* out, int32_t dtype,
+                void* stream);
+
+/* One operand of a product: GMB_MXFP4 records of d_in elements.
+ *   rows     [num_rows], row i of the product being ids[i], or i without ids
+ *            (an id outside the table counts as a row of zeros and sets
+ *            GMB_STATUS_ERANGE)
+ *   weights  [d_out]: output column j's weights, quantised along d_in. */
+typedef struct {
+  const void* rows;
+  int64_t num_rows, row_stride;
+  const int32_t* ids;
+  const void* weights;
+  int64_t weight_stride;
+} gmb_mx_operand;
+
+/* out = act(A W^T [+ A2 W2^T] + bias), the linear layer of Eq. (1) with
+ * microscaled 4-bit rows and weights: exact products, fp32 sums on the
+ * scaled matrix instructions.  No gradient: a model is trained on its fp32
+ * masters (gmb_sage_backward on what the records stand for) and quantised
+ * again.
+ *   a, a2   the operands (a2 may be NULL; its ids must be)
+ *   n_dev   device int32 or NULL: rows, clamped to n_cap
+ *   bias    device fp32 [d_out] or NULL; relu: nonzero for max(0, .)
+ *   out     device [n_cap, d_out] of `dtype`. */
+int gmb_mx_linear(const gmb_mx_operand* a, const gmb_mx_operand* a2, const int32_t* n_dev, int64_t n_cap,
+                  int32_t d_in, int32_t d_out, const float* bias, int32_t relu, void* out, int32_t dtype,
+                  uint32_t* status, void* stream);
+
+/* A GraphSAGE-mean model in GMB_MXFP4: w_self[l], w_neigh[l] device records,
+ * dims[l+1] rows of dims[l] elements at a stride of gmb_mx_row_bytes(dims[l])
+ * (the transposes of gmb_sage_weights' matrices), bias[l] device fp32. */
+typedef struct {
+  int32_t num_layers;
+  int32_t dims[GMB_MAX_LAYERS + 1];
+  const void* w_self[GMB_MAX_LAYERS];
+  const void* w_neigh[GMB_MAX_LAYERS];
+  const float* bias[GMB_MAX_LAYERS];
+} gmb_sage_mx_weights;
+
+/* Bytes of workspace gmb_sage_forward_mx needs (0 for bad arguments), and the
+ * byte offset there of layer l's mean records (hidden 0, [n_dst(l)] of
+ * dims[l]) or hidden records (hidden 1, l < L-1, of dims[l+1]); -1 for a bad
+ * layer. */
+size_t gmb_mx_forward_workspace_bytes(const gmb_blocks* blocks, const gmb_sage_mx_weights* weights);
+int64_t gmb_mx_forward_offset(const gmb_blocks* blocks, const gmb_sage_mx_weights* weights, int32_t layer,
+                              int32_t hidden);
+
+/* gmb_sage_forward_fused of such a model over a GMB_MXFP4 store: layer 0's
+ * mean and its linear term read the store by the vertices' ids, and every
+ * layer's mean and hidden output is quantised (GMB_MXFP4) as it is written.
+ *   table   the store, num_nodes records of dims[0]
+ *   logits  device fp32 [num_seeds, dims[L]]
+ *   ws      device workspace, 256-byte aligned
+ *   status  NULL or a status word: an id outside the store sets
+ *           GMB_STATUS_ERANGE (zeros in the linear term, record 0 in the mean)
+ * An empty batch enqueues nothing (logits may be NULL). */
+int gmb_sage_forward_mx(const gmb_blocks* blocks, const void* table, int64_t num_nodes, int64_t table_stride,
+                        const gmb_sage_mx_weights* weights, float* logits, void* ws, size_t ws_bytes,
+                        uint32_t* status, void* stream);
+
+/* ---- distillation -------------------------------------------------------- */
+
+#define GMB_MAX_TEACHER 1024
+
+/* A teacher's top logits, `top` (1 .. GMB_MAX_TEACHER) entries a row, and how
+ * the student is held to them: temperature T (0.001 .. 1000) and weight alpha
+ * (0 .. 1).
+ *   logits   device fp32 [rows, top]
+ *   classes  device int32 [rows, top], each entry's class.  An entry whose
+ *            class is outside [0, C) (-1 pads a shorter list) or whose logit
+ *            is -inf is left out; entries of one class add up. */
+typedef struct {
+  const float* logits;
+  const int32_t* classes;
+  int32_t top;
+  float alpha;
+  float temperature;
+  int32_t reserved;
+} gmb_teacher;
+
+/* Bytes of workspace gmb_distill_loss needs (0 for bad arguments). */
+size_t gmb_distill_workspace_bytes(int64_t rows, int32_t classes);
+
+/* The mean over the rows of
+ *   alpha T^2 KL(p || softmax(z / T)) + (1 - alpha) (-log softmax(z)_y)
+ * and its gradient in the logits z, with p the softmax of the row's teacher
+ * entries over T.  A row without entries lacks the first term, one whose
+ * label is outside [0, classes) the second, and one whose logits are all
+ * -inf both; their gradients are 0.  (A logit of -inf is a class that cannot
+ * be: probability 0; the loss is infinite if the teacher gives it more.)
+ * Sums and statistics are fp32, in a fixed order.
+ *   logits   device [rows, classes] fp32 or bf16 (`dtype`)
+ *   labels   device int32 [rows] or NULL (no second term)
+ *   dlogits  device [rows, classes] of `dtype`, or NULL for the loss alone;
+ *            not the logits' own array
+ *   loss     device fp32 scalar (0 for no rows)
+ *   ws       device workspace, 256-byte aligned. */
+int gmb_distill_loss(const void* logits, int32_t dtype, int64_t rows, int32_t classes, const gmb_teacher* teacher,
+                     const int32_t* labels, void* dlogits, float* loss, void* ws, size_t ws_bytes, void* stream);
+
+/* gmb_sage_backward (table NULL), or gmb_sage_backward_embedding (table the
+ * embeddings), from that loss instead of the cross-entropy: the same
+ * workspaces (gmb_backward_workspace_bytes, or the embedding's) and
+ * arguments; labels may be NULL; at most 32,768 classes. */
+int gmb_sage_backward_distill(const gmb_blocks* blocks, const void* x, const gmb_sage_weights* weights,
+                              const float* logits, const gmb_teacher* teacher, const int32_t* labels,
+                              const void* fwd_ws, size_t fwd_ws_bytes, const gmb_sage_grads* grads, float* loss,
+                              void* ws, size_t ws_bytes, float* table, int64_t num_nodes, float emb_lr,
+                              void* stream);
 
 #ifdef __cplusplus
 }

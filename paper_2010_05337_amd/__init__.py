@@ -26,6 +26,7 @@ LIB_PATH = os.path.join(_PKG, "libgmb.so")
 
 GMB_MAX_LAYERS = 8
 GMB_F32, GMB_BF16 = 0, 1
+MXFP4, MXFP8 = 4, 8   # microscaled formats: the bits of an element
 ENOSPC = -2
 STATUS = {0: "OK", -1: "EINVAL", -2: "ENOSPC", -3: "EDEVICE", -4: "ERANGE", -5: "EDUP"}
 EXPORTS = (
@@ -36,6 +37,9 @@ EXPORTS = (
     "gmb_sage_backward", "gmb_sgd_update", "gmb_backward_embedding_workspace_bytes",
     "gmb_sage_backward_embedding", "gmb_sample_blocks_noalloc",
     "gmb_validate_blocks", "gmb_sgd_update_bf16",
+    "gmb_mx_row_bytes", "gmb_mx_quantise", "gmb_mx_gather", "gmb_mx_mean", "gmb_mx_linear",
+    "gmb_mx_forward_workspace_bytes", "gmb_mx_forward_offset", "gmb_sage_forward_mx",
+    "gmb_distill_workspace_bytes", "gmb_distill_loss", "gmb_sage_backward_distill",
 )
 
 
@@ -76,6 +80,24 @@ class GradsStruct(ctypes.Structure):
                 ("d_self", ctypes.c_void_p * GMB_MAX_LAYERS),
                 ("d_neigh", ctypes.c_void_p * GMB_MAX_LAYERS),
                 ("d_bias", ctypes.c_void_p * GMB_MAX_LAYERS)]
+
+
+class MxOperandStruct(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_void_p), ("num_rows", ctypes.c_int64), ("row_stride", ctypes.c_int64),
+                ("ids", ctypes.c_void_p), ("weights", ctypes.c_void_p), ("weight_stride", ctypes.c_int64)]
+
+
+class MxWeightsStruct(ctypes.Structure):
+    _fields_ = [("num_layers", ctypes.c_int32),
+                ("dims", ctypes.c_int32 * (GMB_MAX_LAYERS + 1)),
+                ("w_self", ctypes.c_void_p * GMB_MAX_LAYERS),
+                ("w_neigh", ctypes.c_void_p * GMB_MAX_LAYERS),
+                ("bias", ctypes.c_void_p * GMB_MAX_LAYERS)]
+
+
+class TeacherStruct(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("classes", ctypes.c_void_p), ("top", ctypes.c_int32),
+                ("alpha", ctypes.c_float), ("temperature", ctypes.c_float), ("reserved", ctypes.c_int32)]
 
 
 _lib = None
@@ -146,6 +168,33 @@ def lib() -> ctypes.CDLL:
         L.gmb_sgd_update.restype = ctypes.c_int
         L.gmb_sgd_update.argtypes = [ctypes.POINTER(WeightsStruct), ctypes.POINTER(GradsStruct),
                                      ctypes.c_float, vp]
+        f32 = ctypes.c_float
+        L.gmb_mx_row_bytes.restype = i64
+        L.gmb_mx_row_bytes.argtypes = [i32, i32]
+        L.gmb_mx_quantise.restype = ctypes.c_int
+        L.gmb_mx_quantise.argtypes = [vp, i32, i64, i64, vp, vp, i64, i32, i32, vp, i64, i64, vp, sz, vp, vp]
+        L.gmb_mx_gather.restype = ctypes.c_int
+        L.gmb_mx_gather.argtypes = [vp, vp, i64, vp, i64, i64, i32, i32, vp, i32, vp, vp]
+        L.gmb_mx_mean.restype = ctypes.c_int
+        L.gmb_mx_mean.argtypes = [vp, vp, vp, i64, vp, i64, i64, i32, i32, vp, i32, vp]
+        L.gmb_mx_linear.restype = ctypes.c_int
+        L.gmb_mx_linear.argtypes = [ctypes.POINTER(MxOperandStruct), ctypes.POINTER(MxOperandStruct), vp, i64, i32,
+                                    i32, vp, i32, vp, i32, vp, vp]
+        L.gmb_mx_forward_workspace_bytes.restype = sz
+        L.gmb_mx_forward_workspace_bytes.argtypes = [ctypes.POINTER(BlocksStruct), ctypes.POINTER(MxWeightsStruct)]
+        L.gmb_mx_forward_offset.restype = i64
+        L.gmb_mx_forward_offset.argtypes = [ctypes.POINTER(BlocksStruct), ctypes.POINTER(MxWeightsStruct), i32, i32]
+        L.gmb_sage_forward_mx.restype = ctypes.c_int
+        L.gmb_sage_forward_mx.argtypes = [ctypes.POINTER(BlocksStruct), vp, i64, i64, ctypes.POINTER(MxWeightsStruct),
+                                          vp, vp, sz, vp, vp]
+        L.gmb_distill_workspace_bytes.restype = sz
+        L.gmb_distill_workspace_bytes.argtypes = [i64, i32]
+        L.gmb_distill_loss.restype = ctypes.c_int
+        L.gmb_distill_loss.argtypes = [vp, i32, i64, i32, ctypes.POINTER(TeacherStruct), vp, vp, vp, vp, sz, vp]
+        L.gmb_sage_backward_distill.restype = ctypes.c_int
+        L.gmb_sage_backward_distill.argtypes = [ctypes.POINTER(BlocksStruct), vp, ctypes.POINTER(WeightsStruct), vp,
+                                                ctypes.POINTER(TeacherStruct), vp, vp, sz,
+                                                ctypes.POINTER(GradsStruct), vp, vp, sz, vp, i64, f32, vp]
         _lib = L
     return _lib
 
@@ -522,17 +571,21 @@ def backward_embedding_workspace_bytes(blocks: Blocks, weights: SageWeights) -> 
 def sage_backward(blocks: Blocks, feats: torch.Tensor, weights: SageWeights, logits: torch.Tensor,
                   labels: torch.Tensor, fwd_workspace: torch.Tensor, grads: SageGrads | None = None,
                   loss: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
-                  embedding: torch.Tensor | None = None, emb_lr: float = 0.0):
+                  embedding: torch.Tensor | None = None, emb_lr: float = 0.0, teacher: "Teacher | None" = None):
     """Gradients of the mean softmax cross-entropy of `logits` (from the
     sage_forward call that used `fwd_workspace`) against `labels` (device
-    int32, one per seed).  Returns (grads, loss) with loss a 1-element
+    int32, one per seed), or, with `teacher`, of the loss of distill_loss
+    (labels may be None then).  Returns (grads, loss) with loss a 1-element
     float32 device tensor.  With `embedding` (the fp32 [num_nodes, dims[0]]
     table the layer-0 inputs were taken from) the gradient in the input
     rows is applied to the table as an SGD step of size emb_lr.  A NaN loss
     may also mean that a bounded wait on the device ran out (gmb.h)."""
-    _require_cuda(labels, "labels")
-    if labels.dtype != torch.int32 or labels.numel() < blocks.num_seeds:
-        raise TypeError("labels must be int32 with one entry per seed")
+    if labels is not None or teacher is None:
+        _require_cuda(labels, "labels")
+        if labels.dtype != torch.int32 or labels.numel() < blocks.num_seeds:
+            raise TypeError("labels must be int32 with one entry per seed")
+    if teacher is not None and teacher.rows < blocks.num_seeds:
+        raise ValueError("teacher must have one row per seed")
     if embedding is not None:
         _require_cuda(embedding, "embedding")
         if embedding.dtype != torch.float32 or embedding.dim() != 2 or embedding.shape[1] != weights.dims[0] \
@@ -550,10 +603,15 @@ def sage_backward(blocks: Blocks, feats: torch.Tensor, weights: SageWeights, log
     if loss is None:
         loss = torch.empty(1, dtype=torch.float32, device=feats.device)
     common = (ctypes.byref(blocks.struct), ctypes.c_void_p(feats.data_ptr()), ctypes.byref(weights.struct),
-              ctypes.c_void_p(logits.data_ptr()), ctypes.c_void_p(labels.data_ptr()),
+              ctypes.c_void_p(logits.data_ptr()),
+              None if labels is None else ctypes.c_void_p(labels.data_ptr()),
               ctypes.c_void_p(fwd_workspace.data_ptr()), fwd_workspace.numel(), ctypes.byref(grads.struct),
               ctypes.c_void_p(loss.data_ptr()), ctypes.c_void_p(workspace.data_ptr()), workspace.numel())
-    if embedding is None:
+    if teacher is not None:
+        table = (None, 0, 0.0) if embedding is None else (embedding.data_ptr(), embedding.shape[0], float(emb_lr))
+        _check(lib().gmb_sage_backward_distill(*common[:4], ctypes.byref(teacher.struct), *common[4:], *table,
+                                               _stream_handle()))
+    elif embedding is None:
         _check(lib().gmb_sage_backward(*common, _stream_handle()))
     else:
         _check(lib().gmb_sage_backward_embedding(*common, ctypes.c_void_p(embedding.data_ptr()),
@@ -573,3 +631,350 @@ def sgd_update_bf16(weights: SageWeights, master: SageWeights, grads: SageGrads,
     (the biases, fp32 in both, are updated in the master and copied)."""
     _check(lib().gmb_sgd_update_bf16(ctypes.byref(weights.struct), ctypes.byref(master.struct),
                                      ctypes.byref(grads.struct), float(lr), _stream_handle()))
+
+
+# ---------------------------------------------------------------- microscaled store and model
+
+_DTYPES = {torch.float32: GMB_F32, torch.bfloat16: GMB_BF16}
+
+
+def _on_device(*tensors):
+    """Refuses tensors that are not on the current device (the kernels run on
+    its stream)."""
+    dev = None
+    for t, name in tensors:
+        if t is None:
+            continue
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+        if dev is None:
+            dev = torch._C._cuda_getDevice()
+        if t.get_device() != dev:
+            raise ValueError(f"{name} is on device {t.get_device()}, the current device is {dev}")
+
+
+def _dtype_code(dtype) -> int:
+    code = _DTYPES.get(dtype)
+    if code is None:
+        raise TypeError("dtype must be torch.float32 or torch.bfloat16")
+    return code
+
+
+def _int32(t, name: str):
+    if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous():
+        raise TypeError(f"{name} must be a contiguous 1-d int32 tensor")
+
+
+_row_bytes: dict = {}
+
+
+def mx_row_bytes(dim: int, bits: int) -> int:
+    """Bytes of the record of a row of `dim` elements in MXFP4 or MXFP8."""
+    n = _row_bytes.get((dim, bits))
+    if n is None:
+        n = lib().gmb_mx_row_bytes(dim, bits)
+        if n == 0:
+            _check(-1)
+        _row_bytes[dim, bits] = n
+    return n
+
+
+def _records(t: torch.Tensor, dim: int, bits: int, name: str):
+    """Checks a table of records: uint8 [rows, >= row bytes], rows at a stride."""
+    if t.dtype != torch.uint8 or t.dim() != 2 or t.stride(1) != 1:
+        raise TypeError(f"{name} must be a uint8 [rows, row bytes] tensor with contiguous rows")
+    if t.shape[1] < mx_row_bytes(dim, bits):
+        raise ValueError(f"{name} has {t.shape[1]} bytes a row, {mx_row_bytes(dim, bits)} needed")
+
+
+def _stride(t: torch.Tensor) -> int:
+    """The row stride in bytes (of one row, any: its length rounded down to 16)."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] // 16 * 16
+
+
+def _rows_of(ids, n, table_rows: int, status_word):
+    """(ids pointer, device count pointer, rows, status word) of a Blocks (its
+    input vertices), an int32 tensor, or None (every row of the table)."""
+    if isinstance(ids, Blocks):
+        if n is not None:
+            raise ValueError("n goes with an id tensor")
+        return (ids.struct.blk[0].src_ids, ids.input_count_ptr, ids.input_capacity,
+                ids.csr.status_word if status_word is None else status_word)
+    if ids is None:
+        cap = table_rows if n is None else int(n)
+        if not 0 <= cap <= table_rows:
+            raise ValueError("n exceeds the table's rows")
+        return None, None, cap, status_word
+    _int32(ids, "ids")
+    cap = ids.numel() if n is None else int(n)
+    if not 0 <= cap <= ids.numel():
+        raise ValueError("n exceeds ids")
+    return ids.data_ptr() if cap else None, None, cap, status_word
+
+
+def mx_quantise(x: torch.Tensor, bits: int, ids=None, table: torch.Tensor | None = None, csr: CSRGraph | None = None,
+                status_word: int | None = None) -> torch.Tensor:
+    """Quantises the rows of x (float32 or bfloat16 [n, dim], any non-negative
+    strides: w.t() for a weight matrix) into microscaled records and returns
+    their table (uint8 [rows, row bytes]).  With `ids` (int32, one a row, or a
+    Blocks: x holds its input rows) they replace those rows of `table`: ids
+    are distinct, or, with `csr` (a graph of table's rows, whose sampler state
+    is used), an id's last row counts.  Without ids, row i is record i of
+    `table` or of a new one."""
+    _on_device((x, "x"), (table, "table"), (None if isinstance(ids, Blocks) else ids, "ids"))
+    if x.dim() != 2:
+        raise ValueError("x must be [rows, dim]")
+    dtype = _dtype_code(x.dtype)
+    rows, dim = x.shape
+    if table is None:
+        if ids is not None:
+            raise ValueError("ids need a table")
+        table = torch.empty((rows, mx_row_bytes(dim, bits)), dtype=torch.uint8, device=x.device)
+    else:
+        _records(table, dim, bits, "table")
+        if ids is None and rows > table.shape[0]:
+            raise ValueError("x has more rows than the table")
+    ids_ptr, n_dev, cap, status = _rows_of(ids, None if ids is not None else rows, table.shape[0], status_word)
+    if ids is not None and not isinstance(ids, Blocks) and cap != rows:
+        raise ValueError("ids must have one entry per row of x")
+    if isinstance(ids, Blocks) and rows < cap:
+        raise ValueError("x must have the blocks' input capacity in rows")
+    state = (None, 0)
+    if csr is not None:
+        if ids is None or csr.num_nodes != table.shape[0]:
+            raise ValueError("csr needs ids and a table of its graph's vertices")
+        state = (csr.state.data_ptr(), csr.state_bytes)
+    if cap == 0:
+        return table
+    _check(lib().gmb_mx_quantise(x.data_ptr(), dtype, x.stride(0) if rows > 1 else 0, x.stride(1), ids_ptr, n_dev,
+                                 cap, dim, bits, table.data_ptr(), table.shape[0], _stride(table), *state,
+                                 status or None, _stream_handle()))
+    return table
+
+
+def mx_gather(ids, table: torch.Tensor, dim: int, bits: int, dtype: torch.dtype = torch.float32,
+              n: int | None = None, out: torch.Tensor | None = None, status_word: int | None = None) -> torch.Tensor:
+    """gather_features from a microscaled store: out[i] = the values of record
+    ids[i] as float32 or bfloat16.  `ids` is a Blocks (its input vertices), an
+    int32 tensor (all of it, or the first n), or None (the table's rows, or
+    the first n)."""
+    _on_device((table, "table"), (out, "out"), (None if isinstance(ids, Blocks) else ids, "ids"))
+    _records(table, dim, bits, "table")
+    code = _dtype_code(dtype)
+    ids_ptr, n_dev, cap, status = _rows_of(ids, n, table.shape[0], status_word)
+    if out is None:
+        out = torch.empty((cap, dim), dtype=dtype, device=table.device)
+    elif out.dim() != 2 or out.shape[0] < cap or out.shape[1] != dim or out.dtype != dtype or not out.is_contiguous():
+        raise ValueError("out must be a contiguous [rows, dim] tensor of the given dtype")
+    if cap:
+        _check(lib().gmb_mx_gather(ids_ptr, n_dev, cap, table.data_ptr(), table.shape[0], _stride(table), dim, bits,
+                                   out.data_ptr(), code, status or None, _stream_handle()))
+    return out
+
+
+def mx_mean(block, table: torch.Tensor, dim: int, bits: int, dtype: torch.dtype = torch.float32,
+            out: torch.Tensor | None = None) -> torch.Tensor:
+    """The mean of every destination's neighbours' rows, straight from a
+    microscaled store (0 for a destination without any).  `block` is (indptr,
+    ids): int32 row offsets and the neighbours' records, or a Blocks (block
+    0's destinations, at their capacity, and sampled vertices)."""
+    if isinstance(block, Blocks):
+        b = block.struct.blk[0]
+        ptrs, n_dev, rows = (b.indptr, b.nbr), b.sizes, int(b.cap_dst)
+        _on_device((table, "table"), (out, "out"))
+    else:
+        indptr, ids = block
+        _on_device((table, "table"), (out, "out"), (indptr, "indptr"), (ids, "ids"))
+        _int32(indptr, "indptr")
+        _int32(ids, "ids")
+        if indptr.numel() < 1:
+            raise ValueError("indptr needs one entry more than rows")
+        # (a graph without edges has no ids to point at; none is read)
+        ptrs, n_dev, rows = (indptr.data_ptr(), ids.data_ptr() or indptr.data_ptr()), None, indptr.numel() - 1
+    _records(table, dim, bits, "table")
+    code = _dtype_code(dtype)
+    if out is None:
+        out = torch.empty((rows, dim), dtype=dtype, device=table.device)
+    elif out.dim() != 2 or out.shape[0] < rows or out.shape[1] != dim or out.dtype != dtype or not out.is_contiguous():
+        raise ValueError("out must be a contiguous [rows, dim] tensor of the given dtype")
+    if rows:
+        _check(lib().gmb_mx_mean(*ptrs, n_dev, rows, table.data_ptr(), table.shape[0], _stride(table), dim, bits,
+                                 out.data_ptr(), code, _stream_handle()))
+    return out
+
+
+def mx_linear(a: torch.Tensor, w: torch.Tensor, d_in: int, bias: torch.Tensor | None = None,
+              a2: torch.Tensor | None = None, w2: torch.Tensor | None = None, ids: torch.Tensor | None = None,
+              relu: bool = False, dtype: torch.dtype = torch.float32, out: torch.Tensor | None = None,
+              status_word: int | None = None) -> torch.Tensor:
+    """act(A W^T [+ A2 W2^T] + bias) of MXFP4 records of d_in elements: a
+    [rows, .], w [d_out, .] (mx_quantise(matrix.t(), MXFP4) of a [d_in, d_out]
+    matrix), a2 and w2 a second pair.  With `ids` row i of A is record ids[i]
+    of `a`."""
+    _on_device((a, "a"), (w, "w"), (bias, "bias"), (a2, "a2"), (w2, "w2"), (ids, "ids"), (out, "out"))
+    _records(a, d_in, MXFP4, "a")
+    _records(w, d_in, MXFP4, "w")
+    code, d_out, rows = _dtype_code(dtype), w.shape[0], a.shape[0]
+    if ids is not None:
+        _int32(ids, "ids")
+        rows = ids.numel()
+    first = MxOperandStruct(a.data_ptr(), a.shape[0], _stride(a), None if ids is None else ids.data_ptr(),
+                            w.data_ptr(), _stride(w))
+    second = None
+    if a2 is not None or w2 is not None:
+        if a2 is None or w2 is None:
+            raise ValueError("a2 and w2 go together")
+        _records(a2, d_in, MXFP4, "a2")
+        _records(w2, d_in, MXFP4, "w2")
+        if a2.shape[0] < rows or w2.shape[0] != d_out:
+            raise ValueError("a2 must have a row for each of the product's, w2 one for each column")
+        second = ctypes.byref(MxOperandStruct(a2.data_ptr(), a2.shape[0], _stride(a2), None, w2.data_ptr(),
+                                              _stride(w2)))
+    if bias is not None and (bias.dtype != torch.float32 or bias.shape != (d_out,) or not bias.is_contiguous()):
+        raise ValueError("bias must be a contiguous float32 [d_out] tensor")
+    if out is None:
+        out = torch.empty((rows, d_out), dtype=dtype, device=a.device)
+    elif out.dim() != 2 or out.shape[0] < rows or out.shape[1] != d_out or out.dtype != dtype \
+            or not out.is_contiguous():
+        raise ValueError("out must be a contiguous [rows, d_out] tensor of the given dtype")
+    if rows and d_out:
+        _check(lib().gmb_mx_linear(ctypes.byref(first), second, None, rows, d_in, d_out,
+                                   None if bias is None else bias.data_ptr(), 1 if relu else 0, out.data_ptr(), code,
+                                   status_word or None, _stream_handle()))
+    return out
+
+
+class SageMxWeights:
+    """A GraphSAGE-mean model's weights in MXFP4: the records of the
+    transposed matrices of a SageWeights, and its biases (shared)."""
+
+    def __init__(self, weights: SageWeights):
+        self.dims = list(weights.dims)
+        self.bias = weights.bias
+        self.w_self = [mx_quantise(w.t(), MXFP4) for w in weights.w_self]
+        self.w_neigh = [mx_quantise(w.t(), MXFP4) for w in weights.w_neigh]
+        s = MxWeightsStruct()
+        s.num_layers = len(self.w_self)
+        for i, d in enumerate(self.dims):
+            s.dims[i] = d
+        for l in range(s.num_layers):
+            s.w_self[l] = self.w_self[l].data_ptr()
+            s.w_neigh[l] = self.w_neigh[l].data_ptr()
+            s.bias[l] = self.bias[l].data_ptr()
+        self.struct = s
+
+    def requantise(self, weights: SageWeights):
+        """The records of `weights` (the same widths) in place of the old."""
+        if list(weights.dims) != self.dims:
+            raise ValueError("the widths differ")
+        for l in range(len(self.w_self)):
+            mx_quantise(weights.w_self[l].t(), MXFP4, table=self.w_self[l])
+            mx_quantise(weights.w_neigh[l].t(), MXFP4, table=self.w_neigh[l])
+
+    def values(self) -> SageWeights:
+        """What the records stand for, as float32 weights: what sage_forward
+        and sage_backward take to train the model on float32 masters."""
+        def mat(rec, d_in):
+            return mx_gather(None, rec, d_in, MXFP4).t().contiguous()
+        return SageWeights([mat(w, d) for w, d in zip(self.w_self, self.dims)],
+                           [mat(w, d) for w, d in zip(self.w_neigh, self.dims)], self.bias)
+
+
+def mx_forward_workspace_bytes(blocks: Blocks, weights: SageMxWeights) -> int:
+    return lib().gmb_mx_forward_workspace_bytes(ctypes.byref(blocks.struct), ctypes.byref(weights.struct))
+
+
+def sage_forward_mx(blocks: Blocks, table: torch.Tensor, weights: SageMxWeights,
+                    workspace: torch.Tensor | None = None, logits: torch.Tensor | None = None) -> torch.Tensor:
+    """The forward of an MXFP4 model over an MXFP4 store (table: one record of
+    dims[0] elements a vertex); the layers' means and hidden outputs are
+    quantised as they are written.  Returns logits [num_seeds, C] float32."""
+    _on_device((table, "table"), (workspace, "workspace"), (logits, "logits"))
+    _records(table, weights.dims[0], MXFP4, "table")
+    B, C = blocks.num_seeds, weights.dims[-1]
+    if logits is None:
+        logits = torch.empty((max(B, 0), C), dtype=torch.float32, device=table.device)
+    elif logits.dtype != torch.float32 or logits.shape != (B, C) or not logits.is_contiguous():
+        raise ValueError("logits must be a contiguous float32 [num_seeds, C] tensor")
+    L, stream, status = lib(), _stream_handle(), blocks.csr.status_word
+
+    def call(ws):
+        return L.gmb_sage_forward_mx(ctypes.byref(blocks.struct), table.data_ptr(), table.shape[0], _stride(table),
+                                     ctypes.byref(weights.struct), logits.data_ptr(), ws.data_ptr(), ws.numel(),
+                                     status, stream)
+
+    code = ENOSPC
+    if workspace is not None and workspace.numel() > 0 and workspace.data_ptr() % 256 == 0:
+        code = call(workspace)
+    if code == ENOSPC:
+        need = mx_forward_workspace_bytes(blocks, weights)
+        if need == 0:
+            _check(-1)
+        _, workspace = _aligned_bytes(need, table.device)
+        code = call(workspace)
+    _check(code)
+    return logits
+
+
+# ---------------------------------------------------------------- distillation
+
+class Teacher:
+    """A teacher's top logits for a student: `logits` float32 [rows, k] and
+    their `classes` int32 [rows, k] (-1 pads a shorter list), the weight alpha
+    of the teacher against the labels, and the temperature."""
+
+    def __init__(self, logits: torch.Tensor, classes: torch.Tensor, alpha: float = 0.5, temperature: float = 1.0):
+        _on_device((logits, "logits"), (classes, "classes"))
+        if logits.dtype != torch.float32 or logits.dim() != 2 or not logits.is_contiguous():
+            raise TypeError("the teacher's logits must be a contiguous float32 [rows, k] tensor")
+        if classes.dtype != torch.int32 or classes.shape != logits.shape or not classes.is_contiguous():
+            raise TypeError("the teacher's classes must be a contiguous int32 tensor of the logits' shape")
+        self.logits, self.classes = logits, classes
+        self.rows = logits.shape[0]
+        self.struct = TeacherStruct(logits.data_ptr(), classes.data_ptr(), logits.shape[1], alpha, temperature, 0)
+
+
+def distill_loss(logits: torch.Tensor, teacher_logits: torch.Tensor, teacher_classes: torch.Tensor,
+                 labels: torch.Tensor | None = None, alpha: float = 0.5, temperature: float = 1.0,
+                 grad: torch.Tensor | bool = True, loss: torch.Tensor | None = None,
+                 workspace: torch.Tensor | None = None):
+    """The mean over the rows of alpha T^2 KL(teacher || student) over the
+    teacher's top entries plus (1 - alpha) times the cross-entropy against
+    `labels` (int32, -1 for none), and its gradient in `logits` (float32 or
+    bfloat16 [rows, C]).  Returns (loss, grad): a 1-element float32 tensor and
+    a tensor like logits (None for grad=False)."""
+    _on_device((logits, "logits"), (labels, "labels"), (None if isinstance(grad, bool) else grad, "grad"),
+               (loss, "loss"), (workspace, "workspace"))
+    if logits.dim() != 2 or not logits.is_contiguous():
+        raise ValueError("logits must be a contiguous [rows, classes] tensor")
+    dtype = _dtype_code(logits.dtype)
+    rows, classes = logits.shape
+    teacher = Teacher(teacher_logits, teacher_classes, alpha, temperature)
+    if teacher.rows != rows:
+        raise ValueError("the teacher must have one row per row of logits")
+    if labels is not None:
+        _int32(labels, "labels")
+        if labels.numel() != rows:
+            raise ValueError("labels must have one entry per row")
+    if grad is True:
+        grad = torch.empty_like(logits)
+    elif grad is False:
+        grad = None
+    elif grad.shape != logits.shape or grad.dtype != logits.dtype or not grad.is_contiguous() \
+            or (rows and grad.data_ptr() == logits.data_ptr()):
+        raise ValueError("grad must be a contiguous tensor like logits, and another one")
+    if loss is None:
+        loss = torch.empty(1, dtype=torch.float32, device=logits.device)
+    elif loss.dtype != torch.float32 or loss.numel() != 1:
+        raise ValueError("loss must be a 1-element float32 tensor")
+    L = lib()
+    need = L.gmb_distill_workspace_bytes(rows, classes)
+    if need == 0:
+        _check(-1)
+    if workspace is None or workspace.numel() < need or workspace.data_ptr() % 256:
+        _, workspace = _aligned_bytes(need, logits.device)
+    _check(L.gmb_distill_loss(logits.data_ptr(), dtype, rows, classes, ctypes.byref(teacher.struct),
+                              None if labels is None else labels.data_ptr(),
+                              None if grad is None else grad.data_ptr(), loss.data_ptr(), workspace.data_ptr(),
+                              workspace.numel(), _stream_handle()))
+    return loss, grad

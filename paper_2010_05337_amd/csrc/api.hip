@@ -11,6 +11,7 @@
 #include <mutex>
 #include <string>
 
+#include "api_common.hpp"
 #include "gmb.h"
 #include "kernels.hpp"
 
@@ -895,12 +896,13 @@ struct Bf16Sources {
   const void* hidden[GMB_MAX_LAYERS];
 };
 
-// The backward from the loss down; with table != NULL layer 0's input
-// gradient is applied to the embedding rows of block 0's sources.
+// The backward from the loss down (`how`, or the cross-entropy against
+// `labels`); with table != NULL layer 0's input gradient is applied to the
+// embedding rows of block 0's sources.
 int run_backward(const gmb_blocks* blocks, const void* x, const gmb_sage_weights* weights, const float* logits,
                  const int32_t* labels, const void* fwd_ws, size_t fwd_ws_bytes, const gmb_sage_grads* grads,
                  float* loss, void* ws, size_t ws_bytes, float* table, int64_t num_nodes, float emb_lr,
-                 void* stream, const Bf16Sources* lo = nullptr) {
+                 void* stream, const gmb::LossLaunch* how = nullptr, const Bf16Sources* lo = nullptr) {
   const bool embed = table != nullptr;
   BackwardPlan p;
   int st = plan_backward(blocks, weights, &p, embed);
@@ -953,7 +955,7 @@ int run_backward(const gmb_blocks* blocks, const void* x, const gmb_sage_weights
       if (e != hipSuccess) return hip_fail(e, "widen launch");
     }
     return run_backward(blocks, x, &w32, logits, labels, base + p.off_shadow, f32.total, grads, loss, ws, p.fp32_total,
-                        nullptr, 0, 0.f, stream, &lo);
+                        nullptr, 0, 0.f, stream, how, &lo);
   }
   if (blocks->num_seeds == 0) {
     // an empty batch: the mean over no seeds is taken as 0, so are the
@@ -972,7 +974,7 @@ int run_backward(const gmb_blocks* blocks, const void* x, const gmb_sage_weights
     if (e != hipSuccess) return hip_fail(e, "zero-fill launch");
     return ok();
   }
-  if (!x || !logits || !labels) return fail(GMB_EINVAL, "x, logits or labels is NULL");
+  if (!x || !logits || (!labels && !how)) return fail(GMB_EINVAL, "x, logits or labels is NULL");
   char* base = static_cast<char*>(ws);
   const char* fbase = static_cast<const char*>(fwd_ws);
   float* cur = reinterpret_cast<float*>(base + p.off_a);
@@ -985,8 +987,9 @@ int run_backward(const gmb_blocks* blocks, const void* x, const gmb_sage_weights
   int2* csc = reinterpret_cast<int2*>(base + p.off_csc);
   int32_t* long_rows = reinterpret_cast<int32_t*>(base + p.off_long);
   float* loss_rows = reinterpret_cast<float*>(base + p.off_lossrows);
-  hipError_t e = gmb::launch_xent(logits, labels, blocks->num_seeds, weights->dims[L], p.ldz[L - 1], cur,
-                                  loss_rows, cnt, p.clear_len, s);
+  hipError_t e = how ? how->launch(how->what, cur, p.ldz[L - 1], loss_rows, cnt, p.clear_len, s)
+                     : gmb::launch_xent(logits, labels, blocks->num_seeds, weights->dims[L], p.ldz[L - 1], cur,
+                                        loss_rows, cnt, p.clear_len, s);
   if (e != hipSuccess) return hip_fail(e, "loss launch");
   for (int l = L - 1; l >= 0; --l) {
     const gmb_block& bk = blocks->blk[l];
@@ -1131,3 +1134,26 @@ int gmb_sgd_update_bf16(const gmb_sage_weights* weights, const gmb_sage_weights*
 }
 
 }  // extern "C"
+
+namespace gmb {
+
+int abi_fail(int status, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  return fail(status, "%s", buf);
+}
+
+int abi_check_blocks(const gmb_blocks* b) { return check_blocks(b); }
+
+int abi_backward_from(const LossLaunch& how, const gmb_blocks* blocks, const void* x,
+                      const gmb_sage_weights* weights, const float* logits, const void* fwd_ws, size_t fwd_ws_bytes,
+                      const gmb_sage_grads* grads, float* loss, void* ws, size_t ws_bytes, float* table,
+                      int64_t num_nodes, float emb_lr, void* stream) {
+  return run_backward(blocks, x, weights, logits, nullptr, fwd_ws, fwd_ws_bytes, grads, loss, ws, ws_bytes, table,
+                      num_nodes, emb_lr, stream, &how);
+}
+
+}  // namespace gmb

@@ -1,0 +1,423 @@
+// The microscaled vertex store on gfx950: rows written into it, read back
+// from it, and averaged straight out of it (mx.hpp has the format).
+//
+//   k_mx_write       rows x -> records: four lanes take a block, eight
+//                    elements each; the block's largest magnitude in two
+//                    lane exchanges
+//   k_mx_write_cols  the same for rows that lie across memory (a weight
+//                    matrix read by its columns): a lane takes a whole block,
+//                    neighbouring lanes neighbouring rows
+//   k_mx_claim       the last of several rows written to one vertex wins
+//   k_mx_read        records -> rows
+//   k_mx_mean        m_v = (1/k_v) sum_e value(table[ids[e]]), fp32 sums: a
+//                    lane takes one block of a destination, so a neighbour is
+//                    one 16-byte (4 bits) or two (8 bits) reads and a scale
+#include "mx.hpp"
+#include "mx_kernels.hpp"
+
+namespace gmb {
+
+namespace {
+
+constexpr int kMaxGrid = 1 << 16;
+
+__device__ __forceinline__ int64_t row_count(const int32_t* n_dev, int64_t n_cap) {
+  if (!n_dev) return n_cap;
+  const int64_t m = load_size(n_dev);
+  return m < 0 ? 0 : (m < n_cap ? m : n_cap);
+}
+
+// Eight elements of a row from column c on, zeros past `dim`.
+__device__ __forceinline__ void load8(const float* p, int left, float (&v)[8]) {
+  if (left >= 8) {
+    float4 a, b;
+    __builtin_memcpy(&a, p, 16);
+    __builtin_memcpy(&b, p + 4, 16);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : 0.f;
+  }
+}
+__device__ __forceinline__ void load8(const uint16_t* p, int left, float (&v)[8]) {
+  if (left >= 8) {
+    uint4 a;
+    __builtin_memcpy(&a, p, 16);
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(w[i] << 16);
+      v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < left ? bf16_to_f32(p[i]) : 0.f;
+  }
+}
+__device__ __forceinline__ float load1(const float* p) { return *p; }
+__device__ __forceinline__ float load1(const uint16_t* p) { return bf16_to_f32(*p); }
+
+// Where row `row` of a write goes: its vertex's record, or nothing (an id
+// outside the table, or a row that a later one of the same vertex replaces).
+__device__ __forceinline__ uint8_t* write_to(const MxWriteArgs& a, int64_t row, bool& bad) {
+  if (!a.ids) return a.table + row * a.table_stride;
+  const int32_t id = a.ids[row];
+  if (!valid_vertex(id, a.table_rows)) {
+    bad = true;
+    return nullptr;
+  }
+  if (a.slots && a.slots[id] != kEdgeTag - 1 - static_cast<uint32_t>(row)) return nullptr;
+  return a.table + id * a.table_stride;
+}
+
+template <typename T, int BITS, int G>
+__global__ __launch_bounds__(256) void k_mx_write(MxWriteArgs a) {
+  constexpr int kCode = 4 * BITS;   // element bytes of a block
+  const int lane = threadIdx.x & (G - 1);
+  const int64_t n = row_count(a.n_dev, a.n_cap);
+  const T* x = static_cast<const T*>(a.x);
+  bool bad = false;
+  for (int64_t row = static_cast<int64_t>(blockIdx.x) * (256 / G) + threadIdx.x / G; row < n;
+       row += static_cast<int64_t>(gridDim.x) * (256 / G)) {
+    uint8_t* rec = write_to(a, row, bad);   // the group's lanes agree
+    if (!rec) continue;
+    const T* xr = x + row * a.row_stride;
+    for (int b = lane / 4; b < a.blocks; b += G / 4) {
+      const int at = b * kMxBlock + (lane & 3) * 8;
+      float v[8];
+      load8(xr + (at < a.dim ? at : 0), a.dim - at, v);
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t m = __float_as_uint(v[i]) & 0x7FFFFFFFu;
+        top = m > top ? m : top;
+      }
+      uint32_t o = __shfl_xor(top, 1, 4);
+      top = o > top ? o : top;
+      o = __shfl_xor(top, 2, 4);
+      top = o > top ? o : top;
+      const uint32_t code = mx_scale_code<BITS>(top);
+      uint32_t w[BITS / 4];
+      mx_pack8<BITS>(v, code, w);
+      __builtin_memcpy(rec + b * kCode + (lane & 3) * BITS, w, BITS);
+      if ((lane & 3) == 0) rec[a.blocks * kCode + b] = static_cast<uint8_t>(code);
+    }
+    for (int i = a.blocks * (kCode + 1) + lane; i < a.record; i += G) rec[i] = 0;
+  }
+  if (bad) raise_status(a.status, GMB_STATUS_ERANGE);
+}
+
+template <typename T, int BITS>
+__global__ __launch_bounds__(256) void k_mx_write_cols(MxWriteArgs a) {
+  constexpr int kCode = 4 * BITS;
+  const int64_t n = row_count(a.n_dev, a.n_cap);
+  const T* x = static_cast<const T*>(a.x);
+  const int b = blockIdx.y;
+  bool bad = false;
+  for (int64_t row = static_cast<int64_t>(blockIdx.x) * 64 + (threadIdx.x & 63); row < n;
+       row += static_cast<int64_t>(gridDim.x) * 64) {
+    uint8_t* rec = write_to(a, row, bad);
+    if (!rec) continue;
+    const T* xr = x + row * a.row_stride;
+    for (int blk = b * 4 + (threadIdx.x >> 6); blk < a.blocks; blk += 4 * gridDim.y) {
+      float v[kMxBlock];
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < kMxBlock; ++i) {
+        const int c = blk * kMxBlock + i;
+        v[i] = c < a.dim ? load1(xr + c * a.col_stride) : 0.f;
+        const uint32_t m = __float_as_uint(v[i]) & 0x7FFFFFFFu;
+        top = m > top ? m : top;
+      }
+      const uint32_t code = mx_scale_code<BITS>(top);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float u[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[i] = v[8 * q + i];
+        uint32_t w[BITS / 4];
+        mx_pack8<BITS>(u, code, w);
+        __builtin_memcpy(rec + blk * kCode + q * BITS, w, BITS);
+      }
+      rec[a.blocks * kCode + blk] = static_cast<uint8_t>(code);
+      if (blk == 0)
+        for (int i = a.blocks * (kCode + 1); i < a.record; ++i) rec[i] = 0;
+    }
+  }
+  if (bad) raise_status(a.status, GMB_STATUS_ERANGE);
+}
+
+// The vertex's slot takes the smallest of (2^31 - 1 - position) over the
+// rows written to it: the last row.  release: every slot empty again.
+__global__ __launch_bounds__(256) void k_mx_claim(const int32_t* ids, const int32_t* n_dev, int64_t n_cap,
+                                                  int64_t rows, uint32_t* slots, int release) {
+  const int64_t n = row_count(n_dev, n_cap);
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n;
+       i += static_cast<int64_t>(gridDim.x) * 256) {
+    const int32_t id = ids[i];
+    if (!valid_vertex(id, rows)) continue;
+    if (release)
+      slots[id] = kEmpty;
+    else
+      atomicMin(&slots[id], kEdgeTag - 1 - static_cast<uint32_t>(i));
+  }
+}
+
+// U rows of a group in flight; every load unconditional from a clamped
+// address (row 0 for a group without a row or with an id outside the table).
+template <typename T, int BITS, int G, int U>
+__global__ __launch_bounds__(256) void k_mx_read(MxReadArgs a) {
+  constexpr int kCode = 4 * BITS;
+  const int lane = threadIdx.x & (G - 1);
+  const int64_t n = row_count(a.n_dev, a.n_cap);
+  const int64_t stride = static_cast<int64_t>(gridDim.x) * (256 / G);
+  T* out = static_cast<T*>(a.out);
+  bool bad = false;
+  for (int64_t row = static_cast<int64_t>(blockIdx.x) * (256 / G) + threadIdx.x / G; row < n; row += stride * U) {
+    int64_t id[U];
+    bool in[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t r = row + u * stride;
+      id[u] = a.ids ? static_cast<int64_t>(a.ids[r < n ? r : row]) : r;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const bool here = row + u * stride < n, ok = id[u] >= 0 && id[u] < a.table_rows;
+      bad |= here & !ok;
+      in[u] = here & ok;
+      id[u] = in[u] ? id[u] : 0;
+    }
+    for (int b = lane / 4; b < a.blocks; b += G / 4) {
+      const int q = lane & 3, at = b * kMxBlock + q * 8;
+      uint32_t w[U][BITS / 4];
+      uint32_t code[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const uint8_t* rec = a.table + id[u] * a.table_stride;
+        __builtin_memcpy(w[u], rec + b * kCode + q * BITS, BITS);
+        code[u] = rec[a.blocks * kCode + b];
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t r = row + u * stride;
+        if (r >= n || at >= a.dim) continue;
+        float v[8];
+        mx_unpack8<BITS>(w[u], code[u], v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = in[u] ? v[i] : 0.f;
+        mx_store8(out + r * a.dim + at, v, a.dim - at);
+      }
+    }
+  }
+  if (bad) raise_status(a.status, GMB_STATUS_ERANGE);
+}
+
+// OUT: 0 fp32 rows, 1 bf16 rows, 2 records of 4 bits.  Lane l of a
+// destination's G lanes owns blocks l, l + G, ...; U neighbours in flight.
+// An id outside the table is read as row 0 (k_mean's rule).
+template <int BITS, int OUT, int G, int U>
+__global__ __launch_bounds__(256) void k_mx_mean(MxMeanArgs a) {
+  constexpr int kCode = 4 * BITS;
+  const int64_t row = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) / G;
+  const int lane = threadIdx.x & (G - 1);
+  const int64_t rc = row < a.n_cap ? row : a.n_cap - 1;
+  const int32_t beg = a.indptr[rc], end = a.indptr[rc + 1];
+  if (row >= row_count(a.n_dev, a.n_cap)) return;
+  const int32_t k = end - beg;
+  for (int b = lane; b < a.blocks; b += G) {
+    float acc[kMxBlock];
+#pragma unroll
+    for (int i = 0; i < kMxBlock; ++i) acc[i] = 0.f;
+    for (int32_t e = 0; e < k; e += U) {
+      int64_t id[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int32_t i = a.ids[beg + (e + u < k ? e + u : e)];
+        id[u] = valid_vertex(i, a.table_rows) ? i : 0;
+      }
+      uint4 w[U][BITS / 4];
+      uint32_t code[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const uint8_t* rec = a.table + id[u] * a.table_stride;
+        __builtin_memcpy(w[u], rec + b * kCode, kCode);
+        code[u] = rec[a.blocks * kCode + b];
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        // a slot past the row's end: zeros at scale 1 (adding +0 changes
+        // nothing)
+        const bool in = e + u < k;
+        const uint32_t c = in ? code[u] : 127u;
+        uint32_t words[BITS];
+        __builtin_memcpy(words, w[u], kCode);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          uint32_t part[BITS / 4];
+#pragma unroll
+          for (int j = 0; j < BITS / 4; ++j) part[j] = in ? words[q * (BITS / 4) + j] : 0u;
+          float v[8];
+          mx_unpack8<BITS>(part, c, v);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) acc[8 * q + i] += v[i];
+        }
+      }
+    }
+    if (k > 0) {
+      const float kf = static_cast<float>(k);
+#pragma unroll
+      for (int i = 0; i < kMxBlock; ++i) acc[i] = acc[i] / kf;
+    }
+    if constexpr (OUT == 2) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < kMxBlock; ++i) {
+        const uint32_t m = __float_as_uint(acc[i]) & 0x7FFFFFFFu;
+        top = m > top ? m : top;
+      }
+      const uint32_t code = mx_scale_code<4>(top);
+      uint8_t* rec = static_cast<uint8_t*>(a.out) + row * a.out_stride;
+      uint32_t w[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = acc[8 * q + i];
+        uint32_t part[1];
+        mx_pack8<4>(v, code, part);
+        w[q] = part[0];
+      }
+      __builtin_memcpy(rec + b * 16, w, 16);
+      rec[a.blocks * 16 + b] = static_cast<uint8_t>(code);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int at = b * kMxBlock + 8 * q;
+        if (at >= a.dim) break;
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = acc[8 * q + i];
+        if constexpr (OUT == 0)
+          mx_store8(static_cast<float*>(a.out) + row * a.dim + at, v, a.dim - at);
+        else
+          mx_store8(static_cast<uint16_t*>(a.out) + row * a.dim + at, v, a.dim - at);
+      }
+    }
+  }
+  if constexpr (OUT == 2) {
+    uint8_t* rec = static_cast<uint8_t*>(a.out) + row * a.out_stride;
+    for (int i = a.blocks * 17 + lane; i < a.out_record; i += G) rec[i] = 0;
+  }
+}
+
+unsigned grid_for(int64_t rows, int64_t per_block) {
+  int64_t g = (rows + per_block - 1) / per_block;
+  g = g < 1 ? 1 : (g > kMaxGrid ? kMaxGrid : g);
+  return static_cast<unsigned>(g);
+}
+
+// lanes of a row: a power of two that holds `units`, lo .. 64
+int lanes_for(int units, int lo) {
+  int g = lo;
+  while (g < 64 && g < units) g *= 2;
+  return g;
+}
+
+template <typename T, int BITS>
+void write_dispatch(const MxWriteArgs& a, hipStream_t s) {
+  if (a.col_stride != 1) {
+    const unsigned gy = static_cast<unsigned>(a.blocks < 4 * 64 ? (a.blocks + 3) / 4 : 64);
+    hipLaunchKernelGGL((k_mx_write_cols<T, BITS>), dim3(grid_for(a.n_cap, 64), gy), dim3(256), 0, s, a);
+    return;
+  }
+#define GMB_MX_WRITE(GG) hipLaunchKernelGGL((k_mx_write<T, BITS, GG>), dim3(grid_for(a.n_cap, 256 / GG)), dim3(256), 0, s, a)
+  switch (lanes_for(4 * a.blocks, 4)) {
+    case 4: GMB_MX_WRITE(4); break;
+    case 8: GMB_MX_WRITE(8); break;
+    case 16: GMB_MX_WRITE(16); break;
+    case 32: GMB_MX_WRITE(32); break;
+    default: GMB_MX_WRITE(64); break;
+  }
+#undef GMB_MX_WRITE
+}
+
+template <typename T, int BITS>
+void read_dispatch(const MxReadArgs& a, hipStream_t s) {
+  constexpr int U = 4;
+#define GMB_MX_READ(GG) hipLaunchKernelGGL((k_mx_read<T, BITS, GG, U>), dim3(grid_for(a.n_cap, (256 / GG) * U)), dim3(256), 0, s, a)
+  switch (lanes_for(4 * a.blocks, 4)) {
+    case 4: GMB_MX_READ(4); break;
+    case 8: GMB_MX_READ(8); break;
+    case 16: GMB_MX_READ(16); break;
+    case 32: GMB_MX_READ(32); break;
+    default: GMB_MX_READ(64); break;
+  }
+#undef GMB_MX_READ
+}
+
+template <int BITS, int OUT>
+void mean_dispatch(const MxMeanArgs& a, hipStream_t s) {
+  constexpr int U = BITS == 4 ? 16 : 8;
+  const int g = lanes_for(a.blocks, 1);
+  const dim3 grid(static_cast<unsigned>((a.n_cap * g + 255) / 256));
+#define GMB_MX_MEAN(GG) hipLaunchKernelGGL((k_mx_mean<BITS, OUT, GG, U>), grid, dim3(256), 0, s, a)
+  switch (g) {
+    case 1: GMB_MX_MEAN(1); break;
+    case 2: GMB_MX_MEAN(2); break;
+    case 4: GMB_MX_MEAN(4); break;
+    case 8: GMB_MX_MEAN(8); break;
+    case 16: GMB_MX_MEAN(16); break;
+    case 32: GMB_MX_MEAN(32); break;
+    default: GMB_MX_MEAN(64); break;
+  }
+#undef GMB_MX_MEAN
+}
+
+}  // namespace
+
+hipError_t launch_mx_write(const MxWriteArgs& args, int bf16, int bits, uint32_t* slots, hipStream_t s) {
+  MxWriteArgs a = args;
+  a.slots = a.ids ? slots : nullptr;
+  if (a.slots)
+    hipLaunchKernelGGL(k_mx_claim, dim3(grid_for(a.n_cap, 256)), dim3(256), 0, s, a.ids, a.n_dev, a.n_cap,
+                       a.table_rows, slots, 0);
+  if (bits == 4) {
+    if (bf16) write_dispatch<uint16_t, 4>(a, s);
+    else write_dispatch<float, 4>(a, s);
+  } else {
+    if (bf16) write_dispatch<uint16_t, 8>(a, s);
+    else write_dispatch<float, 8>(a, s);
+  }
+  if (a.slots)
+    hipLaunchKernelGGL(k_mx_claim, dim3(grid_for(a.n_cap, 256)), dim3(256), 0, s, a.ids, a.n_dev, a.n_cap,
+                       a.table_rows, slots, 1);
+  return hipGetLastError();
+}
+
+hipError_t launch_mx_read(const MxReadArgs& a, int bf16, int bits, hipStream_t s) {
+  if (bits == 4) {
+    if (bf16) read_dispatch<uint16_t, 4>(a, s);
+    else read_dispatch<float, 4>(a, s);
+  } else {
+    if (bf16) read_dispatch<uint16_t, 8>(a, s);
+    else read_dispatch<float, 8>(a, s);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_mx_mean(const MxMeanArgs& a, int bits, int out, hipStream_t s) {
+  if (bits == 4) {
+    if (out == kMxOutRecords) mean_dispatch<4, 2>(a, s);
+    else if (out == kMxOutBf16) mean_dispatch<4, 1>(a, s);
+    else mean_dispatch<4, 0>(a, s);
+  } else {
+    if (out == kMxOutRecords) mean_dispatch<8, 2>(a, s);
+    else if (out == kMxOutBf16) mean_dispatch<8, 1>(a, s);
+    else mean_dispatch<8, 0>(a, s);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace gmb
