@@ -16,10 +16,12 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef int intx4 __attribute__((ext_vector_type(4)));
 typedef int intx8 __attribute__((ext_vector_type(8)));
 
+// Byte SEL of ws and as is the scale.  The 4-bit format (4) reads the first
+// four words of an operand.
+template <int SEL = 0>
 __device__ __forceinline__ floatx4 mfma_mx4(const intx4& w, uint32_t ws, const intx4& a, uint32_t as, floatx4 c) {
-  // the 4-bit format (4) reads the first four words of an operand
   const intx8 w8 = {w[0], w[1], w[2], w[3], 0, 0, 0, 0}, a8 = {a[0], a[1], a[2], a[3], 0, 0, 0, 0};
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w8, a8, c, 4, 4, 0, static_cast<int>(ws), 0,
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w8, a8, c, 4, 4, SEL, static_cast<int>(ws), SEL,
                                                           static_cast<int>(as));
 }
 
@@ -224,6 +226,152 @@ __global__ __launch_bounds__(64 * WC * WK) void k_mx_linear(MxLinearArgs p) {
   if (c0 < p.d_out) epilogue<RT, CT, OUT>(p, n, r0, c0, lane, acc);
 }
 
+// ---- products that the matrix cores bound ---------------------------------
+
+// A workgroup of eight waves has 256 rows and 256 columns; wave (wr, wc) of
+// 2 x 4 has 128 rows and 64 columns of them.  The sum goes in stages of eight
+// blocks (256 elements); two stages are in LDS, one being read and one
+// arriving (global_load_lds: no registers in between).
+//   LDS, elements: a fragment is 16 rows by 4 blocks in the order that one
+//   load instruction leaves it, slot 16 g' + r for block 4 f + g' of row r;
+//   fragments (16-row tile t, half f) at 1 KB each, 32 a side and stage.
+//   Scales: 8 bytes a row and stage.
+// Step s of a stage takes block 2 g + s for lane group g, so that a lane's two
+// scales are neighbours (one 16-bit read, the byte picked by the
+// instruction's selector).  Blocks past the row's end and rows without a
+// record load zeros from kZeros.
+constexpr int kBigTile = 256;
+constexpr int kBigSide = 32 * 1024;               // element bytes of a side and stage
+constexpr int kBigScales = kBigTile * 8;
+constexpr int kBigStage = 2 * (kBigSide + kBigScales);
+
+__device__ __align__(16) const uint32_t kZeros[4] = {0, 0, 0, 0};
+
+__device__ __forceinline__ void load_lds(const void* g, void* l, int bytes) {
+  typedef const __attribute__((address_space(1))) void* gp;
+  typedef __attribute__((address_space(3))) void* lp;
+  if (bytes == 16)
+    __builtin_amdgcn_global_load_lds((gp)g, (lp)l, 16, 0, 0);
+  else
+    __builtin_amdgcn_global_load_lds((gp)g, (lp)l, 4, 0, 0);
+}
+
+struct BigRows {
+  const uint8_t* rec[4];    // the lane's row of four of the wave's 16-row tiles (NULL: none)
+  const uint8_t* scales[2]; // the lane's row of two of the wave's scale loads
+};
+
+// Loads stage k of one side: wave `w` of eight brings tiles 4 (w % 4) ..
+// + 3 of side w / 4, and the scales of rows 64 (w % 4) .. + 63.
+__device__ __forceinline__ void big_load(const BigRows& r, int k, int blocks, uint8_t* elems, uint8_t* scales, int tile0,
+                                         int row0, int lane) {
+  const int g = lane >> 4;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int f = 0; f < 2; ++f) {
+      const int b = 8 * k + 4 * f + g;
+      const void* at = r.rec[i] && b < blocks ? static_cast<const void*>(r.rec[i] + b * 16) : kZeros;
+      load_lds(at, elems + ((tile0 + i) * 2 + f) * 1024, 16);
+    }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int b = 8 * k + 4 * (lane & 1);
+    const int last = (blocks - 1) & ~3;           // (scales of no block belong to zeros)
+    const void* at = r.scales[i] ? static_cast<const void*>(r.scales[i] + (b < blocks ? b : last)) : kZeros;
+    load_lds(at, scales + (row0 + 32 * i) * 8, 4);
+  }
+}
+
+template <int OUT>
+__global__ __launch_bounds__(512, 2) void k_mx_linear_big(MxLinearArgs p, int gm, int gn) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * kBigStage];
+  int64_t n = p.n_cap;
+  if (p.n_dev) {
+    const int64_t m = load_size(p.n_dev);
+    n = m < 0 ? 0 : (m < n ? m : n);
+  }
+  // workgroup ids go round the eight XCDs: each takes a contiguous run of
+  // tiles, eight row tiles wide, so that its L2 holds what they share
+  const int tiles = gm * gn, per = (tiles + 7) / 8;
+  const int id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  if (id >= tiles) return;
+  const int band = id / (8 * gn), in_band = id - band * 8 * gn;
+  const int height = gm - 8 * band < 8 ? gm - 8 * band : 8;
+  const int64_t r0 = static_cast<int64_t>(8 * band + in_band % height) * kBigTile;
+  const int c0 = in_band / height * kBigTile;
+  if (r0 >= n) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int wr = wave >> 2, wc = wave & 3, g = lane >> 4;
+  const int side = wave >> 2, quarter = wave & 3;
+  const int stages = (p.blocks + 7) / 8;
+  floatx4 acc[8][4];
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+  for (int pr = 0; pr < p.pairs; ++pr) {
+    const MxPair& m = p.pair[pr];
+    BigRows rows;
+    auto record = [&](int r) -> const uint8_t* {   // row r of the tile on this wave's side
+      if (side == 0) {
+        const int64_t row = r0 + r < n ? r0 + r : n - 1;
+        if (!m.ids) return m.a + row * m.a_stride;
+        const int32_t v = m.ids[row];
+        if (valid_vertex(v, m.a_rows)) return m.a + v * m.a_stride;
+        raise_status(p.status, GMB_STATUS_ERANGE);
+        return nullptr;
+      }
+      const int c = c0 + r < p.d_out ? c0 + r : p.d_out - 1;
+      return m.w + static_cast<int64_t>(c) * m.w_stride;
+    };
+#pragma unroll
+    for (int i = 0; i < 4; ++i) rows.rec[i] = record(64 * quarter + 16 * i + (lane & 15));
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint8_t* q = record(64 * quarter + 32 * i + lane / 2);
+      rows.scales[i] = q ? q + p.blocks * 16 : nullptr;
+    }
+    auto fetch = [&](int k, int buf) {
+      uint8_t* base = lds + buf * kBigStage + side * (kBigSide + kBigScales);
+      big_load(rows, k, p.blocks, base, base + kBigSide, 4 * quarter, 64 * quarter, lane);
+    };
+    __syncthreads();            // the last pair's reads
+    fetch(0, 0);
+    __syncthreads();
+    for (int k = 0; k < stages; ++k) {
+      const uint8_t* la = lds + (k & 1) * kBigStage;
+      const uint8_t* lw = la + kBigSide + kBigScales;
+      if (k + 1 < stages) fetch(k + 1, (k + 1) & 1);
+      uint32_t sa[8], sw[4];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        sa[i] = *reinterpret_cast<const uint16_t*>(la + kBigSide + (wr * 128 + 16 * i + (lane & 15)) * 8 + 2 * g);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        sw[j] = *reinterpret_cast<const uint16_t*>(lw + kBigSide + (wc * 64 + 16 * j + (lane & 15)) * 8 + 2 * g);
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const int at = (g >> 1) * 1024 + (2 * (g & 1) + s) * 256 + (lane & 15) * 16;
+        intx4 qa[8], qw[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) qw[j] = *reinterpret_cast<const intx4*>(lw + (wc * 4 + j) * 2048 + at);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) qa[i] = *reinterpret_cast<const intx4*>(la + (wr * 8 + i) * 2048 + at);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            acc[i][j] = s == 0 ? mfma_mx4<0>(qw[j], sw[j], qa[i], sa[i], acc[i][j])
+                               : mfma_mx4<1>(qw[j], sw[j], qa[i], sa[i], acc[i][j]);
+      }
+      __syncthreads();          // stage k is read, stage k + 1 has arrived
+    }
+  }
+  const int cw = c0 + 64 * wc;
+  if (cw < p.d_out) epilogue<8, 4, OUT>(p, n, r0 + 128 * wr, cw, lane, acc);
+}
+
 template <int RT, int CT, int WC, int WK, int OUT>
 void run(const MxLinearArgs& p, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>((p.n_cap + 16 * RT - 1) / (16 * RT)),
@@ -234,7 +382,11 @@ void run(const MxLinearArgs& p, hipStream_t s) {
 template <int OUT>
 void dispatch(const MxLinearArgs& p, hipStream_t s) {
   const int64_t tiles = ((p.n_cap + 63) / 64) * ((p.d_out + 63) / 64);
-  if (tiles >= 1024) {
+  const int64_t big = ((p.n_cap + kBigTile - 1) / kBigTile) * ((p.d_out + kBigTile - 1) / kBigTile);
+  if (big >= 128 && p.blocks >= 16 && p.d_out > 128) {
+    const int gm = static_cast<int>((p.n_cap + kBigTile - 1) / kBigTile), gn = (p.d_out + kBigTile - 1) / kBigTile;
+    hipLaunchKernelGGL((k_mx_linear_big<OUT>), dim3((gm * gn + 7) / 8 * 8), dim3(512), 0, s, p, gm, gn);
+  } else if (tiles >= 1024) {
     if (p.d_out > 128) run<4, 4, 4, 1, OUT>(p, s);
     else if (p.d_out > 64) run<4, 4, 2, 1, OUT>(p, s);
     else run<4, 4, 1, 1, OUT>(p, s);
