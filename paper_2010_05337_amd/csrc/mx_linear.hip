@@ -1,10 +1,25 @@
 // The product of microscaled 4-bit rows and weights on gfx950:
 // out = act(A W^T [+ A2 W2^T] + b) with v_mfma_scale_f32_16x16x128_f8f6f4,
-// which takes 16 x 128 elements of each side with a scale for every 32 of a
-// row and sums in fp32.  A row's record is what a lane wants as it is: lane l
-// of a wave supplies row l % 16 and the 32 elements of block 4 s + l / 16 of
-// step s, 16 bytes and a scale byte.  The weights are the instruction's first
-// operand, so that a lane holds four neighbouring output columns of one row.
+// which takes 16 rows of 128 elements of each side, a scale for every 32
+// elements of a row, and sums in fp32.  Lane l = 16 g + r of a wave supplies
+// row r of its side, the 32 elements (16 bytes) of one of the four blocks and
+// that block's scale byte; which blocks of the sum make up a step is free as
+// long as both sides agree.  Accumulator register e of lane (g, r) is row
+// 4 g + e of A and row r of W.  W's rows are dealt to the tiles of a wave so
+// that a lane's CT column tiles are CT neighbouring columns: it stores them at
+// once, and the lanes of a row store one contiguous piece.
+//
+//   k_mx_linear_rows      few rows: the waves of a workgroup split the sum
+//   k_mx_linear_resident  short sums, many rows: the weights' whole records
+//                         stay in LDS while the workgroup goes over row tiles
+//   k_mx_linear_tiles     the rest: tiles of both sides in stages through LDS
+//
+// Loads: the vector memory unit takes neighbouring lanes' pieces of one
+// 64-byte segment together, and a lane alone otherwise.  An operand read
+// straight into its lanes (neighbouring lanes, different rows) is 64 accesses
+// a kilobyte; the LDS kernels therefore load four neighbouring lanes a row (16
+// accesses) and take the operands' order when they read LDS.  (8192 x 4096 x
+// 4096, LDS filled in operand order: 125 us.)
 #include "mx.hpp"
 #include "mx_kernels.hpp"
 
@@ -16,144 +31,341 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef int intx4 __attribute__((ext_vector_type(4)));
 typedef int intx8 __attribute__((ext_vector_type(8)));
 
-// Byte SEL of ws and as is the scale.  The 4-bit format (4) reads the first
+// Byte SEL of as and ws is the scale.  The 4-bit format (4) reads the first
 // four words of an operand.
 template <int SEL = 0>
-__device__ __forceinline__ floatx4 mfma_mx4(const intx4& w, uint32_t ws, const intx4& a, uint32_t as, floatx4 c) {
-  const intx8 w8 = {w[0], w[1], w[2], w[3], 0, 0, 0, 0}, a8 = {a[0], a[1], a[2], a[3], 0, 0, 0, 0};
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w8, a8, c, 4, 4, SEL, static_cast<int>(ws), SEL,
-                                                          static_cast<int>(as));
+__device__ __forceinline__ floatx4 mfma_mx4(const intx4& a, uint32_t as, const intx4& w, uint32_t ws, floatx4 c) {
+  const intx8 a8 = {a[0], a[1], a[2], a[3], 0, 0, 0, 0}, w8 = {w[0], w[1], w[2], w[3], 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, w8, c, 4, 4, SEL, static_cast<int>(as), SEL,
+                                                          static_cast<int>(ws));
 }
 
-// One row's block for a lane: its elements and its scale, zeros at scale 1
-// past the row's last block.
-__device__ __forceinline__ void load_block(const uint8_t* rec, int blk, int blocks, intx4& q, uint32_t& sc) {
-  const bool in = blk < blocks;
-  const int b = in ? blk : 0;
-  __builtin_memcpy(&q, rec + b * 16, 16);
-  sc = rec[blocks * 16 + b];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) q[i] = in ? q[i] : 0;
-  sc = in ? sc : 127u;
+// What rows without a record, and blocks past a row's last, are loaded from.
+__device__ __align__(16) const uint32_t kZeros[4] = {0, 0, 0, 0};
+
+// 16 bytes a lane from global memory to LDS, at l + 16 lane.
+__device__ __forceinline__ void load_lds(const void* g, void* l) {
+  typedef const __attribute__((address_space(1))) void* gp;
+  typedef __attribute__((address_space(3))) void* lp;
+  __builtin_amdgcn_global_load_lds((gp)g, (lp)l, 16, 0, 0);
 }
 
-// Bias, activation and the store of one lane's four columns c .. c + 3 of
-// `row`, fp32 or bf16.
-template <int OUT>
-__device__ __forceinline__ void store4(const MxLinearArgs& p, int64_t row, int c, const float (&z)[4]) {
+__device__ __forceinline__ int64_t count_rows(const MxLinearArgs& p) {
+  if (!p.n_dev) return p.n_cap;
+  const int64_t m = load_size(p.n_dev);
+  return m < 0 ? 0 : (m < p.n_cap ? m : p.n_cap);
+}
+
+// Row `row` (< n) of a pair's A: its record, or NULL for an id outside the
+// table, which is reported.
+__device__ __forceinline__ const uint8_t* a_record(const MxLinearArgs& p, const MxPair& m, int64_t row) {
+  if (!m.ids) return m.a + row * m.a_stride;
+  const int32_t v = m.ids[row];
+  if (valid_vertex(v, m.a_rows)) return m.a + v * m.a_stride;
+  raise_status(p.status, GMB_STATUS_ERANGE);
+  return nullptr;
+}
+// Output column c's weights (the last column's past it: never stored).
+__device__ __forceinline__ const uint8_t* w_record(const MxLinearArgs& p, const MxPair& m, int c) {
+  return m.w + static_cast<int64_t>(c < p.d_out ? c : p.d_out - 1) * m.w_stride;
+}
+
+// CT neighbouring values of a row, from column c on.
+template <int OUT, int CT>
+__device__ __forceinline__ void store_values(const MxLinearArgs& p, int64_t row, int c, const float (&z)[CT]) {
+  const int left = p.d_out - c;
   if constexpr (OUT == kMxOutF32) {
     float* o = static_cast<float*>(p.out) + row * p.d_out + c;
-    if (c + 4 <= p.d_out) {
-      const float4 v = make_float4(z[0], z[1], z[2], z[3]);
-      __builtin_memcpy(o, &v, 16);
+    if (left >= CT) {
+      __builtin_memcpy(o, z, 4 * CT);
     } else {
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if (c + r < p.d_out) o[r] = z[r];
+      for (int j = 0; j < CT; ++j)
+        if (j < left) o[j] = z[j];
     }
   } else {
     uint16_t* o = static_cast<uint16_t*>(p.out) + row * p.d_out + c;
-    const uint2 v = make_uint2(mx_bf16x2_bits(z[0], z[1]), mx_bf16x2_bits(z[2], z[3]));
-    if (c + 4 <= p.d_out) {
-      __builtin_memcpy(o, &v, 8);
-    } else {
-      const uint32_t w[2] = {v.x, v.y};
+    uint32_t w[CT / 2];
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if (c + r < p.d_out) o[r] = static_cast<uint16_t>(w[r / 2] >> (16 * (r & 1)));
+    for (int j = 0; j < CT / 2; ++j) w[j] = mx_bf16x2_bits(z[2 * j], z[2 * j + 1]);
+    if (left >= CT) {
+      __builtin_memcpy(o, w, 2 * CT);
+    } else {
+#pragma unroll
+      for (int j = 0; j < CT; ++j)
+        if (j < left) o[j] = static_cast<uint16_t>(w[j / 2] >> (16 * (j & 1)));
     }
   }
 }
 
-__device__ __forceinline__ void finish4(const MxLinearArgs& p, int c, const floatx4& acc, float (&z)[4]) {
+// CT values of a row as elements of its output record: 32 / CT lanes hold a
+// block.  Every lane takes part (its values are 0 past d_out).
+template <int CT>
+__device__ __forceinline__ void store_elements(const MxLinearArgs& p, bool in, int64_t row, int c,
+                                               const float (&z)[CT]) {
+  constexpr int LANES = 32 / CT;
+  const int blocks = (p.d_out + 31) / 32;
+  uint32_t top = 0;
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    z[r] = acc[r] + (p.bias && c + r < p.d_out ? p.bias[c + r] : 0.f);
-    if (p.relu) z[r] = z[r] > 0.f ? z[r] : 0.f;
+  for (int j = 0; j < CT; ++j) {
+    const uint32_t m = __float_as_uint(z[j]) & 0x7FFFFFFFu;
+    top = m > top ? m : top;
   }
+#pragma unroll
+  for (int o = 1; o < LANES; o <<= 1) {
+    const uint32_t x = __shfl_xor(top, o, 64);
+    top = x > top ? x : top;
+  }
+  const uint32_t code = mx_scale_code<4>(top);
+  float v[8] = {};
+#pragma unroll
+  for (int j = 0; j < CT; ++j) v[j] = z[j];
+  uint32_t w[1];
+  mx_pack8<4>(v, code, w);
+  const int blk = c / 32;
+  if (!in || blk >= blocks) return;
+  uint8_t* rec = static_cast<uint8_t*>(p.out) + row * p.out_stride;
+  __builtin_memcpy(rec + c / 2, w, CT / 2);
+  if (c % 32 == 0) rec[blocks * 16 + blk] = static_cast<uint8_t>(code);
+  if (blk == blocks - 1)
+    for (int b = blocks * 17 + (c % 32) / CT; b < p.out_record; b += LANES) rec[b] = 0;
 }
 
-// The epilogue of a wave's RT x CT tiles: rows r0 + 16 i + l % 16, columns
-// c0 + 16 j + 4 (l / 16) .. + 3.
+// Bias, activation and store of a wave's tiles: rows r0 + 16 i + 4 g + e,
+// columns c0 + CT r + j.
 template <int RT, int CT, int OUT>
 __device__ __forceinline__ void epilogue(const MxLinearArgs& p, int64_t n, int64_t r0, int c0, int lane,
                                          const floatx4 (&acc)[RT][CT]) {
-  const int g = lane >> 4;
-  if constexpr (OUT != kMxOutRecords) {
+  const int c = c0 + CT * (lane & 15);
+  float bias[CT];
 #pragma unroll
-    for (int i = 0; i < RT; ++i) {
-      const int64_t row = r0 + 16 * i + (lane & 15);
+  for (int j = 0; j < CT; ++j) bias[j] = p.bias && c + j < p.d_out ? p.bias[c + j] : 0.f;
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int64_t row = r0 + 16 * i + 4 * (lane >> 4) + e;
+      float z[CT];
 #pragma unroll
       for (int j = 0; j < CT; ++j) {
-        const int c = c0 + 16 * j + 4 * g;
-        if (row >= n || c >= p.d_out) continue;
-        float z[4];
-        finish4(p, c, acc[i][j], z);
-        store4<OUT>(p, row, c, z);
+        z[j] = acc[i][j][e] + bias[j];
+        if (p.relu) z[j] = z[j] > 0.f ? z[j] : 0.f;
+        if (OUT == kMxOutRecords && c + j >= p.d_out) z[j] = 0.f;
       }
+      if constexpr (OUT == kMxOutRecords)
+        store_elements<CT>(p, row < n, row, c, z);
+      else if (row < n && c < p.d_out)
+        store_values<OUT, CT>(p, row, c, z);
     }
-  } else {
-    // a record's block is two column tiles: eight values a lane, four lanes
-    const int blocks = (p.d_out + 31) / 32;
+}
+
+// ---- few rows -------------------------------------------------------------
+
+// A workgroup of WK waves has 16 RT rows and 16 CT columns; wave k takes the
+// units k, k + WK, ... of 16 blocks, of which lane group g has blocks 4 g ..
+// 4 g + 3 (one scale word); the waves' sums meet in LDS in a fixed order.
+template <int RT, int CT, int WK, int OUT>
+__global__ __launch_bounds__(64 * WK) void k_mx_linear_rows(MxLinearArgs p) {
+  const int lane = threadIdx.x & 63, wk = threadIdx.x >> 6, g = lane >> 4, r = lane & 15;
+  const int64_t n = count_rows(p);
+  const int64_t r0 = static_cast<int64_t>(blockIdx.x) * (16 * RT);
+  if (r0 >= n) return;
+  const int c0 = blockIdx.y * 16 * CT;
+  floatx4 acc[RT][CT];
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+#pragma unroll
+    for (int j = 0; j < CT; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+  const int units = (p.blocks + 15) / 16;
+  for (int pr = 0; pr < p.pairs; ++pr) {
+    const MxPair& m = p.pair[pr];
+    const uint8_t* rec[RT + CT];
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
-      const int64_t row = r0 + 16 * i + (lane & 15);
+      const int64_t row = r0 + 16 * i + r;
+      rec[i] = a_record(p, m, row < n ? row : n - 1);
+    }
 #pragma unroll
-      for (int j = 0; j < CT; j += 2) {
-        float v[8];
+    for (int j = 0; j < CT; ++j) rec[RT + j] = w_record(p, m, c0 + CT * r + j);
+    for (int u = wk; u < units; u += WK) {
+      const int b0 = 16 * u + 4 * g;
+      intx4 q[RT + CT][4];
+      uint32_t sc[RT + CT];
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const int c = c0 + 16 * (j + t) + 4 * g;
-          float z[4];
-          finish4(p, c, acc[i][j + t], z);
+      for (int i = 0; i < RT + CT; ++i) {
+        const uint8_t* some = reinterpret_cast<const uint8_t*>(kZeros);
+        // (a record is padded to 16 bytes, so the scale word of a block in it
+        // lies in it)
+        const uint8_t* at = rec[i] && b0 < p.blocks ? rec[i] + p.blocks * 16 + b0 : some;
+        __builtin_memcpy(&sc[i], at, 4);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) v[4 * t + r] = c + r < p.d_out ? z[r] : 0.f;
-        }
-        uint32_t top = 0;
-#pragma unroll
-        for (int r = 0; r < 8; ++r) {
-          const uint32_t m = __float_as_uint(v[r]) & 0x7FFFFFFFu;
-          top = m > top ? m : top;
-        }
-        uint32_t o = __shfl_xor(top, 16, 64);
-        top = o > top ? o : top;
-        o = __shfl_xor(top, 32, 64);
-        top = o > top ? o : top;
-        const uint32_t code = mx_scale_code<4>(top);
-        uint32_t w[1];
-        mx_pack8<4>(v, code, w);
-        const int blk = (c0 + 16 * j) / 32;
-        if (row < n && blk < blocks) {
-          uint8_t* rec = static_cast<uint8_t*>(p.out) + row * p.out_stride;
-          const uint16_t lo = static_cast<uint16_t>(w[0]), hi = static_cast<uint16_t>(w[0] >> 16);
-          __builtin_memcpy(rec + blk * 16 + 2 * g, &lo, 2);
-          __builtin_memcpy(rec + blk * 16 + 8 + 2 * g, &hi, 2);
-          if (g == 0) rec[blocks * 16 + blk] = static_cast<uint8_t>(code);
-          if (blk == blocks - 1)
-            for (int b = blocks * 17 + g; b < p.out_record; b += 4) rec[b] = 0;
+        for (int s = 0; s < 4; ++s) {
+          at = rec[i] && b0 + s < p.blocks ? rec[i] + (b0 + s) * 16 : some;
+          __builtin_memcpy(&q[i][s], at, 16);
         }
       }
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int j = 0; j < CT; ++j) {
+          acc[i][j] = mfma_mx4<0>(q[i][0], sc[i], q[RT + j][0], sc[RT + j], acc[i][j]);
+          acc[i][j] = mfma_mx4<1>(q[i][1], sc[i], q[RT + j][1], sc[RT + j], acc[i][j]);
+          acc[i][j] = mfma_mx4<2>(q[i][2], sc[i], q[RT + j][2], sc[RT + j], acc[i][j]);
+          acc[i][j] = mfma_mx4<3>(q[i][3], sc[i], q[RT + j][3], sc[RT + j], acc[i][j]);
+        }
     }
+  }
+  if constexpr (WK > 1) {
+    __shared__ floatx4 part[(WK - 1) * RT * CT * 64];
+    if (wk > 0) {
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int j = 0; j < CT; ++j) part[(((wk - 1) * RT + i) * CT + j) * 64 + lane] = acc[i][j];
+    }
+    __syncthreads();
+    if (wk > 0) return;
+#pragma unroll 1
+    for (int k = 0; k < WK - 1; ++k)
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int j = 0; j < CT; ++j) acc[i][j] += part[((k * RT + i) * CT + j) * 64 + lane];
+  }
+  epilogue<RT, CT, OUT>(p, n, r0, c0, lane, acc);
+}
+
+// ---- short sums, many rows ------------------------------------------------
+
+// A workgroup of WR x WC waves has 64 WC columns, whose whole records lie in
+// LDS from the start, and goes over tiles of 64 WR rows, whose records it
+// loads tile by tile (two workgroups a CU take turns).  In LDS a record is
+// `slots` 16-byte pieces, an odd number: sixteen rows' reads of one block
+// fall on different banks.
+constexpr int kResidentLds = 80 * 1024 - 64;
+
+__host__ __device__ inline int resident_slots(int blocks) { return (((blocks * 17 + 15) / 16) | 1); }
+__host__ __device__ inline int resident_bytes(int rows, int pairs, int blocks) {
+  return (rows * pairs * resident_slots(blocks) * 16 + 1023) / 1024 * 1024;
+}
+
+template <int WR, int WC, int OUT>
+__global__ __launch_bounds__(64 * WR * WC, 2) void k_mx_linear_resident(MxLinearArgs p, int tiles) {
+  constexpr int WAVES = WR * WC, ROWS = 64 * WR, COLS = 64 * WC;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kResidentLds];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, r = lane & 15;
+  const int wr = wave / WC, wc = wave % WC;
+  const int64_t n = count_rows(p);
+  const int c0 = blockIdx.y * COLS;
+  const int slots = resident_slots(p.blocks), pieces = (p.blocks * 17 + 15) / 16;
+  uint8_t* lw = lds;
+  uint8_t* la = lds + resident_bytes(COLS, p.pairs, p.blocks);
+  if (static_cast<int64_t>(blockIdx.x) * ROWS >= n) return;
+  // `count` records (record q of them at q * slots pieces) by 64 pieces a load
+  auto bring = [&](uint8_t* to, int count, auto&& record) {
+    const int total = count * slots;
+    for (int q0 = 64 * wave; q0 < total; q0 += 64 * WAVES) {
+      const int q = q0 + lane, at = q / slots, piece = q - at * slots;
+      const uint8_t* rec = at < count ? record(at) : nullptr;
+      load_lds(rec && piece < pieces ? static_cast<const void*>(rec + piece * 16) : kZeros, to + q0 * 16);
+    }
+  };
+  bring(lw, p.pairs * COLS, [&](int at) {
+    // LDS order: 16-column tile j of 64 columns has columns 4 r + j
+    const MxPair& m = p.pair[at / COLS];
+    const int i = at % COLS;
+    return w_record(p, m, c0 + (i & ~63) + 4 * (i & 15) + ((i >> 4) & 3));
+  });
+  const int steps = (p.blocks + 3) / 4;
+  for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
+    const int64_t r0 = static_cast<int64_t>(t) * ROWS;
+    if (r0 >= n) break;
+    bring(la, p.pairs * ROWS, [&](int at) -> const uint8_t* {
+      const int64_t row = r0 + at % ROWS;
+      return row < n ? a_record(p, p.pair[at / ROWS], row) : nullptr;
+    });
+    __syncthreads();            // what was loaded has arrived
+    floatx4 acc[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int pr = 0; pr < p.pairs; ++pr) {
+      const uint8_t* ra = la + (pr * ROWS + 64 * wr + r) * slots * 16;
+      const uint8_t* rw = lw + (pr * COLS + 64 * wc + r) * slots * 16;
+      for (int s = 0; s < steps; ++s) {
+        const int b = 4 * s + g;
+        const bool in = b < p.blocks;
+        const int at = in ? b : 0;
+        intx4 qa[4], qw[4];
+        uint32_t sa[4], sw[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint8_t* x = ra + i * 16 * slots * 16;
+          qa[i] = *reinterpret_cast<const intx4*>(x + at * 16);
+          sa[i] = x[p.blocks * 16 + at];
+          const uint8_t* y = rw + i * 16 * slots * 16;
+          qw[i] = *reinterpret_cast<const intx4*>(y + at * 16);
+          sw[i] = y[p.blocks * 16 + at];
+        }
+        if (4 * s + 4 > p.blocks) {
+          // a block past the last: zeros on one side, and no scale that is
+          // not a number
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) qa[i][e] = in ? qa[i][e] : 0;
+            sa[i] = in ? sa[i] : 127u;
+            sw[i] = in ? sw[i] : 127u;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[i][j] = mfma_mx4<0>(qa[i], sa[i], qw[j], sw[j], acc[i][j]);
+      }
+    }
+    __syncthreads();            // the rows are read
+    if (c0 + 64 * wc < p.d_out) epilogue<4, 4, OUT>(p, n, r0 + 64 * wr, c0 + 64 * wc, lane, acc);
   }
 }
 
-// A workgroup of WC x WK waves: wave (wc, wk) has the 16 RT rows of the
-// workgroup, columns [16 CT (WC y + wc), + 16 CT), and the steps wk, wk + WK,
-// ... of the sum; the WK sums meet in LDS in a fixed order.
-template <int RT, int CT, int WC, int WK, int OUT>
-__global__ __launch_bounds__(64 * WC * WK) void k_mx_linear(MxLinearArgs p) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int wc = wave % WC, wk = wave / WC;
-  int64_t n = p.n_cap;
-  if (p.n_dev) {
-    const int64_t m = load_size(p.n_dev);
-    n = m < 0 ? 0 : (m < n ? m : n);
-  }
-  const int64_t r0 = static_cast<int64_t>(blockIdx.x) * (16 * RT);
+// ---- tiles through LDS ----------------------------------------------------
+
+// A workgroup of WM x WN waves has TM rows and TN columns, a wave TM / WM by
+// TN / WN of them.  The sum goes in stages of eight blocks (256 elements); two
+// stages are in LDS, one being read and one arriving straight from global
+// memory.
+//   Elements: 16 rows by four blocks are 1 KB, filled by one load, lane l
+//   bringing row l / 4; piece (row, x) of them holds block x ^ swizzle(row),
+//   so that the reads of sixteen rows' block fall on different banks.
+//   Scales: 16 bytes a row, for two stages, one lane a row.
+// Step s of a stage takes block 2 g + s for lane group g: a lane's two scales
+// are neighbours (one 16-bit read, the byte picked by the instruction).
+__device__ __forceinline__ int tile_swizzle(int r) { return ((r >> 1) & 3) ^ (r >> 3); }
+
+template <int TM, int TN, int WM, int WN, int OUT>
+__global__ __launch_bounds__(64 * WM * WN, 2) void k_mx_linear_tiles(MxLinearArgs p, int gm, int gn) {
+  constexpr int WAVES = WM * WN, T16 = (TM + TN) / 16, PER = T16 / WAVES;   // 16-row loads, of a wave
+  constexpr int RT = TM / WM / 16, CT = TN / WN / 16;
+  constexpr int SLOADS = ((TM + TN) / 64 + WAVES - 1) / WAVES;   // scale loads of a wave, 64 rows each
+  static_assert(T16 % WAVES == 0 && CT == 4 && TM % 64 == 0 && TN % 64 == 0, "tile");
+  constexpr int kStage = T16 * 2048, kScales = (TM + TN) * 16;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * (kStage + kScales)];
+  const int64_t n = count_rows(p);
+  // workgroup ids go round the eight XCDs: each takes a contiguous run of
+  // tiles, eight row tiles wide, so that its L2 holds what they share
+  const int tiles = gm * gn, per = (tiles + 7) / 8;
+  const int id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  if ((blockIdx.x >> 3) >= per || id >= tiles) return;
+  const int band = id / (8 * gn), in_band = id - band * 8 * gn;
+  const int height = gm - 8 * band < 8 ? gm - 8 * band : 8;
+  const int64_t r0 = static_cast<int64_t>(8 * band + in_band % height) * TM;
+  const int c0 = in_band / height * TN;
   if (r0 >= n) return;
-  const int c0 = (blockIdx.y * WC + wc) * 16 * CT;
-  const int g = lane >> 4;
-  const int steps = (p.blocks + 3) / 4;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int wr = wave / WN, wc = wave % WN, g = lane >> 4, r = lane & 15;
+  const int stages = (p.blocks + 7) / 8;
   floatx4 acc[RT][CT];
 #pragma unroll
   for (int i = 0; i < RT; ++i)
@@ -161,239 +373,130 @@ __global__ __launch_bounds__(64 * WC * WK) void k_mx_linear(MxLinearArgs p) {
     for (int j = 0; j < CT; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
   for (int pr = 0; pr < p.pairs; ++pr) {
     const MxPair& m = p.pair[pr];
-    const uint8_t* ra[RT];
-    bool ok[RT];
-#pragma unroll
-    for (int i = 0; i < RT; ++i) {
-      const int64_t row = r0 + 16 * i + (lane & 15);
-      const int64_t rc = row < n ? row : n - 1;
-      int64_t at = rc;
-      ok[i] = true;
-      if (m.ids) {
-        const int32_t id = m.ids[rc];
-        ok[i] = valid_vertex(id, m.a_rows);
-        if (!ok[i] && wave == 0 && blockIdx.y == 0) raise_status(p.status, GMB_STATUS_ERANGE);
-        at = ok[i] ? id : 0;
-      }
-      ra[i] = m.a + at * m.a_stride;
-    }
-    const uint8_t* rw[CT];
-#pragma unroll
-    for (int j = 0; j < CT; ++j) {
-      const int c = c0 + 16 * j + (lane & 15);
-      rw[j] = m.w + static_cast<int64_t>(c < p.d_out ? c : p.d_out - 1) * m.w_stride;
-    }
-    for (int s = wk; s < steps; s += WK) {
-      intx4 qa[RT], qw[CT];
-      uint32_t sa[RT], sw[CT];
-#pragma unroll
-      for (int i = 0; i < RT; ++i) load_block(ra[i], 4 * s + g, p.blocks, qa[i], sa[i]);
-#pragma unroll
-      for (int j = 0; j < CT; ++j) load_block(rw[j], 4 * s + g, p.blocks, qw[j], sw[j]);
-#pragma unroll
-      for (int i = 0; i < RT; ++i)
-#pragma unroll
-        for (int j = 0; j < CT; ++j) acc[i][j] = mfma_mx4(qw[j], sw[j], qa[i], sa[i], acc[i][j]);
-    }
-    // a row whose id is outside the table counts as zeros (only the first
-    // pair has ids, so what is summed so far is that row's)
-    if (m.ids) {
-#pragma unroll
-      for (int i = 0; i < RT; ++i)
-#pragma unroll
-        for (int j = 0; j < CT; ++j)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) acc[i][j][r] = ok[i] ? acc[i][j][r] : 0.f;
-    }
-  }
-  if constexpr (WK > 1) {
-    __shared__ floatx4 part[(WK - 1) * WC * RT * CT * 64];
-    if (wk > 0) {
-#pragma unroll
-      for (int i = 0; i < RT; ++i)
-#pragma unroll
-        for (int j = 0; j < CT; ++j)
-          part[((((wk - 1) * WC + wc) * RT + i) * CT + j) * 64 + lane] = acc[i][j];
-    }
-    __syncthreads();
-    if (wk > 0) return;
-#pragma unroll
-    for (int i = 0; i < RT; ++i)
-#pragma unroll
-      for (int j = 0; j < CT; ++j)
-        for (int k = 0; k < WK - 1; ++k) acc[i][j] += part[(((k * WC + wc) * RT + i) * CT + j) * 64 + lane];
-  }
-  if (c0 < p.d_out) epilogue<RT, CT, OUT>(p, n, r0, c0, lane, acc);
-}
-
-// ---- products that the matrix cores bound ---------------------------------
-
-// A workgroup of eight waves has 256 rows and 256 columns; wave (wr, wc) of
-// 2 x 4 has 128 rows and 64 columns of them.  The sum goes in stages of eight
-// blocks (256 elements); two stages are in LDS, one being read and one
-// arriving (global_load_lds: no registers in between).
-//   LDS, elements: a fragment is 16 rows by 4 blocks in the order that one
-//   load instruction leaves it, slot 16 g' + r for block 4 f + g' of row r;
-//   fragments (16-row tile t, half f) at 1 KB each, 32 a side and stage.
-//   Scales: 8 bytes a row and stage.
-// Step s of a stage takes block 2 g + s for lane group g, so that a lane's two
-// scales are neighbours (one 16-bit read, the byte picked by the
-// instruction's selector).  Blocks past the row's end and rows without a
-// record load zeros from kZeros.
-constexpr int kBigTile = 256;
-constexpr int kBigSide = 32 * 1024;               // element bytes of a side and stage
-constexpr int kBigScales = kBigTile * 8;
-constexpr int kBigStage = 2 * (kBigSide + kBigScales);
-
-__device__ __align__(16) const uint32_t kZeros[4] = {0, 0, 0, 0};
-
-__device__ __forceinline__ void load_lds(const void* g, void* l, int bytes) {
-  typedef const __attribute__((address_space(1))) void* gp;
-  typedef __attribute__((address_space(3))) void* lp;
-  if (bytes == 16)
-    __builtin_amdgcn_global_load_lds((gp)g, (lp)l, 16, 0, 0);
-  else
-    __builtin_amdgcn_global_load_lds((gp)g, (lp)l, 4, 0, 0);
-}
-
-struct BigRows {
-  const uint8_t* rec[4];    // the lane's row of four of the wave's 16-row tiles (NULL: none)
-  const uint8_t* scales[2]; // the lane's row of two of the wave's scale loads
-};
-
-// Loads stage k of one side: wave `w` of eight brings tiles 4 (w % 4) ..
-// + 3 of side w / 4, and the scales of rows 64 (w % 4) .. + 63.
-__device__ __forceinline__ void big_load(const BigRows& r, int k, int blocks, uint8_t* elems, uint8_t* scales, int tile0,
-                                         int row0, int lane) {
-  const int g = lane >> 4;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int f = 0; f < 2; ++f) {
-      const int b = 8 * k + 4 * f + g;
-      const void* at = r.rec[i] && b < blocks ? static_cast<const void*>(r.rec[i] + b * 16) : kZeros;
-      load_lds(at, elems + ((tile0 + i) * 2 + f) * 1024, 16);
-    }
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int b = 8 * k + 4 * (lane & 1);
-    const int last = (blocks - 1) & ~3;           // (scales of no block belong to zeros)
-    const void* at = r.scales[i] ? static_cast<const void*>(r.scales[i] + (b < blocks ? b : last)) : kZeros;
-    load_lds(at, scales + (row0 + 32 * i) * 8, 4);
-  }
-}
-
-template <int OUT>
-__global__ __launch_bounds__(512, 2) void k_mx_linear_big(MxLinearArgs p, int gm, int gn) {
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * kBigStage];
-  int64_t n = p.n_cap;
-  if (p.n_dev) {
-    const int64_t m = load_size(p.n_dev);
-    n = m < 0 ? 0 : (m < n ? m : n);
-  }
-  // workgroup ids go round the eight XCDs: each takes a contiguous run of
-  // tiles, eight row tiles wide, so that its L2 holds what they share
-  const int tiles = gm * gn, per = (tiles + 7) / 8;
-  const int id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-  if (id >= tiles) return;
-  const int band = id / (8 * gn), in_band = id - band * 8 * gn;
-  const int height = gm - 8 * band < 8 ? gm - 8 * band : 8;
-  const int64_t r0 = static_cast<int64_t>(8 * band + in_band % height) * kBigTile;
-  const int c0 = in_band / height * kBigTile;
-  if (r0 >= n) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int wr = wave >> 2, wc = wave & 3, g = lane >> 4;
-  const int side = wave >> 2, quarter = wave & 3;
-  const int stages = (p.blocks + 7) / 8;
-  floatx4 acc[8][4];
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-  for (int pr = 0; pr < p.pairs; ++pr) {
-    const MxPair& m = p.pair[pr];
-    BigRows rows;
-    auto record = [&](int r) -> const uint8_t* {   // row r of the tile on this wave's side
-      if (side == 0) {
-        const int64_t row = r0 + r < n ? r0 + r : n - 1;
-        if (!m.ids) return m.a + row * m.a_stride;
-        const int32_t v = m.ids[row];
-        if (valid_vertex(v, m.a_rows)) return m.a + v * m.a_stride;
-        raise_status(p.status, GMB_STATUS_ERANGE);
-        return nullptr;
-      }
-      const int c = c0 + r < p.d_out ? c0 + r : p.d_out - 1;
-      return m.w + static_cast<int64_t>(c) * m.w_stride;
+    // LDS row x: A's rows, then W's, dealt to a wave's column tiles
+    auto record = [&](int x) -> const uint8_t* {
+      if (x < TM) return a_record(p, m, r0 + x < n ? r0 + x : n - 1);
+      const int i = x - TM;
+      return w_record(p, m, c0 + (i & ~63) + 4 * (i & 15) + ((i >> 4) & 3));
     };
+    const uint8_t* rec[PER];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) rows.rec[i] = record(64 * quarter + 16 * i + (lane & 15));
+    for (int i = 0; i < PER; ++i) rec[i] = record(16 * (PER * wave + i) + lane / 4);
+    const uint8_t* scales[SLOADS];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint8_t* q = record(64 * quarter + 32 * i + lane / 2);
-      rows.scales[i] = q ? q + p.blocks * 16 : nullptr;
+    for (int i = 0; i < SLOADS; ++i) {
+      const int at = 64 * (SLOADS * wave + i);
+      scales[i] = at < TM + TN ? record(at + lane) : nullptr;
     }
-    auto fetch = [&](int k, int buf) {
-      uint8_t* base = lds + buf * kBigStage + side * (kBigSide + kBigScales);
-      big_load(rows, k, p.blocks, base, base + kBigSide, 4 * quarter, 64 * quarter, lane);
+    const int x = (lane & 3) ^ tile_swizzle(lane / 4);
+    auto fetch = [&](int k) {
+      uint8_t* to = lds + (k & 1) * kStage + PER * wave * 2048;
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+          const int b = 8 * k + 4 * f + x;
+          load_lds(rec[i] && b < p.blocks ? static_cast<const void*>(rec[i] + b * 16) : kZeros,
+                   to + (2 * i + f) * 1024);
+        }
+      // (16 scale bytes of blocks that there are lie in the padded record)
+      if ((k & 1) == 0) {
+#pragma unroll
+        for (int i = 0; i < SLOADS; ++i) {
+          const int at = SLOADS * wave + i;
+          if (64 * at < TM + TN)
+            load_lds(scales[i] ? static_cast<const void*>(scales[i] + p.blocks * 16 + 8 * k) : kZeros,
+                     lds + 2 * kStage + ((k >> 1) & 1) * kScales + at * 1024);
+        }
+      }
     };
     __syncthreads();            // the last pair's reads
-    fetch(0, 0);
+    fetch(0);
     __syncthreads();
     for (int k = 0; k < stages; ++k) {
-      const uint8_t* la = lds + (k & 1) * kBigStage;
-      const uint8_t* lw = la + kBigSide + kBigScales;
-      if (k + 1 < stages) fetch(k + 1, (k + 1) & 1);
-      uint32_t sa[8], sw[4];
+      const uint8_t* la = lds + (k & 1) * kStage + RT * wr * 2048;
+      const uint8_t* lw = lds + (k & 1) * kStage + (TM / 16 + CT * wc) * 2048;
+      const uint8_t* ls = lds + 2 * kStage + ((k >> 1) & 1) * kScales + r * 16 + (k & 1) * 8 + 2 * g;
+      if (k + 1 < stages) fetch(k + 1);
+      uint32_t sa[RT], sw[CT];
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        sa[i] = *reinterpret_cast<const uint16_t*>(la + kBigSide + (wr * 128 + 16 * i + (lane & 15)) * 8 + 2 * g);
+      for (int i = 0; i < RT; ++i) sa[i] = *reinterpret_cast<const uint16_t*>(ls + (RT * wr + i) * 256);
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        sw[j] = *reinterpret_cast<const uint16_t*>(lw + kBigSide + (wc * 64 + 16 * j + (lane & 15)) * 8 + 2 * g);
+      for (int j = 0; j < CT; ++j) sw[j] = *reinterpret_cast<const uint16_t*>(ls + (TM / 16 + CT * wc + j) * 256);
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        const int at = (g >> 1) * 1024 + (2 * (g & 1) + s) * 256 + (lane & 15) * 16;
-        intx4 qa[8], qw[4];
+        const int at = (g >> 1) * 1024 + r * 64 + ((2 * (g & 1) + s) ^ tile_swizzle(r)) * 16;
+        intx4 qa[RT], qw[CT];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) qw[j] = *reinterpret_cast<const intx4*>(lw + (wc * 4 + j) * 2048 + at);
+        for (int j = 0; j < CT; ++j) qw[j] = *reinterpret_cast<const intx4*>(lw + j * 2048 + at);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) qa[i] = *reinterpret_cast<const intx4*>(la + (wr * 8 + i) * 2048 + at);
+        for (int i = 0; i < RT; ++i) qa[i] = *reinterpret_cast<const intx4*>(la + i * 2048 + at);
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < RT; ++i)
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            acc[i][j] = s == 0 ? mfma_mx4<0>(qw[j], sw[j], qa[i], sa[i], acc[i][j])
-                               : mfma_mx4<1>(qw[j], sw[j], qa[i], sa[i], acc[i][j]);
+          for (int j = 0; j < CT; ++j)
+            acc[i][j] = s == 0 ? mfma_mx4<0>(qa[i], sa[i], qw[j], sw[j], acc[i][j])
+                               : mfma_mx4<1>(qa[i], sa[i], qw[j], sw[j], acc[i][j]);
       }
       __syncthreads();          // stage k is read, stage k + 1 has arrived
     }
   }
-  const int cw = c0 + 64 * wc;
-  if (cw < p.d_out) epilogue<8, 4, OUT>(p, n, r0 + 128 * wr, cw, lane, acc);
+  const int cw = c0 + 16 * CT * wc;
+  if (cw < p.d_out) epilogue<RT, CT, OUT>(p, n, r0 + 16 * RT * wr, cw, lane, acc);
 }
 
-template <int RT, int CT, int WC, int WK, int OUT>
-void run(const MxLinearArgs& p, hipStream_t s) {
+// ---- dispatch -------------------------------------------------------------
+
+template <int RT, int CT, int WK, int OUT>
+void run_rows(const MxLinearArgs& p, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>((p.n_cap + 16 * RT - 1) / (16 * RT)),
-                  static_cast<unsigned>((p.d_out + 16 * CT * WC - 1) / (16 * CT * WC)));
-  hipLaunchKernelGGL((k_mx_linear<RT, CT, WC, WK, OUT>), grid, dim3(64 * WC * WK), 0, s, p);
+                  static_cast<unsigned>((p.d_out + 16 * CT - 1) / (16 * CT)));
+  hipLaunchKernelGGL((k_mx_linear_rows<RT, CT, WK, OUT>), grid, dim3(64 * WK), 0, s, p);
+}
+
+template <int TM, int TN, int WM, int WN, int OUT>
+void run_tiles(const MxLinearArgs& p, hipStream_t s) {
+  const int gm = static_cast<int>((p.n_cap + TM - 1) / TM), gn = (p.d_out + TN - 1) / TN;
+  const int64_t tiles = static_cast<int64_t>(gm) * gn;
+  hipLaunchKernelGGL((k_mx_linear_tiles<TM, TN, WM, WN, OUT>), dim3(static_cast<unsigned>((tiles + 7) / 8 * 8)),
+                     dim3(64 * WM * WN), 0, s, p, gm, gn);
+}
+
+template <int WR, int WC, int OUT>
+void run_resident(const MxLinearArgs& p, hipStream_t s) {
+  const int64_t tiles = (p.n_cap + 64 * WR - 1) / (64 * WR);
+  const unsigned gy = static_cast<unsigned>((p.d_out + 64 * WC - 1) / (64 * WC));
+  const int64_t most = gy >= 512 ? 1 : 512 / gy;
+  hipLaunchKernelGGL((k_mx_linear_resident<WR, WC, OUT>), dim3(static_cast<unsigned>(tiles < most ? tiles : most), gy),
+                     dim3(64 * WR * WC), 0, s, p, static_cast<int>(tiles));
+}
+
+template <int WR, int WC>
+bool resident_fits(const MxLinearArgs& p) {
+  return resident_bytes(64 * WC, p.pairs, p.blocks) + resident_bytes(64 * WR, p.pairs, p.blocks) <= kResidentLds;
 }
 
 template <int OUT>
 void dispatch(const MxLinearArgs& p, hipStream_t s) {
-  const int64_t tiles = ((p.n_cap + 63) / 64) * ((p.d_out + 63) / 64);
-  const int64_t big = ((p.n_cap + kBigTile - 1) / kBigTile) * ((p.d_out + kBigTile - 1) / kBigTile);
-  if (big >= 128 && p.blocks >= 16 && p.d_out > 128) {
-    const int gm = static_cast<int>((p.n_cap + kBigTile - 1) / kBigTile), gn = (p.d_out + kBigTile - 1) / kBigTile;
-    hipLaunchKernelGGL((k_mx_linear_big<OUT>), dim3((gm * gn + 7) / 8 * 8), dim3(512), 0, s, p, gm, gn);
-  } else if (tiles >= 1024) {
-    if (p.d_out > 128) run<4, 4, 4, 1, OUT>(p, s);
-    else if (p.d_out > 64) run<4, 4, 2, 1, OUT>(p, s);
-    else run<4, 4, 1, 1, OUT>(p, s);
-  } else if (p.n_cap > 16) {
-    run<4, 2, 1, 8, OUT>(p, s);
+  auto tiles_of = [&](int tm, int tn) { return ((p.n_cap + tm - 1) / tm) * ((p.d_out + tn - 1) / tn); };
+  if (p.n_cap <= 16) {
+    run_rows<1, 2, 8, OUT>(p, s);
+  } else if (p.n_cap <= 64) {
+    run_rows<2, 2, 8, OUT>(p, s);
+  } else if (p.d_out > 128 && resident_fits<1, 4>(p)) {
+    run_resident<1, 4, OUT>(p, s);
+  } else if (p.d_out > 64 && resident_fits<2, 2>(p)) {
+    run_resident<2, 2, OUT>(p, s);
+  } else if (p.d_out <= 64 && resident_fits<4, 1>(p)) {
+    run_resident<4, 1, OUT>(p, s);
+  } else if (p.d_out <= 64 && tiles_of(128, 64) >= 128) {
+    run_tiles<128, 64, 2, 1, OUT>(p, s);
+  } else if (p.d_out > 128 && tiles_of(256, 256) >= 128) {
+    run_tiles<256, 256, 2, 4, OUT>(p, s);
+  } else if (tiles_of(128, 128) >= 128) {
+    run_tiles<128, 128, 2, 2, OUT>(p, s);
   } else {
-    run<1, 2, 1, 8, OUT>(p, s);
+    run_tiles<64, 64, 2, 1, OUT>(p, s);
   }
 }
 

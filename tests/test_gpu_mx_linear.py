@@ -44,7 +44,8 @@ def check(got, pairs, bias, relu, dtype):
 SHAPES = [(1, 1, 1), (1, 256, 47), (3, 33, 5), (16, 128, 16), (17, 100, 33), (64, 64, 64), (65, 129, 65),
           (100, 515, 130), (33, 4096, 70), (300, 16, 8), (1, 4096, 1030), (257, 384, 256), (1000, 75, 41),
           (2, 65536, 3), (20, 40, 5000), (4500, 100, 256), (9000, 300, 129), (70000, 33, 17), (3000, 1030, 520),
-          (16500, 530, 600), (33000, 515, 130), (2000, 1500, 4200)]
+          (16500, 530, 600), (33000, 515, 130), (2000, 1500, 4200), (17000, 700, 60), (300, 2000, 90),
+          (64, 600, 33), (500, 512, 128)]
 
 
 @pytest.mark.parametrize("n, d_in, d_out", SHAPES)
