@@ -638,19 +638,20 @@ def sgd_update_bf16(weights: SageWeights, master: SageWeights, grads: SageGrads,
 _DTYPES = {torch.float32: GMB_F32, torch.bfloat16: GMB_BF16}
 
 
-def _on_device(*tensors):
-    """Refuses tensors that are not on the current device (the kernels run on
-    its stream)."""
-    dev = None
-    for t, name in tensors:
-        if t is None:
-            continue
-        if not isinstance(t, torch.Tensor) or not t.is_cuda:
-            raise TypeError(f"{name} must be a CUDA (HIP) tensor")
-        if dev is None:
-            dev = torch._C._cuda_getDevice()
-        if t.get_device() != dev:
-            raise ValueError(f"{name} is on device {t.get_device()}, the current device is {dev}")
+def _current_device(t, name: str) -> int:
+    """The device of the tensor `t`, which has to be the current one (the
+    kernels run on its current stream)."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    dev, now = t.get_device(), torch._C._cuda_getDevice()
+    if dev != now:
+        raise ValueError(f"{name} is on device {dev}, the current device is {now}")
+    return dev
+
+
+def _same_device(t, dev: int, name: str):
+    if not isinstance(t, torch.Tensor) or t.get_device() != dev:
+        _current_device(t, name)
 
 
 def _dtype_code(dtype) -> int:
@@ -660,9 +661,12 @@ def _dtype_code(dtype) -> int:
     return code
 
 
-def _int32(t, name: str):
-    if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous():
+def _int32(t, dev: int, name: str) -> int:
+    """The length of a contiguous 1-d int32 tensor on `dev`."""
+    _same_device(t, dev, name)
+    if t.dtype is not torch.int32 or t.dim() != 1 or not t.is_contiguous():
         raise TypeError(f"{name} must be a contiguous 1-d int32 tensor")
+    return t.shape[0]
 
 
 _row_bytes: dict = {}
@@ -679,20 +683,32 @@ def mx_row_bytes(dim: int, bits: int) -> int:
     return n
 
 
-def _records(t: torch.Tensor, dim: int, bits: int, name: str):
-    """Checks a table of records: uint8 [rows, >= row bytes], rows at a stride."""
-    if t.dtype != torch.uint8 or t.dim() != 2 or t.stride(1) != 1:
-        raise TypeError(f"{name} must be a uint8 [rows, row bytes] tensor with contiguous rows")
-    if t.shape[1] < mx_row_bytes(dim, bits):
-        raise ValueError(f"{name} has {t.shape[1]} bytes a row, {mx_row_bytes(dim, bits)} needed")
+def _records(t, dim: int, bits: int, name: str):
+    """(rows, row stride in bytes) of a table of records: uint8 [rows, >= row
+    bytes], rows contiguous and at a stride.  (One row has any: its length,
+    rounded down to 16.)"""
+    if t.dtype is not torch.uint8 or t.dim() != 2:
+        raise TypeError(f"{name} must be a uint8 [rows, row bytes] tensor")
+    rows, width = t.shape
+    stride, inner = t.stride()
+    if inner != 1:
+        raise TypeError(f"{name} must have contiguous rows")
+    if width < mx_row_bytes(dim, bits):
+        raise ValueError(f"{name} has {width} bytes a row, {mx_row_bytes(dim, bits)} needed")
+    return rows, stride if rows > 1 else width // 16 * 16
 
 
-def _stride(t: torch.Tensor) -> int:
-    """The row stride in bytes (of one row, any: its length rounded down to 16)."""
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] // 16 * 16
+def _output(out, rows: int, cols: int, dtype, like: torch.Tensor) -> torch.Tensor:
+    """`out`, or a new [rows, cols] tensor beside `like`."""
+    if out is None:
+        return like.new_empty((rows, cols), dtype=dtype)
+    _same_device(out, like.get_device(), "out")
+    if out.dim() != 2 or out.shape[0] < rows or out.shape[1] != cols or out.dtype != dtype or not out.is_contiguous():
+        raise ValueError(f"out must be a contiguous [{rows} or more, {cols}] {dtype} tensor")
+    return out
 
 
-def _rows_of(ids, n, table_rows: int, status_word):
+def _rows_of(ids, n, table_rows: int, dev: int, status_word):
     """(ids pointer, device count pointer, rows, status word) of a Blocks (its
     input vertices), an int32 tensor, or None (every row of the table)."""
     if isinstance(ids, Blocks):
@@ -700,16 +716,11 @@ def _rows_of(ids, n, table_rows: int, status_word):
             raise ValueError("n goes with an id tensor")
         return (ids.struct.blk[0].src_ids, ids.input_count_ptr, ids.input_capacity,
                 ids.csr.status_word if status_word is None else status_word)
-    if ids is None:
-        cap = table_rows if n is None else int(n)
-        if not 0 <= cap <= table_rows:
-            raise ValueError("n exceeds the table's rows")
-        return None, None, cap, status_word
-    _int32(ids, "ids")
-    cap = ids.numel() if n is None else int(n)
-    if not 0 <= cap <= ids.numel():
-        raise ValueError("n exceeds ids")
-    return ids.data_ptr() if cap else None, None, cap, status_word
+    have = table_rows if ids is None else _int32(ids, dev, "ids")
+    cap = have if n is None else int(n)
+    if not 0 <= cap <= have:
+        raise ValueError("n exceeds the rows")
+    return ids.data_ptr() if ids is not None and cap else None, None, cap, status_word
 
 
 def mx_quantise(x: torch.Tensor, bits: int, ids=None, table: torch.Tensor | None = None, csr: CSRGraph | None = None,
@@ -721,34 +732,39 @@ def mx_quantise(x: torch.Tensor, bits: int, ids=None, table: torch.Tensor | None
     are distinct, or, with `csr` (a graph of table's rows, whose sampler state
     is used), an id's last row counts.  Without ids, row i is record i of
     `table` or of a new one."""
-    _on_device((x, "x"), (table, "table"), (None if isinstance(ids, Blocks) else ids, "ids"))
+    dev = _current_device(x, "x")
     if x.dim() != 2:
         raise ValueError("x must be [rows, dim]")
-    dtype = _dtype_code(x.dtype)
+    code = _dtype_code(x.dtype)
     rows, dim = x.shape
     if table is None:
         if ids is not None:
             raise ValueError("ids need a table")
-        table = torch.empty((rows, mx_row_bytes(dim, bits)), dtype=torch.uint8, device=x.device)
+        table = x.new_empty((rows, mx_row_bytes(dim, bits)), dtype=torch.uint8)
     else:
-        _records(table, dim, bits, "table")
-        if ids is None and rows > table.shape[0]:
+        _same_device(table, dev, "table")
+    table_rows, stride = _records(table, dim, bits, "table")
+    if ids is None:
+        if rows > table_rows:
             raise ValueError("x has more rows than the table")
-    ids_ptr, n_dev, cap, status = _rows_of(ids, None if ids is not None else rows, table.shape[0], status_word)
-    if ids is not None and not isinstance(ids, Blocks) and cap != rows:
-        raise ValueError("ids must have one entry per row of x")
-    if isinstance(ids, Blocks) and rows < cap:
-        raise ValueError("x must have the blocks' input capacity in rows")
-    state = (None, 0)
+        ids_ptr, n_dev, cap, status = None, None, rows, status_word
+    else:
+        ids_ptr, n_dev, cap, status = _rows_of(ids, None, table_rows, dev, status_word)
+        if rows < cap or (rows > cap and n_dev is None):
+            raise ValueError("x must have one row per id (or the blocks' input capacity in rows)")
+    state, state_bytes = None, 0
     if csr is not None:
-        if ids is None or csr.num_nodes != table.shape[0]:
+        if ids is None or csr.num_nodes != table_rows:
             raise ValueError("csr needs ids and a table of its graph's vertices")
-        state = (csr.state.data_ptr(), csr.state_bytes)
+        state, state_bytes = csr.state.data_ptr(), csr.state_bytes
     if cap == 0:
         return table
-    _check(lib().gmb_mx_quantise(x.data_ptr(), dtype, x.stride(0) if rows > 1 else 0, x.stride(1), ids_ptr, n_dev,
-                                 cap, dim, bits, table.data_ptr(), table.shape[0], _stride(table), *state,
-                                 status or None, _stream_handle()))
+    row_stride, col_stride = x.stride()
+    code = lib().gmb_mx_quantise(x.data_ptr(), code, row_stride if rows > 1 else 0, col_stride, ids_ptr, n_dev, cap,
+                                 dim, bits, table.data_ptr(), table_rows, stride, state, state_bytes, status or None,
+                                 _stream_handle())
+    if code:
+        _check(code)
     return table
 
 
@@ -758,17 +774,16 @@ def mx_gather(ids, table: torch.Tensor, dim: int, bits: int, dtype: torch.dtype 
     ids[i] as float32 or bfloat16.  `ids` is a Blocks (its input vertices), an
     int32 tensor (all of it, or the first n), or None (the table's rows, or
     the first n)."""
-    _on_device((table, "table"), (out, "out"), (None if isinstance(ids, Blocks) else ids, "ids"))
-    _records(table, dim, bits, "table")
+    dev = _current_device(table, "table")
+    rows, stride = _records(table, dim, bits, "table")
     code = _dtype_code(dtype)
-    ids_ptr, n_dev, cap, status = _rows_of(ids, n, table.shape[0], status_word)
-    if out is None:
-        out = torch.empty((cap, dim), dtype=dtype, device=table.device)
-    elif out.dim() != 2 or out.shape[0] < cap or out.shape[1] != dim or out.dtype != dtype or not out.is_contiguous():
-        raise ValueError("out must be a contiguous [rows, dim] tensor of the given dtype")
+    ids_ptr, n_dev, cap, status = _rows_of(ids, n, rows, dev, status_word)
+    out = _output(out, cap, dim, dtype, table)
     if cap:
-        _check(lib().gmb_mx_gather(ids_ptr, n_dev, cap, table.data_ptr(), table.shape[0], _stride(table), dim, bits,
-                                   out.data_ptr(), code, status or None, _stream_handle()))
+        code = lib().gmb_mx_gather(ids_ptr, n_dev, cap, table.data_ptr(), rows, stride, dim, bits, out.data_ptr(),
+                                   code, status or None, _stream_handle())
+        if code:
+            _check(code)
     return out
 
 
@@ -778,28 +793,27 @@ def mx_mean(block, table: torch.Tensor, dim: int, bits: int, dtype: torch.dtype 
     microscaled store (0 for a destination without any).  `block` is (indptr,
     ids): int32 row offsets and the neighbours' records, or a Blocks (block
     0's destinations, at their capacity, and sampled vertices)."""
+    dev = _current_device(table, "table")
+    table_rows, stride = _records(table, dim, bits, "table")
     if isinstance(block, Blocks):
         b = block.struct.blk[0]
-        ptrs, n_dev, rows = (b.indptr, b.nbr), b.sizes, int(b.cap_dst)
-        _on_device((table, "table"), (out, "out"))
+        indptr_ptr, ids_ptr, n_dev, rows = b.indptr, b.nbr, b.sizes, int(b.cap_dst)
     else:
         indptr, ids = block
-        _on_device((table, "table"), (out, "out"), (indptr, "indptr"), (ids, "ids"))
-        _int32(indptr, "indptr")
-        _int32(ids, "ids")
-        if indptr.numel() < 1:
+        rows = _int32(indptr, dev, "indptr") - 1
+        _int32(ids, dev, "ids")
+        if rows < 0:
             raise ValueError("indptr needs one entry more than rows")
-        # (a graph without edges has no ids to point at; none is read)
-        ptrs, n_dev, rows = (indptr.data_ptr(), ids.data_ptr() or indptr.data_ptr()), None, indptr.numel() - 1
-    _records(table, dim, bits, "table")
+        # (without edges there are no ids to point at; none is read)
+        indptr_ptr = indptr.data_ptr()
+        ids_ptr, n_dev = ids.data_ptr() or indptr_ptr, None
     code = _dtype_code(dtype)
-    if out is None:
-        out = torch.empty((rows, dim), dtype=dtype, device=table.device)
-    elif out.dim() != 2 or out.shape[0] < rows or out.shape[1] != dim or out.dtype != dtype or not out.is_contiguous():
-        raise ValueError("out must be a contiguous [rows, dim] tensor of the given dtype")
+    out = _output(out, rows, dim, dtype, table)
     if rows:
-        _check(lib().gmb_mx_mean(*ptrs, n_dev, rows, table.data_ptr(), table.shape[0], _stride(table), dim, bits,
-                                 out.data_ptr(), code, _stream_handle()))
+        code = lib().gmb_mx_mean(indptr_ptr, ids_ptr, n_dev, rows, table.data_ptr(), table_rows, stride, dim, bits,
+                                 out.data_ptr(), code, _stream_handle())
+        if code:
+            _check(code)
     return out
 
 
@@ -811,36 +825,36 @@ def mx_linear(a: torch.Tensor, w: torch.Tensor, d_in: int, bias: torch.Tensor | 
     [rows, .], w [d_out, .] (mx_quantise(matrix.t(), MXFP4) of a [d_in, d_out]
     matrix), a2 and w2 a second pair.  With `ids` row i of A is record ids[i]
     of `a`."""
-    _on_device((a, "a"), (w, "w"), (bias, "bias"), (a2, "a2"), (w2, "w2"), (ids, "ids"), (out, "out"))
-    _records(a, d_in, MXFP4, "a")
-    _records(w, d_in, MXFP4, "w")
-    code, d_out, rows = _dtype_code(dtype), w.shape[0], a.shape[0]
+    dev = _current_device(a, "a")
+    _same_device(w, dev, "w")
+    a_rows, a_stride = _records(a, d_in, MXFP4, "a")
+    d_out, w_stride = _records(w, d_in, MXFP4, "w")
+    code, rows, ids_ptr = _dtype_code(dtype), a_rows, None
     if ids is not None:
-        _int32(ids, "ids")
-        rows = ids.numel()
-    first = MxOperandStruct(a.data_ptr(), a.shape[0], _stride(a), None if ids is None else ids.data_ptr(),
-                            w.data_ptr(), _stride(w))
+        rows = _int32(ids, dev, "ids")
+        ids_ptr = ids.data_ptr()
+    first = MxOperandStruct(a.data_ptr(), a_rows, a_stride, ids_ptr, w.data_ptr(), w_stride)
     second = None
     if a2 is not None or w2 is not None:
         if a2 is None or w2 is None:
             raise ValueError("a2 and w2 go together")
-        _records(a2, d_in, MXFP4, "a2")
-        _records(w2, d_in, MXFP4, "w2")
-        if a2.shape[0] < rows or w2.shape[0] != d_out:
+        _same_device(a2, dev, "a2")
+        _same_device(w2, dev, "w2")
+        a2_rows, a2_stride = _records(a2, d_in, MXFP4, "a2")
+        w2_rows, w2_stride = _records(w2, d_in, MXFP4, "w2")
+        if a2_rows < rows or w2_rows != d_out:
             raise ValueError("a2 must have a row for each of the product's, w2 one for each column")
-        second = ctypes.byref(MxOperandStruct(a2.data_ptr(), a2.shape[0], _stride(a2), None, w2.data_ptr(),
-                                              _stride(w2)))
-    if bias is not None and (bias.dtype != torch.float32 or bias.shape != (d_out,) or not bias.is_contiguous()):
-        raise ValueError("bias must be a contiguous float32 [d_out] tensor")
-    if out is None:
-        out = torch.empty((rows, d_out), dtype=dtype, device=a.device)
-    elif out.dim() != 2 or out.shape[0] < rows or out.shape[1] != d_out or out.dtype != dtype \
-            or not out.is_contiguous():
-        raise ValueError("out must be a contiguous [rows, d_out] tensor of the given dtype")
+        second = MxOperandStruct(a2.data_ptr(), a2_rows, a2_stride, None, w2.data_ptr(), w2_stride)
+    if bias is not None:
+        _same_device(bias, dev, "bias")
+        if bias.dtype is not torch.float32 or bias.dim() != 1 or bias.shape[0] != d_out or not bias.is_contiguous():
+            raise ValueError("bias must be a contiguous float32 [d_out] tensor")
+    out = _output(out, rows, d_out, dtype, a)
     if rows and d_out:
-        _check(lib().gmb_mx_linear(ctypes.byref(first), second, None, rows, d_in, d_out,
-                                   None if bias is None else bias.data_ptr(), 1 if relu else 0, out.data_ptr(), code,
-                                   status_word or None, _stream_handle()))
+        code = lib().gmb_mx_linear(first, second, None, rows, d_in, d_out, None if bias is None else bias.data_ptr(),
+                                   1 if relu else 0, out.data_ptr(), code, status_word or None, _stream_handle())
+        if code:
+            _check(code)
     return out
 
 
@@ -889,17 +903,16 @@ def sage_forward_mx(blocks: Blocks, table: torch.Tensor, weights: SageMxWeights,
     """The forward of an MXFP4 model over an MXFP4 store (table: one record of
     dims[0] elements a vertex); the layers' means and hidden outputs are
     quantised as they are written.  Returns logits [num_seeds, C] float32."""
-    _on_device((table, "table"), (workspace, "workspace"), (logits, "logits"))
-    _records(table, weights.dims[0], MXFP4, "table")
+    dev = _current_device(table, "table")
+    rows, stride = _records(table, weights.dims[0], MXFP4, "table")
     B, C = blocks.num_seeds, weights.dims[-1]
-    if logits is None:
-        logits = torch.empty((max(B, 0), C), dtype=torch.float32, device=table.device)
-    elif logits.dtype != torch.float32 or logits.shape != (B, C) or not logits.is_contiguous():
-        raise ValueError("logits must be a contiguous float32 [num_seeds, C] tensor")
+    logits = _output(logits, B, C, torch.float32, table)
+    if workspace is not None:
+        _same_device(workspace, dev, "workspace")
     L, stream, status = lib(), _stream_handle(), blocks.csr.status_word
 
     def call(ws):
-        return L.gmb_sage_forward_mx(ctypes.byref(blocks.struct), table.data_ptr(), table.shape[0], _stride(table),
+        return L.gmb_sage_forward_mx(ctypes.byref(blocks.struct), table.data_ptr(), rows, stride,
                                      ctypes.byref(weights.struct), logits.data_ptr(), ws.data_ptr(), ws.numel(),
                                      status, stream)
 
@@ -918,20 +931,28 @@ def sage_forward_mx(blocks: Blocks, table: torch.Tensor, weights: SageMxWeights,
 
 # ---------------------------------------------------------------- distillation
 
+def _teacher(logits, classes, alpha: float, temperature: float) -> TeacherStruct:
+    dev = _current_device(logits, "the teacher's logits")
+    _same_device(classes, dev, "the teacher's classes")
+    if logits.dtype is not torch.float32 or logits.dim() != 2 or not logits.is_contiguous():
+        raise TypeError("the teacher's logits must be a contiguous float32 [rows, k] tensor")
+    if classes.dtype is not torch.int32 or classes.shape != logits.shape or not classes.is_contiguous():
+        raise TypeError("the teacher's classes must be a contiguous int32 tensor of the logits' shape")
+    return TeacherStruct(logits.data_ptr(), classes.data_ptr(), logits.shape[1], alpha, temperature, 0)
+
+
 class Teacher:
     """A teacher's top logits for a student: `logits` float32 [rows, k] and
     their `classes` int32 [rows, k] (-1 pads a shorter list), the weight alpha
     of the teacher against the labels, and the temperature."""
 
     def __init__(self, logits: torch.Tensor, classes: torch.Tensor, alpha: float = 0.5, temperature: float = 1.0):
-        _on_device((logits, "logits"), (classes, "classes"))
-        if logits.dtype != torch.float32 or logits.dim() != 2 or not logits.is_contiguous():
-            raise TypeError("the teacher's logits must be a contiguous float32 [rows, k] tensor")
-        if classes.dtype != torch.int32 or classes.shape != logits.shape or not classes.is_contiguous():
-            raise TypeError("the teacher's classes must be a contiguous int32 tensor of the logits' shape")
+        self.struct = _teacher(logits, classes, alpha, temperature)
         self.logits, self.classes = logits, classes
         self.rows = logits.shape[0]
-        self.struct = TeacherStruct(logits.data_ptr(), classes.data_ptr(), logits.shape[1], alpha, temperature, 0)
+
+
+_distill_bytes: dict = {}
 
 
 def distill_loss(logits: torch.Tensor, teacher_logits: torch.Tensor, teacher_classes: torch.Tensor,
@@ -943,38 +964,49 @@ def distill_loss(logits: torch.Tensor, teacher_logits: torch.Tensor, teacher_cla
     `labels` (int32, -1 for none), and its gradient in `logits` (float32 or
     bfloat16 [rows, C]).  Returns (loss, grad): a 1-element float32 tensor and
     a tensor like logits (None for grad=False)."""
-    _on_device((logits, "logits"), (labels, "labels"), (None if isinstance(grad, bool) else grad, "grad"),
-               (loss, "loss"), (workspace, "workspace"))
+    dev = _current_device(logits, "logits")
     if logits.dim() != 2 or not logits.is_contiguous():
         raise ValueError("logits must be a contiguous [rows, classes] tensor")
-    dtype = _dtype_code(logits.dtype)
+    code = _dtype_code(logits.dtype)
     rows, classes = logits.shape
-    teacher = Teacher(teacher_logits, teacher_classes, alpha, temperature)
-    if teacher.rows != rows:
+    teacher = _teacher(teacher_logits, teacher_classes, alpha, temperature)
+    if teacher_logits.shape[0] != rows:
         raise ValueError("the teacher must have one row per row of logits")
-    if labels is not None:
-        _int32(labels, "labels")
-        if labels.numel() != rows:
-            raise ValueError("labels must have one entry per row")
+    if labels is not None and _int32(labels, dev, "labels") != rows:
+        raise ValueError("labels must have one entry per row")
     if grad is True:
         grad = torch.empty_like(logits)
     elif grad is False:
         grad = None
-    elif grad.shape != logits.shape or grad.dtype != logits.dtype or not grad.is_contiguous() \
-            or (rows and grad.data_ptr() == logits.data_ptr()):
-        raise ValueError("grad must be a contiguous tensor like logits, and another one")
+    else:
+        _same_device(grad, dev, "grad")
+        if grad.shape != logits.shape or grad.dtype != logits.dtype or not grad.is_contiguous() \
+                or (rows and grad.data_ptr() == logits.data_ptr()):
+            raise ValueError("grad must be a contiguous tensor like logits, and another one")
     if loss is None:
-        loss = torch.empty(1, dtype=torch.float32, device=logits.device)
-    elif loss.dtype != torch.float32 or loss.numel() != 1:
-        raise ValueError("loss must be a 1-element float32 tensor")
+        loss = logits.new_empty(1, dtype=torch.float32)
+    else:
+        _same_device(loss, dev, "loss")
+        if loss.dtype != torch.float32 or loss.numel() != 1:
+            raise ValueError("loss must be a 1-element float32 tensor")
     L = lib()
-    need = L.gmb_distill_workspace_bytes(rows, classes)
-    if need == 0:
-        _check(-1)
+    need = _distill_bytes.get((rows, classes))
+    if need is None:
+        need = L.gmb_distill_workspace_bytes(rows, classes)
+        if need == 0:
+            _check(-1)
+        if len(_distill_bytes) < 4096:
+            _distill_bytes[rows, classes] = need
+    if workspace is not None:
+        _same_device(workspace, dev, "workspace")
     if workspace is None or workspace.numel() < need or workspace.data_ptr() % 256:
-        _, workspace = _aligned_bytes(need, logits.device)
-    _check(L.gmb_distill_loss(logits.data_ptr(), dtype, rows, classes, ctypes.byref(teacher.struct),
+        workspace = logits.new_empty(need, dtype=torch.uint8)
+        if workspace.data_ptr() % 256:   # (torch's own blocks are aligned)
+            _, workspace = _aligned_bytes(need, logits.device)
+    code = L.gmb_distill_loss(logits.data_ptr(), code, rows, classes, teacher,
                               None if labels is None else labels.data_ptr(),
                               None if grad is None else grad.data_ptr(), loss.data_ptr(), workspace.data_ptr(),
-                              workspace.numel(), _stream_handle()))
+                              workspace.numel(), _stream_handle())
+    if code:
+        _check(code)
     return loss, grad
