@@ -35,15 +35,18 @@ __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(
 __device__ __forceinline__ float load_logit(const float* p) { return *p; }
 __device__ __forceinline__ float load_logit(const uint16_t* p) { return bf16_to_f32(*p); }
 
+// 16 bytes of logits.
 template <typename T>
 struct Chunk;
 template <>
 struct Chunk<float> {
   static constexpr int N = 4;
-  static __device__ __forceinline__ void load(const float* p, float (&v)[4]) {
-    float4 x;
-    __builtin_memcpy(&x, p, 16);
-    v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+  static constexpr uint32_t kMasked = 0xFF800000u;   // -inf, in each of a word's values
+  static __device__ __forceinline__ void unpack(const uint4& x, float (&v)[4]) {
+    v[0] = __uint_as_float(x.x);
+    v[1] = __uint_as_float(x.y);
+    v[2] = __uint_as_float(x.z);
+    v[3] = __uint_as_float(x.w);
   }
   static __device__ __forceinline__ void store(float* p, const float (&v)[4]) {
     const float4 x = make_float4(v[0], v[1], v[2], v[3]);
@@ -54,9 +57,8 @@ struct Chunk<float> {
 template <>
 struct Chunk<uint16_t> {
   static constexpr int N = 8;
-  static __device__ __forceinline__ void load(const uint16_t* p, float (&v)[8]) {
-    uint4 x;
-    __builtin_memcpy(&x, p, 16);
+  static constexpr uint32_t kMasked = 0xFF80FF80u;
+  static __device__ __forceinline__ void unpack(const uint4& x, float (&v)[8]) {
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -70,7 +72,34 @@ struct Chunk<uint16_t> {
   }
 };
 
-// Reductions over the TH threads of a row (a wave, or the workgroup).
+// The chunk of classes c .. c + N - 1, -inf at `end` and past it.
+template <typename T>
+__device__ __forceinline__ uint4 load_chunk(const T* z, int64_t c, int64_t end) {
+  uint4 x;
+  if (c + Chunk<T>::N <= end) {
+    __builtin_memcpy(&x, z + c, 16);
+  } else {
+    x = make_uint4(Chunk<T>::kMasked, Chunk<T>::kMasked, Chunk<T>::kMasked, Chunk<T>::kMasked);
+    T* e = reinterpret_cast<T*>(&x);
+#pragma unroll
+    for (int i = 0; i < Chunk<T>::N; ++i)
+      if (c + i < end) e[i] = z[c + i];
+  }
+  return x;
+}
+template <typename T>
+__device__ __forceinline__ void store_chunk(T* grad, int64_t c, int64_t end, const float (&g)[Chunk<T>::N]) {
+  if (c + Chunk<T>::N <= end) {
+    Chunk<T>::store(grad + c, g);
+  } else {
+#pragma unroll
+    for (int i = 0; i < Chunk<T>::N; ++i)
+      if (c + i < end) Chunk<T>::store1(grad + c + i, g[i]);
+  }
+}
+
+// Reductions over the TH threads of a row (a part of a wave, a wave, or the
+// workgroup).
 struct Max {
   __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
 };
@@ -80,7 +109,7 @@ struct Sum {
 template <int TH, typename Op>
 __device__ __forceinline__ float row_reduce(float x, Op op, float* red) {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x = op(x, __shfl_xor(x, o, 64));
+  for (int o = (TH < 64 ? TH : 64) / 2; o > 0; o >>= 1) x = op(x, __shfl_xor(x, o, 64));
   if constexpr (TH > 64) {
     constexpr int W = TH / 64;
     const int wave = threadIdx.x >> 6;
@@ -94,14 +123,58 @@ __device__ __forceinline__ float row_reduce(float x, Op op, float* red) {
   return x;
 }
 
+// How exp(z - m) follows from u = exp((z - m) / T): it is u^T for T = 1, 2
+// and 4 (POW), one exponential a class and pass instead of two; else (POW 0)
+// it takes its own.
+template <int POW>
+__device__ __forceinline__ float hard_exp(float u, float d) {
+  if constexpr (POW == 1) return u;
+  if constexpr (POW == 2) return u * u;
+  if constexpr (POW == 4) return (u * u) * (u * u);
+  return exp2_(d * kLog2e);
+}
+
+// What a thread asks for before it has the row's statistics: its first
+// teacher entry and the label, with their logits.
+struct Early {
+  int32_t id;      // -1: none
+  float t, z;      // the entry's logit over T, and the student's at its class
+  int32_t label;   // -1: none
+  float zl;
+};
+
+template <typename T>
+__device__ __forceinline__ Early early_loads(const DistillArgs& a, int64_t row, bool live, const T* z, int t) {
+  Early e{-1, -INFINITY, 0.f, -1, 0.f};
+  const bool taught = live && a.alpha > 0.f && t < a.k, labelled = live && a.labels && a.alpha < 1.f;
+  int32_t id = -1, y = -1;
+  float v = -INFINITY;
+  if (taught) {
+    id = a.top_ids[row * a.k + t];
+    v = a.top[row * a.k + t];
+  }
+  if (labelled) y = a.labels[row];
+  if (id >= 0 && id < a.classes && !(v == -INFINITY)) {
+    e.id = id;
+    e.t = v / a.temperature;
+    e.z = load_logit(z + id);
+  }
+  if (y >= 0 && y < a.classes) {
+    e.label = y;
+    e.zl = load_logit(z + y);
+  }
+  return e;
+}
+
 // What a row's gradient and loss are made of.
 struct RowTerms {
   float m;          // the largest logit (0 where all are -inf)
-  float kt, k1;     // log2(e) / T, log2(e)
+  float kt;         // log2(e) / T
   float ft, f1;     // factors of exp((z - m) / T) and exp(z - m) in the gradient
   float fp;         // a teacher probability's share of the gradient: alpha T / n
   float fy;         // the label's: (1 - alpha) / n
   int label;        // -1: none
+  bool none;        // no term at all: no gradient
 };
 
 // The teacher's entries of a row in LDS (classes in `ids`, -1 for an invalid
@@ -109,22 +182,23 @@ struct RowTerms {
 // st and s1 are the row's statistics.  Every thread of the row calls it.
 template <typename T, int TH>
 __device__ __forceinline__ RowTerms row_terms(const DistillArgs& a, int64_t row, bool live, const T* z, float m,
-                                              float st, float s1, int t, int32_t* ids, float* ps, float* red,
-                                              float& loss) {
+                                              float st, float s1, const Early& first, int t, int32_t* ids, float* ps,
+                                              float* red, float& loss) {
   RowTerms r;
   const float inv_t = 1.f / a.temperature;
   const float inv_n = 1.f / static_cast<float>(a.rows);
   r.m = m;
   r.kt = kLog2e * inv_t;
-  r.k1 = kLog2e;
-  const bool some = !(st == 0.f);   // not: every logit is -inf
+  const bool some = live && !(st == 0.f);   // not: every logit is -inf
   // the teacher
   float mt = -INFINITY;
-  const bool taught = live && some && a.alpha > 0.f;
   for (int j = t; j < a.k; j += TH) {
     int32_t id = -1;
     float v = -INFINITY;
-    if (taught) {
+    if (j == t) {
+      id = some ? first.id : -1;
+      v = some ? first.t : -INFINITY;
+    } else if (some && a.alpha > 0.f) {
       id = a.top_ids[row * a.k + j];
       v = a.top[row * a.k + j] * inv_t;
       if (id < 0 || id >= a.classes || v == -INFINITY) {
@@ -150,48 +224,74 @@ __device__ __forceinline__ RowTerms row_terms(const DistillArgs& a, int64_t row,
       const float u = ps[j] - mt;
       const float p = exp2_(u * kLog2e) * inv_sum;
       ps[j] = p;
-      if (id >= 0 && !(p == 0.f)) kl += p * ((u - log_sum) - ((load_logit(z + id) - m) * inv_t - log_st));
+      if (id >= 0 && !(p == 0.f)) {
+        const float zj = j == t ? first.z : load_logit(z + id);
+        kl += p * ((u - log_sum) - ((zj - m) * inv_t - log_st));
+      }
     }
   }
   kl = row_reduce<TH>(kl, Sum(), red);
   r.ft = any ? a.alpha * a.temperature * inv_n / st : 0.f;
   r.fp = a.alpha * a.temperature * inv_n;
-  // the label
-  r.label = -1;
-  if (live && some && a.labels && a.alpha < 1.f) {
-    const int32_t y = a.labels[row];
-    if (y >= 0 && y < a.classes) r.label = y;
-  }
+  r.label = some ? first.label : -1;
   r.fy = (1.f - a.alpha) * inv_n;
   r.f1 = r.label >= 0 ? r.fy / s1 : 0.f;
+  r.none = !any && r.label < 0;
   loss = any ? a.alpha * a.temperature * a.temperature * kl : 0.f;
-  if (r.label >= 0) loss += (1.f - a.alpha) * (logf(s1) - (load_logit(z + r.label) - m));
+  if (r.label >= 0) loss += (1.f - a.alpha) * (logf(s1) - (first.zl - m));
   return r;
 }
 
-// The classes that the teacher's entries name, in [lo, hi): the whole
-// gradient again with their probabilities taken off.  Entries of one class
-// add up in the entries' order and all write the same value.
-template <typename T, int TH>
-__device__ __forceinline__ void correct_entries(const DistillArgs& a, const RowTerms& r, const T* z, T* grad, int t,
-                                                const int32_t* ids, const float* ps, int64_t lo, int64_t hi) {
-  if (r.ft == 0.f) return;
-  for (int j = t; j < a.k; j += TH) {
-    const int32_t id = ids[j];
-    if (id < lo || id >= hi) continue;
-    float p = 0.f;
-    for (int i = 0; i < a.k; ++i) p += ids[i] == id ? ps[i] : 0.f;
-    const float d = load_logit(z + id) - r.m;
-    float g = r.ft * exp2_(d * r.kt) - r.fp * p;
-    if (r.label >= 0) g += r.f1 * exp2_(d * r.k1) - (id == r.label ? r.fy : 0.f);
-    Chunk<T>::store1(grad + id, g);
+// The gradient of one chunk, what the teacher and the label take off left
+// out (correct_entries).
+template <int POW, typename T>
+__device__ __forceinline__ void chunk_gradient(const RowTerms& r, const uint4& q, float (&g)[Chunk<T>::N]) {
+  Chunk<T>::unpack(q, g);
+#pragma unroll
+  for (int e = 0; e < Chunk<T>::N; ++e) {
+    const float d = g[e] - r.m, u = exp2_(d * r.kt);
+    g[e] = r.ft * u + r.f1 * hard_exp<POW>(u, d);
   }
 }
 
-// TH threads hold a row of up to TH * V classes, V values each.
-template <typename T, int TH, int V>
-__global__ __launch_bounds__(TH < 256 ? 256 : TH) void k_distill_held(DistillArgs a) {
-  constexpr int E = Chunk<T>::N, K = V / E;
+// The classes in [lo, hi) that the teacher's entries or the label name: the
+// whole gradient again, less their shares.  Entries of one class add up in the
+// entries' order, and all that name a class write the same value.
+template <typename T, int TH>
+__device__ __forceinline__ void correct_entries(const DistillArgs& a, const RowTerms& r, const T* z, T* grad,
+                                                const Early& first, int t, const int32_t* ids, const float* ps,
+                                                int64_t lo, int64_t hi) {
+  if (r.none) return;
+  auto write = [&](int32_t id, float zi) {
+    if (id < lo || id >= hi) return;
+    float p = 0.f;
+    for (int i = 0; i < a.k; ++i) p += ids[i] == id ? ps[i] : 0.f;
+    const float d = zi - r.m;
+    Chunk<T>::store1(grad + id, r.ft * exp2_(d * r.kt) - r.fp * p + r.f1 * exp2_(d * kLog2e) -
+                                    (id == r.label ? r.fy : 0.f));
+  };
+  for (int j = t; j < a.k; j += TH) {
+    const int32_t id = ids[j];
+    if (id >= 0) write(id, j == t ? first.z : load_logit(z + id));
+  }
+  if (t == TH - 1 && r.label >= 0) write(r.label, first.zl);
+}
+
+// Makes loaded chunks opaque, so that what one pass computed of them (their
+// values, differences, exponentials) is not kept in registers for the next.
+template <int K>
+__device__ __forceinline__ void forget(uint4 (&q)[K]) {
+#pragma unroll
+  for (int k = 0; k < K; ++k) asm volatile("" : "+v"(q[k].x), "+v"(q[k].y), "+v"(q[k].z), "+v"(q[k].w));
+}
+
+// TH threads hold a row of up to TH * K chunks as they were loaded (the
+// values twice over would halve the rows that a CU has in flight); WAVES: the
+// waves a SIMD is to hold.
+template <typename T, int TH, int K, int POW, int WAVES>
+__global__ __launch_bounds__(TH < 256 ? 256 : TH) __attribute__((amdgpu_waves_per_eu(WAVES)))
+void k_distill_held(DistillArgs a) {
+  constexpr int E = Chunk<T>::N;
   constexpr int ROWS = TH < 256 ? 256 / TH : 1;
   extern __shared__ uint32_t lds[];
   __shared__ float red[16];
@@ -205,64 +305,83 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) void k_distill_held(DistillArg
   const bool live = row < a.rows;
   if (!live) row = a.rows - 1;
   const T* z = static_cast<const T*>(a.logits) + row * a.classes;
-  float v[K][E];
-  float m = -INFINITY;
+  // the chunk that the row ends in, if it is not whole, by the thread whose it is
+  const int whole = a.classes / E;
+  uint4 tail = load_chunk(z, t == whole % TH ? whole * E : a.classes, a.classes);
+  uint4 q[K];
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     const int c = (k * TH + t) * E;
-    if (c + E <= a.classes) {
-      Chunk<T>::load(z + c, v[k]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e) v[k][e] = c + e < a.classes ? load_logit(z + c + e) : -INFINITY;
-    }
+    q[k] = tail;
+    if (c + E <= a.classes) __builtin_memcpy(&q[k], z + c, 16);
   }
+  if (whole % TH == t) {
+    // (past that chunk there is nothing)
+    const uint32_t masked = Chunk<T>::kMasked;
 #pragma unroll
-  for (int k = 0; k < K; ++k)
+    for (int k = 0; k < K; ++k)
+      if (k * TH + t > whole) q[k] = make_uint4(masked, masked, masked, masked);
+  }
+  const Early first = early_loads(a, row, live, z, t);
+  float m = -INFINITY;
 #pragma unroll
-    for (int e = 0; e < E; ++e) m = fmaxf(m, v[k][e]);
+  for (int k = 0; k < K; ++k) {
+    float v[E];
+    Chunk<T>::unpack(q[k], v);
+#pragma unroll
+    for (int e = 0; e < E; ++e) m = fmaxf(m, v[e]);
+  }
   m = row_reduce<TH>(m, Max(), red);
   m = m == -INFINITY ? 0.f : m;
+  forget(q);
   const float kt = kLog2e / a.temperature;
-  float st = 0.f, s1 = 0.f;
   const bool hard = a.labels && a.alpha < 1.f;
+  float st = 0.f, s1 = 0.f;
+  if (hard) {
 #pragma unroll
-  for (int k = 0; k < K; ++k)
+    for (int k = 0; k < K; ++k) {
+      float v[E];
+      Chunk<T>::unpack(q[k], v);
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      st += exp2_((v[k][e] - m) * kt);
-      if (hard) s1 += exp2_((v[k][e] - m) * kLog2e);
+      for (int e = 0; e < E; ++e) {
+        const float d = v[e] - m, u = exp2_(d * kt);
+        st += u;
+        s1 += hard_exp<POW>(u, d);
+      }
+      __builtin_amdgcn_sched_barrier(0);   // one chunk's values at a time
     }
+  } else {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      float v[E];
+      Chunk<T>::unpack(q[k], v);
+#pragma unroll
+      for (int e = 0; e < E; ++e) st += exp2_((v[e] - m) * kt);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
   st = row_reduce<TH>(st, Sum(), red);
   if (hard) s1 = row_reduce<TH>(s1, Sum(), red);
   float loss;
-  const RowTerms r = row_terms<T, TH>(a, row, live, z, m, st, s1, t, ids, ps, red, loss);
+  const RowTerms r = row_terms<T, TH>(a, row, live, z, m, st, s1, first, t, ids, ps, red, loss);
   if (live && t == 0) a.loss_rows[row] = loss;
   if (!a.grad) return;
   T* grad = static_cast<T*>(a.grad) + row * a.ld_grad;
+  forget(q);
   if (live) {
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int c = (k * TH + t) * E;
-      float g[E];
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const float d = v[k][e] - m;
-        g[e] = r.ft == 0.f ? 0.f : r.ft * exp2_(d * r.kt);
-        if (r.label >= 0) g[e] += r.f1 * exp2_(d * r.k1) - (c + e == r.label ? r.fy : 0.f);
-      }
-      if (c + E <= a.classes) {
-        Chunk<T>::store(grad + c, g);
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (c + e < a.classes) Chunk<T>::store1(grad + c + e, g[e]);
-      }
+      if (c >= a.classes) break;
+      float g[E] = {};
+      if (!r.none) chunk_gradient<POW, T>(r, q[k], g);   // (0 whatever the logits are)
+      store_chunk(grad, c, a.classes, g);
+      __builtin_amdgcn_sched_barrier(0);
     }
     for (int64_t c = a.classes + t; c < a.ld_grad; c += TH) Chunk<T>::store1(grad + c, 0.f);
   }
   __syncthreads();   // the entries' classes are written again
-  if (live) correct_entries<T, TH>(a, r, z, grad, t, ids, ps, 0, a.classes);
+  if (live) correct_entries<T, TH>(a, r, z, grad, first, t, ids, ps, 0, a.classes);
 }
 
 // The range of classes of part `part`: whole chunks.
@@ -287,12 +406,7 @@ __global__ __launch_bounds__(kSplitThreads) void k_distill_stats(DistillArgs a) 
   float m = -INFINITY, st = 0.f, s1 = 0.f;   // the thread's own, joined at the end
   for (int64_t c = lo + threadIdx.x * E; c < hi; c += kSplitThreads * E) {
     float v[E];
-    if (c + E <= hi) {
-      Chunk<T>::load(z + c, v);
-    } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e) v[e] = c + e < hi ? load_logit(z + c + e) : -INFINITY;
-    }
+    Chunk<T>::unpack(load_chunk(z, c, hi), v);
     float top = v[0];
 #pragma unroll
     for (int e = 1; e < E; ++e) top = fmaxf(top, v[e]);
@@ -326,93 +440,88 @@ __global__ __launch_bounds__(kSplitThreads) void k_distill_grad(DistillArgs a) {
   constexpr int E = Chunk<T>::N;
   extern __shared__ uint32_t lds[];
   __shared__ float red[16];
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < a.clear_n;
-       i += static_cast<int64_t>(gridDim.x) * blockDim.x)
-    a.clear[i] = 0;
   const int t = threadIdx.x;
   int32_t* ids = reinterpret_cast<int32_t*>(lds);
   float* ps = reinterpret_cast<float*>(lds + a.k);
   const int64_t row = blockIdx.x / a.parts;
   const int part = static_cast<int>(blockIdx.x % a.parts);
   const T* z = static_cast<const T*>(a.logits) + row * a.classes;
+  const Early first = early_loads(a, row, true, z, t);
   const float kt = kLog2e / a.temperature;
+  // the parts' statistics, each thread some of them (a row has at most as many parts as threads)
   const float* stats = a.stats + 3 * row * a.parts;
-  float m = -INFINITY;
-  for (int i = 0; i < a.parts; ++i) m = fmaxf(m, stats[3 * i]);
+  const bool has = t < a.parts;
+  const float mi = has ? stats[3 * t] : -INFINITY;
+  float m = row_reduce<kSplitThreads>(mi, Max(), red);
   m = m == -INFINITY ? 0.f : m;
-  float st = 0.f, s1 = 0.f;
-  for (int i = 0; i < a.parts; ++i) {
-    const float mi = stats[3 * i];
-    st += stats[3 * i + 1] * (mi == -INFINITY ? 1.f : exp2_((mi - m) * kt));
-    s1 += stats[3 * i + 2] * (mi == -INFINITY ? 1.f : exp2_((mi - m) * kLog2e));
-  }
+  const float st = row_reduce<kSplitThreads>(
+      has ? stats[3 * t + 1] * (mi == -INFINITY ? 1.f : exp2_((mi - m) * kt)) : 0.f, Sum(), red);
+  const float s1 = row_reduce<kSplitThreads>(
+      has ? stats[3 * t + 2] * (mi == -INFINITY ? 1.f : exp2_((mi - m) * kLog2e)) : 0.f, Sum(), red);
   float loss;
-  const RowTerms r = row_terms<T, kSplitThreads>(a, row, true, z, m, st, s1, t, ids, ps, red, loss);
+  const RowTerms r = row_terms<T, kSplitThreads>(a, row, true, z, m, st, s1, first, t, ids, ps, red, loss);
   if (part == 0 && t == 0) a.loss_rows[row] = loss;
   if (!a.grad) return;
   T* grad = static_cast<T*>(a.grad) + row * a.ld_grad;
   int64_t lo, hi;
   part_range(a.classes, a.parts, part, lo, hi);
   for (int64_t c = lo + t * E; c < hi; c += kSplitThreads * E) {
-    float v[E], g[E];
-    const bool whole = c + E <= hi;
-    if (whole) {
-      Chunk<T>::load(z + c, v);
-    } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e) v[e] = c + e < hi ? load_logit(z + c + e) : -INFINITY;
-    }
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const float d = v[e] - m;
-      g[e] = r.ft == 0.f ? 0.f : r.ft * exp2_(d * r.kt);
-      if (r.label >= 0) g[e] += r.f1 * exp2_(d * r.k1) - (c + e == r.label ? r.fy : 0.f);
-    }
-    if (whole) {
-      Chunk<T>::store(grad + c, g);
-    } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e)
-        if (c + e < hi) Chunk<T>::store1(grad + c + e, g[e]);
-    }
+    float g[E] = {};
+    if (!r.none) chunk_gradient<0, T>(r, load_chunk(z, c, hi), g);
+    store_chunk(grad, c, hi, g);
   }
-  if (part == 0)
-    for (int64_t c = a.classes + t; c < a.ld_grad; c += kSplitThreads) Chunk<T>::store1(grad + c, 0.f);
   __syncthreads();
-  correct_entries<T, kSplitThreads>(a, r, z, grad, t, ids, ps, lo, hi);
+  correct_entries<T, kSplitThreads>(a, r, z, grad, first, t, ids, ps, lo, hi);
 }
 
 __global__ __launch_bounds__(1024) void k_loss_mean(const float* rows, int64_t n, float* loss) {
   __shared__ float red[16];
-  float s = 0.f;
-  for (int64_t i = threadIdx.x; i < n; i += 1024) s += rows[i];
-  s = row_reduce<1024>(s, Sum(), red);
-  if (threadIdx.x == 0) *loss = s / static_cast<float>(n);
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int64_t i = threadIdx.x; i < n; i += 4096) {
+    float v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = rows[i + 1024 * u < n ? i + 1024 * u : i];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) s[u] += i + 1024 * u < n ? v[u] : 0.f;
+  }
+  const float all = row_reduce<1024>((s[0] + s[1]) + (s[2] + s[3]), Sum(), red);
+  if (threadIdx.x == 0) *loss = all / static_cast<float>(n);
 }
 
-template <typename T, int TH, int V>
+template <typename T, int TH, int K, int WAVES>
 void held(const DistillArgs& a, hipStream_t s) {
   constexpr int ROWS = TH < 256 ? 256 / TH : 1;
-  hipLaunchKernelGGL((k_distill_held<T, TH, V>), dim3(static_cast<unsigned>((a.rows + ROWS - 1) / ROWS)),
-                     dim3(TH < 256 ? 256 : TH), 8 * static_cast<size_t>(a.k) * ROWS, s, a);
+  const dim3 grid(static_cast<unsigned>((a.rows + ROWS - 1) / ROWS)), block(TH < 256 ? 256 : TH);
+  const size_t lds = 8 * static_cast<size_t>(a.k) * ROWS;
+  const float t = a.temperature;
+  if (t == 1.f) hipLaunchKernelGGL((k_distill_held<T, TH, K, 1, WAVES>), grid, block, lds, s, a);
+  else if (t == 2.f) hipLaunchKernelGGL((k_distill_held<T, TH, K, 2, WAVES>), grid, block, lds, s, a);
+  else if (t == 4.f) hipLaunchKernelGGL((k_distill_held<T, TH, K, 4, WAVES>), grid, block, lds, s, a);
+  else hipLaunchKernelGGL((k_distill_held<T, TH, K, 0, WAVES>), grid, block, lds, s, a);
 }
 
 template <typename T>
 void dispatch(const DistillArgs& a, hipStream_t s) {
+  constexpr int E = Chunk<T>::N;
+  const int chunks = (a.classes + E - 1) / E;
   if (a.stats) {
     const dim3 grid(static_cast<unsigned>(a.rows * a.parts));
     hipLaunchKernelGGL((k_distill_stats<T>), grid, dim3(kSplitThreads), 0, s, a);
     hipLaunchKernelGGL((k_distill_grad<T>), grid, dim3(kSplitThreads), 8 * static_cast<size_t>(a.k), s, a);
-  } else if (a.classes <= 512) {
-    held<T, 64, 8>(a, s);
-  } else if (a.classes <= 1024) {
-    held<T, 64, 16>(a, s);
-  } else if (a.classes <= 4096) {
-    held<T, 256, 16>(a, s);
-  } else if (a.classes <= 8192) {
-    held<T, 256, 32>(a, s);
-  } else {
-    held<T, 1024, 32>(a, s);
+  } else if (chunks <= 16 && a.k <= 256) {   // (sixteen rows' entries in LDS: 32 KB at most)
+    held<T, 16, 1, 4>(a, s);
+  } else if (chunks <= 64) {
+    held<T, 64, 1, 4>(a, s);
+  } else if (chunks <= 256) {
+    held<T, 64, 4, 8>(a, s);
+  } else if (chunks <= 1024) {
+    held<T, 256, 4, 8>(a, s);
+  } else if (chunks <= 2048) {
+    held<T, 256, 8, 5>(a, s);
+  } else if (chunks <= 4096) {
+    held<T, 512, 8, 5>(a, s);
+  } else if constexpr (E == 4) {
+    held<T, 1024, 8, 8>(a, s);
   }
 }
 
@@ -423,6 +532,7 @@ int distill_parts(int64_t rows, int64_t classes) {
     int64_t parts = (2048 + rows - 1) / rows;
     const int64_t most = (classes + 2047) / 2048;
     parts = parts < most ? parts : most;
+    parts = parts < kSplitThreads ? parts : kSplitThreads;
     return static_cast<int>(parts < 1 ? 1 : parts);
   }
   return 0;
