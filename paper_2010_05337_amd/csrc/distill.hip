@@ -48,10 +48,6 @@ struct Chunk<float> {
     v[2] = __uint_as_float(x.z);
     v[3] = __uint_as_float(x.w);
   }
-  static __device__ __forceinline__ void store(float* p, const float (&v)[4]) {
-    const float4 x = make_float4(v[0], v[1], v[2], v[3]);
-    __builtin_memcpy(p, &x, 16);
-  }
   static __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 };
 template <>
@@ -66,7 +62,6 @@ struct Chunk<uint16_t> {
       v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
     }
   }
-  static __device__ __forceinline__ void store(uint16_t* p, const float (&v)[8]) { mx_store8(p, v, 8); }
   static __device__ __forceinline__ void store1(uint16_t* p, float v) {
     *p = static_cast<uint16_t>(mx_bf16x2_bits(v, 0.f));
   }
@@ -88,14 +83,10 @@ __device__ __forceinline__ uint4 load_chunk(const T* z, int64_t c, int64_t end) 
   return x;
 }
 template <typename T>
-__device__ __forceinline__ void store_chunk(T* grad, int64_t c, int64_t end, const float (&g)[Chunk<T>::N]) {
-  if (c + Chunk<T>::N <= end) {
-    Chunk<T>::store(grad + c, g);
-  } else {
-#pragma unroll
-    for (int i = 0; i < Chunk<T>::N; ++i)
-      if (c + i < end) Chunk<T>::store1(grad + c + i, g[i]);
-  }
+__device__ __forceinline__ void store_chunk(T* grad, int64_t c, int64_t end, const float (&g)[Chunk<T>::N],
+                                            bool stream) {
+  const int64_t left = end - c;
+  mx_store(grad + c, g, left < Chunk<T>::N ? static_cast<int>(left) : Chunk<T>::N, stream);
 }
 
 // Reductions over the TH threads of a row (a part of a wave, a wave, or the
@@ -313,7 +304,10 @@ void k_distill_held(DistillArgs a) {
   for (int k = 0; k < K; ++k) {
     const int c = (k * TH + t) * E;
     q[k] = tail;
-    if (c + E <= a.classes) __builtin_memcpy(&q[k], z + c, 16);
+    if (c + E <= a.classes) {
+      if (a.stream) mx_get_once<16>(&q[k], z + c);
+      else __builtin_memcpy(&q[k], z + c, 16);
+    }
   }
   if (whole % TH == t) {
     // (past that chunk there is nothing)
@@ -375,7 +369,7 @@ void k_distill_held(DistillArgs a) {
       if (c >= a.classes) break;
       float g[E] = {};
       if (!r.none) chunk_gradient<POW, T>(r, q[k], g);   // (0 whatever the logits are)
-      store_chunk(grad, c, a.classes, g);
+      store_chunk(grad, c, a.classes, g, a.stream);
       __builtin_amdgcn_sched_barrier(0);
     }
     for (int64_t c = a.classes + t; c < a.ld_grad; c += TH) Chunk<T>::store1(grad + c, 0.f);
@@ -468,7 +462,7 @@ __global__ __launch_bounds__(kSplitThreads) void k_distill_grad(DistillArgs a) {
   for (int64_t c = lo + t * E; c < hi; c += kSplitThreads * E) {
     float g[E] = {};
     if (!r.none) chunk_gradient<0, T>(r, load_chunk(z, c, hi), g);
-    store_chunk(grad, c, hi, g);
+    store_chunk(grad, c, hi, g, a.stream);
   }
   __syncthreads();
   correct_entries<T, kSplitThreads>(a, r, z, grad, first, t, ids, ps, lo, hi);
@@ -538,7 +532,12 @@ int distill_parts(int64_t rows, int64_t classes) {
   return 0;
 }
 
-hipError_t launch_distill(const DistillArgs& a, int bf16, hipStream_t s) {
+hipError_t launch_distill(const DistillArgs& args, int bf16, hipStream_t s) {
+  // a large gradient goes past the caches, and the logits it is made of too
+  // (4,099 x 32,768 bf16: 153.5 us plain, 145.6 with its stores, 142.3 with both;
+  // 8,000 x 1,000 fp32, 32 MB: 19.2, 19.2, 19.9)
+  DistillArgs a = args;
+  a.stream = a.rows * a.classes * (bf16 ? 2 : 4) >= 4 * kStreamBytes;
   if (bf16) dispatch<uint16_t>(a, s);
   else dispatch<float>(a, s);
   return hipGetLastError();

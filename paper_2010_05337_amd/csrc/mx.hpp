@@ -38,23 +38,29 @@ __device__ __forceinline__ uint32_t mx_scale_code(uint32_t top) {
 // fp32 (field 0 stands for 2^-127, field 255 makes every result NaN).
 __device__ __forceinline__ float mx_scale(uint32_t code) { return __uint_as_float(code << 23); }
 
-// Eight values as elements at scale `code`: one word (4 bits) or two.
-template <int BITS>
-__device__ __forceinline__ void mx_pack8(const float (&v)[8], uint32_t code, uint32_t (&w)[BITS / 4]) {
+// N values (4, or a multiple of 8) as elements at scale `code`: N BITS / 32
+// words, the first one's low half alone for four 4-bit elements.
+template <int BITS, int N>
+__device__ __forceinline__ void mx_pack(const float (&v)[N], uint32_t code, uint32_t (&w)[(N * BITS + 31) / 32]) {
   const float s = mx_scale(code);
   if constexpr (BITS == 4) {
-    uint32_t x = 0;
-    x = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(x, v[0], v[1], s, 0);
-    x = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(x, v[2], v[3], s, 1);
-    x = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(x, v[4], v[5], s, 2);
-    x = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(x, v[6], v[7], s, 3);
-    w[0] = code == 255 ? 0u : x;
+#pragma unroll
+    for (int i = 0; i < (N + 7) / 8; ++i) {
+      uint32_t x = 0;
+      x = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(x, v[8 * i], v[8 * i + 1], s, 0);
+      x = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(x, v[8 * i + 2], v[8 * i + 3], s, 1);
+      if constexpr (N >= 8) {
+        x = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(x, v[8 * i + 4], v[8 * i + 5], s, 2);
+        x = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(x, v[8 * i + 6], v[8 * i + 7], s, 3);
+      }
+      w[i] = code == 255 ? 0u : x;
+    }
   } else {
     // the 8-bit conversion turns what is past 448 into NaN: clamp to 448
     // scales first (1.75 * 2^8, at most 2^(246 + 8 - 127))
     const float most = __uint_as_float(((code + 8) << 23) | 0x600000u);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < N / 4; ++i) {
       float c[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) c[j] = fminf(fmaxf(v[4 * i + j], -most), most);
@@ -66,27 +72,54 @@ __device__ __forceinline__ void mx_pack8(const float (&v)[8], uint32_t code, uin
   }
 }
 
-// What eight elements stand for.
-template <int BITS>
-__device__ __forceinline__ void mx_unpack8(const uint32_t (&w)[BITS / 4], uint32_t code, float (&v)[8]) {
+// What N elements stand for.
+template <int BITS, int N>
+__device__ __forceinline__ void mx_unpack(const uint32_t (&w)[(N * BITS + 31) / 32], uint32_t code, float (&v)[N]) {
   const float s = mx_scale(code);
-  mx_f32x2 p[4];
+  auto put = [&](int at, mx_f32x2 p) {
+    v[at] = p[0];
+    v[at + 1] = p[1];
+  };
   if constexpr (BITS == 4) {
-    p[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[0], s, 0);
-    p[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[0], s, 1);
-    p[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[0], s, 2);
-    p[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[0], s, 3);
-  } else {
-    p[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[0], s, false);
-    p[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[0], s, true);
-    p[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[1], s, false);
-    p[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[1], s, true);
-  }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[2 * i] = p[i][0];
-    v[2 * i + 1] = p[i][1];
+    for (int i = 0; i < (N + 7) / 8; ++i) {
+      put(8 * i, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], s, 0));
+      put(8 * i + 2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], s, 1));
+      if constexpr (N >= 8) {
+        put(8 * i + 4, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], s, 2));
+        put(8 * i + 6, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], s, 3));
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+      put(4 * i, __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[i], s, false));
+      put(4 * i + 2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[i], s, true));
+    }
   }
+}
+
+// The largest magnitude's fp32 bits among v.
+template <int N>
+__device__ __forceinline__ uint32_t mx_top(const float (&v)[N]) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint32_t m = __float_as_uint(v[i]) & 0x7FFFFFFFu;
+    top = m > top ? m : top;
+  }
+  return top;
+}
+
+// The largest of the words of LANES (4 or 8) neighbouring lanes: their
+// neighbour's, the other pair's, the other four's.
+template <int LANES>
+__device__ __forceinline__ uint32_t mx_lanes_max(uint32_t x) {
+  auto with = [&](uint32_t o) { x = o > x ? o : x; };
+  with(__builtin_amdgcn_mov_dpp(static_cast<int>(x), 0xB1, 0xF, 0xF, true));                           // 1 0 3 2
+  with(__builtin_amdgcn_mov_dpp(static_cast<int>(x), 0x4E, 0xF, 0xF, true));                           // 2 3 0 1
+  if constexpr (LANES == 8) with(__builtin_amdgcn_mov_dpp(static_cast<int>(x), 0x141, 0xF, 0xF, true));  // 7 .. 0
+  return x;
 }
 
 // Two values as bf16 bits, to nearest even (v_cvt_pk_bf16_f32).
@@ -95,28 +128,46 @@ __device__ __forceinline__ uint32_t mx_bf16x2_bits(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, mx_bf16x2));
 }
 
-// Eight values to p, fp32 or bf16; `count` of them (8 at once where whole).
-__device__ __forceinline__ void mx_store8(float* p, const float (&v)[8], int count) {
-  if (count >= 8) {
-    const float4 a = make_float4(v[0], v[1], v[2], v[3]), b = make_float4(v[4], v[5], v[6], v[7]);
-    __builtin_memcpy(p, &a, 16);
-    __builtin_memcpy(p + 4, &b, 16);
+// BYTES bytes from or to p (any alignment).  stream: without a place in the
+// caches (non-temporal).
+template <int BYTES>
+struct MxWords {
+  typedef uint32_t Type __attribute__((ext_vector_type(BYTES / 4), aligned(2)));
+};
+template <int BYTES>
+__device__ __forceinline__ void mx_put(void* p, const void* v, bool stream) {
+  using Words = typename MxWords<BYTES>::Type;
+  Words x;
+  __builtin_memcpy(&x, v, BYTES);
+  if (stream)
+    __builtin_nontemporal_store(x, static_cast<Words*>(p));
+  else
+    *static_cast<Words*>(p) = x;
+}
+template <int BYTES>
+__device__ __forceinline__ void mx_get_once(void* v, const void* p) {
+  using Words = typename MxWords<BYTES>::Type;
+  const Words x = __builtin_nontemporal_load(static_cast<const Words*>(p));
+  __builtin_memcpy(v, &x, BYTES);
+}
+
+// 16 bytes of values to p, fp32 (4) or bf16 (8), or the first `count` of them.
+__device__ __forceinline__ void mx_store(float* p, const float (&v)[4], int count, bool stream) {
+  if (count >= 4) {
+    mx_put<16>(p, v, stream);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < 4; ++i)
       if (i < count) p[i] = v[i];
   }
 }
-__device__ __forceinline__ void mx_store8(uint16_t* p, const float (&v)[8], int count) {
-  uint4 x;
-  x.x = mx_bf16x2_bits(v[0], v[1]);
-  x.y = mx_bf16x2_bits(v[2], v[3]);
-  x.z = mx_bf16x2_bits(v[4], v[5]);
-  x.w = mx_bf16x2_bits(v[6], v[7]);
+__device__ __forceinline__ void mx_store(uint16_t* p, const float (&v)[8], int count, bool stream) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = mx_bf16x2_bits(v[2 * i], v[2 * i + 1]);
   if (count >= 8) {
-    __builtin_memcpy(p, &x, 16);
+    mx_put<16>(p, w, stream);
   } else {
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if (i < count) p[i] = static_cast<uint16_t>(w[i / 2] >> (16 * (i & 1)));

@@ -13,6 +13,14 @@ namespace gmb {
 // What a launcher writes: fp32 rows, bf16 rows, or 4-bit records.
 constexpr int kMxOutF32 = 0, kMxOutBf16 = 1, kMxOutRecords = 2;
 
+// Outputs of at least this many bytes are stored past the caches: the L2s (32
+// MB together) could not keep them for a reader, and writing them there costs
+// what it evicts.  Plain against streaming stores: reads of the store, 8 MB
+// of fp32 rows 4.5 / 4.0 us, 16 MB 6.5 / 5.9, 64 MB 21.7 / 17.2, 138 MB 54.6 /
+// 34.3; the linear layer, 23 MB 18.2 / 17.1, 46 MB 28.6 / 19.3, 205 MB 95.2 /
+// 48.8.  Smaller ones stay where the next kernel finds them.
+constexpr int64_t kStreamBytes = 16 << 20;
+
 inline int64_t mx_blocks(int64_t dim) { return (dim + 31) / 32; }
 inline int64_t mx_record(int64_t dim, int bits) {
   return (mx_blocks(dim) * (4 * bits + 1) + 15) / 16 * 16;
@@ -40,6 +48,7 @@ struct MxReadArgs {
   int64_t table_rows, table_stride;
   void* out;
   uint32_t* status;
+  bool stream;                      // set by the launchers, here and below
 };
 
 struct MxMeanArgs {
@@ -82,6 +91,7 @@ struct MxLinearArgs {
   int64_t out_stride;               // records: bytes
   int out_record;
   uint32_t* status;
+  bool stream;
 };
 hipError_t launch_mx_linear(const MxLinearArgs& a, int out, hipStream_t s);
 
@@ -103,6 +113,7 @@ struct DistillArgs {
   int parts;                        // workgroups of a row, with stats
   int32_t* clear;                   // cleared by the launch, clear_n words
   int64_t clear_n;
+  bool stream;
 };
 // Classes that a launch without stats can hold.
 constexpr int kDistillHeld = 32768;

@@ -77,7 +77,7 @@ __device__ __forceinline__ void store_values(const MxLinearArgs& p, int64_t row,
   if constexpr (OUT == kMxOutF32) {
     float* o = static_cast<float*>(p.out) + row * p.d_out + c;
     if (left >= CT) {
-      __builtin_memcpy(o, z, 4 * CT);
+      mx_put<4 * CT>(o, z, p.stream);
     } else {
 #pragma unroll
       for (int j = 0; j < CT; ++j)
@@ -89,7 +89,7 @@ __device__ __forceinline__ void store_values(const MxLinearArgs& p, int64_t row,
 #pragma unroll
     for (int j = 0; j < CT / 2; ++j) w[j] = mx_bf16x2_bits(z[2 * j], z[2 * j + 1]);
     if (left >= CT) {
-      __builtin_memcpy(o, w, 2 * CT);
+      mx_put<2 * CT>(o, w, p.stream);
     } else {
 #pragma unroll
       for (int j = 0; j < CT; ++j)
@@ -105,23 +105,18 @@ __device__ __forceinline__ void store_elements(const MxLinearArgs& p, bool in, i
                                                const float (&z)[CT]) {
   constexpr int LANES = 32 / CT;
   const int blocks = (p.d_out + 31) / 32;
-  uint32_t top = 0;
-#pragma unroll
-  for (int j = 0; j < CT; ++j) {
-    const uint32_t m = __float_as_uint(z[j]) & 0x7FFFFFFFu;
-    top = m > top ? m : top;
-  }
+  uint32_t top = mx_top(z);
 #pragma unroll
   for (int o = 1; o < LANES; o <<= 1) {
     const uint32_t x = __shfl_xor(top, o, 64);
     top = x > top ? x : top;
   }
   const uint32_t code = mx_scale_code<4>(top);
-  float v[8] = {};
+  float v[4] = {};
 #pragma unroll
   for (int j = 0; j < CT; ++j) v[j] = z[j];
   uint32_t w[1];
-  mx_pack8<4>(v, code, w);
+  mx_pack<4, 4>(v, code, w);
   const int blk = c / 32;
   if (!in || blk >= blocks) return;
   uint8_t* rec = static_cast<uint8_t*>(p.out) + row * p.out_stride;
@@ -502,7 +497,9 @@ void dispatch(const MxLinearArgs& p, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_mx_linear(const MxLinearArgs& p, int out, hipStream_t s) {
+hipError_t launch_mx_linear(const MxLinearArgs& args, int out, hipStream_t s) {
+  MxLinearArgs p = args;
+  p.stream = p.n_cap * p.d_out * (out == kMxOutBf16 ? 2 : 4) >= kStreamBytes;
   if (out == kMxOutRecords) dispatch<kMxOutRecords>(p, s);
   else if (out == kMxOutBf16) dispatch<kMxOutBf16>(p, s);
   else dispatch<kMxOutF32>(p, s);

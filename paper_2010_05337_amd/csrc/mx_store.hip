@@ -1,9 +1,9 @@
 // The microscaled vertex store on gfx950: rows written into it, read back
 // from it, and averaged straight out of it (mx.hpp has the format).
 //
-//   k_mx_write       rows x -> records: four lanes take a block, eight
-//                    elements each; the block's largest magnitude in two
-//                    lane exchanges
+//   k_mx_write       rows x -> records: a lane takes 16 bytes of a row, four
+//                    (bf16) or eight (fp32) lanes a block; the block's largest
+//                    magnitude in two or three lane exchanges
 //   k_mx_write_cols  the same for rows that lie across memory (a weight
 //                    matrix read by its columns): a lane takes a whole block,
 //                    neighbouring lanes neighbouring rows
@@ -12,6 +12,8 @@
 //   k_mx_mean        m_v = (1/k_v) sum_e value(table[ids[e]]), fp32 sums: a
 //                    lane takes one block of a destination, so a neighbour is
 //                    one 16-byte (4 bits) or two (8 bits) reads and a scale
+#include <type_traits>
+
 #include "mx.hpp"
 #include "mx_kernels.hpp"
 
@@ -27,24 +29,20 @@ __device__ __forceinline__ int64_t row_count(const int32_t* n_dev, int64_t n_cap
   return m < 0 ? 0 : (m < n_cap ? m : n_cap);
 }
 
-// Eight elements of a row from column c on, zeros past `dim`.
-__device__ __forceinline__ void load8(const float* p, int left, float (&v)[8]) {
-  if (left >= 8) {
-    float4 a, b;
-    __builtin_memcpy(&a, p, 16);
-    __builtin_memcpy(&b, p + 4, 16);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+// 16 bytes of a row's values (4 fp32, 8 bf16), zeros from `left` on; read
+// once, so past the caches (350,000 rows of 128 bf16: 39.9 us, 35.0 so).
+__device__ __forceinline__ void load_values(const float* p, int left, float (&v)[4]) {
+  if (left >= 4) {
+    mx_get_once<16>(v, p);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : 0.f;
+    for (int i = 0; i < 4; ++i) v[i] = i < left ? p[i] : 0.f;
   }
 }
-__device__ __forceinline__ void load8(const uint16_t* p, int left, float (&v)[8]) {
+__device__ __forceinline__ void load_values(const uint16_t* p, int left, float (&v)[8]) {
   if (left >= 8) {
-    uint4 a;
-    __builtin_memcpy(&a, p, 16);
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+    uint32_t w[4];
+    mx_get_once<16>(w, p);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       v[2 * i] = __uint_as_float(w[i] << 16);
@@ -71,8 +69,13 @@ __device__ __forceinline__ uint8_t* write_to(const MxWriteArgs& a, int64_t row, 
   return a.table + id * a.table_stride;
 }
 
-template <typename T, int BITS, int G>
+// A lane has 16 bytes of a row (E values), 32 / E lanes a block; a row's
+// values are asked for before its id is known.  TAIL: the scales and the
+// zeros after them are one 16-byte piece (at most 16 blocks, all of them in
+// one pass of the group), which the group's first lanes store at once.
+template <typename T, int BITS, int G, bool TAIL>
 __global__ __launch_bounds__(256) void k_mx_write(MxWriteArgs a) {
+  constexpr int E = 16 / sizeof(T), LB = 32 / E;
   constexpr int kCode = 4 * BITS;   // element bytes of a block
   const int lane = threadIdx.x & (G - 1);
   const int64_t n = row_count(a.n_dev, a.n_cap);
@@ -80,30 +83,33 @@ __global__ __launch_bounds__(256) void k_mx_write(MxWriteArgs a) {
   bool bad = false;
   for (int64_t row = static_cast<int64_t>(blockIdx.x) * (256 / G) + threadIdx.x / G; row < n;
        row += static_cast<int64_t>(gridDim.x) * (256 / G)) {
-    uint8_t* rec = write_to(a, row, bad);   // the group's lanes agree
-    if (!rec) continue;
-    const T* xr = x + row * a.row_stride;
-    for (int b = lane / 4; b < a.blocks; b += G / 4) {
-      const int at = b * kMxBlock + (lane & 3) * 8;
-      float v[8];
-      load8(xr + (at < a.dim ? at : 0), a.dim - at, v);
-      uint32_t top = 0;
+    uint8_t* rec = nullptr;
+    for (int b0 = 0; b0 < a.blocks; b0 += G / LB) {
+      const int b = b0 + lane / LB, at = (b0 * LB + lane) * E;
+      float v[E];
+      load_values(x + row * a.row_stride + (at < a.dim ? at : 0), a.dim - at, v);
+      if (b0 == 0) rec = write_to(a, row, bad);   // the group's lanes agree
+      const uint32_t code = mx_scale_code<BITS>(mx_lanes_max<LB>(mx_top(v)));   // (0 past the last block)
+      uint32_t w[(E * BITS + 31) / 32];
+      mx_pack<BITS, E>(v, code, w);
+      if (b < a.blocks && rec) __builtin_memcpy(rec + at * BITS / 8, w, E * BITS / 8);
+      if constexpr (TAIL) {
+        // lane i of the first four has the scales of blocks 4 i .. 4 i + 3
+        uint32_t word = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint32_t m = __float_as_uint(v[i]) & 0x7FFFFFFFu;
-        top = m > top ? m : top;
+        for (int i = 0; i < 4; ++i) {
+          const int from = LB * (4 * lane + i);
+          const uint32_t c = __shfl(code, from < G ? from : 0, G);
+          word |= (from < G ? c : 0u) << (8 * i);
+        }
+        if (lane < 4 && rec) __builtin_memcpy(rec + a.blocks * kCode + 4 * lane, &word, 4);
+      } else if (lane % LB == 0 && b < a.blocks && rec) {
+        rec[a.blocks * kCode + b] = static_cast<uint8_t>(code);
       }
-      uint32_t o = __shfl_xor(top, 1, 4);
-      top = o > top ? o : top;
-      o = __shfl_xor(top, 2, 4);
-      top = o > top ? o : top;
-      const uint32_t code = mx_scale_code<BITS>(top);
-      uint32_t w[BITS / 4];
-      mx_pack8<BITS>(v, code, w);
-      __builtin_memcpy(rec + b * kCode + (lane & 3) * BITS, w, BITS);
-      if ((lane & 3) == 0) rec[a.blocks * kCode + b] = static_cast<uint8_t>(code);
     }
-    for (int i = a.blocks * (kCode + 1) + lane; i < a.record; i += G) rec[i] = 0;
+    if constexpr (!TAIL)
+      if (rec)
+        for (int i = a.blocks * (kCode + 1) + lane; i < a.record; i += G) rec[i] = 0;
   }
   if (bad) raise_status(a.status, GMB_STATUS_ERANGE);
 }
@@ -122,24 +128,15 @@ __global__ __launch_bounds__(256) void k_mx_write_cols(MxWriteArgs a) {
     const T* xr = x + row * a.row_stride;
     for (int blk = b * 4 + (threadIdx.x >> 6); blk < a.blocks; blk += 4 * gridDim.y) {
       float v[kMxBlock];
-      uint32_t top = 0;
 #pragma unroll
       for (int i = 0; i < kMxBlock; ++i) {
         const int c = blk * kMxBlock + i;
         v[i] = c < a.dim ? load1(xr + c * a.col_stride) : 0.f;
-        const uint32_t m = __float_as_uint(v[i]) & 0x7FFFFFFFu;
-        top = m > top ? m : top;
       }
-      const uint32_t code = mx_scale_code<BITS>(top);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        float u[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) u[i] = v[8 * q + i];
-        uint32_t w[BITS / 4];
-        mx_pack8<BITS>(u, code, w);
-        __builtin_memcpy(rec + blk * kCode + q * BITS, w, BITS);
-      }
+      const uint32_t code = mx_scale_code<BITS>(mx_top(v));
+      uint32_t w[BITS];
+      mx_pack<BITS, kMxBlock>(v, code, w);
+      __builtin_memcpy(rec + blk * kCode, w, kCode);
       rec[a.blocks * kCode + blk] = static_cast<uint8_t>(code);
       if (blk == 0)
         for (int i = a.blocks * (kCode + 1); i < a.record; ++i) rec[i] = 0;
@@ -164,14 +161,18 @@ __global__ __launch_bounds__(256) void k_mx_claim(const int32_t* ids, const int3
   }
 }
 
-// U rows of a group in flight; every load unconditional from a clamped
-// address (row 0 for a group without a row or with an id outside the table).
+// A lane writes 16 bytes of a row (E values), so that a group's stores are one
+// contiguous piece (346,000 rows of 100 fp32: 55 us, 69 where four lanes' 64
+// bytes lay 128 apart, 34 with streaming stores).  U rows of a group in flight; every load
+// unconditional from a clamped address (row 0 for a group without a row or
+// with an id outside the table).
 template <typename T, int BITS, int G, int U>
 __global__ __launch_bounds__(256) void k_mx_read(MxReadArgs a) {
-  constexpr int kCode = 4 * BITS;
+  constexpr int E = 16 / sizeof(T), kBytes = E * BITS / 8;
   const int lane = threadIdx.x & (G - 1);
   const int64_t n = row_count(a.n_dev, a.n_cap);
   const int64_t stride = static_cast<int64_t>(gridDim.x) * (256 / G);
+  const int chunks = (a.dim + E - 1) / E, scales = a.blocks * 4 * BITS;
   T* out = static_cast<T*>(a.out);
   bool bad = false;
   for (int64_t row = static_cast<int64_t>(blockIdx.x) * (256 / G) + threadIdx.x / G; row < n; row += stride * U) {
@@ -189,47 +190,47 @@ __global__ __launch_bounds__(256) void k_mx_read(MxReadArgs a) {
       in[u] = here & ok;
       id[u] = in[u] ? id[u] : 0;
     }
-    for (int b = lane / 4; b < a.blocks; b += G / 4) {
-      const int q = lane & 3, at = b * kMxBlock + q * 8;
-      uint32_t w[U][BITS / 4];
+    for (int c = lane; c < chunks; c += G) {
+      uint32_t w[U][(E * BITS + 31) / 32];
       uint32_t code[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const uint8_t* rec = a.table + id[u] * a.table_stride;
-        __builtin_memcpy(w[u], rec + b * kCode + q * BITS, BITS);
-        code[u] = rec[a.blocks * kCode + b];
+        if constexpr (kBytes == 2) w[u][0] = 0;
+        __builtin_memcpy(w[u], rec + c * kBytes, kBytes);
+        code[u] = rec[scales + c / (32 / E)];
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int64_t r = row + u * stride;
-        if (r >= n || at >= a.dim) continue;
-        float v[8];
-        mx_unpack8<BITS>(w[u], code[u], v);
+        float v[E];
+        mx_unpack<BITS, E>(w[u], code[u], v);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = in[u] ? v[i] : 0.f;
-        mx_store8(out + r * a.dim + at, v, a.dim - at);
+        for (int i = 0; i < E; ++i) v[i] = in[u] ? v[i] : 0.f;
+        if (r < n) mx_store(out + r * a.dim + c * E, v, a.dim - c * E, a.stream);
       }
     }
   }
   if (bad) raise_status(a.status, GMB_STATUS_ERANGE);
 }
 
-// OUT: 0 fp32 rows, 1 bf16 rows, 2 records of 4 bits.  Lane l of a
-// destination's G lanes owns blocks l, l + G, ...; U neighbours in flight.
-// An id outside the table is read as row 0 (k_mean's rule).
+// OUT: 0 fp32 rows, 1 bf16 rows, 2 records of 4 bits.  A lane has E elements
+// of a destination (16 bytes of its row), G lanes a destination; U neighbours
+// in flight.  An id outside the table is read as row 0 (k_mean's rule).
 template <int BITS, int OUT, int G, int U>
 __global__ __launch_bounds__(256) void k_mx_mean(MxMeanArgs a) {
-  constexpr int kCode = 4 * BITS;
+  constexpr int E = OUT == 0 ? 4 : 8, LB = 32 / E, kBytes = E * BITS / 8, kWords = (E * BITS + 31) / 32;
   const int64_t row = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) / G;
   const int lane = threadIdx.x & (G - 1);
   const int64_t rc = row < a.n_cap ? row : a.n_cap - 1;
   const int32_t beg = a.indptr[rc], end = a.indptr[rc + 1];
   if (row >= row_count(a.n_dev, a.n_cap)) return;
   const int32_t k = end - beg;
-  for (int b = lane; b < a.blocks; b += G) {
-    float acc[kMxBlock];
+  const int chunks = OUT == 2 ? a.blocks * LB : (a.dim + E - 1) / E, scales = a.blocks * 4 * BITS;
+  for (int c = lane; c < chunks; c += G) {
+    float acc[E];
 #pragma unroll
-    for (int i = 0; i < kMxBlock; ++i) acc[i] = 0.f;
+    for (int i = 0; i < E; ++i) acc[i] = 0.f;
     for (int32_t e = 0; e < k; e += U) {
       int64_t id[U];
 #pragma unroll
@@ -237,73 +238,43 @@ __global__ __launch_bounds__(256) void k_mx_mean(MxMeanArgs a) {
         const int32_t i = a.ids[beg + (e + u < k ? e + u : e)];
         id[u] = valid_vertex(i, a.table_rows) ? i : 0;
       }
-      uint4 w[U][BITS / 4];
+      uint32_t w[U][kWords];
       uint32_t code[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const uint8_t* rec = a.table + id[u] * a.table_stride;
-        __builtin_memcpy(w[u], rec + b * kCode, kCode);
-        code[u] = rec[a.blocks * kCode + b];
+        if constexpr (kBytes == 2) w[u][0] = 0;
+        __builtin_memcpy(w[u], rec + c * kBytes, kBytes);
+        code[u] = rec[scales + c / LB];
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         // a slot past the row's end: zeros at scale 1 (adding +0 changes
         // nothing)
         const bool in = e + u < k;
-        const uint32_t c = in ? code[u] : 127u;
-        uint32_t words[BITS];
-        __builtin_memcpy(words, w[u], kCode);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          uint32_t part[BITS / 4];
+        for (int j = 0; j < kWords; ++j) w[u][j] = in ? w[u][j] : 0u;
+        float v[E];
+        mx_unpack<BITS, E>(w[u], in ? code[u] : 127u, v);
 #pragma unroll
-          for (int j = 0; j < BITS / 4; ++j) part[j] = in ? words[q * (BITS / 4) + j] : 0u;
-          float v[8];
-          mx_unpack8<BITS>(part, c, v);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) acc[8 * q + i] += v[i];
-        }
+        for (int i = 0; i < E; ++i) acc[i] += v[i];
       }
     }
     if (k > 0) {
       const float kf = static_cast<float>(k);
 #pragma unroll
-      for (int i = 0; i < kMxBlock; ++i) acc[i] = acc[i] / kf;
+      for (int i = 0; i < E; ++i) acc[i] = acc[i] / kf;
     }
     if constexpr (OUT == 2) {
-      uint32_t top = 0;
-#pragma unroll
-      for (int i = 0; i < kMxBlock; ++i) {
-        const uint32_t m = __float_as_uint(acc[i]) & 0x7FFFFFFFu;
-        top = m > top ? m : top;
-      }
-      const uint32_t code = mx_scale_code<4>(top);
+      const uint32_t code = mx_scale_code<4>(mx_lanes_max<LB>(mx_top(acc)));
       uint8_t* rec = static_cast<uint8_t*>(a.out) + row * a.out_stride;
-      uint32_t w[4];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        float v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = acc[8 * q + i];
-        uint32_t part[1];
-        mx_pack8<4>(v, code, part);
-        w[q] = part[0];
-      }
-      __builtin_memcpy(rec + b * 16, w, 16);
-      rec[a.blocks * 16 + b] = static_cast<uint8_t>(code);
+      uint32_t w[1];
+      mx_pack<4, E>(acc, code, w);
+      __builtin_memcpy(rec + c * 4, w, 4);
+      if (c % LB == 0) rec[a.blocks * 16 + c / LB] = static_cast<uint8_t>(code);
     } else {
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int at = b * kMxBlock + 8 * q;
-        if (at >= a.dim) break;
-        float v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = acc[8 * q + i];
-        if constexpr (OUT == 0)
-          mx_store8(static_cast<float*>(a.out) + row * a.dim + at, v, a.dim - at);
-        else
-          mx_store8(static_cast<uint16_t*>(a.out) + row * a.dim + at, v, a.dim - at);
-      }
+      using O = std::conditional_t<OUT == 0, float, uint16_t>;
+      mx_store(static_cast<O*>(a.out) + row * a.dim + c * E, acc, a.dim - c * E, false);
     }
   }
   if constexpr (OUT == 2) {
@@ -332,22 +303,29 @@ void write_dispatch(const MxWriteArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((k_mx_write_cols<T, BITS>), dim3(grid_for(a.n_cap, 64), gy), dim3(256), 0, s, a);
     return;
   }
-#define GMB_MX_WRITE(GG) hipLaunchKernelGGL((k_mx_write<T, BITS, GG>), dim3(grid_for(a.n_cap, 256 / GG)), dim3(256), 0, s, a)
-  switch (lanes_for(4 * a.blocks, 4)) {
-    case 4: GMB_MX_WRITE(4); break;
-    case 8: GMB_MX_WRITE(8); break;
-    case 16: GMB_MX_WRITE(16); break;
-    case 32: GMB_MX_WRITE(32); break;
-    default: GMB_MX_WRITE(64); break;
+#define GMB_MX_WRITE(GG, TAIL) \
+  hipLaunchKernelGGL((k_mx_write<T, BITS, GG, TAIL>), dim3(grid_for(a.n_cap, 256 / GG)), dim3(256), 0, s, a)
+  constexpr int LB = 2 * static_cast<int>(sizeof(T));   // lanes of a block
+  switch (lanes_for(LB * a.blocks, LB)) {
+    case 4: GMB_MX_WRITE(LB, true); break;
+    case 8: GMB_MX_WRITE(8, true); break;
+    case 16: GMB_MX_WRITE(16, true); break;
+    case 32: GMB_MX_WRITE(32, true); break;
+    default:
+      if (LB * a.blocks <= 64) GMB_MX_WRITE(64, true);
+      else GMB_MX_WRITE(64, false);
+      break;
   }
 #undef GMB_MX_WRITE
 }
 
 template <typename T, int BITS>
 void read_dispatch(const MxReadArgs& a, hipStream_t s) {
-  constexpr int U = 4;
-#define GMB_MX_READ(GG) hipLaunchKernelGGL((k_mx_read<T, BITS, GG, U>), dim3(grid_for(a.n_cap, (256 / GG) * U)), dim3(256), 0, s, a)
-  switch (lanes_for(4 * a.blocks, 4)) {
+  constexpr int U = 4, E = 16 / static_cast<int>(sizeof(T));
+#define GMB_MX_READ(GG) \
+  hipLaunchKernelGGL((k_mx_read<T, BITS, GG, U>), dim3(grid_for(a.n_cap, (256 / GG) * U)), dim3(256), 0, s, a)
+  switch (lanes_for((a.dim + E - 1) / E, 2)) {
+    case 2: GMB_MX_READ(2); break;
     case 4: GMB_MX_READ(4); break;
     case 8: GMB_MX_READ(8); break;
     case 16: GMB_MX_READ(16); break;
@@ -359,13 +337,11 @@ void read_dispatch(const MxReadArgs& a, hipStream_t s) {
 
 template <int BITS, int OUT>
 void mean_dispatch(const MxMeanArgs& a, hipStream_t s) {
-  constexpr int U = BITS == 4 ? 16 : 8;
-  const int g = lanes_for(a.blocks, 1);
+  constexpr int U = 8, E = OUT == 0 ? 4 : 8;
+  const int g = lanes_for(OUT == 2 ? a.blocks * 4 : (a.dim + E - 1) / E, 4);
   const dim3 grid(static_cast<unsigned>((a.n_cap * g + 255) / 256));
 #define GMB_MX_MEAN(GG) hipLaunchKernelGGL((k_mx_mean<BITS, OUT, GG, U>), grid, dim3(256), 0, s, a)
   switch (g) {
-    case 1: GMB_MX_MEAN(1); break;
-    case 2: GMB_MX_MEAN(2); break;
     case 4: GMB_MX_MEAN(4); break;
     case 8: GMB_MX_MEAN(8); break;
     case 16: GMB_MX_MEAN(16); break;
@@ -396,7 +372,9 @@ hipError_t launch_mx_write(const MxWriteArgs& args, int bf16, int bits, uint32_t
   return hipGetLastError();
 }
 
-hipError_t launch_mx_read(const MxReadArgs& a, int bf16, int bits, hipStream_t s) {
+hipError_t launch_mx_read(const MxReadArgs& args, int bf16, int bits, hipStream_t s) {
+  MxReadArgs a = args;
+  a.stream = a.n_cap * a.dim * (bf16 ? 2 : 4) >= kStreamBytes;
   if (bits == 4) {
     if (bf16) read_dispatch<uint16_t, 4>(a, s);
     else read_dispatch<float, 4>(a, s);
