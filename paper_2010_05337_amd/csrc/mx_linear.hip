@@ -20,6 +20,7 @@
 // a kilobyte; the LDS kernels therefore load four neighbouring lanes a row (16
 // accesses) and take the operands' order when they read LDS.  (8192 x 4096 x
 // 4096, LDS filled in operand order: 125 us.)
+#include "kernels.hpp"
 #include "mx.hpp"
 #include "mx_kernels.hpp"
 
@@ -56,14 +57,15 @@ __device__ __forceinline__ int64_t count_rows(const MxLinearArgs& p) {
   return m < 0 ? 0 : (m < p.n_cap ? m : p.n_cap);
 }
 
-// Row `row` (< n) of a pair's A: its record, or NULL for an id outside the
-// table, which is reported.
-__device__ __forceinline__ const uint8_t* a_record(const MxLinearArgs& p, const MxPair& m, int64_t row) {
-  if (!m.ids) return m.a + row * m.a_stride;
-  const int32_t v = m.ids[row];
+// The record of id v, or NULL for one outside the table, which is reported.
+__device__ __forceinline__ const uint8_t* id_record(const MxLinearArgs& p, const MxPair& m, int32_t v) {
   if (valid_vertex(v, m.a_rows)) return m.a + v * m.a_stride;
   raise_status(p.status, GMB_STATUS_ERANGE);
   return nullptr;
+}
+// Row `row` (< n) of a pair's A.
+__device__ __forceinline__ const uint8_t* a_record(const MxLinearArgs& p, const MxPair& m, int64_t row) {
+  return m.ids ? id_record(p, m, m.ids[row]) : m.a + row * m.a_stride;
 }
 // Output column c's weights (the last column's past it: never stored).
 __device__ __forceinline__ const uint8_t* w_record(const MxLinearArgs& p, const MxPair& m, int c) {
@@ -126,15 +128,20 @@ __device__ __forceinline__ void store_elements(const MxLinearArgs& p, bool in, i
     for (int b = blocks * 17 + (c % 32) / CT; b < p.out_record; b += LANES) rec[b] = 0;
 }
 
+// The bias of a lane's columns.
+template <int CT>
+__device__ __forceinline__ void load_bias(const MxLinearArgs& p, int c0, int lane, float (&bias)[CT]) {
+  const int c = c0 + CT * (lane & 15);
+#pragma unroll
+  for (int j = 0; j < CT; ++j) bias[j] = p.bias && c + j < p.d_out ? p.bias[c + j] : 0.f;
+}
+
 // Bias, activation and store of a wave's tiles: rows r0 + 16 i + 4 g + e,
 // columns c0 + CT r + j.
 template <int RT, int CT, int OUT>
 __device__ __forceinline__ void epilogue(const MxLinearArgs& p, int64_t n, int64_t r0, int c0, int lane,
-                                         const floatx4 (&acc)[RT][CT]) {
+                                         const float (&bias)[CT], const floatx4 (&acc)[RT][CT]) {
   const int c = c0 + CT * (lane & 15);
-  float bias[CT];
-#pragma unroll
-  for (int j = 0; j < CT; ++j) bias[j] = p.bias && c + j < p.d_out ? p.bias[c + j] : 0.f;
 #pragma unroll
   for (int i = 0; i < RT; ++i)
 #pragma unroll
@@ -227,67 +234,86 @@ __global__ __launch_bounds__(64 * WK) void k_mx_linear_rows(MxLinearArgs p) {
 #pragma unroll
         for (int j = 0; j < CT; ++j) acc[i][j] += part[((k * RT + i) * CT + j) * 64 + lane];
   }
-  epilogue<RT, CT, OUT>(p, n, r0, c0, lane, acc);
+  float bias[CT];
+  load_bias(p, c0, lane, bias);
+  epilogue<RT, CT, OUT>(p, n, r0, c0, lane, bias, acc);
 }
 
 // ---- short sums, many rows ------------------------------------------------
 
 // A workgroup of WR x WC waves has 64 WC columns, whose whole records lie in
 // LDS from the start, and goes over tiles of 64 WR rows, whose records it
-// loads tile by tile (two workgroups a CU take turns).  In LDS a record is
-// `slots` 16-byte pieces, an odd number: sixteen rows' reads of one block
-// fall on different banks.
-constexpr int kResidentLds = 80 * 1024 - 64;
+// brings tile by tile; three workgroups a CU hide each other's waits (two with
+// 80 KB each: 14.4 us against 12.6 for 45,000 rows, two pairs of 100 by 256;
+// the next tile's rows arriving during this one's products, in a second
+// buffer, changed nothing).  In LDS a record is `slots` 16-byte pieces, an odd
+// number: sixteen rows' reads of one block fall on different banks.
+constexpr int kResidentLds = 50 * 1024;
 
 __host__ __device__ inline int resident_slots(int blocks) { return (((blocks * 17 + 15) / 16) | 1); }
-__host__ __device__ inline int resident_bytes(int rows, int pairs, int blocks) {
-  return (rows * pairs * resident_slots(blocks) * 16 + 1023) / 1024 * 1024;
+
+// x / d for x < 2^16 and d >= 1 by one multiplication: m = floor((2^32 - 1) / d)
+// + 1 is above 2^32 / d by at most 1, so x m is off by less than 2^16 of 2^32 a
+// unit of the quotient, and a fraction of x / d is at most 1 - 1 / d.
+__device__ __forceinline__ int quotient(int x, uint32_t m) {
+  return static_cast<int>(__umulhi(static_cast<uint32_t>(x), m));
 }
 
 template <int WR, int WC, int OUT>
-__global__ __launch_bounds__(64 * WR * WC, 2) void k_mx_linear_resident(MxLinearArgs p, int tiles) {
+__global__ __launch_bounds__(64 * WR * WC, 2) void k_mx_linear_resident(MxLinearArgs p) {
   constexpr int WAVES = WR * WC, ROWS = 64 * WR, COLS = 64 * WC;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[kResidentLds];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, r = lane & 15;
   const int wr = wave / WC, wc = wave % WC;
   const int64_t n = count_rows(p);
-  const int c0 = blockIdx.y * COLS;
+  const int tiles = static_cast<int>((n + ROWS - 1) / ROWS);
+  const int c0 = blockIdx.y * COLS, cw = c0 + 64 * wc;
   const int slots = resident_slots(p.blocks), pieces = (p.blocks * 17 + 15) / 16;
-  uint8_t* lw = lds;
-  uint8_t* la = lds + resident_bytes(COLS, p.pairs, p.blocks);
-  if (static_cast<int64_t>(blockIdx.x) * ROWS >= n) return;
-  // `count` records (record q of them at q * slots pieces) by 64 pieces a load
+  const uint32_t by_slots = 0xFFFFFFFFu / static_cast<uint32_t>(slots) + 1;   // (slots >= 3)
+  const int a_side = ROWS * slots * 16, w_side = COLS * slots * 16;           // bytes of a pair's records
+  uint8_t* lw = lds + p.pairs * a_side;
+  int t = blockIdx.x;
+  if (t >= tiles) return;
+  // `count` records (record q of them at q * slots pieces), 64 pieces a load
   auto bring = [&](uint8_t* to, int count, auto&& record) {
     const int total = count * slots;
     for (int q0 = 64 * wave; q0 < total; q0 += 64 * WAVES) {
-      const int q = q0 + lane, at = q / slots, piece = q - at * slots;
-      const uint8_t* rec = at < count ? record(at) : nullptr;
-      load_lds(rec && piece < pieces ? static_cast<const void*>(rec + piece * 16) : kZeros, to + q0 * 16);
+      const int q = q0 + lane, at = quotient(q, by_slots), piece = q - at * slots;
+      if (q < total) {
+        const uint8_t* rec = record(at);
+        load_lds(rec && piece < pieces ? static_cast<const void*>(rec + piece * 16) : kZeros, to + q0 * 16);
+      }
     }
   };
-  bring(lw, p.pairs * COLS, [&](int at) {
-    // LDS order: 16-column tile j of 64 columns has columns 4 r + j
-    const MxPair& m = p.pair[at / COLS];
-    const int i = at % COLS;
-    return w_record(p, m, c0 + (i & ~63) + 4 * (i & 15) + ((i >> 4) & 3));
-  });
-  const int steps = (p.blocks + 3) / 4;
-  for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
-    const int64_t r0 = static_cast<int64_t>(t) * ROWS;
-    if (r0 >= n) break;
-    bring(la, p.pairs * ROWS, [&](int at) -> const uint8_t* {
-      const int64_t row = r0 + at % ROWS;
-      return row < n ? a_record(p, p.pair[at / ROWS], row) : nullptr;
+  auto bring_rows = [&](int tile) {
+    const int64_t r0 = static_cast<int64_t>(tile) * ROWS;
+    for (int pr = 0; pr < p.pairs; ++pr) {
+      const MxPair& m = p.pair[pr];
+      bring(lds + pr * a_side, ROWS,
+            [&](int at) -> const uint8_t* { return r0 + at < n ? a_record(p, m, r0 + at) : nullptr; });
+    }
+  };
+  float bias[4];
+  load_bias(p, cw, lane, bias);
+  for (int pr = 0; pr < p.pairs; ++pr) {
+    const MxPair& m = p.pair[pr];
+    bring(lw + pr * w_side, COLS, [&](int at) {
+      // LDS order: 16-column tile j of 64 columns has columns 4 r + j
+      return w_record(p, m, c0 + (at & ~63) + 4 * (at & 15) + ((at >> 4) & 3));
     });
-    __syncthreads();            // what was loaded has arrived
+  }
+  bring_rows(t);
+  const int steps = (p.blocks + 3) / 4;
+  for (;;) {
+    __syncthreads();            // the tile has arrived
     floatx4 acc[4][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
     for (int pr = 0; pr < p.pairs; ++pr) {
-      const uint8_t* ra = la + (pr * ROWS + 64 * wr + r) * slots * 16;
-      const uint8_t* rw = lw + (pr * COLS + 64 * wc + r) * slots * 16;
+      const uint8_t* ra = lds + pr * a_side + (64 * wr + r) * slots * 16;
+      const uint8_t* rw = lw + pr * w_side + (64 * wc + r) * slots * 16;
       for (int s = 0; s < steps; ++s) {
         const int b = 4 * s + g;
         const bool in = b < p.blocks;
@@ -320,8 +346,14 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_mx_linear_resident(MxLinear
           for (int j = 0; j < 4; ++j) acc[i][j] = mfma_mx4<0>(qa[i], sa[i], qw[j], sw[j], acc[i][j]);
       }
     }
-    __syncthreads();            // the rows are read
-    if (c0 + 64 * wc < p.d_out) epilogue<4, 4, OUT>(p, n, r0 + 64 * wr, c0 + 64 * wc, lane, acc);
+    const int64_t r0 = static_cast<int64_t>(t) * ROWS + 64 * wr;
+    t += gridDim.x;
+    if (t < tiles) {
+      __syncthreads();          // the rows are read
+      bring_rows(t);
+    }
+    if (cw < p.d_out) epilogue<4, 4, OUT>(p, n, r0, cw, lane, bias, acc);
+    if (t >= tiles) break;
   }
 }
 
@@ -368,20 +400,27 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_mx_linear_tiles(MxLinearArg
     for (int j = 0; j < CT; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
   for (int pr = 0; pr < p.pairs; ++pr) {
     const MxPair& m = p.pair[pr];
-    // LDS row x: A's rows, then W's, dealt to a wave's column tiles
-    auto record = [&](int x) -> const uint8_t* {
-      if (x < TM) return a_record(p, m, r0 + x < n ? r0 + x : n - 1);
-      const int i = x - TM;
-      return w_record(p, m, c0 + (i & ~63) + 4 * (i & 15) + ((i >> 4) & 3));
-    };
-    const uint8_t* rec[PER];
+    // LDS row x: A's rows, then W's, dealt to a wave's column tiles.  The ids
+    // are asked for together.
+    int at[PER + SLOADS];
+    int32_t id[PER + SLOADS];
 #pragma unroll
-    for (int i = 0; i < PER; ++i) rec[i] = record(16 * (PER * wave + i) + lane / 4);
-    const uint8_t* scales[SLOADS];
+    for (int i = 0; i < PER + SLOADS; ++i)
+      at[i] = i < PER ? 16 * (PER * wave + i) + lane / 4 : 64 * (SLOADS * wave + i - PER) + lane;
+    if (m.ids) {
 #pragma unroll
-    for (int i = 0; i < SLOADS; ++i) {
-      const int at = 64 * (SLOADS * wave + i);
-      scales[i] = at < TM + TN ? record(at + lane) : nullptr;
+      for (int i = 0; i < PER + SLOADS; ++i) id[i] = m.ids[at[i] < TM && r0 + at[i] < n ? r0 + at[i] : n - 1];
+    }
+    const uint8_t* from[PER + SLOADS];
+#pragma unroll
+    for (int i = 0; i < PER + SLOADS; ++i) {
+      if (at[i] < TM) {
+        const int64_t row = r0 + at[i] < n ? r0 + at[i] : n - 1;
+        from[i] = m.ids ? id_record(p, m, id[i]) : m.a + row * m.a_stride;
+      } else {
+        const int c = at[i] - TM;
+        from[i] = w_record(p, m, c0 + (c & ~63) + 4 * (c & 15) + ((c >> 4) & 3));
+      }
     }
     const int x = (lane & 3) ^ tile_swizzle(lane / 4);
     auto fetch = [&](int k) {
@@ -391,17 +430,17 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_mx_linear_tiles(MxLinearArg
 #pragma unroll
         for (int f = 0; f < 2; ++f) {
           const int b = 8 * k + 4 * f + x;
-          load_lds(rec[i] && b < p.blocks ? static_cast<const void*>(rec[i] + b * 16) : kZeros,
+          load_lds(from[i] && b < p.blocks ? static_cast<const void*>(from[i] + b * 16) : kZeros,
                    to + (2 * i + f) * 1024);
         }
       // (16 scale bytes of blocks that there are lie in the padded record)
       if ((k & 1) == 0) {
 #pragma unroll
         for (int i = 0; i < SLOADS; ++i) {
-          const int at = SLOADS * wave + i;
-          if (64 * at < TM + TN)
-            load_lds(scales[i] ? static_cast<const void*>(scales[i] + p.blocks * 16 + 8 * k) : kZeros,
-                     lds + 2 * kStage + ((k >> 1) & 1) * kScales + at * 1024);
+          const uint8_t* rec = from[PER + i];
+          if (64 * (SLOADS * wave + i) < TM + TN)
+            load_lds(rec ? static_cast<const void*>(rec + p.blocks * 16 + 8 * k) : kZeros,
+                     lds + 2 * kStage + ((k >> 1) & 1) * kScales + (SLOADS * wave + i) * 1024);
         }
       }
     };
@@ -437,7 +476,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_mx_linear_tiles(MxLinearArg
     }
   }
   const int cw = c0 + 16 * CT * wc;
-  if (cw < p.d_out) epilogue<RT, CT, OUT>(p, n, r0 + 16 * RT * wr, cw, lane, acc);
+  float bias[CT];
+  load_bias(p, cw, lane, bias);
+  if (cw < p.d_out) epilogue<RT, CT, OUT>(p, n, r0 + 16 * RT * wr, cw, lane, bias, acc);
 }
 
 // ---- dispatch -------------------------------------------------------------
@@ -461,34 +502,46 @@ template <int WR, int WC, int OUT>
 void run_resident(const MxLinearArgs& p, hipStream_t s) {
   const int64_t tiles = (p.n_cap + 64 * WR - 1) / (64 * WR);
   const unsigned gy = static_cast<unsigned>((p.d_out + 64 * WC - 1) / (64 * WC));
-  const int64_t most = gy >= 512 ? 1 : 512 / gy;
+  const int64_t most = gy >= 768 ? 1 : 768 / gy;
   hipLaunchKernelGGL((k_mx_linear_resident<WR, WC, OUT>), dim3(static_cast<unsigned>(tiles < most ? tiles : most), gy),
-                     dim3(64 * WR * WC), 0, s, p, static_cast<int>(tiles));
+                     dim3(64 * WR * WC), 0, s, p);
 }
 
+// Whether both sides' records fit LDS.
 template <int WR, int WC>
 bool resident_fits(const MxLinearArgs& p) {
-  return resident_bytes(64 * WC, p.pairs, p.blocks) + resident_bytes(64 * WR, p.pairs, p.blocks) <= kResidentLds;
+  return p.blocks < 64 && 64 * (WC + WR) * p.pairs * resident_slots(p.blocks) * 16 <= kResidentLds;
 }
 
+// Which kernel, by the workgroups that its tiles give (us, bf16 results):
+//   - up to two workgroups a CU of 16 rows by 32 columns: k_mx_linear_rows (64
+//     x 4,096 x 1,024: 7.0, in 64 x 64 tiles 12.3; 300 x 1,024 x 256: 4.2 and
+//     6.4; but 1,000 x 256 x 1,024, 2,016 workgroups: 10.3 and 5.1);
+//   - resident weights where they fit and there are most of two tiles a CU
+//     (30,000 x 100 x 256: 8.0, tiles 10.7, 8.9 and 11.3 by size; 200,000 x 256
+//     x 256: 28.2, 50.2, 41.6, 41.5; but 16,000 x 256 x 256, 250 tiles: 7.9
+//     and 6.6);
+//   - else 256 x 256 tiles if there are three for every four CUs (8,192 x 4,096
+//     x 4,096: 82, in 128 x 128 96, in 64 x 64 141; but 8,000 x 1,024 x 1,024,
+//     128 of them: 18.4, 14.4, 18.2);
+//   - 128 x 128 if there are three for two CUs (2,000 x 4,096 x 4,096: 28.9,
+//     in 64 x 64 46.5; but 1,000 x 256 x 4,096, 256 of them: 7.5 and 6.6);
+//   - 64 x 64.
 template <int OUT>
 void dispatch(const MxLinearArgs& p, hipStream_t s) {
-  auto tiles_of = [&](int tm, int tn) { return ((p.n_cap + tm - 1) / tm) * ((p.d_out + tn - 1) / tn); };
-  if (p.n_cap <= 16) {
+  auto tiles = [&](int tm, int tn) { return ((p.n_cap + tm - 1) / tm) * ((p.d_out + tn - 1) / tn); };
+  constexpr int64_t kResidentTiles = 448;
+  if (tiles(16, 32) <= 2 * kComputeUnits) {
     run_rows<1, 2, 8, OUT>(p, s);
-  } else if (p.n_cap <= 64) {
-    run_rows<2, 2, 8, OUT>(p, s);
-  } else if (p.d_out > 128 && resident_fits<1, 4>(p)) {
+  } else if (p.d_out > 128 && resident_fits<1, 4>(p) && tiles(64, 256) >= kResidentTiles) {
     run_resident<1, 4, OUT>(p, s);
-  } else if (p.d_out > 64 && resident_fits<2, 2>(p)) {
+  } else if (p.d_out > 64 && p.d_out <= 128 && resident_fits<2, 2>(p) && tiles(128, 128) >= kResidentTiles) {
     run_resident<2, 2, OUT>(p, s);
-  } else if (p.d_out <= 64 && resident_fits<4, 1>(p)) {
+  } else if (p.d_out <= 64 && resident_fits<4, 1>(p) && tiles(256, 64) >= kResidentTiles) {
     run_resident<4, 1, OUT>(p, s);
-  } else if (p.d_out <= 64 && tiles_of(128, 64) >= 128) {
-    run_tiles<128, 64, 2, 1, OUT>(p, s);
-  } else if (p.d_out > 128 && tiles_of(256, 256) >= 128) {
+  } else if (p.d_out > 128 && tiles(256, 256) >= kComputeUnits * 3 / 4) {
     run_tiles<256, 256, 2, 4, OUT>(p, s);
-  } else if (tiles_of(128, 128) >= 128) {
+  } else if (p.d_out > 64 && tiles(128, 128) >= kComputeUnits * 3 / 2) {
     run_tiles<128, 128, 2, 2, OUT>(p, s);
   } else {
     run_tiles<64, 64, 2, 1, OUT>(p, s);
