@@ -509,7 +509,7 @@ typedef struct {
  * masters (gmb_sage_backward on what the records stand for) and quantised
  * again.
  *   a, a2   the operands (a2 may be NULL; its ids must be)
- *   n_dev   device int32 or NULL: rows, clamped to n_cap
+ *   n_dev   device int32 or NULL: rows, clamped to n_cap (at most 2^31 - 1024)
  *   bias    device fp32 [d_out] or NULL; relu: nonzero for max(0, .)
  *   out     device [n_cap, d_out] of `dtype`. */
 int gmb_mx_linear(const gmb_mx_operand* a, const gmb_mx_operand* a2, const int32_t* n_dev, int64_t n_cap,
@@ -582,7 +582,7 @@ size_t gmb_distill_workspace_bytes(int64_t rows, int32_t classes);
  *   logits   device [rows, classes] fp32 or bf16 (`dtype`)
  *   labels   device int32 [rows] or NULL (no second term)
  *   dlogits  device [rows, classes] of `dtype`, or NULL for the loss alone;
- *            not the logits' own array
+ *            apart from the logits (GMB_EINVAL if they overlap)
  *   loss     device fp32 scalar (0 for no rows)
  *   ws       device workspace, 256-byte aligned. */
 int gmb_distill_loss(const void* logits, int32_t dtype, int64_t rows, int32_t classes, const gmb_teacher* teacher,

@@ -584,8 +584,10 @@ def sage_backward(blocks: Blocks, feats: torch.Tensor, weights: SageWeights, log
         _require_cuda(labels, "labels")
         if labels.dtype != torch.int32 or labels.numel() < blocks.num_seeds:
             raise TypeError("labels must be int32 with one entry per seed")
-    if teacher is not None and teacher.rows < blocks.num_seeds:
-        raise ValueError("teacher must have one row per seed")
+    if teacher is not None:
+        _current_device(teacher.logits, "teacher")
+        if teacher.rows < blocks.num_seeds:
+            raise ValueError("teacher must have one row per seed")
     if embedding is not None:
         _require_cuda(embedding, "embedding")
         if embedding.dtype != torch.float32 or embedding.dim() != 2 or embedding.shape[1] != weights.dims[0] \
@@ -714,6 +716,7 @@ def _rows_of(ids, n, table_rows: int, dev: int, status_word):
     if isinstance(ids, Blocks):
         if n is not None:
             raise ValueError("n goes with an id tensor")
+        _same_device(ids.workspace, dev, "the blocks")
         return (ids.struct.blk[0].src_ids, ids.input_count_ptr, ids.input_capacity,
                 ids.csr.status_word if status_word is None else status_word)
     have = table_rows if ids is None else _int32(ids, dev, "ids")
@@ -756,6 +759,7 @@ def mx_quantise(x: torch.Tensor, bits: int, ids=None, table: torch.Tensor | None
     if csr is not None:
         if ids is None or csr.num_nodes != table_rows:
             raise ValueError("csr needs ids and a table of its graph's vertices")
+        _same_device(csr.state, dev, "csr")
         state, state_bytes = csr.state.data_ptr(), csr.state_bytes
     if cap == 0:
         return table
@@ -796,6 +800,7 @@ def mx_mean(block, table: torch.Tensor, dim: int, bits: int, dtype: torch.dtype 
     dev = _current_device(table, "table")
     table_rows, stride = _records(table, dim, bits, "table")
     if isinstance(block, Blocks):
+        _same_device(block.workspace, dev, "the blocks")
         b = block.struct.blk[0]
         indptr_ptr, ids_ptr, n_dev, rows = b.indptr, b.nbr, b.sizes, int(b.cap_dst)
     else:
@@ -904,6 +909,8 @@ def sage_forward_mx(blocks: Blocks, table: torch.Tensor, weights: SageMxWeights,
     dims[0] elements a vertex); the layers' means and hidden outputs are
     quantised as they are written.  Returns logits [num_seeds, C] float32."""
     dev = _current_device(table, "table")
+    _same_device(blocks.workspace, dev, "the blocks")
+    _same_device(weights.w_self[0], dev, "weights")
     rows, stride = _records(table, weights.dims[0], MXFP4, "table")
     B, C = blocks.num_seeds, weights.dims[-1]
     logits = _output(logits, B, C, torch.float32, table)

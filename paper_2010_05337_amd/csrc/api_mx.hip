@@ -17,6 +17,7 @@ using gmb::abi_fail;
 
 constexpr int64_t kMaxInt32 = 0x7FFFFFFF;
 constexpr int32_t kMaxDim = 65536;
+constexpr int64_t kMaxLinearRows = kMaxInt32 - 1023;   // in tiles of 64, one launch's threads fit 32 bits
 
 int hip_fail(hipError_t e, const char* what) { return abi_fail(GMB_EDEVICE, "%s: %s", what, hipGetErrorString(e)); }
 hipStream_t as_stream(void* s) { return static_cast<hipStream_t>(s); }
@@ -172,6 +173,8 @@ int gmb_mx_linear(const gmb_mx_operand* a, const gmb_mx_operand* a2, const int32
   if (st == GMB_OK) st = check_count(n_cap);
   if (st != GMB_OK) return st;
   if (!a) return abi_fail(GMB_EINVAL, "a is NULL");
+  if (n_cap > kMaxLinearRows)
+    return abi_fail(GMB_EINVAL, "n_cap=%lld above 2^31 - 1024", static_cast<long long>(n_cap));
   if (n_cap == 0) return GMB_OK;
   gmb::MxLinearArgs p{};
   p.pairs = a2 ? 2 : 1;
@@ -225,6 +228,9 @@ int plan_mx_forward(const gmb_blocks* b, const gmb_sage_mx_weights* w, MxForward
     if (st != GMB_OK) return st;
   }
   for (int l = 0; l < w->num_layers; ++l) {
+    if (b->blk[l].cap_dst > kMaxLinearRows)
+      return abi_fail(GMB_EINVAL, "block %d: %lld destinations above 2^31 - 1024", l,
+                      static_cast<long long>(b->blk[l].cap_dst));
     const int64_t rec = gmb::mx_record(w->dims[l], GMB_MXFP4);
     st = check_table(w->w_self[l], w->dims[l + 1], rec, w->dims[l], GMB_MXFP4, "w_self");
     if (st == GMB_OK) st = check_table(w->w_neigh[l], w->dims[l + 1], rec, w->dims[l], GMB_MXFP4, "w_neigh");
@@ -416,6 +422,10 @@ int gmb_distill_loss(const void* logits, int32_t dtype, int64_t rows, int32_t cl
   st = check_teacher(teacher);
   if (st != GMB_OK) return st;
   if (!logits) return abi_fail(GMB_EINVAL, "logits is NULL");
+  const uintptr_t from = reinterpret_cast<uintptr_t>(logits), to = reinterpret_cast<uintptr_t>(dlogits);
+  const uintptr_t size = static_cast<uintptr_t>(rows) * classes * (dtype == GMB_BF16 ? 2 : 4);
+  if (dlogits && from < to + size && to < from + size)
+    return abi_fail(GMB_EINVAL, "dlogits overlaps the logits");
   if (!ws) return abi_fail(GMB_EINVAL, "workspace is NULL");
   if (reinterpret_cast<uintptr_t>(ws) % gmb::kAbiAlign)
     return abi_fail(GMB_EINVAL, "workspace is not 256-byte aligned");

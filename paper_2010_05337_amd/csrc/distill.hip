@@ -129,7 +129,7 @@ __device__ __forceinline__ float hard_exp(float u, float d) {
 // teacher entry and the label, with their logits.
 struct Early {
   int32_t id;      // -1: none
-  float t, z;      // the entry's logit over T, and the student's at its class
+  float t, z;      // the entry's logit, and the student's at its class
   int32_t label;   // -1: none
   float zl;
 };
@@ -147,7 +147,7 @@ __device__ __forceinline__ Early early_loads(const DistillArgs& a, int64_t row, 
   if (labelled) y = a.labels[row];
   if (id >= 0 && id < a.classes && !(v == -INFINITY)) {
     e.id = id;
-    e.t = v / a.temperature;
+    e.t = v;
     e.z = load_logit(z + id);
   }
   if (y >= 0 && y < a.classes) {
@@ -191,7 +191,7 @@ __device__ __forceinline__ RowTerms row_terms(const DistillArgs& a, int64_t row,
       v = some ? first.t : -INFINITY;
     } else if (some && a.alpha > 0.f) {
       id = a.top_ids[row * a.k + j];
-      v = a.top[row * a.k + j] * inv_t;
+      v = a.top[row * a.k + j];
       if (id < 0 || id >= a.classes || v == -INFINITY) {
         id = -1;
         v = -INFINITY;
@@ -204,7 +204,8 @@ __device__ __forceinline__ RowTerms row_terms(const DistillArgs& a, int64_t row,
   mt = row_reduce<TH>(mt, Max(), red);
   mt = mt == -INFINITY ? 0.f : mt;
   float sum = 0.f;
-  for (int j = t; j < a.k; j += TH) sum += exp2_((ps[j] - mt) * kLog2e);
+  // (over T after the difference: the type's lowest value over T < 1 is -inf)
+  for (int j = t; j < a.k; j += TH) sum += exp2_((ps[j] - mt) * r.kt);
   sum = row_reduce<TH>(sum, Sum(), red);
   const bool any = !(sum == 0.f);
   const float log_sum = logf(sum), log_st = logf(st), inv_sum = any ? 1.f / sum : 0.f;
@@ -213,11 +214,11 @@ __device__ __forceinline__ RowTerms row_terms(const DistillArgs& a, int64_t row,
     for (int j = t; j < a.k; j += TH) {
       const int32_t id = ids[j];
       const float u = ps[j] - mt;
-      const float p = exp2_(u * kLog2e) * inv_sum;
+      const float p = exp2_(u * r.kt) * inv_sum;
       ps[j] = p;
       if (id >= 0 && !(p == 0.f)) {
         const float zj = j == t ? first.z : load_logit(z + id);
-        kl += p * ((u - log_sum) - ((zj - m) * inv_t - log_st));
+        kl += p * ((u * inv_t - log_sum) - ((zj - m) * inv_t - log_st));
       }
     }
   }
@@ -292,7 +293,7 @@ void k_distill_held(DistillArgs a) {
   const int sub = threadIdx.x / TH, t = threadIdx.x % TH;
   int32_t* ids = reinterpret_cast<int32_t*>(lds) + sub * a.k;
   float* ps = reinterpret_cast<float*>(lds + ROWS * a.k) + sub * a.k;
-  int64_t row = static_cast<int64_t>(blockIdx.x) * ROWS + sub;
+  int64_t row = a.row0 + static_cast<int64_t>(blockIdx.x) * ROWS + sub;
   const bool live = row < a.rows;
   if (!live) row = a.rows - 1;
   const T* z = static_cast<const T*>(a.logits) + row * a.classes;
@@ -483,15 +484,21 @@ __global__ __launch_bounds__(1024) void k_loss_mean(const float* rows, int64_t n
 }
 
 template <typename T, int TH, int K, int WAVES>
-void held(const DistillArgs& a, hipStream_t s) {
+void held(const DistillArgs& args, hipStream_t s) {
   constexpr int ROWS = TH < 256 ? 256 / TH : 1;
-  const dim3 grid(static_cast<unsigned>((a.rows + ROWS - 1) / ROWS)), block(TH < 256 ? 256 : TH);
+  constexpr int64_t kRows = kLaunchThreads / TH;   // of a launch
+  DistillArgs a = args;
   const size_t lds = 8 * static_cast<size_t>(a.k) * ROWS;
   const float t = a.temperature;
-  if (t == 1.f) hipLaunchKernelGGL((k_distill_held<T, TH, K, 1, WAVES>), grid, block, lds, s, a);
-  else if (t == 2.f) hipLaunchKernelGGL((k_distill_held<T, TH, K, 2, WAVES>), grid, block, lds, s, a);
-  else if (t == 4.f) hipLaunchKernelGGL((k_distill_held<T, TH, K, 4, WAVES>), grid, block, lds, s, a);
-  else hipLaunchKernelGGL((k_distill_held<T, TH, K, 0, WAVES>), grid, block, lds, s, a);
+  for (a.row0 = 0; a.row0 < a.rows; a.row0 += kRows) {
+    const int64_t rows = a.rows - a.row0 < kRows ? a.rows - a.row0 : kRows;
+    const dim3 grid(static_cast<unsigned>((rows + ROWS - 1) / ROWS)), block(TH < 256 ? 256 : TH);
+    if (t == 1.f) hipLaunchKernelGGL((k_distill_held<T, TH, K, 1, WAVES>), grid, block, lds, s, a);
+    else if (t == 2.f) hipLaunchKernelGGL((k_distill_held<T, TH, K, 2, WAVES>), grid, block, lds, s, a);
+    else if (t == 4.f) hipLaunchKernelGGL((k_distill_held<T, TH, K, 4, WAVES>), grid, block, lds, s, a);
+    else hipLaunchKernelGGL((k_distill_held<T, TH, K, 0, WAVES>), grid, block, lds, s, a);
+    a.clear_n = 0;
+  }
 }
 
 template <typename T>

@@ -21,6 +21,9 @@ constexpr int kMxOutF32 = 0, kMxOutBf16 = 1, kMxOutRecords = 2;
 // 48.8.  Smaller ones stay where the next kernel finds them.
 constexpr int64_t kStreamBytes = 16 << 20;
 
+// Threads of one launch: a grid counts them in 32 bits.
+constexpr int64_t kLaunchThreads = int64_t{1} << 31;
+
 inline int64_t mx_blocks(int64_t dim) { return (dim + 31) / 32; }
 inline int64_t mx_record(int64_t dim, int bits) {
   return (mx_blocks(dim) * (4 * bits + 1) + 15) / 16 * 16;
@@ -62,6 +65,7 @@ struct MxMeanArgs {
   void* out;
   int64_t out_stride;               // records: bytes
   int out_record;
+  int64_t row0;                     // set by the launcher: the launch's first row
 };
 
 // slots: the sampler state's table (the last row written to a vertex wins),
@@ -113,7 +117,8 @@ struct DistillArgs {
   int parts;                        // workgroups of a row, with stats
   int32_t* clear;                   // cleared by the launch, clear_n words
   int64_t clear_n;
-  bool stream;
+  bool stream;                      // set by the launcher, as is row0: the launch's first row
+  int64_t row0;
 };
 // Classes that a launch without stats can hold.
 constexpr int kDistillHeld = 32768;

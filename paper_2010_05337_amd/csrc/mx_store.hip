@@ -220,7 +220,7 @@ __global__ __launch_bounds__(256) void k_mx_read(MxReadArgs a) {
 template <int BITS, int OUT, int G, int U>
 __global__ __launch_bounds__(256) void k_mx_mean(MxMeanArgs a) {
   constexpr int E = OUT == 0 ? 4 : 8, LB = 32 / E, kBytes = E * BITS / 8, kWords = (E * BITS + 31) / 32;
-  const int64_t row = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) / G;
+  const int64_t row = a.row0 + (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) / G;
   const int lane = threadIdx.x & (G - 1);
   const int64_t rc = row < a.n_cap ? row : a.n_cap - 1;
   const int32_t beg = a.indptr[rc], end = a.indptr[rc + 1];
@@ -336,17 +336,21 @@ void read_dispatch(const MxReadArgs& a, hipStream_t s) {
 }
 
 template <int BITS, int OUT>
-void mean_dispatch(const MxMeanArgs& a, hipStream_t s) {
+void mean_dispatch(const MxMeanArgs& args, hipStream_t s) {
   constexpr int U = 8, E = OUT == 0 ? 4 : 8;
+  MxMeanArgs a = args;
   const int g = lanes_for(OUT == 2 ? a.blocks * 4 : (a.dim + E - 1) / E, 4);
-  const dim3 grid(static_cast<unsigned>((a.n_cap * g + 255) / 256));
+  for (a.row0 = 0; a.row0 < a.n_cap; a.row0 += kLaunchThreads / g) {
+    const int64_t rows = a.n_cap - a.row0 < kLaunchThreads / g ? a.n_cap - a.row0 : kLaunchThreads / g;
+    const dim3 grid(static_cast<unsigned>((rows * g + 255) / 256));
 #define GMB_MX_MEAN(GG) hipLaunchKernelGGL((k_mx_mean<BITS, OUT, GG, U>), grid, dim3(256), 0, s, a)
-  switch (g) {
-    case 4: GMB_MX_MEAN(4); break;
-    case 8: GMB_MX_MEAN(8); break;
-    case 16: GMB_MX_MEAN(16); break;
-    case 32: GMB_MX_MEAN(32); break;
-    default: GMB_MX_MEAN(64); break;
+    switch (g) {
+      case 4: GMB_MX_MEAN(4); break;
+      case 8: GMB_MX_MEAN(8); break;
+      case 16: GMB_MX_MEAN(16); break;
+      case 32: GMB_MX_MEAN(32); break;
+      default: GMB_MX_MEAN(64); break;
+    }
   }
 #undef GMB_MX_MEAN
 }

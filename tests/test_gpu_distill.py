@@ -158,6 +158,45 @@ def test_an_impossible_class_that_the_teacher_wants():
     assert float(grad[0, 4]) == -0.5 and np.isfinite(grad.cpu().numpy()).all()
 
 
+@pytest.mark.parametrize("C", [10, 40000])
+@pytest.mark.parametrize("T", [0.25, 1.0, 8.0])
+def test_a_teacher_of_the_lowest_value(C, T):
+    """Rows whose teacher logits are all the type's lowest value (equal shares,
+    also where the value over T is past the type), and some of them."""
+    z, top, cls, labels = inputs(4, C, 5, 3)
+    cls = np.tile(np.arange(5, dtype=np.int32), (4, 1))
+    low = np.finfo(np.float32).min
+    top[0] = low
+    top[1, 1:] = low
+    top[2, :] = [3e38, -3e38, 3e38, low, 0.0]
+    dev = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+    loss, grad = gmb.distill_loss(z.cuda(), dev(top), dev(cls), alpha=1.0, temperature=T)
+    ref, g, size = mx_ref.distill(z.numpy().astype(np.float64), top.astype(np.float64), cls, None, 1.0, T)
+    assert np.all(np.abs(grad.cpu().numpy() - g) <= EPS * (np.abs(g) + T / 4))
+    assert abs(float(loss) - ref.mean()) <= (EPS * (size + T * T + 1)).mean() * 2
+
+
+def test_more_rows_than_a_grid_counts():
+    """2^28 + 3 rows of 16 threads are more than 32 bits count.  All rows are
+    one of two, and a thread of the mean adds 2^16 terms: its sum is off by
+    2^16 half-steps at most, and those of the rows by EPS each."""
+    n = (1 << 28) + 3
+    print(f"distill: {n} rows", flush=True)
+    zero = torch.tensor([[0.0, 1.0], [2.0, 0.0]])
+    z = torch.empty((n, 2), dtype=torch.bfloat16, device="cuda")
+    z[0::2], z[1::2] = zero[0].cuda(), zero[1].cuda()
+    top = torch.ones((n, 1), device="cuda")
+    cls = torch.zeros((n, 1), dtype=torch.int32, device="cuda")
+    loss, grad = gmb.distill_loss(z, top, cls, alpha=1.0)
+    per, g, _ = mx_ref.distill(zero.double().numpy(), np.ones((2, 1)), np.zeros((2, 1), np.int32), None, 1.0, 1.0)
+    want = ((n + 1) // 2 * per[0] + n // 2 * per[1]) / n
+    assert abs(float(loss) - want) <= (2.0 ** 16 * U32 + EPS) * want
+    got = torch.cat([grad[:2], grad[n // 2 - n // 2 % 2:][:2], grad[n - 3:n - 1]]).float().cpu().numpy()
+    g = np.tile(g * 2 / n, (3, 1))               # (of two rows' mean there)
+    assert np.all(np.abs(got - g) <= (UBF16 + EPS) * np.abs(g) + 2 * EPS / n)
+    assert bool((grad.float().abs().amax(1) > 0).all())
+
+
 def test_the_gradient_is_the_loss_s_difference():
     """Central differences of the GPU's own loss (fp32: steps of 2^-5 and a
     bound of the differences' second order and rounding)."""

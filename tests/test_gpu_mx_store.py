@@ -253,6 +253,26 @@ def test_addresses_past_32_bits():
     assert same(gmb.mx_linear(table, w, dim, ids=ids).cpu().numpy(), v.astype(np.float32))
 
 
+def test_a_mean_of_more_rows_than_a_grid_counts():
+    """2^26 + 9 rows of 64 lanes are more threads than 32 bits count."""
+    n, dim = (1 << 26) + 9, 257
+    print(f"mean: {n} rows of {dim}", flush=True)
+    x = torch.from_numpy(np.random.default_rng(1).normal(size=(9, dim)).astype(np.float32)).cuda()
+    table = gmb.mx_quantise(x, 4)
+    indptr = torch.zeros(n + 1, dtype=torch.int32, device="cuda")
+    indptr[-9:] = torch.arange(1, 10, dtype=torch.int32, device="cuda")
+    out = torch.empty((n, dim), dtype=torch.bfloat16, device="cuda")
+    out[:: 4097] = float("nan")
+    out[-9:] = float("nan")
+    ids = torch.arange(8, -1, -1, dtype=torch.int32, device="cuda")
+    gmb.mx_mean((indptr, ids), table, dim, 4, dtype=torch.bfloat16, out=out)
+    want = gmb.mx_gather(ids, table, dim, 4, dtype=torch.bfloat16)
+    assert torch.equal(out[-9:], want)
+    assert bool((out[:-9][:: 4097] == 0).all())
+    del out
+    torch.cuda.empty_cache()
+
+
 def test_another_stream_and_a_graph():
     """Work on a stream of its own, and captured and replayed with other rows
     in the same buffers."""

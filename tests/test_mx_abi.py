@@ -99,6 +99,15 @@ def test_linear_refuses(L, bad):
     assert linear(L, **bad) == EINVAL
 
 
+def test_rows_past_one_launch_are_refused(L):
+    # in the product's smallest tiles, a thread for every two rows: 2^32 of them
+    n = (1 << 31) - 1
+    assert linear(L, first=dict(num_rows=n), n=n, out=None) == EINVAL
+    assert b"2^31 - 1024" in L.gmb_last_error()
+    b, w = model([(n, n, 1000)], [100, 47])
+    assert forward(L, b, w) == EINVAL and L.gmb_mx_forward_workspace_bytes(ctypes.byref(b), ctypes.byref(w)) == 0
+
+
 def test_linear_refuses_no_operand(L):
     assert L.gmb_mx_linear(None, None, None, 1, 32, 32, None, 0, P, 0, None, None) == EINVAL
 
@@ -167,8 +176,8 @@ def teacher(**over):
     return gmb.TeacherStruct(**dict(dict(logits=P, classes=P, top=4, alpha=0.5, temperature=2.0, reserved=0), **over))
 
 
-def loss(L, t, logits=P, dtype=0, rows=10, classes=47, out=P, ws=P, ws_bytes=1 << 20):
-    return L.gmb_distill_loss(logits, dtype, rows, classes, None if t is None else ctypes.byref(t), None, None, out,
+def loss(L, t, logits=P, dtype=0, rows=10, classes=47, out=P, ws=P, ws_bytes=1 << 20, grad=None):
+    return L.gmb_distill_loss(logits, dtype, rows, classes, None if t is None else ctypes.byref(t), None, grad, out,
                               ws, ws_bytes, None)
 
 
@@ -193,6 +202,14 @@ def test_distill_refuses(L):
     # rows that workgroups share leave three words each and part
     assert L.gmb_distill_workspace_bytes(1, 131072) > L.gmb_distill_workspace_bytes(1, 47)
     assert L.gmb_distill_workspace_bytes(-1, 47) == 0 and L.gmb_distill_workspace_bytes(10, 0) == 0
+
+
+@pytest.mark.parametrize("dtype, size", [(0, 4), (1, 2)])
+def test_a_gradient_over_the_logits_is_refused(L, dtype, size):
+    # (a workspace that is too small is looked at afterwards)
+    n = 10 * 47 * size
+    for grad, want in ((P, EINVAL), (P + n - size, EINVAL), (P - n + size, EINVAL), (P + n, ENOSPC), (P - n, ENOSPC)):
+        assert loss(L, teacher(), dtype=dtype, grad=grad, ws_bytes=16) == want, grad - P
 
 
 def backward(L, t, dims=(100, 64, 47), table=None, nodes=1000, ws_bytes=1 << 40):
