@@ -354,3 +354,82 @@ def test_a_student_in_four_bits(dg, graph):
         changed = mx_ref.quantise(rows[:len(src)].cpu().numpy(), 4)
         assert np.array_equal(table.cpu().numpy()[src], changed)
     csr.check_status()
+
+
+def test_a_captured_step_and_two_graphs_of_one_workspace(dg, graph):
+    """A training step from the records to the records again as one graph, and
+    the serving of two batches as two graphs of one workspace, replayed in
+    turn: each replay gives what the eager calls give (the step's sums in
+    another order)."""
+    g, csr = graph
+    dims, fanouts, B = [64, 32, 20], [6, 5], 90
+    masters = to_torch_weights(dg.sage_weights(dims, 3))
+    mxw = gmb.SageMxWeights(masters)
+    feats = torch.from_numpy(dg.features(g.num_nodes, dims[0], 5, "f32")).cuda()
+    table = gmb.mx_quantise(feats, gmb.MXFP4)
+    batches = [gmb.sample_blocks(csr, torch.from_numpy(dg.permutation(g.num_nodes, s)[:B]).cuda(), fanouts, s)
+               for s in (1, 2)]
+    top, cls, labels = teacher_of(B, 20, 4, 8)
+    top, y = torch.from_numpy(top).cuda(), torch.from_numpy(labels).cuda()
+    t = gmb.Teacher(top, torch.from_numpy(cls).cuda(), 0.5, 2.0)
+    x = gmb.mx_gather(batches[0], table, dims[0], gmb.MXFP4)
+    w = mxw.values()
+    aligned = lambda n: gmb._aligned_bytes(n, x.device)[1]  # noqa: E731
+    fws, bws = aligned(gmb.forward_workspace_bytes(batches[0], w)), aligned(gmb.backward_workspace_bytes(batches[0], w))
+    logits, loss, grads = torch.empty(B, 20, device="cuda"), torch.empty(1, device="cuda"), gmb.SageGrads(w)
+
+    def step():
+        gmb.mx_gather(batches[0], table, dims[0], gmb.MXFP4, out=x)
+        for l in range(2):
+            w.w_self[l].copy_(gmb.mx_gather(None, mxw.w_self[l], dims[l], gmb.MXFP4).t())
+            w.w_neigh[l].copy_(gmb.mx_gather(None, mxw.w_neigh[l], dims[l], gmb.MXFP4).t())
+        gmb.sage_forward(batches[0], x, w, logits=logits, workspace=fws)
+        gmb.sage_backward(batches[0], x, w, logits, y, fws, grads=grads, loss=loss, workspace=bws, teacher=t)
+        gmb.sgd_update(masters, grads, 0.5)
+        mxw.requantise(masters)
+
+    step()                                       # (first uses, outside the graph)
+    torch.cuda.synchronize()
+    cg = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(cg):
+        step()
+    params = [a for ms in (masters.w_self, masters.w_neigh, masters.bias) for a in ms]
+    for seed in range(3):
+        top.copy_(torch.from_numpy(teacher_of(B, 20, 4, seed)[0]))
+        start = [a.clone() for a in params]
+        mxw.requantise(masters)
+        step()
+        want, exact = [a.clone() for a in params], [loss.clone(), logits.clone()]
+        for a, b in zip(params, start):
+            a.copy_(b)
+        mxw.requantise(masters)
+        torch.cuda.synchronize()
+        cg.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip([loss, logits], exact))
+        # (the mean's backward adds a row's edges in the order in which they
+        # arrived: each side is within this file's 2e-4 of the exact step, and
+        # rounds the new value once)
+        for a, b, c in zip(params, want, start):
+            assert float((a - b).abs().max()) <= 4e-4 * float((b - c).abs().max()) + 2 * U32 * float(b.abs().max())
+        for l in range(2):
+            assert np.array_equal(mxw.w_self[l].cpu().numpy(), mx_ref.quantise(masters.w_self[l].t().cpu().numpy(), 4))
+        assert any(not torch.equal(a, b) for a, b in zip(params, start))
+    ws = aligned(max(gmb.mx_forward_workspace_bytes(b, mxw) for b in batches))
+    outs = [torch.empty(B, 20, device="cuda") for _ in batches]
+    graphs = []
+    for b, o in zip(batches, outs):
+        gmb.sage_forward_mx(b, table, mxw, workspace=ws, logits=o)
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            gmb.sage_forward_mx(b, table, mxw, workspace=ws, logits=o)
+    want = [gmb.sage_forward_mx(b, table, mxw) for b in batches]
+    for _ in range(3):
+        for o in outs:
+            o.zero_()
+        for gr in graphs:
+            gr.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, v) for o, v in zip(outs, want))
+    csr.check_status()
