@@ -11,8 +11,9 @@
 // -inf; without one the first term is nothing, without a label in [0, C) the
 // second, and a row whose logits are all -inf adds nothing at all.
 //
-//   k_distill_held   a wave (C up to 1,024) or a workgroup holds the row in
-//                    registers: one read, one write of the logits' size
+//   k_distill_held   part of a wave (up to 256 pieces of 16 bytes) or a
+//                    workgroup holds the row in registers: one read, one write
+//                    of the logits' size
 //   k_distill_stats, k_distill_grad
 //                    rows too long for that, and few rows: workgroups share a
 //                    row, each with a range of classes; the first kernel
@@ -168,8 +169,11 @@ struct RowTerms {
   bool none;        // no term at all: no gradient
 };
 
+// A row's entries in LDS: whole fours of them.
+__host__ __device__ inline int entry_room(int k) { return (k + 3) / 4 * 4; }
+
 // The teacher's entries of a row in LDS (classes in `ids`, -1 for an invalid
-// one; probabilities in `ps`), then the loss and the gradient's factors; m,
+// one and past the last; probabilities in `ps`), then the loss and the gradient's factors; m,
 // st and s1 are the row's statistics.  Every thread of the row calls it.
 template <typename T, int TH>
 __device__ __forceinline__ RowTerms row_terms(const DistillArgs& a, int64_t row, bool live, const T* z, float m,
@@ -183,13 +187,14 @@ __device__ __forceinline__ RowTerms row_terms(const DistillArgs& a, int64_t row,
   const bool some = live && !(st == 0.f);   // not: every logit is -inf
   // the teacher
   float mt = -INFINITY;
-  for (int j = t; j < a.k; j += TH) {
+  const int room = entry_room(a.k);
+  for (int j = t; j < room; j += TH) {
     int32_t id = -1;
     float v = -INFINITY;
     if (j == t) {
       id = some ? first.id : -1;
       v = some ? first.t : -INFINITY;
-    } else if (some && a.alpha > 0.f) {
+    } else if (j < a.k && some && a.alpha > 0.f) {
       id = a.top_ids[row * a.k + j];
       v = a.top[row * a.k + j];
       if (id < 0 || id >= a.classes || v == -INFINITY) {
@@ -254,19 +259,29 @@ __device__ __forceinline__ void correct_entries(const DistillArgs& a, const RowT
                                                 const Early& first, int t, const int32_t* ids, const float* ps,
                                                 int64_t lo, int64_t hi) {
   if (r.none) return;
-  auto write = [&](int32_t id, float zi) {
+  auto write = [&](int32_t id, int j, float zi) {
     if (id < lo || id >= hi) return;
+    // (mostly there is one entry of a class, if any)
+    int same = 0;
+    for (int i = 0; i < entry_room(a.k); i += 4) {
+      const int4 v = *reinterpret_cast<const int4*>(ids + i);
+      same += (v.x == id) + (v.y == id) + (v.z == id) + (v.w == id);
+    }
     float p = 0.f;
-    for (int i = 0; i < a.k; ++i) p += ids[i] == id ? ps[i] : 0.f;
+    if (same == 1 && j >= 0) {
+      p = ps[j];
+    } else if (same > 0) {
+      for (int i = 0; i < a.k; ++i) p += ids[i] == id ? ps[i] : 0.f;
+    }
     const float d = zi - r.m;
     Chunk<T>::store1(grad + id, r.ft * exp2_(d * r.kt) - r.fp * p + r.f1 * exp2_(d * kLog2e) -
                                     (id == r.label ? r.fy : 0.f));
   };
   for (int j = t; j < a.k; j += TH) {
     const int32_t id = ids[j];
-    if (id >= 0) write(id, j == t ? first.z : load_logit(z + id));
+    if (id >= 0) write(id, j, j == t ? first.z : load_logit(z + id));
   }
-  if (t == TH - 1 && r.label >= 0) write(r.label, first.zl);
+  if (t == TH - 1 && r.label >= 0) write(r.label, -1, first.zl);
 }
 
 // Makes loaded chunks opaque, so that what one pass computed of them (their
@@ -285,14 +300,15 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) __attribute__((amdgpu_waves_pe
 void k_distill_held(DistillArgs a) {
   constexpr int E = Chunk<T>::N;
   constexpr int ROWS = TH < 256 ? 256 / TH : 1;
-  extern __shared__ uint32_t lds[];
+  extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
   __shared__ float red[16];
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < a.clear_n;
        i += static_cast<int64_t>(gridDim.x) * blockDim.x)
     a.clear[i] = 0;
   const int sub = threadIdx.x / TH, t = threadIdx.x % TH;
-  int32_t* ids = reinterpret_cast<int32_t*>(lds) + sub * a.k;
-  float* ps = reinterpret_cast<float*>(lds + ROWS * a.k) + sub * a.k;
+  const int room = entry_room(a.k);
+  int32_t* ids = reinterpret_cast<int32_t*>(lds) + sub * room;
+  float* ps = reinterpret_cast<float*>(lds + ROWS * room) + sub * room;
   int64_t row = a.row0 + static_cast<int64_t>(blockIdx.x) * ROWS + sub;
   const bool live = row < a.rows;
   if (!live) row = a.rows - 1;
@@ -305,10 +321,7 @@ void k_distill_held(DistillArgs a) {
   for (int k = 0; k < K; ++k) {
     const int c = (k * TH + t) * E;
     q[k] = tail;
-    if (c + E <= a.classes) {
-      if (a.stream) mx_get_once<16>(&q[k], z + c);
-      else __builtin_memcpy(&q[k], z + c, 16);
-    }
+    if (c + E <= a.classes) mx_get<16>(&q[k], z + c);
   }
   if (whole % TH == t) {
     // (past that chunk there is nothing)
@@ -433,11 +446,11 @@ __global__ __launch_bounds__(kSplitThreads) void k_distill_stats(DistillArgs a) 
 template <typename T>
 __global__ __launch_bounds__(kSplitThreads) void k_distill_grad(DistillArgs a) {
   constexpr int E = Chunk<T>::N;
-  extern __shared__ uint32_t lds[];
+  extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
   __shared__ float red[16];
   const int t = threadIdx.x;
   int32_t* ids = reinterpret_cast<int32_t*>(lds);
-  float* ps = reinterpret_cast<float*>(lds + a.k);
+  float* ps = reinterpret_cast<float*>(lds + entry_room(a.k));
   const int64_t row = blockIdx.x / a.parts;
   const int part = static_cast<int>(blockIdx.x % a.parts);
   const T* z = static_cast<const T*>(a.logits) + row * a.classes;
@@ -488,7 +501,7 @@ void held(const DistillArgs& args, hipStream_t s) {
   constexpr int ROWS = TH < 256 ? 256 / TH : 1;
   constexpr int64_t kRows = kLaunchThreads / TH;   // of a launch
   DistillArgs a = args;
-  const size_t lds = 8 * static_cast<size_t>(a.k) * ROWS;
+  const size_t lds = 8 * static_cast<size_t>(entry_room(a.k)) * ROWS;
   const float t = a.temperature;
   for (a.row0 = 0; a.row0 < a.rows; a.row0 += kRows) {
     const int64_t rows = a.rows - a.row0 < kRows ? a.rows - a.row0 : kRows;
@@ -501,6 +514,16 @@ void held(const DistillArgs& args, hipStream_t s) {
   }
 }
 
+// Threads of a row.  Short rows: as few as hold them, so that a wave has several
+// rows and shares their reductions (30,000 x 200 bf16: 64 threads 31.1 us, 16
+// threads 16.3; 60,000 x 47 fp32: 16 threads 16.4, 8 threads 12.5; 8,000 x 601
+// fp32: 64 threads 15.9, 32 threads 13.4); but their rows' entries are to fit 32
+// KB of LDS.  Longer rows: 256 or 512, and of the waves of a SIMD the most whose
+// registers hold their chunks without spilling (one register at 512 x 8): a row
+// waits for its loads and its reductions, and another's exponentials fill the
+// time.  4,099 x 32,768 bf16, 512 threads: 149.6 us at five (two workgroups a CU),
+// 140.7 at six (three), 177 at eight (27 registers spilled); 2,000 x 30,000 fp32:
+// 154.3 us in 1,024 threads of 8 chunks, 106.9 in 512 of 16.
 template <typename T>
 void dispatch(const DistillArgs& a, hipStream_t s) {
   constexpr int E = Chunk<T>::N;
@@ -508,11 +531,13 @@ void dispatch(const DistillArgs& a, hipStream_t s) {
   if (a.stats) {
     const dim3 grid(static_cast<unsigned>(a.rows * a.parts));
     hipLaunchKernelGGL((k_distill_stats<T>), grid, dim3(kSplitThreads), 0, s, a);
-    hipLaunchKernelGGL((k_distill_grad<T>), grid, dim3(kSplitThreads), 8 * static_cast<size_t>(a.k), s, a);
-  } else if (chunks <= 16 && a.k <= 256) {   // (sixteen rows' entries in LDS: 32 KB at most)
-    held<T, 16, 1, 4>(a, s);
-  } else if (chunks <= 64) {
-    held<T, 64, 1, 4>(a, s);
+    hipLaunchKernelGGL((k_distill_grad<T>), grid, dim3(kSplitThreads), 8 * static_cast<size_t>(entry_room(a.k)), s, a);
+  } else if (chunks <= 16 && a.k <= 128) {
+    held<T, 8, 2, 4>(a, s);
+  } else if (chunks <= 64 && a.k <= 256) {
+    held<T, 16, 4, 4>(a, s);
+  } else if (chunks <= 256 && a.k <= 512) {
+    held<T, 32, 8, 5>(a, s);
   } else if (chunks <= 256) {
     held<T, 64, 4, 8>(a, s);
   } else if (chunks <= 1024) {
@@ -520,9 +545,9 @@ void dispatch(const DistillArgs& a, hipStream_t s) {
   } else if (chunks <= 2048) {
     held<T, 256, 8, 5>(a, s);
   } else if (chunks <= 4096) {
-    held<T, 512, 8, 5>(a, s);
+    held<T, 512, 8, 6>(a, s);
   } else if constexpr (E == 4) {
-    held<T, 1024, 8, 8>(a, s);
+    held<T, 512, 16, 4>(a, s);
   }
 }
 
@@ -540,9 +565,8 @@ int distill_parts(int64_t rows, int64_t classes) {
 }
 
 hipError_t launch_distill(const DistillArgs& args, int bf16, hipStream_t s) {
-  // a large gradient goes past the caches, and the logits it is made of too
-  // (4,099 x 32,768 bf16: 153.5 us plain, 145.6 with its stores, 142.3 with both;
-  // 8,000 x 1,000 fp32, 32 MB: 19.2, 19.2, 19.9)
+  // a large gradient goes past the caches (4,099 x 32,768 bf16: 138.6 us plain,
+  // 137.5 so; 2,000 x 30,000 fp32: 105.4, 102.9; 8,000 x 1,000 fp32, 32 MB: 20.8, 22.8)
   DistillArgs a = args;
   a.stream = a.rows * a.classes * (bf16 ? 2 : 4) >= 4 * kStreamBytes;
   if (bf16) dispatch<uint16_t>(a, s);

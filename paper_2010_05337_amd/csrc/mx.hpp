@@ -145,6 +145,12 @@ __device__ __forceinline__ void mx_put(void* p, const void* v, bool stream) {
     *static_cast<Words*>(p) = x;
 }
 template <int BYTES>
+__device__ __forceinline__ void mx_get(void* v, const void* p) {
+  using Words = typename MxWords<BYTES>::Type;
+  const Words x = *static_cast<const Words*>(p);
+  __builtin_memcpy(v, &x, BYTES);
+}
+template <int BYTES>
 __device__ __forceinline__ void mx_get_once(void* v, const void* p) {
   using Words = typename MxWords<BYTES>::Type;
   const Words x = __builtin_nontemporal_load(static_cast<const Words*>(p));

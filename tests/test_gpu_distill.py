@@ -94,6 +94,18 @@ def test_loss_and_gradient(n, C, k, dtype):
     check(z, top, cls, labels, 0.5, 2.0)
 
 
+@pytest.mark.parametrize("n, C, k", [(40, 3, 3), (33, 50, 128), (20, 50, 129), (20, 60, 257), (37, 200, 255),
+                                     (20, 200, 257), (9, 900, 512), (9, 900, 513), (70, 1000, 1024), (3, 40000, 1023),
+                                     (5, 20000, 33), (9, 31000, 5)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+def test_entries_beside_classes(n, C, k, dtype):
+    """Entries by the ones, whole fours and more than classes (so that most of
+    a class's entries add up)."""
+    print(f"{n} rows of {C} classes, {k} entries, {dtype}", flush=True)
+    z, top, cls, labels = inputs(n, C, k, n + k, dtype)
+    check(z, top, cls, labels, 0.6, 1.5)
+
+
 @pytest.mark.parametrize("alpha, T", [(0.0, 1.0), (1.0, 1.0), (0.3, 4.0), (0.9, 0.5), (1.0, 100.0), (0.25, 1.0)])
 @pytest.mark.parametrize("C", [47, 3001, 40000])
 @pytest.mark.parametrize("with_labels", [False, True])
