@@ -68,26 +68,35 @@ struct Chunk<uint16_t> {
   }
 };
 
-// The chunk of classes c .. c + N - 1, -inf at `end` and past it.
 template <typename T>
-__device__ __forceinline__ uint4 load_chunk(const T* z, int64_t c, int64_t end) {
-  uint4 x;
-  if (c + Chunk<T>::N <= end) {
-    __builtin_memcpy(&x, z + c, 16);
-  } else {
-    x = make_uint4(Chunk<T>::kMasked, Chunk<T>::kMasked, Chunk<T>::kMasked, Chunk<T>::kMasked);
-    T* e = reinterpret_cast<T*>(&x);
+__device__ __forceinline__ uint4 masked_chunk() {
+  constexpr uint32_t m = Chunk<T>::kMasked;
+  return make_uint4(m, m, m, m);
+}
+// The chunk of classes c .. c + N - 1 (c < end), -inf at `end` and past it; its
+// values are asked for together (the last one for those past it).
+template <typename T>
+__device__ __forceinline__ uint4 load_tail(const T* z, int64_t c, int64_t end) {
+  T v[Chunk<T>::N];
 #pragma unroll
-    for (int i = 0; i < Chunk<T>::N; ++i)
-      if (c + i < end) e[i] = z[c + i];
-  }
+  for (int i = 0; i < Chunk<T>::N; ++i) v[i] = z[c + i < end ? c + i : end - 1];
+  uint4 x = masked_chunk<T>();
+  T* e = reinterpret_cast<T*>(&x);
+#pragma unroll
+  for (int i = 0; i < Chunk<T>::N; ++i) e[i] = c + i < end ? v[i] : e[i];
   return x;
 }
 template <typename T>
-__device__ __forceinline__ void store_chunk(T* grad, int64_t c, int64_t end, const float (&g)[Chunk<T>::N],
-                                            bool stream) {
+__device__ __forceinline__ uint4 load_chunk(const T* z, int64_t c, int64_t end) {
+  if (c + Chunk<T>::N > end) return load_tail(z, c, end);
+  uint4 x;
+  mx_get<16>(&x, z + c);
+  return x;
+}
+template <typename T>
+__device__ __forceinline__ void store_chunk(T* grad, int64_t c, int64_t end, const float (&g)[Chunk<T>::N]) {
   const int64_t left = end - c;
-  mx_store(grad + c, g, left < Chunk<T>::N ? static_cast<int>(left) : Chunk<T>::N, stream);
+  mx_store(grad + c, g, left < Chunk<T>::N ? static_cast<int>(left) : Chunk<T>::N, false);
 }
 
 // Reductions over the TH threads of a row (a part of a wave, a wave, or the
@@ -127,7 +136,7 @@ __device__ __forceinline__ float hard_exp(float u, float d) {
 }
 
 // What a thread asks for before it has the row's statistics: its first
-// teacher entry and the label, with their logits.
+// teacher entry and the label, then their logits.
 struct Early {
   int32_t id;      // -1: none
   float t, z;      // the entry's logit, and the student's at its class
@@ -135,27 +144,26 @@ struct Early {
   float zl;
 };
 
-template <typename T>
-__device__ __forceinline__ Early early_loads(const DistillArgs& a, int64_t row, bool live, const T* z, int t) {
+__device__ __forceinline__ Early early_entry(const DistillArgs& a, int64_t row, bool live, int t) {
   Early e{-1, -INFINITY, 0.f, -1, 0.f};
-  const bool taught = live && a.alpha > 0.f && t < a.k, labelled = live && a.labels && a.alpha < 1.f;
-  int32_t id = -1, y = -1;
-  float v = -INFINITY;
-  if (taught) {
-    id = a.top_ids[row * a.k + t];
-    v = a.top[row * a.k + t];
+  if (live && a.alpha > 0.f && t < a.k) {
+    e.id = a.top_ids[row * a.k + t];
+    e.t = a.top[row * a.k + t];
   }
-  if (labelled) y = a.labels[row];
-  if (id >= 0 && id < a.classes && !(v == -INFINITY)) {
-    e.id = id;
-    e.t = v;
-    e.z = load_logit(z + id);
-  }
-  if (y >= 0 && y < a.classes) {
-    e.label = y;
-    e.zl = load_logit(z + y);
-  }
+  if (live && a.labels && a.alpha < 1.f) e.label = a.labels[row];
   return e;
+}
+template <typename T>
+__device__ __forceinline__ void early_logits(const DistillArgs& a, const T* z, Early& e) {
+  if (e.id < 0 || e.id >= a.classes || e.t == -INFINITY) {
+    e.id = -1;
+    e.t = -INFINITY;
+  }
+  if (e.label >= a.classes) e.label = -1;
+  // (both at once, of some class if there is none)
+  const T zi = z[e.id < 0 ? 0 : e.id], zl = z[e.label < 0 ? 0 : e.label];
+  e.z = load_logit(&zi);
+  e.zl = load_logit(&zl);
 }
 
 // What a row's gradient and loss are made of.
@@ -313,24 +321,30 @@ void k_distill_held(DistillArgs a) {
   const bool live = row < a.rows;
   if (!live) row = a.rows - 1;
   const T* z = static_cast<const T*>(a.logits) + row * a.classes;
-  // the chunk that the row ends in, if it is not whole, by the thread whose it is
-  const int whole = a.classes / E;
-  uint4 tail = load_chunk(z, t == whole % TH ? whole * E : a.classes, a.classes);
+  // the row's loads, its entries' and its last chunk's are on the way together
+  // (each waited for by itself: 4,099 x 32,768 bf16 135 us, so 125)
   uint4 q[K];
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     const int c = (k * TH + t) * E;
-    q[k] = tail;
+    q[k] = masked_chunk<T>();
     if (c + E <= a.classes) mx_get<16>(&q[k], z + c);
   }
-  if (whole % TH == t) {
-    // (past that chunk there is nothing)
-    const uint32_t masked = Chunk<T>::kMasked;
+  Early first = early_entry(a, row, live, t);
+  // the chunk that the row ends in, if it is not whole, by the thread whose it is
+  const int whole = a.classes / E;
+  if (whole * E < a.classes && whole % TH == t) {
+    const uint4 tail = load_tail(z, whole * E, a.classes);
 #pragma unroll
-    for (int k = 0; k < K; ++k)
-      if (k * TH + t > whole) q[k] = make_uint4(masked, masked, masked, masked);
+    for (int k = 0; k < K; ++k) {
+      const bool here = k == whole / TH;
+      q[k].x = here ? tail.x : q[k].x;
+      q[k].y = here ? tail.y : q[k].y;
+      q[k].z = here ? tail.z : q[k].z;
+      q[k].w = here ? tail.w : q[k].w;
+    }
   }
-  const Early first = early_loads(a, row, live, z, t);
+  early_logits(a, z, first);
   float m = -INFINITY;
 #pragma unroll
   for (int k = 0; k < K; ++k) {
@@ -383,7 +397,7 @@ void k_distill_held(DistillArgs a) {
       if (c >= a.classes) break;
       float g[E] = {};
       if (!r.none) chunk_gradient<POW, T>(r, q[k], g);   // (0 whatever the logits are)
-      store_chunk(grad, c, a.classes, g, a.stream);
+      store_chunk(grad, c, a.classes, g);
       __builtin_amdgcn_sched_barrier(0);
     }
     for (int64_t c = a.classes + t; c < a.ld_grad; c += TH) Chunk<T>::store1(grad + c, 0.f);
@@ -454,7 +468,8 @@ __global__ __launch_bounds__(kSplitThreads) void k_distill_grad(DistillArgs a) {
   const int64_t row = blockIdx.x / a.parts;
   const int part = static_cast<int>(blockIdx.x % a.parts);
   const T* z = static_cast<const T*>(a.logits) + row * a.classes;
-  const Early first = early_loads(a, row, true, z, t);
+  Early first = early_entry(a, row, true, t);
+  early_logits(a, z, first);
   const float kt = kLog2e / a.temperature;
   // the parts' statistics, each thread some of them (a row has at most as many parts as threads)
   const float* stats = a.stats + 3 * row * a.parts;
@@ -476,7 +491,7 @@ __global__ __launch_bounds__(kSplitThreads) void k_distill_grad(DistillArgs a) {
   for (int64_t c = lo + t * E; c < hi; c += kSplitThreads * E) {
     float g[E] = {};
     if (!r.none) chunk_gradient<0, T>(r, load_chunk(z, c, hi), g);
-    store_chunk(grad, c, hi, g, a.stream);
+    store_chunk(grad, c, hi, g);
   }
   __syncthreads();
   correct_entries<T, kSplitThreads>(a, r, z, grad, first, t, ids, ps, lo, hi);
@@ -521,9 +536,10 @@ void held(const DistillArgs& args, hipStream_t s) {
 // KB of LDS.  Longer rows: 256 or 512, and of the waves of a SIMD the most whose
 // registers hold their chunks without spilling (one register at 512 x 8): a row
 // waits for its loads and its reductions, and another's exponentials fill the
-// time.  4,099 x 32,768 bf16, 512 threads: 149.6 us at five (two workgroups a CU),
-// 140.7 at six (three), 177 at eight (27 registers spilled); 2,000 x 30,000 fp32:
-// 154.3 us in 1,024 threads of 8 chunks, 106.9 in 512 of 16.
+// time.  4,099 x 32,768 bf16, 512 threads: 135.0 us at five (two workgroups a CU),
+// 124.0 at six (three), 157 at eight (27 registers spilled); 2,000 x 30,000 fp32:
+// 183 us in 1,024 threads of 8 chunks, 101.4 in 512 of 16.  (Stores past the
+// caches changed nothing: 125.9 and 101.7.)
 template <typename T>
 void dispatch(const DistillArgs& a, hipStream_t s) {
   constexpr int E = Chunk<T>::N;
@@ -564,11 +580,7 @@ int distill_parts(int64_t rows, int64_t classes) {
   return 0;
 }
 
-hipError_t launch_distill(const DistillArgs& args, int bf16, hipStream_t s) {
-  // a large gradient goes past the caches (4,099 x 32,768 bf16: 138.6 us plain,
-  // 137.5 so; 2,000 x 30,000 fp32: 105.4, 102.9; 8,000 x 1,000 fp32, 32 MB: 20.8, 22.8)
-  DistillArgs a = args;
-  a.stream = a.rows * a.classes * (bf16 ? 2 : 4) >= 4 * kStreamBytes;
+hipError_t launch_distill(const DistillArgs& a, int bf16, hipStream_t s) {
   if (bf16) dispatch<uint16_t>(a, s);
   else dispatch<float>(a, s);
   return hipGetLastError();

@@ -117,8 +117,7 @@ struct DistillArgs {
   int parts;                        // workgroups of a row, with stats
   int32_t* clear;                   // cleared by the launch, clear_n words
   int64_t clear_n;
-  int64_t row0;                     // set by the launcher, as is stream: the launch's first row
-  bool stream;
+  int64_t row0;                     // set by the launcher: the launch's first row
 };
 // Classes that a launch without stats can hold.
 constexpr int kDistillHeld = 32768;
