@@ -96,7 +96,7 @@ __device__ __forceinline__ uint4 load_chunk(const T* z, int64_t c, int64_t end) 
 template <typename T>
 __device__ __forceinline__ void store_chunk(T* grad, int64_t c, int64_t end, const float (&g)[Chunk<T>::N]) {
   const int64_t left = end - c;
-  mx_store(grad + c, g, left < Chunk<T>::N ? static_cast<int>(left) : Chunk<T>::N, false);
+  mx_store<false>(grad + c, g, left < Chunk<T>::N ? static_cast<int>(left) : Chunk<T>::N);
 }
 
 // Reductions over the TH threads of a row (a part of a wave, a wave, or the

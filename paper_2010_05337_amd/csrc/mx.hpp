@@ -128,18 +128,19 @@ __device__ __forceinline__ uint32_t mx_bf16x2_bits(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, mx_bf16x2));
 }
 
-// BYTES bytes from or to p (any alignment).  stream: without a place in the
-// caches (non-temporal).
+// BYTES bytes from or to p (any alignment).  STREAM: without a place in the
+// caches (non-temporal).  (A template: behind a branch on a value the compiler
+// joins the two stores into one plain one.)
 template <int BYTES>
 struct MxWords {
   typedef uint32_t Type __attribute__((ext_vector_type(BYTES / 4), aligned(2)));
 };
-template <int BYTES>
-__device__ __forceinline__ void mx_put(void* p, const void* v, bool stream) {
+template <int BYTES, bool STREAM>
+__device__ __forceinline__ void mx_put(void* p, const void* v) {
   using Words = typename MxWords<BYTES>::Type;
   Words x;
   __builtin_memcpy(&x, v, BYTES);
-  if (stream)
+  if constexpr (STREAM)
     __builtin_nontemporal_store(x, static_cast<Words*>(p));
   else
     *static_cast<Words*>(p) = x;
@@ -158,21 +159,23 @@ __device__ __forceinline__ void mx_get_once(void* v, const void* p) {
 }
 
 // 16 bytes of values to p, fp32 (4) or bf16 (8), or the first `count` of them.
-__device__ __forceinline__ void mx_store(float* p, const float (&v)[4], int count, bool stream) {
+template <bool STREAM>
+__device__ __forceinline__ void mx_store(float* p, const float (&v)[4], int count) {
   if (count >= 4) {
-    mx_put<16>(p, v, stream);
+    mx_put<16, STREAM>(p, v);
   } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       if (i < count) p[i] = v[i];
   }
 }
-__device__ __forceinline__ void mx_store(uint16_t* p, const float (&v)[8], int count, bool stream) {
+template <bool STREAM>
+__device__ __forceinline__ void mx_store(uint16_t* p, const float (&v)[8], int count) {
   uint32_t w[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) w[i] = mx_bf16x2_bits(v[2 * i], v[2 * i + 1]);
   if (count >= 8) {
-    mx_put<16>(p, w, stream);
+    mx_put<16, STREAM>(p, w);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)

@@ -51,7 +51,6 @@ struct MxReadArgs {
   int64_t table_rows, table_stride;
   void* out;
   uint32_t* status;
-  bool stream;                      // set by the launchers, here and below
 };
 
 struct MxMeanArgs {
@@ -95,7 +94,6 @@ struct MxLinearArgs {
   int64_t out_stride;               // records: bytes
   int out_record;
   uint32_t* status;
-  bool stream;
 };
 hipError_t launch_mx_linear(const MxLinearArgs& a, int out, hipStream_t s);
 

@@ -72,14 +72,17 @@ __device__ __forceinline__ const uint8_t* w_record(const MxLinearArgs& p, const 
   return m.w + static_cast<int64_t>(c < p.d_out ? c : p.d_out - 1) * m.w_stride;
 }
 
+// Beside the form of the results (kMxOut...): stored past the caches.
+constexpr int kStreamed = 4;
+
 // CT neighbouring values of a row, from column c on.
 template <int OUT, int CT>
 __device__ __forceinline__ void store_values(const MxLinearArgs& p, int64_t row, int c, const float (&z)[CT]) {
   const int left = p.d_out - c;
-  if constexpr (OUT == kMxOutF32) {
+  if constexpr ((OUT & 3) == kMxOutF32) {
     float* o = static_cast<float*>(p.out) + row * p.d_out + c;
     if (left >= CT) {
-      mx_put<4 * CT>(o, z, p.stream);
+      mx_put<4 * CT, (OUT & kStreamed) != 0>(o, z);
     } else {
 #pragma unroll
       for (int j = 0; j < CT; ++j)
@@ -91,7 +94,7 @@ __device__ __forceinline__ void store_values(const MxLinearArgs& p, int64_t row,
 #pragma unroll
     for (int j = 0; j < CT / 2; ++j) w[j] = mx_bf16x2_bits(z[2 * j], z[2 * j + 1]);
     if (left >= CT) {
-      mx_put<2 * CT>(o, w, p.stream);
+      mx_put<2 * CT, (OUT & kStreamed) != 0>(o, w);
     } else {
 #pragma unroll
       for (int j = 0; j < CT; ++j)
@@ -534,9 +537,10 @@ template <int OUT>
 void dispatch(const MxLinearArgs& p, hipStream_t s) {
   auto tiles = [&](int tm, int tn) { return ((p.n_cap + tm - 1) / tm) * ((p.d_out + tn - 1) / tn); };
   constexpr int64_t kResidentTiles = 448;
-  if (tiles(16, 32) <= 2 * kComputeUnits) {
-    run_rows<1, 2, 8, OUT>(p, s);
-  } else if (p.d_out > 128 && resident_fits<1, 4>(p) && tiles(64, 256) >= kResidentTiles) {
+  if constexpr ((OUT & kStreamed) == 0) {   // (1 MB of results at most)
+    if (tiles(16, 32) <= 2 * kComputeUnits) return run_rows<1, 2, 8, OUT>(p, s);
+  }
+  if (p.d_out > 128 && resident_fits<1, 4>(p) && tiles(64, 256) >= kResidentTiles) {
     run_resident<1, 4, OUT>(p, s);
   } else if (p.d_out > 64 && p.d_out <= 128 && resident_fits<2, 2>(p) && tiles(128, 128) >= kResidentTiles) {
     run_resident<2, 2, OUT>(p, s);
@@ -553,12 +557,11 @@ void dispatch(const MxLinearArgs& p, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_mx_linear(const MxLinearArgs& args, int out, hipStream_t s) {
-  MxLinearArgs p = args;
-  p.stream = p.n_cap * p.d_out * (out == kMxOutBf16 ? 2 : 4) >= kStreamBytes;
+hipError_t launch_mx_linear(const MxLinearArgs& p, int out, hipStream_t s) {
+  const bool stream = p.n_cap * p.d_out * (out == kMxOutBf16 ? 2 : 4) >= kStreamBytes;
   if (out == kMxOutRecords) dispatch<kMxOutRecords>(p, s);
-  else if (out == kMxOutBf16) dispatch<kMxOutBf16>(p, s);
-  else dispatch<kMxOutF32>(p, s);
+  else if (out == kMxOutBf16) stream ? dispatch<kMxOutBf16 | kStreamed>(p, s) : dispatch<kMxOutBf16>(p, s);
+  else stream ? dispatch<kMxOutF32 | kStreamed>(p, s) : dispatch<kMxOutF32>(p, s);
   return hipGetLastError();
 }
 

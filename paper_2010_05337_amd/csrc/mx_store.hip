@@ -50,17 +50,26 @@ __device__ __forceinline__ void load_values(const uint16_t* p, int left, float (
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < left ? bf16_to_f32(p[i]) : 0.f;
+    for (int i = 0; i < 8; ++i) v[i] = 0.f;
+    if (left > 0) {
+      // (together: one by one each is widened, and waited for, before the next;
+      // 346,000 rows of 100 to 8 bits 55 us, so 43)
+      uint16_t u[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) u[i] = p[i < left ? i : 0];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = i < left ? bf16_to_f32(u[i]) : 0.f;
+    }
   }
 }
 __device__ __forceinline__ float load1(const float* p) { return *p; }
 __device__ __forceinline__ float load1(const uint16_t* p) { return bf16_to_f32(*p); }
 
-// Where row `row` of a write goes: its vertex's record, or nothing (an id
-// outside the table, or a row that a later one of the same vertex replaces).
-__device__ __forceinline__ uint8_t* write_to(const MxWriteArgs& a, int64_t row, bool& bad) {
+// Where row `row` of a write goes: the record of its vertex `id`, or nothing
+// (an id outside the table, or a row that a later one of the same vertex
+// replaces).
+__device__ __forceinline__ uint8_t* write_to(const MxWriteArgs& a, int64_t row, int32_t id, bool& bad) {
   if (!a.ids) return a.table + row * a.table_stride;
-  const int32_t id = a.ids[row];
   if (!valid_vertex(id, a.table_rows)) {
     bad = true;
     return nullptr;
@@ -70,7 +79,7 @@ __device__ __forceinline__ uint8_t* write_to(const MxWriteArgs& a, int64_t row, 
 }
 
 // A lane has 16 bytes of a row (E values), 32 / E lanes a block; a row's
-// values are asked for before its id is known.  TAIL: the scales and the
+// values and its id are asked for together.  TAIL: the scales and the
 // zeros after them are one 16-byte piece (at most 16 blocks, all of them in
 // one pass of the group), which the group's first lanes store at once.
 template <typename T, int BITS, int G, bool TAIL>
@@ -84,11 +93,12 @@ __global__ __launch_bounds__(256) void k_mx_write(MxWriteArgs a) {
   for (int64_t row = static_cast<int64_t>(blockIdx.x) * (256 / G) + threadIdx.x / G; row < n;
        row += static_cast<int64_t>(gridDim.x) * (256 / G)) {
     uint8_t* rec = nullptr;
+    const int32_t id = a.ids ? a.ids[row] : 0;
     for (int b0 = 0; b0 < a.blocks; b0 += G / LB) {
       const int b = b0 + lane / LB, at = (b0 * LB + lane) * E;
       float v[E];
       load_values(x + row * a.row_stride + (at < a.dim ? at : 0), a.dim - at, v);
-      if (b0 == 0) rec = write_to(a, row, bad);   // the group's lanes agree
+      if (b0 == 0) rec = write_to(a, row, id, bad);   // the group's lanes agree
       const uint32_t code = mx_scale_code<BITS>(mx_lanes_max<LB>(mx_top(v)));   // (0 past the last block)
       uint32_t w[(E * BITS + 31) / 32];
       mx_pack<BITS, E>(v, code, w);
@@ -123,7 +133,7 @@ __global__ __launch_bounds__(256) void k_mx_write_cols(MxWriteArgs a) {
   bool bad = false;
   for (int64_t row = static_cast<int64_t>(blockIdx.x) * 64 + (threadIdx.x & 63); row < n;
        row += static_cast<int64_t>(gridDim.x) * 64) {
-    uint8_t* rec = write_to(a, row, bad);
+    uint8_t* rec = write_to(a, row, a.ids ? a.ids[row] : 0, bad);
     if (!rec) continue;
     const T* xr = x + row * a.row_stride;
     for (int blk = b * 4 + (threadIdx.x >> 6); blk < a.blocks; blk += 4 * gridDim.y) {
@@ -166,7 +176,7 @@ __global__ __launch_bounds__(256) void k_mx_claim(const int32_t* ids, const int3
 // bytes lay 128 apart, 34 with streaming stores).  U rows of a group in flight; every load
 // unconditional from a clamped address (row 0 for a group without a row or
 // with an id outside the table).
-template <typename T, int BITS, int G, int U>
+template <typename T, int BITS, int G, int U, bool STREAM>
 __global__ __launch_bounds__(256) void k_mx_read(MxReadArgs a) {
   constexpr int E = 16 / sizeof(T), kBytes = E * BITS / 8;
   const int lane = threadIdx.x & (G - 1);
@@ -178,10 +188,12 @@ __global__ __launch_bounds__(256) void k_mx_read(MxReadArgs a) {
   for (int64_t row = static_cast<int64_t>(blockIdx.x) * (256 / G) + threadIdx.x / G; row < n; row += stride * U) {
     int64_t id[U];
     bool in[U];
+    if (a.ids) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t r = row + u * stride;
-      id[u] = a.ids ? static_cast<int64_t>(a.ids[r < n ? r : row]) : r;
+      for (int u = 0; u < U; ++u) id[u] = a.ids[row + u * stride < n ? row + u * stride : row];
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u) id[u] = row + u * stride;
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -207,7 +219,7 @@ __global__ __launch_bounds__(256) void k_mx_read(MxReadArgs a) {
         mx_unpack<BITS, E>(w[u], code[u], v);
 #pragma unroll
         for (int i = 0; i < E; ++i) v[i] = in[u] ? v[i] : 0.f;
-        if (r < n) mx_store(out + r * a.dim + c * E, v, a.dim - c * E, a.stream);
+        if (r < n) mx_store<STREAM>(out + r * a.dim + c * E, v, a.dim - c * E);
       }
     }
   }
@@ -274,7 +286,7 @@ __global__ __launch_bounds__(256) void k_mx_mean(MxMeanArgs a) {
       if (c % LB == 0) rec[a.blocks * 16 + c / LB] = static_cast<uint8_t>(code);
     } else {
       using O = std::conditional_t<OUT == 0, float, uint16_t>;
-      mx_store(static_cast<O*>(a.out) + row * a.dim + c * E, acc, a.dim - c * E, false);
+      mx_store<false>(static_cast<O*>(a.out) + row * a.dim + c * E, acc, a.dim - c * E);
     }
   }
   if constexpr (OUT == 2) {
@@ -319,11 +331,11 @@ void write_dispatch(const MxWriteArgs& a, hipStream_t s) {
 #undef GMB_MX_WRITE
 }
 
-template <typename T, int BITS>
-void read_dispatch(const MxReadArgs& a, hipStream_t s) {
+template <typename T, int BITS, bool STREAM>
+void read_rows(const MxReadArgs& a, hipStream_t s) {
   constexpr int U = 4, E = 16 / static_cast<int>(sizeof(T));
 #define GMB_MX_READ(GG) \
-  hipLaunchKernelGGL((k_mx_read<T, BITS, GG, U>), dim3(grid_for(a.n_cap, (256 / GG) * U)), dim3(256), 0, s, a)
+  hipLaunchKernelGGL((k_mx_read<T, BITS, GG, U, STREAM>), dim3(grid_for(a.n_cap, (256 / GG) * U)), dim3(256), 0, s, a)
   switch (lanes_for((a.dim + E - 1) / E, 2)) {
     case 2: GMB_MX_READ(2); break;
     case 4: GMB_MX_READ(4); break;
@@ -333,6 +345,12 @@ void read_dispatch(const MxReadArgs& a, hipStream_t s) {
     default: GMB_MX_READ(64); break;
   }
 #undef GMB_MX_READ
+}
+
+template <typename T, int BITS>
+void read_dispatch(const MxReadArgs& a, hipStream_t s) {
+  if (a.n_cap * a.dim * static_cast<int64_t>(sizeof(T)) >= kStreamBytes) read_rows<T, BITS, true>(a, s);
+  else read_rows<T, BITS, false>(a, s);
 }
 
 template <int BITS, int OUT>
@@ -376,9 +394,7 @@ hipError_t launch_mx_write(const MxWriteArgs& args, int bf16, int bits, uint32_t
   return hipGetLastError();
 }
 
-hipError_t launch_mx_read(const MxReadArgs& args, int bf16, int bits, hipStream_t s) {
-  MxReadArgs a = args;
-  a.stream = a.n_cap * a.dim * (bf16 ? 2 : 4) >= kStreamBytes;
+hipError_t launch_mx_read(const MxReadArgs& a, int bf16, int bits, hipStream_t s) {
   if (bits == 4) {
     if (bf16) read_dispatch<uint16_t, 4>(a, s);
     else read_dispatch<float, 4>(a, s);
