@@ -93,10 +93,10 @@ __device__ __forceinline__ uint4 load_chunk(const T* z, int64_t c, int64_t end) 
   mx_get<16>(&x, z + c);
   return x;
 }
-template <typename T>
+template <bool STREAM, typename T>
 __device__ __forceinline__ void store_chunk(T* grad, int64_t c, int64_t end, const float (&g)[Chunk<T>::N]) {
   const int64_t left = end - c;
-  mx_store<false>(grad + c, g, left < Chunk<T>::N ? static_cast<int>(left) : Chunk<T>::N);
+  mx_store<STREAM>(grad + c, g, left < Chunk<T>::N ? static_cast<int>(left) : Chunk<T>::N);
 }
 
 // Reductions over the TH threads of a row (a part of a wave, a wave, or the
@@ -303,7 +303,7 @@ __device__ __forceinline__ void forget(uint4 (&q)[K]) {
 // TH threads hold a row of up to TH * K chunks as they were loaded (the
 // values twice over would halve the rows that a CU has in flight); WAVES: the
 // waves a SIMD is to hold.
-template <typename T, int TH, int K, int POW, int WAVES>
+template <typename T, int TH, int K, int POW, int WAVES, bool STREAM>
 __global__ __launch_bounds__(TH < 256 ? 256 : TH) __attribute__((amdgpu_waves_per_eu(WAVES)))
 void k_distill_held(DistillArgs a) {
   constexpr int E = Chunk<T>::N;
@@ -328,7 +328,10 @@ void k_distill_held(DistillArgs a) {
   for (int k = 0; k < K; ++k) {
     const int c = (k * TH + t) * E;
     q[k] = masked_chunk<T>();
-    if (c + E <= a.classes) mx_get<16>(&q[k], z + c);
+    if (c + E <= a.classes) {
+      if constexpr (STREAM) mx_get_once<16>(&q[k], z + c);
+      else mx_get<16>(&q[k], z + c);
+    }
   }
   Early first = early_entry(a, row, live, t);
   // the chunk that the row ends in, if it is not whole, by the thread whose it is
@@ -397,7 +400,7 @@ void k_distill_held(DistillArgs a) {
       if (c >= a.classes) break;
       float g[E] = {};
       if (!r.none) chunk_gradient<POW, T>(r, q[k], g);   // (0 whatever the logits are)
-      store_chunk(grad, c, a.classes, g);
+      store_chunk<STREAM>(grad, c, a.classes, g);
       __builtin_amdgcn_sched_barrier(0);
     }
     for (int64_t c = a.classes + t; c < a.ld_grad; c += TH) Chunk<T>::store1(grad + c, 0.f);
@@ -491,7 +494,7 @@ __global__ __launch_bounds__(kSplitThreads) void k_distill_grad(DistillArgs a) {
   for (int64_t c = lo + t * E; c < hi; c += kSplitThreads * E) {
     float g[E] = {};
     if (!r.none) chunk_gradient<0, T>(r, load_chunk(z, c, hi), g);
-    store_chunk(grad, c, hi, g);
+    store_chunk<false>(grad, c, hi, g);
   }
   __syncthreads();
   correct_entries<T, kSplitThreads>(a, r, z, grad, first, t, ids, ps, lo, hi);
@@ -511,7 +514,7 @@ __global__ __launch_bounds__(1024) void k_loss_mean(const float* rows, int64_t n
   if (threadIdx.x == 0) *loss = all / static_cast<float>(n);
 }
 
-template <typename T, int TH, int K, int WAVES>
+template <typename T, int TH, int K, int WAVES, bool STREAM = false>
 void held(const DistillArgs& args, hipStream_t s) {
   constexpr int ROWS = TH < 256 ? 256 / TH : 1;
   constexpr int64_t kRows = kLaunchThreads / TH;   // of a launch
@@ -521,10 +524,10 @@ void held(const DistillArgs& args, hipStream_t s) {
   for (a.row0 = 0; a.row0 < a.rows; a.row0 += kRows) {
     const int64_t rows = a.rows - a.row0 < kRows ? a.rows - a.row0 : kRows;
     const dim3 grid(static_cast<unsigned>((rows + ROWS - 1) / ROWS)), block(TH < 256 ? 256 : TH);
-    if (t == 1.f) hipLaunchKernelGGL((k_distill_held<T, TH, K, 1, WAVES>), grid, block, lds, s, a);
-    else if (t == 2.f) hipLaunchKernelGGL((k_distill_held<T, TH, K, 2, WAVES>), grid, block, lds, s, a);
-    else if (t == 4.f) hipLaunchKernelGGL((k_distill_held<T, TH, K, 4, WAVES>), grid, block, lds, s, a);
-    else hipLaunchKernelGGL((k_distill_held<T, TH, K, 0, WAVES>), grid, block, lds, s, a);
+    if (t == 1.f) hipLaunchKernelGGL((k_distill_held<T, TH, K, 1, WAVES, STREAM>), grid, block, lds, s, a);
+    else if (t == 2.f) hipLaunchKernelGGL((k_distill_held<T, TH, K, 2, WAVES, STREAM>), grid, block, lds, s, a);
+    else if (t == 4.f) hipLaunchKernelGGL((k_distill_held<T, TH, K, 4, WAVES, STREAM>), grid, block, lds, s, a);
+    else hipLaunchKernelGGL((k_distill_held<T, TH, K, 0, WAVES, STREAM>), grid, block, lds, s, a);
     a.clear_n = 0;
   }
 }
@@ -538,8 +541,25 @@ void held(const DistillArgs& args, hipStream_t s) {
 // waits for its loads and its reductions, and another's exponentials fill the
 // time.  4,099 x 32,768 bf16, 512 threads: 135.0 us at five (two workgroups a CU),
 // 124.0 at six (three), 157 at eight (27 registers spilled); 2,000 x 30,000 fp32:
-// 183 us in 1,024 threads of 8 chunks, 101.4 in 512 of 16.  (Stores past the
-// caches changed nothing: 125.9 and 101.7.)
+// 183 us in 1,024 threads of 8 chunks, 101.4 in 512 of 16.
+//   Long rows with a large gradient: logits and gradient past the caches (those
+// 127.2 -> 119.4 and 101.0 -> 98.5; 16,000 x 4,000 fp32, 256 MB, 95.4 -> 89.6; but
+// 8,000 x 1,000, 32 MB, 17.0 -> 18.9).
+template <typename T, bool STREAM>
+void long_rows(const DistillArgs& a, hipStream_t s) {
+  constexpr int E = Chunk<T>::N;
+  const int chunks = (a.classes + E - 1) / E;
+  if (chunks <= 1024) {
+    held<T, 256, 4, 8, STREAM>(a, s);
+  } else if (chunks <= 2048) {
+    held<T, 256, 8, 5, STREAM>(a, s);
+  } else if (chunks <= 4096) {
+    held<T, 512, 8, 6, STREAM>(a, s);
+  } else if constexpr (E == 4) {
+    held<T, 512, 16, 4, STREAM>(a, s);
+  }
+}
+
 template <typename T>
 void dispatch(const DistillArgs& a, hipStream_t s) {
   constexpr int E = Chunk<T>::N;
@@ -556,14 +576,10 @@ void dispatch(const DistillArgs& a, hipStream_t s) {
     held<T, 32, 8, 5>(a, s);
   } else if (chunks <= 256) {
     held<T, 64, 4, 8>(a, s);
-  } else if (chunks <= 1024) {
-    held<T, 256, 4, 8>(a, s);
-  } else if (chunks <= 2048) {
-    held<T, 256, 8, 5>(a, s);
-  } else if (chunks <= 4096) {
-    held<T, 512, 8, 6>(a, s);
-  } else if constexpr (E == 4) {
-    held<T, 512, 16, 4>(a, s);
+  } else if (a.rows * a.classes * static_cast<int64_t>(sizeof(T)) >= 4 * kStreamBytes) {
+    long_rows<T, true>(a, s);
+  } else {
+    long_rows<T, false>(a, s);
   }
 }
 

@@ -15,10 +15,11 @@ constexpr int kMxOutF32 = 0, kMxOutBf16 = 1, kMxOutRecords = 2;
 
 // Outputs of at least this many bytes are stored past the caches: the L2s (32
 // MB together) could not keep them for a reader, and writing them there costs
-// what it evicts.  Plain against streaming stores: reads of the store, 8 MB
-// of fp32 rows 4.5 / 4.0 us, 16 MB 6.5 / 5.9, 64 MB 21.7 / 17.2, 138 MB 54.6 /
-// 34.3; the linear layer, 23 MB 18.2 / 17.1, 46 MB 28.6 / 19.3, 205 MB 95.2 /
-// 48.8.  Smaller ones stay where the next kernel finds them.
+// what it evicts.  Plain against streaming stores: reads of the store, 16 MB of
+// fp32 rows 5.7 / 5.2 us, 64 MB 19.2 / 16.7, 138 MB 42.9 / 33.0, 205 MB 59.3 / 40.6;
+// the linear layer, 23 MB 11.4 / 9.8, 33 MB 20.5 / 18.5, 102 MB 34.9 / 26.9, 205
+// MB 48.7 / 44.3; means, 120 MB 70.4 / 60.0.  Smaller ones stay where the next
+// kernel finds them.
 constexpr int64_t kStreamBytes = 16 << 20;
 
 // Threads of one launch: a grid counts them in 32 bits.

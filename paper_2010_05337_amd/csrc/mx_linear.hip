@@ -246,11 +246,11 @@ __global__ __launch_bounds__(64 * WK) void k_mx_linear_rows(MxLinearArgs p) {
 
 // A workgroup of WR x WC waves has 64 WC columns, whose whole records lie in
 // LDS from the start, and goes over tiles of 64 WR rows, whose records it
-// brings tile by tile; three workgroups a CU hide each other's waits (two with
-// 80 KB each: 14.4 us against 12.6 for 45,000 rows, two pairs of 100 by 256;
-// the next tile's rows arriving during this one's products, in a second
-// buffer, changed nothing).  In LDS a record is `slots` 16-byte pieces, an odd
-// number: sixteen rows' reads of one block fall on different banks.
+// brings tile by tile; three workgroups a CU hide each other's waits (45,000
+// rows, two pairs of 100 by 256, plain stores: two with 80 KB each 14.4 us,
+// three 12.6; the next tile's rows arriving during this one's products, in a
+// second buffer, changed nothing).  In LDS a record is `slots` 16-byte pieces,
+// an odd number: sixteen rows' reads of one block fall on different banks.
 constexpr int kResidentLds = 50 * 1024;
 
 __host__ __device__ inline int resident_slots(int blocks) { return (((blocks * 17 + 15) / 16) | 1); }

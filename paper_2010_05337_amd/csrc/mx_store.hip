@@ -30,7 +30,7 @@ __device__ __forceinline__ int64_t row_count(const int32_t* n_dev, int64_t n_cap
 }
 
 // 16 bytes of a row's values (4 fp32, 8 bf16), zeros from `left` on; read
-// once, so past the caches (350,000 rows of 128 bf16: 39.9 us, 35.0 so).
+// once, so past the caches (350,000 rows of 128 bf16: 39.4 us, 30.7 so).
 __device__ __forceinline__ void load_values(const float* p, int left, float (&v)[4]) {
   if (left >= 4) {
     mx_get_once<16>(v, p);
@@ -172,10 +172,11 @@ __global__ __launch_bounds__(256) void k_mx_claim(const int32_t* ids, const int3
 }
 
 // A lane writes 16 bytes of a row (E values), so that a group's stores are one
-// contiguous piece (346,000 rows of 100 fp32: 55 us, 69 where four lanes' 64
-// bytes lay 128 apart, 34 with streaming stores).  U rows of a group in flight; every load
-// unconditional from a clamped address (row 0 for a group without a row or
-// with an id outside the table).
+// contiguous piece (346,000 rows of 100 fp32, plain stores: 55 us, 69 where four
+// lanes' 64 bytes lay 128 apart).  U rows of a group in flight, their ids asked
+// for together (one by one 47.7 us, so 43.0; U = 2 47.5, 8 45.1; with streaming
+// stores 33.0); every load unconditional from a clamped address (row 0 for a
+// group without a row or with an id outside the table).
 template <typename T, int BITS, int G, int U, bool STREAM>
 __global__ __launch_bounds__(256) void k_mx_read(MxReadArgs a) {
   constexpr int E = 16 / sizeof(T), kBytes = E * BITS / 8;
@@ -229,7 +230,7 @@ __global__ __launch_bounds__(256) void k_mx_read(MxReadArgs a) {
 // OUT: 0 fp32 rows, 1 bf16 rows, 2 records of 4 bits.  A lane has E elements
 // of a destination (16 bytes of its row), G lanes a destination; U neighbours
 // in flight.  An id outside the table is read as row 0 (k_mean's rule).
-template <int BITS, int OUT, int G, int U>
+template <int BITS, int OUT, int G, int U, bool STREAM>
 __global__ __launch_bounds__(256) void k_mx_mean(MxMeanArgs a) {
   constexpr int E = OUT == 0 ? 4 : 8, LB = 32 / E, kBytes = E * BITS / 8, kWords = (E * BITS + 31) / 32;
   const int64_t row = a.row0 + (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) / G;
@@ -286,7 +287,7 @@ __global__ __launch_bounds__(256) void k_mx_mean(MxMeanArgs a) {
       if (c % LB == 0) rec[a.blocks * 16 + c / LB] = static_cast<uint8_t>(code);
     } else {
       using O = std::conditional_t<OUT == 0, float, uint16_t>;
-      mx_store<false>(static_cast<O*>(a.out) + row * a.dim + c * E, acc, a.dim - c * E);
+      mx_store<STREAM>(static_cast<O*>(a.out) + row * a.dim + c * E, acc, a.dim - c * E);
     }
   }
   if constexpr (OUT == 2) {
@@ -353,15 +354,15 @@ void read_dispatch(const MxReadArgs& a, hipStream_t s) {
   else read_rows<T, BITS, false>(a, s);
 }
 
-template <int BITS, int OUT>
-void mean_dispatch(const MxMeanArgs& args, hipStream_t s) {
+template <int BITS, int OUT, bool STREAM>
+void mean_rows(const MxMeanArgs& args, hipStream_t s) {
   constexpr int U = 8, E = OUT == 0 ? 4 : 8;
   MxMeanArgs a = args;
   const int g = lanes_for(OUT == 2 ? a.blocks * 4 : (a.dim + E - 1) / E, 4);
   for (a.row0 = 0; a.row0 < a.n_cap; a.row0 += kLaunchThreads / g) {
     const int64_t rows = a.n_cap - a.row0 < kLaunchThreads / g ? a.n_cap - a.row0 : kLaunchThreads / g;
     const dim3 grid(static_cast<unsigned>((rows * g + 255) / 256));
-#define GMB_MX_MEAN(GG) hipLaunchKernelGGL((k_mx_mean<BITS, OUT, GG, U>), grid, dim3(256), 0, s, a)
+#define GMB_MX_MEAN(GG) hipLaunchKernelGGL((k_mx_mean<BITS, OUT, GG, U, STREAM>), grid, dim3(256), 0, s, a)
     switch (g) {
       case 4: GMB_MX_MEAN(4); break;
       case 8: GMB_MX_MEAN(8); break;
@@ -371,6 +372,14 @@ void mean_dispatch(const MxMeanArgs& args, hipStream_t s) {
     }
   }
 #undef GMB_MX_MEAN
+}
+
+template <int BITS, int OUT>
+void mean_dispatch(const MxMeanArgs& a, hipStream_t s) {
+  if constexpr (OUT != kMxOutRecords) {   // (records are the next layer's input)
+    if (a.n_cap * a.dim * (OUT == kMxOutBf16 ? 2 : 4) >= kStreamBytes) return mean_rows<BITS, OUT, true>(a, s);
+  }
+  mean_rows<BITS, OUT, false>(a, s);
 }
 
 }  // namespace
