@@ -250,7 +250,9 @@ __global__ __launch_bounds__(64 * WK) void k_mx_linear_rows(MxLinearArgs p) {
 // rows, two pairs of 100 by 256, plain stores: two with 80 KB each 14.4 us,
 // three 12.6; the next tile's rows arriving during this one's products, in a
 // second buffer, changed nothing).  In LDS a record is `slots` 16-byte pieces,
-// an odd number: sixteen rows' reads of one block fall on different banks.
+// an odd number: sixteen rows' reads of one block fall on different banks.  (The
+// LDS serves half of such a sixteen with half of the next one's; pairs of blocks
+// exchanged in rows 4 - 11 took those conflicts out, and 10.1 us for 9.7.)
 constexpr int kResidentLds = 50 * 1024;
 
 __host__ __device__ inline int resident_slots(int blocks) { return (((blocks * 17 + 15) / 16) | 1); }
@@ -523,10 +525,12 @@ bool resident_fits(const MxLinearArgs& p) {
 //   - up to two workgroups a CU of 16 rows by 32 columns: k_mx_linear_rows (64
 //     x 4,096 x 1,024: 7.0, in 64 x 64 tiles 12.3; 300 x 1,024 x 256: 4.2 and
 //     6.4; but 1,000 x 256 x 1,024, 2,016 workgroups: 10.3 and 5.1);
-//   - resident weights where they fit and there are most of two tiles a CU
+//   - resident weights where they fit and there are more tiles than CUs
 //     (30,000 x 100 x 256: 8.0, tiles 10.7, 8.9 and 11.3 by size; 200,000 x 256
-//     x 256: 28.2, 50.2, 41.6, 41.5; but 16,000 x 256 x 256, 250 tiles: 7.9
-//     and 6.6);
+//     x 256: 28.2, 50.2, 41.6, 41.5; 281 tiles of 18,000 x 100 x 256: 7.1, tiles
+//     8.8; 375 of 24,000 x 2 x 100 x 256: 9.5 and 12.8; 282 of 36,000 x 256 x 128:
+//     8.2 and 8.8; slower at most by 8%, 422 of 27,000 x 256 x 256: 9.2 and 8.6;
+//     but 250 of 16,000 x 256 x 256: 7.9 and 6.3);
 //   - else 256 x 256 tiles if there are three for every four CUs (8,192 x 4,096
 //     x 4,096: 82, in 128 x 128 96, in 64 x 64 141; but 8,000 x 1,024 x 1,024,
 //     128 of them: 18.4, 14.4, 18.2);
@@ -536,15 +540,14 @@ bool resident_fits(const MxLinearArgs& p) {
 template <int OUT>
 void dispatch(const MxLinearArgs& p, hipStream_t s) {
   auto tiles = [&](int tm, int tn) { return ((p.n_cap + tm - 1) / tm) * ((p.d_out + tn - 1) / tn); };
-  constexpr int64_t kResidentTiles = 448;
   if constexpr ((OUT & kStreamed) == 0) {   // (1 MB of results at most)
     if (tiles(16, 32) <= 2 * kComputeUnits) return run_rows<1, 2, 8, OUT>(p, s);
   }
-  if (p.d_out > 128 && resident_fits<1, 4>(p) && tiles(64, 256) >= kResidentTiles) {
+  if (p.d_out > 128 && resident_fits<1, 4>(p) && tiles(64, 256) > kComputeUnits) {
     run_resident<1, 4, OUT>(p, s);
-  } else if (p.d_out > 64 && p.d_out <= 128 && resident_fits<2, 2>(p) && tiles(128, 128) >= kResidentTiles) {
+  } else if (p.d_out > 64 && p.d_out <= 128 && resident_fits<2, 2>(p) && tiles(128, 128) > kComputeUnits) {
     run_resident<2, 2, OUT>(p, s);
-  } else if (p.d_out <= 64 && resident_fits<4, 1>(p) && tiles(256, 64) >= kResidentTiles) {
+  } else if (p.d_out <= 64 && resident_fits<4, 1>(p) && tiles(256, 64) > kComputeUnits) {
     run_resident<4, 1, OUT>(p, s);
   } else if (p.d_out > 128 && tiles(256, 256) >= kComputeUnits * 3 / 4) {
     run_tiles<256, 256, 2, 4, OUT>(p, s);

@@ -114,6 +114,31 @@ def test_weights_and_temperatures(alpha, T, C, with_labels):
     check(z, top, cls, labels if with_labels else None, alpha, T)
 
 
+@pytest.mark.parametrize("C, dtype", [(1100, torch.float32), (4100, torch.bfloat16), (8190, torch.float32),
+                                      (20003, torch.bfloat16), (20003, torch.float32), (32768, torch.float32)], ids=str)
+def test_large_gradients(C, dtype):
+    """Gradients past 64 MB: the rows are a few ones again and again, and each
+    gets the gradient of the same row of a small batch (times their numbers)."""
+    few = 8
+    n = (1 << 26) // (C * (4 if dtype == torch.float32 else 2)) // few * few + few
+    print(f"{n} rows of {C} {dtype}", flush=True)
+    z, top, cls, labels = inputs(few, C, 5, C, dtype)
+    dev = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+    rep = lambda a: a.repeat(n // few, *[1] * (a.dim() - 1))  # noqa: E731
+    kw = dict(alpha=0.5, temperature=2.0)
+    loss, grad = gmb.distill_loss(rep(z.cuda()), rep(dev(top)), rep(dev(cls)), labels=rep(dev(labels)), **kw)
+    zh = z.float().numpy().astype(np.float64)
+    ref, g, size = mx_ref.distill(zh, top, cls, labels, 0.5, 2.0)
+    tol = (EPS * (size + 2.0 + 1) + n * U32 * size).mean() * 2
+    assert abs(float(loss) - ref.mean()) <= tol
+    bound = EPS * (parts(zh, 0.5, 2.0, few, labels) + np.abs(g) + (0.5 * 2.0 + 0.5) * 5 / few)
+    if dtype == torch.bfloat16:
+        bound = bound + UBF16 * (np.abs(g) + bound)
+    got = grad.view(n // few, few, C).double() * (n / few)
+    off = (got - torch.from_numpy(g).cuda()).abs() - torch.from_numpy(bound + 2.0 ** -100).cuda()
+    assert float(off.max()) <= 0
+
+
 def test_loss_alone():
     z, top, cls, labels = inputs(50, 60, 6, 1)
     check(z, top, cls, labels, 0.5, 2.0, want_grad=False)

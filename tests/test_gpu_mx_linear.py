@@ -83,6 +83,29 @@ def test_two_pairs_bias_relu(n, d_in, d_out, by_id):
         check(got, [(av, wv), (a2v, w2v)], bias.astype(np.float64), True, dtype)
 
 
+@pytest.mark.parametrize("d_in, d_out", [(2100, 60), (2100, 128), (2100, 130), (40, 64), (40, 127), (40, 255)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+def test_large_results(d_in, d_out, dtype):
+    """Results past 16 MB, from 50 rows by id, in tiles of every size and with
+    resident weights; what lies behind them stays."""
+    n = (1 << 24) // (d_out * (4 if dtype == torch.float32 else 2)) + 77
+    print(f"{n} x {d_in} x {d_out} {dtype}", flush=True)
+    rng = np.random.default_rng(d_in + d_out)
+    a, av = records(50, d_in, rng)
+    w, wv = records(d_out, d_in, rng, 1)
+    ids = rng.integers(0, 50, size=n).astype(np.int32)
+    out = torch.full((n + 3, d_out), 7.0, dtype=dtype, device="cuda")
+    gmb.mx_linear(a, w, d_in, ids=torch.from_numpy(ids).cuda(), dtype=dtype, out=out)
+    assert bool((out[n:] == 7).all())
+    y, mag = av @ wv.T, np.abs(av) @ np.abs(wv).T
+    tol = (d_in + 2) * U32 * mag
+    if dtype == torch.bfloat16:
+        tol = tol + UBF16 * (np.abs(y) + tol)
+    got = out[:n].double()
+    at = torch.from_numpy(ids).cuda().long()
+    assert bool(((got - torch.from_numpy(y).cuda()[at]).abs() <= torch.from_numpy(tol).cuda()[at]).all())
+
+
 def test_padded_strides_and_given_output():
     rng = np.random.default_rng(8)
     a, av = records(70, 100, rng)

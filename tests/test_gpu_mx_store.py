@@ -253,6 +253,32 @@ def test_addresses_past_32_bits():
     assert same(gmb.mx_linear(table, w, dim, ids=ids).cpu().numpy(), v.astype(np.float32))
 
 
+@pytest.mark.parametrize("dim", [75, 500])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+def test_large_results(dim, dtype):
+    """Reads and means past 16 MB, of 60 records; what lies behind them stays."""
+    size = 4 if dtype == torch.float32 else 2
+    n = (1 << 24) // (dim * size) + 5
+    print(f"{n} rows of {dim} {dtype}", flush=True)
+    rng = np.random.default_rng(dim)
+    rec = mx_ref.quantise(rng.normal(size=(60, dim)).astype(np.float32), 8)
+    table, val = torch.from_numpy(rec).cuda(), torch.from_numpy(mx_ref.values(rec, dim, 8)).cuda()
+    ids = torch.from_numpy(rng.integers(0, 60, size=2 * n).astype(np.int32)).cuda()
+    out = torch.full((n + 3, dim), 7.0, dtype=dtype, device="cuda")
+    gmb.mx_gather(ids, table, dim, 8, dtype=dtype, n=n, out=out)
+    assert bool((out[n:] == 7).all())
+    # (values of 8 bits: exact in bf16)
+    assert torch.equal(out[:n].double(), val[ids[:n].long()])
+    indptr = torch.arange(0, 2 * n + 1, 2, dtype=torch.int32, device="cuda")
+    out.fill_(7)
+    gmb.mx_mean((indptr, ids), table, dim, 8, dtype=dtype, out=out)
+    assert bool((out[n:] == 7).all())
+    pair = val[ids.long()].view(n, 2, dim)
+    # the sum of two values of 8 bits rounds once (fp32), half of it never, bf16 once more
+    tol = 2.0 ** -24 * pair.abs().sum(1) + (2.0 ** -8 * pair.sum(1).abs() if size == 2 else 0)
+    assert bool(((out[:n].double() - pair.mean(1)).abs() <= tol).all())
+
+
 def test_a_mean_of_more_rows_than_a_grid_counts():
     """2^26 + 9 rows of 64 lanes are more threads than 32 bits count."""
     n, dim = (1 << 26) + 9, 257
