@@ -177,16 +177,85 @@ struct RowTerms {
   bool none;        // no term at all: no gradient
 };
 
-// A row's entries in LDS: whole fours of them.
+// A row's entries in LDS: whole fours of them, 8 bytes each.  With many entries
+// also two sets of bits, 16 bits an entry: a class's bit is in `seen` if an entry
+// names it and in `twice` if two do, so that most entries are known to be alone
+// without a look at the others.  A class's bit is its number where the sets have
+// as many bits as there are classes; else classes share bits, and those whose
+// bit is taken twice are looked for.  (37,472 rows of 357 bf16, 214 entries: by
+// comparing all 207 us, 94 so; 20,000 x 1,000, 64 entries: 44.6 and 34.3; 60,000 x
+// 500, 30 entries: 50.6 and 45.2; with 8 entries comparing is two reads.)
+constexpr int kFewEntries = 8;
 __host__ __device__ inline int entry_room(int k) { return (k + 3) / 4 * 4; }
+__host__ __device__ inline int entry_bytes(int k) { return entry_room(k) * (k > kFewEntries ? 12 : 8); }
+
+struct Entries {
+  int32_t* ids;
+  float* ps;
+  uint32_t *seen, *twice;   // room / 2 words each
+  int room;
+  bool many, exact;
+  __device__ __forceinline__ Entries(uint32_t* lds, const DistillArgs& a, int row, int rows) {
+    room = entry_room(a.k);
+    many = a.k > kFewEntries;
+    exact = a.classes <= 16 * room;
+    ids = reinterpret_cast<int32_t*>(lds) + row * room;
+    ps = reinterpret_cast<float*>(lds + rows * room) + row * room;
+    seen = lds + 2 * rows * room + row * room;
+    twice = seen + room / 2;
+  }
+  // By the row's threads; then a barrier.
+  template <int TH>
+  __device__ __forceinline__ void clear(int t) {
+    if (many)
+      for (int j = t; j < room; j += TH) seen[j] = 0;
+  }
+  __device__ __forceinline__ int place(int32_t id) const {
+    if (exact) return id;
+    return static_cast<int>(__umulhi(static_cast<uint32_t>(id) * 0x9E3779B1u, static_cast<uint32_t>(16 * room)));
+  }
+  __device__ __forceinline__ void put(int32_t id) {
+    const int at = place(id);
+    const uint32_t bit = 1u << (at & 31);
+    if (atomicOr(&seen[at >> 5], bit) & bit) atomicOr(&twice[at >> 5], bit);
+  }
+  __device__ __forceinline__ int count(int32_t id) const {
+    int same = 0;
+    for (int i = 0; i < room; i += 4) {
+      const int4 v = *reinterpret_cast<const int4*>(ids + i);
+      same += (v.x == id) + (v.y == id) + (v.z == id) + (v.w == id);
+    }
+    return same;
+  }
+  // Whether an entry names class id.
+  __device__ __forceinline__ bool named(int32_t id) const {
+    if (many) {
+      const int at = place(id);
+      const bool in = seen[at >> 5] >> (at & 31) & 1;
+      if (exact || !in) return in;
+    }
+    return count(id) > 0;
+  }
+  // What the entries of entry j's class add up to, in their order.
+  __device__ __forceinline__ float share(int32_t id, int j) const {
+    if (many) {
+      const int at = place(id);
+      if (!(twice[at >> 5] >> (at & 31) & 1)) return ps[j];
+    }
+    if (count(id) == 1) return ps[j];
+    float p = 0.f;
+    for (int i = 0; i < room; ++i) p += ids[i] == id ? ps[i] : 0.f;
+    return p;
+  }
+};
 
 // The teacher's entries of a row in LDS (classes in `ids`, -1 for an invalid
 // one and past the last; probabilities in `ps`), then the loss and the gradient's factors; m,
 // st and s1 are the row's statistics.  Every thread of the row calls it.
 template <typename T, int TH>
 __device__ __forceinline__ RowTerms row_terms(const DistillArgs& a, int64_t row, bool live, const T* z, float m,
-                                              float st, float s1, const Early& first, int t, int32_t* ids, float* ps,
-                                              float* red, float& loss) {
+                                              float st, float s1, const Early& first, int t, Entries& in, float* red,
+                                              float& loss) {
   RowTerms r;
   const float inv_t = 1.f / a.temperature;
   const float inv_n = 1.f / static_cast<float>(a.rows);
@@ -195,8 +264,9 @@ __device__ __forceinline__ RowTerms row_terms(const DistillArgs& a, int64_t row,
   const bool some = live && !(st == 0.f);   // not: every logit is -inf
   // the teacher
   float mt = -INFINITY;
-  const int room = entry_room(a.k);
-  for (int j = t; j < room; j += TH) {
+  int32_t* ids = in.ids;
+  float* ps = in.ps;
+  for (int j = t; j < in.room; j += TH) {
     int32_t id = -1;
     float v = -INFINITY;
     if (j == t) {
@@ -212,6 +282,7 @@ __device__ __forceinline__ RowTerms row_terms(const DistillArgs& a, int64_t row,
     }
     ids[j] = id;
     ps[j] = v;
+    if (in.many && id >= 0) in.put(id);
     mt = fmaxf(mt, v);
   }
   mt = row_reduce<TH>(mt, Max(), red);
@@ -261,35 +332,22 @@ __device__ __forceinline__ void chunk_gradient(const RowTerms& r, const uint4& q
 
 // The classes in [lo, hi) that the teacher's entries or the label name: the
 // whole gradient again, less their shares.  Entries of one class add up in the
-// entries' order, and all that name a class write the same value.
+// entries' order, and all that name a class write the same value; the label's
+// class is its entries' to write, if it has any.
 template <typename T, int TH>
 __device__ __forceinline__ void correct_entries(const DistillArgs& a, const RowTerms& r, const T* z, T* grad,
-                                                const Early& first, int t, const int32_t* ids, const float* ps,
-                                                int64_t lo, int64_t hi) {
+                                                const Early& first, int t, const Entries& in, int64_t lo, int64_t hi) {
   if (r.none) return;
-  auto write = [&](int32_t id, int j, float zi) {
-    if (id < lo || id >= hi) return;
-    // (mostly there is one entry of a class, if any)
-    int same = 0;
-    for (int i = 0; i < entry_room(a.k); i += 4) {
-      const int4 v = *reinterpret_cast<const int4*>(ids + i);
-      same += (v.x == id) + (v.y == id) + (v.z == id) + (v.w == id);
-    }
-    float p = 0.f;
-    if (same == 1 && j >= 0) {
-      p = ps[j];
-    } else if (same > 0) {
-      for (int i = 0; i < a.k; ++i) p += ids[i] == id ? ps[i] : 0.f;
-    }
+  auto write = [&](int32_t id, float p, float zi) {
     const float d = zi - r.m;
     Chunk<T>::store1(grad + id, r.ft * exp2_(d * r.kt) - r.fp * p + r.f1 * exp2_(d * kLog2e) -
                                     (id == r.label ? r.fy : 0.f));
   };
   for (int j = t; j < a.k; j += TH) {
-    const int32_t id = ids[j];
-    if (id >= 0) write(id, j, j == t ? first.z : load_logit(z + id));
+    const int32_t id = in.ids[j];
+    if (id >= lo && id < hi) write(id, in.share(id, j), j == t ? first.z : load_logit(z + id));
   }
-  if (t == TH - 1 && r.label >= 0) write(r.label, -1, first.zl);
+  if (t == TH - 1 && r.label >= lo && r.label < hi && !in.named(r.label)) write(r.label, 0.f, first.zl);
 }
 
 // Makes loaded chunks opaque, so that what one pass computed of them (their
@@ -314,9 +372,9 @@ void k_distill_held(DistillArgs a) {
        i += static_cast<int64_t>(gridDim.x) * blockDim.x)
     a.clear[i] = 0;
   const int sub = threadIdx.x / TH, t = threadIdx.x % TH;
-  const int room = entry_room(a.k);
-  int32_t* ids = reinterpret_cast<int32_t*>(lds) + sub * room;
-  float* ps = reinterpret_cast<float*>(lds + ROWS * room) + sub * room;
+  Entries in(lds, a, sub, ROWS);
+  in.clear<TH>(t);
+  __syncthreads();
   int64_t row = a.row0 + static_cast<int64_t>(blockIdx.x) * ROWS + sub;
   const bool live = row < a.rows;
   if (!live) row = a.rows - 1;
@@ -388,7 +446,7 @@ void k_distill_held(DistillArgs a) {
   st = row_reduce<TH>(st, Sum(), red);
   if (hard) s1 = row_reduce<TH>(s1, Sum(), red);
   float loss;
-  const RowTerms r = row_terms<T, TH>(a, row, live, z, m, st, s1, first, t, ids, ps, red, loss);
+  const RowTerms r = row_terms<T, TH>(a, row, live, z, m, st, s1, first, t, in, red, loss);
   if (live && t == 0) a.loss_rows[row] = loss;
   if (!a.grad) return;
   T* grad = static_cast<T*>(a.grad) + row * a.ld_grad;
@@ -406,7 +464,7 @@ void k_distill_held(DistillArgs a) {
     for (int64_t c = a.classes + t; c < a.ld_grad; c += TH) Chunk<T>::store1(grad + c, 0.f);
   }
   __syncthreads();   // the entries' classes are written again
-  if (live) correct_entries<T, TH>(a, r, z, grad, first, t, ids, ps, 0, a.classes);
+  if (live) correct_entries<T, TH>(a, r, z, grad, first, t, in, 0, a.classes);
 }
 
 // The range of classes of part `part`: whole chunks.
@@ -466,8 +524,8 @@ __global__ __launch_bounds__(kSplitThreads) void k_distill_grad(DistillArgs a) {
   extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
   __shared__ float red[16];
   const int t = threadIdx.x;
-  int32_t* ids = reinterpret_cast<int32_t*>(lds);
-  float* ps = reinterpret_cast<float*>(lds + entry_room(a.k));
+  Entries in(lds, a, 0, 1);
+  in.clear<kSplitThreads>(t);   // (the reductions below are barriers)
   const int64_t row = blockIdx.x / a.parts;
   const int part = static_cast<int>(blockIdx.x % a.parts);
   const T* z = static_cast<const T*>(a.logits) + row * a.classes;
@@ -485,7 +543,7 @@ __global__ __launch_bounds__(kSplitThreads) void k_distill_grad(DistillArgs a) {
   const float s1 = row_reduce<kSplitThreads>(
       has ? stats[3 * t + 2] * (mi == -INFINITY ? 1.f : exp2_((mi - m) * kLog2e)) : 0.f, Sum(), red);
   float loss;
-  const RowTerms r = row_terms<T, kSplitThreads>(a, row, true, z, m, st, s1, first, t, ids, ps, red, loss);
+  const RowTerms r = row_terms<T, kSplitThreads>(a, row, true, z, m, st, s1, first, t, in, red, loss);
   if (part == 0 && t == 0) a.loss_rows[row] = loss;
   if (!a.grad) return;
   T* grad = static_cast<T*>(a.grad) + row * a.ld_grad;
@@ -497,7 +555,7 @@ __global__ __launch_bounds__(kSplitThreads) void k_distill_grad(DistillArgs a) {
     store_chunk<false>(grad, c, hi, g);
   }
   __syncthreads();
-  correct_entries<T, kSplitThreads>(a, r, z, grad, first, t, ids, ps, lo, hi);
+  correct_entries<T, kSplitThreads>(a, r, z, grad, first, t, in, lo, hi);
 }
 
 __global__ __launch_bounds__(1024) void k_loss_mean(const float* rows, int64_t n, float* loss) {
@@ -519,7 +577,7 @@ void held(const DistillArgs& args, hipStream_t s) {
   constexpr int ROWS = TH < 256 ? 256 / TH : 1;
   constexpr int64_t kRows = kLaunchThreads / TH;   // of a launch
   DistillArgs a = args;
-  const size_t lds = 8 * static_cast<size_t>(entry_room(a.k)) * ROWS;
+  const size_t lds = static_cast<size_t>(entry_bytes(a.k)) * ROWS;
   const float t = a.temperature;
   for (a.row0 = 0; a.row0 < a.rows; a.row0 += kRows) {
     const int64_t rows = a.rows - a.row0 < kRows ? a.rows - a.row0 : kRows;
@@ -535,7 +593,7 @@ void held(const DistillArgs& args, hipStream_t s) {
 // Threads of a row.  Short rows: as few as hold them, so that a wave has several
 // rows and shares their reductions (30,000 x 200 bf16: 64 threads 31.1 us, 16
 // threads 16.3; 60,000 x 47 fp32: 16 threads 16.4, 8 threads 12.5; 8,000 x 601
-// fp32: 64 threads 15.9, 32 threads 13.4); but their rows' entries are to fit 32
+// fp32: 64 threads 15.9, 32 threads 13.4); but their rows' entries are to fit 48
 // KB of LDS.  Longer rows: 256 or 512, and of the waves of a SIMD the most whose
 // registers hold their chunks without spilling (one register at 512 x 8): a row
 // waits for its loads and its reductions, and another's exponentials fill the
@@ -567,7 +625,7 @@ void dispatch(const DistillArgs& a, hipStream_t s) {
   if (a.stats) {
     const dim3 grid(static_cast<unsigned>(a.rows * a.parts));
     hipLaunchKernelGGL((k_distill_stats<T>), grid, dim3(kSplitThreads), 0, s, a);
-    hipLaunchKernelGGL((k_distill_grad<T>), grid, dim3(kSplitThreads), 8 * static_cast<size_t>(entry_room(a.k)), s, a);
+    hipLaunchKernelGGL((k_distill_grad<T>), grid, dim3(kSplitThreads), entry_bytes(a.k), s, a);
   } else if (chunks <= 16 && a.k <= 128) {
     held<T, 8, 2, 4>(a, s);
   } else if (chunks <= 64 && a.k <= 256) {
