@@ -561,7 +561,13 @@ void dispatch(const MxLinearArgs& p, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_mx_linear(const MxLinearArgs& p, int out, hipStream_t s) {
-  const bool stream = p.n_cap * p.d_out * (out == kMxOutBf16 ? 2 : 4) >= kStreamBytes;
+  // past the caches if large and written by whole 64-byte pieces: rows of such,
+  // or rows that a wave has whole (59,048 x 2 x 32 x 2,272 bf16: 69.4 us, plain
+  // 72.6; x 2,304 61.6, 68.1; 300,000 x 2 x 100 x 47 fp32 25.6, 29.4; but 2,273 168
+  // and 103, 200,000 x 256 x 240 bf16 39.0 and 35.4, 100,000 x 100 x 100 fp32 16.3
+  // and 12.5)
+  const int64_t row = p.d_out * (out == kMxOutBf16 ? 2 : 4);
+  const bool stream = p.n_cap * row >= kStreamBytes && (row % 64 == 0 || p.d_out <= 64);
   if (out == kMxOutRecords) dispatch<kMxOutRecords>(p, s);
   else if (out == kMxOutBf16) stream ? dispatch<kMxOutBf16 | kStreamed>(p, s) : dispatch<kMxOutBf16>(p, s);
   else stream ? dispatch<kMxOutF32 | kStreamed>(p, s) : dispatch<kMxOutF32>(p, s);
