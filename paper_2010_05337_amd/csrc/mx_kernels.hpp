@@ -19,7 +19,7 @@ constexpr int kMxOutF32 = 0, kMxOutBf16 = 1, kMxOutRecords = 2;
 // fp32 rows 5.7 / 5.2 us, 64 MB 19.2 / 16.7, 138 MB 42.9 / 33.0, 205 MB 59.3 / 40.6;
 // the linear layer, 23 MB 11.4 / 9.8, 33 MB 20.5 / 18.5, 102 MB 34.9 / 26.9, 205
 // MB 48.7 / 44.3; means, 120 MB 70.4 / 60.0.  Smaller ones stay where the next
-// kernel finds them.
+// kernel finds them.  (The linear layer has a further condition.)
 constexpr int64_t kStreamBytes = 16 << 20;
 
 // Threads of one launch: a grid counts them in 32 bits.
