@@ -865,11 +865,12 @@ def mx_linear(a: torch.Tensor, w: torch.Tensor, d_in: int, bias: torch.Tensor | 
 
 class SageMxWeights:
     """A GraphSAGE-mean model's weights in MXFP4: the records of the
-    transposed matrices of a SageWeights, and its biases (shared)."""
+    transposed matrices of a SageWeights, and its biases (copies: matrices
+    and biases are those of the last set that was quantised)."""
 
     def __init__(self, weights: SageWeights):
         self.dims = list(weights.dims)
-        self.bias = weights.bias
+        self.bias = [b.clone() for b in self._biases(weights)]
         self.w_self = [mx_quantise(w.t(), MXFP4) for w in weights.w_self]
         self.w_neigh = [mx_quantise(w.t(), MXFP4) for w in weights.w_neigh]
         s = MxWeightsStruct()
@@ -882,17 +883,25 @@ class SageMxWeights:
             s.bias[l] = self.bias[l].data_ptr()
         self.struct = s
 
+    def _biases(self, weights: SageWeights):
+        if any(b.numel() < d for b, d in zip(weights.bias, self.dims[1:])):
+            raise ValueError("a bias must have one entry per column of its layer")
+        return [b.reshape(-1)[:d] for b, d in zip(weights.bias, self.dims[1:])]
+
     def requantise(self, weights: SageWeights):
-        """The records of `weights` (the same widths) in place of the old."""
+        """The records and biases of `weights` (the same widths) in place of
+        the old, at the same addresses (captured graphs serve the new ones)."""
         if list(weights.dims) != self.dims:
             raise ValueError("the widths differ")
-        for l in range(len(self.w_self)):
+        for l, bias in enumerate(self._biases(weights)):
             mx_quantise(weights.w_self[l].t(), MXFP4, table=self.w_self[l])
             mx_quantise(weights.w_neigh[l].t(), MXFP4, table=self.w_neigh[l])
+            self.bias[l].copy_(bias)
 
     def values(self) -> SageWeights:
-        """What the records stand for, as float32 weights: what sage_forward
-        and sage_backward take to train the model on float32 masters."""
+        """What the records stand for, as float32 weights (the model's own
+        biases, not copies): what sage_forward and sage_backward take to train
+        the model on float32 masters."""
         def mat(rec, d_in):
             return mx_gather(None, rec, d_in, MXFP4).t().contiguous()
         return SageWeights([mat(w, d) for w, d in zip(self.w_self, self.dims)],

@@ -155,6 +155,41 @@ def test_a_store_smaller_than_the_graph(dg, graph):
         csr.check_status()
 
 
+def test_other_weights_in_a_served_model(dg, graph):
+    """requantise with another set of weights (a checkpoint, an average) takes
+    its matrices and its biases, also for a graph captured before, and leaves
+    the first set as it was."""
+    g, csr = graph
+    dims = [60, 50, 9]
+    first, second = (to_torch_weights(dg.sage_weights(dims, s)) for s in (2, 3))
+    assert all(not torch.equal(a, b) for a, b in zip(first.bias, second.bias))
+    kept = [b.clone() for b in first.bias]
+    mxw = gmb.SageMxWeights(first)
+    table = gmb.mx_quantise(torch.from_numpy(dg.features(g.num_nodes, 60, 5, "f32")).cuda(), 4)
+    blocks = gmb.sample_blocks(csr, torch.arange(77, dtype=torch.int32, device="cuda"), [5, 4], 3)
+    ws = gmb._aligned_bytes(gmb.mx_forward_workspace_bytes(blocks, mxw), table.device)[1]
+    logits = gmb.sage_forward_mx(blocks, table, mxw, workspace=ws)
+    cg = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(cg):
+        gmb.sage_forward_mx(blocks, table, mxw, workspace=ws, logits=logits)
+    for w in (second, first, second):
+        want = gmb.sage_forward_mx(blocks, table, gmb.SageMxWeights(w))
+        mxw.requantise(w)
+        assert torch.equal(gmb.sage_forward_mx(blocks, table, mxw), want)
+        logits.zero_()
+        torch.cuda.synchronize()
+        cg.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(logits, want)
+        assert all(torch.equal(a, b) for a, b in zip(mxw.values().bias, w.bias))
+    assert all(torch.equal(a, b) for a, b in zip(first.bias, kept))
+    short = to_torch_weights(dg.sage_weights(dims, 2))
+    short.bias[1] = short.bias[1][:1]
+    for call in (lambda: mxw.requantise(short), lambda: gmb.SageMxWeights(short)):
+        with pytest.raises(ValueError):
+            call()
+
+
 # ---------------------------------------------------------------- training
 
 def reference_step(host, x, ws, wn, bs, top, cls, labels, alpha, T):
