@@ -317,6 +317,7 @@ int gmb_sage_forward_mx(const gmb_blocks* blocks, const void* table, int64_t num
     m.out = base + p.off_mean[l];
     m.out_stride = rec_in;
     m.out_record = static_cast<int>(rec_in);
+    m.status = l == 0 ? status : nullptr;   // (above, positions in the layer below)
     hipError_t e = gmb::launch_mx_mean(m, GMB_MXFP4, gmb::kMxOutRecords, s);
     if (e != hipSuccess) return hip_fail(e, "store mean launch");
     gmb::MxLinearArgs a{};

@@ -65,6 +65,7 @@ struct MxMeanArgs {
   void* out;
   int64_t out_stride;               // records: bytes
   int out_record;
+  uint32_t* status;                 // or NULL: not told of an id outside the table
   int64_t row0;                     // set by the launcher: the launch's first row
 };
 

@@ -229,7 +229,9 @@ __global__ __launch_bounds__(256) void k_mx_read(MxReadArgs a) {
 
 // OUT: 0 fp32 rows, 1 bf16 rows, 2 records of 4 bits.  A lane has E elements
 // of a destination (16 bytes of its row), G lanes a destination; U neighbours
-// in flight.  An id outside the table is read as row 0 (k_mean's rule).
+// in flight.  An id outside the table is read as row 0 (k_mean's rule); a
+// model's forward (records) also reports it, by the largest id that it met, a
+// negative one being larger than every row's.
 template <int BITS, int OUT, int G, int U, bool STREAM>
 __global__ __launch_bounds__(256) void k_mx_mean(MxMeanArgs a) {
   constexpr int E = OUT == 0 ? 4 : 8, LB = 32 / E, kBytes = E * BITS / 8, kWords = (E * BITS + 31) / 32;
@@ -240,6 +242,7 @@ __global__ __launch_bounds__(256) void k_mx_mean(MxMeanArgs a) {
   if (row >= row_count(a.n_dev, a.n_cap)) return;
   const int32_t k = end - beg;
   const int chunks = OUT == 2 ? a.blocks * LB : (a.dim + E - 1) / E, scales = a.blocks * 4 * BITS;
+  uint32_t largest = 0;
   for (int c = lane; c < chunks; c += G) {
     float acc[E];
 #pragma unroll
@@ -249,6 +252,7 @@ __global__ __launch_bounds__(256) void k_mx_mean(MxMeanArgs a) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int32_t i = a.ids[beg + (e + u < k ? e + u : e)];
+        if constexpr (OUT == 2) largest = static_cast<uint32_t>(i) > largest ? static_cast<uint32_t>(i) : largest;
         id[u] = valid_vertex(i, a.table_rows) ? i : 0;
       }
       uint32_t w[U][kWords];
@@ -293,6 +297,7 @@ __global__ __launch_bounds__(256) void k_mx_mean(MxMeanArgs a) {
   if constexpr (OUT == 2) {
     uint8_t* rec = static_cast<uint8_t*>(a.out) + row * a.out_stride;
     for (int i = a.blocks * 17 + lane; i < a.out_record; i += G) rec[i] = 0;
+    if (largest >= a.table_rows) raise_status(a.status, GMB_STATUS_ERANGE);
   }
 }
 

@@ -190,6 +190,28 @@ def test_other_weights_in_a_served_model(dg, graph):
             call()
 
 
+def test_neighbours_outside_the_store(dg, graph):
+    """Destinations inside the store, some of their sampled neighbours outside:
+    reported, and read as record 0."""
+    g, csr = graph
+    dims, rows = [60, 9], 4000
+    mxw = gmb.SageMxWeights(to_torch_weights(dg.sage_weights(dims, 2)))
+    feats = torch.from_numpy(dg.features(g.num_nodes, 60, 5, "f32")).cuda()
+    whole = gmb.mx_quantise(feats, 4)
+    blocks = gmb.sample_blocks(csr, torch.arange(0, rows, 7, dtype=torch.int32, device="cuda"), [6], 3)
+    b = blocks.blocks()[0]
+    assert int(b.src_ids[:b.n_dst].max()) < rows and int(b.nbr.max()) >= rows
+    want = whole.clone()
+    want[rows:] = whole[0]
+    want = gmb.sage_forward_mx(blocks, want, mxw)
+    csr.check_status()
+    assert torch.equal(gmb.sage_forward_mx(blocks, whole[:rows], mxw), want)
+    with pytest.raises(gmb.GmbError, match="ERANGE"):
+        csr.check_status()
+    gmb.sage_forward_mx(blocks, whole, mxw)
+    csr.check_status()
+
+
 # ---------------------------------------------------------------- training
 
 def reference_step(host, x, ws, wn, bs, top, cls, labels, alpha, T):
