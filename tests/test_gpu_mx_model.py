@@ -111,6 +111,38 @@ def test_serving(dg, graph, dims, fanouts, seeds):
     assert torch.equal(gmb.sage_forward_mx(blocks, wide, mxw), a)
 
 
+@pytest.fixture(scope="module")
+def wide_graph(dg):
+    g = dg.rmat(17, 100_000, 500_000, (0.57, 0.19, 0.19), 13)
+    return g, csr_on_device(g)
+
+
+@pytest.mark.parametrize("d_in, d_hid", [(100, 256), (100, 100), (100, 60),      # resident weights, each shape
+                                         (140, 200), (140, 100), (140, 60)])     # tiles of 256, 128 and 64
+def test_serving_many_rows(dg, wide_graph, d_in, d_hid):
+    """Hidden records of tens of thousands of destinations; rows of the
+    workspace past the last destination stay as they were."""
+    g, csr = wide_graph
+    dims, seeds = [d_in, d_hid, 8], 24_000
+    print(f"{dims}, {seeds} seeds", flush=True)
+    mxw = gmb.SageMxWeights(to_torch_weights(dg.sage_weights(dims, 6)))
+    table = gmb.mx_quantise(torch.from_numpy(dg.features(g.num_nodes, d_in, 5, "f32")).cuda(), gmb.MXFP4)
+    ids = torch.from_numpy(dg.permutation(g.num_nodes, 7)[:seeds]).cuda()
+    blocks = gmb.sample_blocks(csr, ids, [3, 2], 8)
+    cap = int(blocks.struct.blk[0].cap_dst)
+    assert cap == 3 * seeds
+    want = served(blocks, table, None, mxw)
+    ws = gmb._aligned_bytes(gmb.mx_forward_workspace_bytes(blocks, mxw), table.device)[1]
+    ws.fill_(0xAA)
+    assert torch.equal(gmb.sage_forward_mx(blocks, table, mxw, workspace=ws), want)
+    n = blocks.sizes()[0][0]
+    assert n < cap
+    for hidden in (0, 1):
+        rb = mx_ref.record_bytes(dims[hidden], 4)
+        off = gmb.lib().gmb_mx_forward_offset(ctypes.byref(blocks.struct), ctypes.byref(mxw.struct), 0, hidden)
+        assert bool((ws[off + n * rb:off + cap * rb] == 0xAA).all())
+
+
 def test_serving_replayed_and_empty(dg, graph):
     g, csr = graph
     dims = [60, 50, 9]
