@@ -14,6 +14,7 @@
 //                    one 16-byte (4 bits) or two (8 bits) reads and a scale
 #include <type_traits>
 
+#include "edge_steps.hpp"
 #include "mx.hpp"
 #include "mx_kernels.hpp"
 
@@ -247,11 +248,11 @@ __global__ __launch_bounds__(256) void k_mx_mean(MxMeanArgs a) {
     float acc[E];
 #pragma unroll
     for (int i = 0; i < E; ++i) acc[i] = 0.f;
-    for (int32_t e = 0; e < k; e += U) {
+    edge_steps<U>(beg, end, [&](int32_t e, int32_t n, auto&& at) {
       int64_t id[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int32_t i = a.ids[beg + (e + u < k ? e + u : e)];
+        const int32_t i = a.ids[at(u)];
         if constexpr (OUT == 2) largest = static_cast<uint32_t>(i) > largest ? static_cast<uint32_t>(i) : largest;
         id[u] = valid_vertex(i, a.table_rows) ? i : 0;
       }
@@ -268,7 +269,7 @@ __global__ __launch_bounds__(256) void k_mx_mean(MxMeanArgs a) {
       for (int u = 0; u < U; ++u) {
         // a slot past the row's end: zeros at scale 1 (adding +0 changes
         // nothing)
-        const bool in = e + u < k;
+        const bool in = u < n - e;
 #pragma unroll
         for (int j = 0; j < kWords; ++j) w[u][j] = in ? w[u][j] : 0u;
         float v[E];
@@ -276,7 +277,7 @@ __global__ __launch_bounds__(256) void k_mx_mean(MxMeanArgs a) {
 #pragma unroll
         for (int i = 0; i < E; ++i) acc[i] += v[i];
       }
-    }
+    });
     if (k > 0) {
       const float kf = static_cast<float>(k);
 #pragma unroll
