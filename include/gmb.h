@@ -578,7 +578,7 @@ size_t gmb_distill_workspace_bytes(int64_t rows, int32_t classes);
  * label is outside [0, classes) the second, and one whose logits are all
  * -inf both; their gradients are 0.  (A logit of -inf is a class that cannot
  * be: probability 0; the loss is infinite if the teacher gives it more.)
- * Sums and statistics are fp32, in a fixed order.
+ * Sums and statistics are fp32, the mean over the rows 64 bits, in a fixed order.
  *   logits   device [rows, classes] fp32 or bf16 (`dtype`)
  *   labels   device int32 [rows] or NULL (no second term)
  *   dlogits  device [rows, classes] of `dtype`, or NULL for the loss alone;

@@ -18,7 +18,7 @@
 //                    rows too long for that, and few rows: workgroups share a
 //                    row, each with a range of classes; the first kernel
 //                    leaves their maxima and sums, the second joins them
-//   k_loss_mean      the mean over the rows, in a fixed order
+//   k_loss_mean      the mean over the rows, in 64 bits and a fixed order
 // The statistics are fp32: the running maximum m, sum exp((z - m) / T) and
 // sum exp(z - m).
 #include "common.hpp"
@@ -105,10 +105,13 @@ struct Max {
   __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
 };
 struct Sum {
-  __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
+  template <typename V>
+  __device__ __forceinline__ V operator()(V a, V b) const {
+    return a + b;
+  }
 };
-template <int TH, typename Op>
-__device__ __forceinline__ float row_reduce(float x, Op op, float* red) {
+template <int TH, typename V, typename Op>
+__device__ __forceinline__ V row_reduce(V x, Op op, V* red) {
 #pragma unroll
   for (int o = (TH < 64 ? TH : 64) / 2; o > 0; o >>= 1) x = op(x, __shfl_xor(x, o, 64));
   if constexpr (TH > 64) {
@@ -558,9 +561,12 @@ __global__ __launch_bounds__(kSplitThreads) void k_distill_grad(DistillArgs a) {
   correct_entries<T, kSplitThreads>(a, r, z, grad, first, t, in, lo, hi);
 }
 
+// 64 bits: a thread's chain is n / 4096 terms long, and terms alike are all
+// rounded the same way (2^26 rows of one loss: an fp32 chain was off by 4.9e-5 of
+// it).
 __global__ __launch_bounds__(1024) void k_loss_mean(const float* rows, int64_t n, float* loss) {
-  __shared__ float red[16];
-  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  __shared__ double red[16];
+  double s[4] = {0., 0., 0., 0.};
   for (int64_t i = threadIdx.x; i < n; i += 4096) {
     float v[4];
 #pragma unroll
@@ -568,8 +574,8 @@ __global__ __launch_bounds__(1024) void k_loss_mean(const float* rows, int64_t n
 #pragma unroll
     for (int u = 0; u < 4; ++u) s[u] += i + 1024 * u < n ? v[u] : 0.f;
   }
-  const float all = row_reduce<1024>((s[0] + s[1]) + (s[2] + s[3]), Sum(), red);
-  if (threadIdx.x == 0) *loss = all / static_cast<float>(n);
+  const double all = row_reduce<1024>((s[0] + s[1]) + (s[2] + s[3]), Sum(), red);
+  if (threadIdx.x == 0) *loss = static_cast<float>(all / static_cast<double>(n));
 }
 
 template <typename T, int TH, int K, int WAVES, bool STREAM = false>

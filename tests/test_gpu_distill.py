@@ -234,6 +234,20 @@ def test_more_rows_than_a_grid_counts():
     assert bool((grad.float().abs().amax(1) > 0).all())
 
 
+def test_the_mean_of_many_rows():
+    """2^26 rows of one loss: a running fp32 sum of 2^14 terms, each rounded the
+    same way, would be off by up to 2^14 half-steps.  The mean is off by the
+    row's own error and one rounding."""
+    n = 1 << 26
+    print(f"distill: {n} rows", flush=True)
+    z = torch.empty((n, 2), dtype=torch.bfloat16, device="cuda")
+    z[:, 0], z[:, 1] = 0.0, 1.0
+    loss, _ = gmb.distill_loss(z, torch.ones((n, 1), device="cuda"),
+                               torch.zeros((n, 1), dtype=torch.int32, device="cuda"), alpha=1.0, grad=False)
+    per, _, _ = mx_ref.distill(np.array([[0.0, 1.0]]), np.ones((1, 1)), np.zeros((1, 1), np.int32), None, 1.0, 1.0)
+    assert abs(float(loss) - per[0]) <= (EPS + U32) * per[0], (float(loss), per[0])
+
+
 def test_the_gradient_is_the_loss_s_difference():
     """Central differences of the GPU's own loss (fp32: steps of 2^-5 and a
     bound of the differences' second order and rounding)."""
