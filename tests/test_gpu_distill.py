@@ -248,6 +248,26 @@ def test_the_mean_of_many_rows():
     assert abs(float(loss) - per[0]) <= (EPS + U32) * per[0], (float(loss), per[0])
 
 
+def test_more_threads_than_a_grid_counts():
+    """2^29 + 3 rows of two classes: 8 threads each are more than 32 bits count.
+    All rows are one of two kinds; the mean adds one rounding."""
+    n = (1 << 29) + 3
+    print(f"distill: {n} rows", flush=True)
+    kinds = torch.tensor([[0.0, 1.0], [2.0, 0.0]])
+    z = torch.empty((n, 2), dtype=torch.bfloat16, device="cuda")
+    z[0::2], z[1::2] = kinds[0].cuda(), kinds[1].cuda()
+    loss, grad = gmb.distill_loss(z, torch.ones((n, 1), device="cuda"),
+                                  torch.zeros((n, 1), dtype=torch.int32, device="cuda"), alpha=1.0)
+    per, g, _ = mx_ref.distill(kinds.double().numpy(), np.ones((2, 1)), np.zeros((2, 1), np.int32), None, 1.0, 1.0)
+    want = ((n + 1) // 2 * per[0] + n // 2 * per[1]) / n
+    assert abs(float(loss) - want) <= (EPS + U32) * want
+    # the rows of a kind have the same bits, and those are near the definition's
+    assert bool((grad[0:n - 1:2] == grad[0]).all()) and bool((grad[1::2] == grad[1]).all())
+    assert bool((grad[n - 1] == grad[0]).all())
+    got, g = grad[:2].double().cpu().numpy(), g * 2 / n
+    assert np.all(np.abs(got - g) <= (UBF16 + EPS) * np.abs(g) + 2 * EPS / n)
+
+
 def test_the_gradient_is_the_loss_s_difference():
     """Central differences of the GPU's own loss (fp32: steps of 2^-5 and a
     bound of the differences' second order and rounding)."""
