@@ -106,6 +106,30 @@ def test_large_results(d_in, d_out, dtype):
     assert bool(((got - torch.from_numpy(y).cuda()[at]).abs() <= torch.from_numpy(tol).cuda()[at]).all())
 
 
+@pytest.mark.parametrize("n, d_in, d_out", [(12_300, 2100, 1024), (52_600, 2100, 160), (26_400, 2100, 160),
+                                            (264_000, 40, 64), (87_500, 40, 96), (65_700, 40, 128), (33_000, 40, 256)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+def test_large_results_of_whole_pieces(n, d_in, d_out, dtype):
+    """Results past 16 MB whose rows are whole 64-byte pieces (those are stored
+    past the caches): in tiles of 256 and 128 and with resident weights of each
+    shape, from 50 rows by id; what lies behind them stays."""
+    print(f"{n} x {d_in} x {d_out} {dtype}", flush=True)
+    rng = np.random.default_rng(n)
+    a, av = records(50, d_in, rng)
+    w, wv = records(d_out, d_in, rng, 1)
+    ids = rng.integers(0, 50, size=n).astype(np.int32)
+    out = torch.full((n + 3, d_out), 7.0, dtype=dtype, device="cuda")
+    gmb.mx_linear(a, w, d_in, ids=torch.from_numpy(ids).cuda(), dtype=dtype, out=out)
+    assert bool((out[n:] == 7).all())
+    y, mag = av @ wv.T, np.abs(av) @ np.abs(wv).T
+    tol = (d_in + 2) * U32 * mag
+    if dtype == torch.bfloat16:
+        tol = tol + UBF16 * (np.abs(y) + tol)
+    at = torch.from_numpy(ids).cuda().long()
+    off = (out[:n].double() - torch.from_numpy(y).cuda()[at]).abs() - torch.from_numpy(tol).cuda()[at]
+    assert float(off.max()) <= 0
+
+
 def test_padded_strides_and_given_output():
     rng = np.random.default_rng(8)
     a, av = records(70, 100, rng)
