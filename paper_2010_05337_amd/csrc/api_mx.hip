@@ -158,8 +158,7 @@ int gmb_mx_mean(const int32_t* indptr, const int32_t* ids, const int32_t* n_dev,
   a.table_rows = num_rows;
   a.table_stride = table_stride;
   a.out = out;
-  const hipError_t e =
-      gmb::launch_mx_mean(a, format, dtype == GMB_BF16 ? gmb::kMxOutBf16 : gmb::kMxOutF32, as_stream(stream));
+  const hipError_t e = gmb::launch_mx_mean(a, dtype == GMB_BF16, format, as_stream(stream));
   if (e != hipSuccess) return hip_fail(e, "store mean launch");
   return GMB_OK;
 }
@@ -318,7 +317,7 @@ int gmb_sage_forward_mx(const gmb_blocks* blocks, const void* table, int64_t num
     m.out_stride = rec_in;
     m.out_record = static_cast<int>(rec_in);
     m.status = l == 0 ? status : nullptr;   // (above, positions in the layer below)
-    hipError_t e = gmb::launch_mx_mean(m, GMB_MXFP4, gmb::kMxOutRecords, s);
+    hipError_t e = gmb::launch_mx_mean_records(m, s);
     if (e != hipSuccess) return hip_fail(e, "store mean launch");
     gmb::MxLinearArgs a{};
     a.pairs = 2;

@@ -73,7 +73,9 @@ struct MxMeanArgs {
 // or NULL (the ids are distinct)
 hipError_t launch_mx_write(const MxWriteArgs& a, int bf16, int bits, uint32_t* slots, hipStream_t s);
 hipError_t launch_mx_read(const MxReadArgs& a, int bf16, int bits, hipStream_t s);
-hipError_t launch_mx_mean(const MxMeanArgs& a, int bits, int out, hipStream_t s);
+hipError_t launch_mx_mean(const MxMeanArgs& a, int bf16, int bits, hipStream_t s);
+// 4 bits to 4 bits
+hipError_t launch_mx_mean_records(const MxMeanArgs& a, hipStream_t s);
 
 // One pair of a product: rows of `a` (row ids[i] of rows `a_rows`, or row i)
 // by the records of `w`.

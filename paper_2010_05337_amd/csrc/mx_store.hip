@@ -228,7 +228,7 @@ __global__ __launch_bounds__(256) void k_mx_read(MxReadArgs a) {
   if (bad) raise_status(a.status, GMB_STATUS_ERANGE);
 }
 
-// OUT: 0 fp32 rows, 1 bf16 rows, 2 records of 4 bits.  A lane has E elements
+// OUT: 0 fp32 rows, 1 bf16 rows, 2 records of 4 bits (of a 4-bit table).  A lane has E elements
 // of a destination (16 bytes of its row), G lanes a destination; U neighbours
 // in flight.  An id outside the table is read as row 0 (k_mean's rule); a
 // model's forward (records) also reports it, by the largest id that it met, a
@@ -420,16 +420,19 @@ hipError_t launch_mx_read(const MxReadArgs& a, int bf16, int bits, hipStream_t s
   return hipGetLastError();
 }
 
-hipError_t launch_mx_mean(const MxMeanArgs& a, int bits, int out, hipStream_t s) {
+hipError_t launch_mx_mean(const MxMeanArgs& a, int bf16, int bits, hipStream_t s) {
   if (bits == 4) {
-    if (out == kMxOutRecords) mean_dispatch<4, 2>(a, s);
-    else if (out == kMxOutBf16) mean_dispatch<4, 1>(a, s);
-    else mean_dispatch<4, 0>(a, s);
+    if (bf16) mean_dispatch<4, kMxOutBf16>(a, s);
+    else mean_dispatch<4, kMxOutF32>(a, s);
   } else {
-    if (out == kMxOutRecords) mean_dispatch<8, 2>(a, s);
-    else if (out == kMxOutBf16) mean_dispatch<8, 1>(a, s);
-    else mean_dispatch<8, 0>(a, s);
+    if (bf16) mean_dispatch<8, kMxOutBf16>(a, s);
+    else mean_dispatch<8, kMxOutF32>(a, s);
   }
+  return hipGetLastError();
+}
+
+hipError_t launch_mx_mean_records(const MxMeanArgs& a, hipStream_t s) {
+  mean_dispatch<4, kMxOutRecords>(a, s);
   return hipGetLastError();
 }
 
