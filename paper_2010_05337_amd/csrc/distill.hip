@@ -129,7 +129,9 @@ __device__ __forceinline__ V row_reduce(V x, Op op, V* red) {
 
 // How exp(z - m) follows from u = exp((z - m) / T): it is u^T for T = 1, 2
 // and 4 (POW), one exponential a class and pass instead of two; else (POW 0)
-// it takes its own.
+// it takes its own.  (Rows of T = 1, 2, 4 with POW and without: 4,099 x 32,768
+// bf16 108 / 117 us, 112 / 116, 112 / 116; 2,000 x 30,000 fp32 98.9 / 102, 99.2 /
+// 102, 100 / 102; 30,000 x 200 bf16 19.5 / 21.6, 19.9 / 21.7, 20.2 / 21.6.)
 template <int POW>
 __device__ __forceinline__ float hard_exp(float u, float d) {
   if constexpr (POW == 1) return u;
@@ -185,9 +187,10 @@ struct RowTerms {
 // names it and in `twice` if two do, so that most entries are known to be alone
 // without a look at the others.  A class's bit is its number where the sets have
 // as many bits as there are classes; else classes share bits, and those whose
-// bit is taken twice are looked for.  (37,472 rows of 357 bf16, 214 entries: by
-// comparing all 207 us, 94 so; 20,000 x 1,000, 64 entries: 44.6 and 34.3; 60,000 x
-// 500, 30 entries: 50.6 and 45.2; with 8 entries comparing is two reads.)
+// bit is taken twice are looked for.  (T = 1.5, 37,472 rows of 357 bf16, 214
+// entries: by comparing all 203 us, 118 so; 20,000 x 1,000, 64 entries: 42.0 and
+// 36.0; 60,000 x 500, 30 entries: 50.7 and 46.8; with 8 entries comparing is two
+// reads.)
 constexpr int kFewEntries = 8;
 __host__ __device__ inline int entry_room(int k) { return (k + 3) / 4 * 4; }
 __host__ __device__ inline int entry_bytes(int k) { return entry_room(k) * (k > kFewEntries ? 12 : 8); }
@@ -383,7 +386,7 @@ void k_distill_held(DistillArgs a) {
   if (!live) row = a.rows - 1;
   const T* z = static_cast<const T*>(a.logits) + row * a.classes;
   // the row's loads, its entries' and its last chunk's are on the way together
-  // (each waited for by itself: 4,099 x 32,768 bf16 135 us, so 125)
+  // (a fourteenth less time than each waited for by itself, 4,099 x 32,768 bf16)
   uint4 q[K];
 #pragma unroll
   for (int k = 0; k < K; ++k) {
@@ -602,18 +605,19 @@ void held(const DistillArgs& args, hipStream_t s) {
 }
 
 // Threads of a row.  Short rows: as few as hold them, so that a wave has several
-// rows and shares their reductions (30,000 x 200 bf16: 64 threads 31.1 us, 16
-// threads 16.3; 60,000 x 47 fp32: 16 threads 16.4, 8 threads 12.5; 8,000 x 601
-// fp32: 64 threads 15.9, 32 threads 13.4); but their rows' entries are to fit 48
-// KB of LDS.  Longer rows: 256 or 512, and of the waves of a SIMD the most whose
-// registers hold their chunks without spilling (one register at 512 x 8): a row
-// waits for its loads and its reductions, and another's exponentials fill the
-// time.  4,099 x 32,768 bf16, 512 threads: 135.0 us at five (two workgroups a CU),
-// 124.0 at six (three), 157 at eight (27 registers spilled); 2,000 x 30,000 fp32:
-// 183 us in 1,024 threads of 8 chunks, 101.4 in 512 of 16.
-//   Long rows with a large gradient: logits and gradient past the caches (those
-// 127.2 -> 119.4 and 101.0 -> 98.5; 16,000 x 4,000 fp32, 256 MB, 95.4 -> 89.6; but
-// 8,000 x 1,000, 32 MB, 17.0 -> 18.9).
+// rows and shares their reductions (calls, T = 1.5, 8 entries: 30,000 x 200 bf16
+// in 64 threads 43.4 us, 32 36.8, 16 22.2; 60,000 x 47 fp32 in 64 61.1, 32 43.4, 16
+// 25.0, 8 20.0; 8,000 x 601 fp32 in 64 18.5, 32 16.7); but their rows' entries are
+// to fit 48 KB of LDS.  Longer rows: 256 or 512, and of the waves of a SIMD the
+// most whose registers hold their chunks without spilling (one register at 512 x
+// 8): a row waits for its loads and its reductions, and another's exponentials
+// fill the time.  4,099 x 32,768 bf16, 64 entries, 512 threads: 125 us at five (two
+// workgroups a CU), 117 at six (three), 149 at eight (27 registers spilled); 2,000
+// x 30,000 fp32: 126 us in 1,024 threads of 8 chunks, 102 in 512 of 16.
+//   Long rows with a large gradient: logits and gradient past the caches (plain
+// 121 and streaming 117 us, 105 and 102; 16,000 x 4,000 fp32, 256 MB, 8 entries
+// 102 and 93, but 64 entries 107 and 119, as corrections come back to lines that
+// have left; 8,000 x 1,000, 32 MB, no difference).
 template <typename T, bool STREAM>
 void long_rows(const DistillArgs& a, hipStream_t s) {
   constexpr int E = Chunk<T>::N;

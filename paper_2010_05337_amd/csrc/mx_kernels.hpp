@@ -16,9 +16,9 @@ constexpr int kMxOutF32 = 0, kMxOutBf16 = 1, kMxOutRecords = 2;
 // Outputs of at least this many bytes are stored past the caches: the L2s (32
 // MB together) could not keep them for a reader, and writing them there costs
 // what it evicts.  Plain against streaming stores: reads of the store, 16 MB of
-// fp32 rows 5.7 / 5.2 us, 64 MB 19.2 / 16.7, 138 MB 42.9 / 33.0, 205 MB 59.3 / 40.6;
-// the linear layer, 23 MB 11.4 / 9.8, 33 MB 20.5 / 18.5, 102 MB 34.9 / 26.9, 205
-// MB 48.7 / 44.3; means, 120 MB 70.4 / 60.0.  Smaller ones stay where the next
+// fp32 rows 6.4 / 6.2 us, 64 MB 20.4 / 16.8, 138 MB 42.1 / 33.2, 205 MB 61.0 / 48.2;
+// the linear layer, 23 MB 12.4 / 10.4, 56 MB 30.9 / 25.2, 102 MB 64.4 / 51.5;
+// means (25 neighbours of 500), 120 MB 184 / 183.  Smaller ones stay where the next
 // kernel finds them.  (The linear layer has a further condition.)
 constexpr int64_t kStreamBytes = 16 << 20;
 

@@ -246,10 +246,10 @@ __global__ __launch_bounds__(64 * WK) void k_mx_linear_rows(MxLinearArgs p) {
 
 // A workgroup of WR x WC waves has 64 WC columns, whose whole records lie in
 // LDS from the start, and goes over tiles of 64 WR rows, whose records it
-// brings tile by tile; three workgroups a CU hide each other's waits (45,000
-// rows, two pairs of 100 by 256, plain stores: two with 80 KB each 14.4 us,
-// three 12.6; the next tile's rows arriving during this one's products, in a
-// second buffer, changed nothing).  In LDS a record is `slots` 16-byte pieces,
+// brings tile by tile; workgroups of a CU hide each other's waits (45,000 rows,
+// two pairs of 100 by 256: two a CU with 80 KB each 12.5 us, three 10.4).  With
+// fp32 and bf16 results the registers (138) leave room for three, with records
+// (177) for two.  In LDS a record is `slots` 16-byte pieces,
 // an odd number: sixteen rows' reads of one block fall on different banks.  (The
 // LDS serves half of such a sixteen with half of the next one's; pairs of blocks
 // exchanged in rows 4 - 11 took those conflicts out, and 10.1 us for 9.7.)
@@ -521,21 +521,23 @@ bool resident_fits(const MxLinearArgs& p) {
   return p.blocks < 64 && 64 * (WC + WR) * p.pairs * resident_slots(p.blocks) * 16 <= kResidentLds;
 }
 
-// Which kernel, by the workgroups that its tiles give (us, bf16 results):
+// Which kernel, by the workgroups that its tiles give (us, bf16 results; calls
+// below 7 us wait for the host, their figures are the kernel's own):
 //   - up to two workgroups a CU of 16 rows by 32 columns: k_mx_linear_rows (64
-//     x 4,096 x 1,024: 7.0, in 64 x 64 tiles 12.3; 300 x 1,024 x 256: 4.2 and
-//     6.4; but 1,000 x 256 x 1,024, 2,016 workgroups: 10.3 and 5.1);
+//     x 4,096 x 1,024: 7.0, in 64 x 64 tiles 12.2; 300 x 1,024 x 256: 4.2 and
+//     6.4; but 1,000 x 256 x 1,024, 2,016 workgroups: 9.7 and 7.1);
 //   - resident weights where they fit and there are more tiles than CUs
-//     (30,000 x 100 x 256: 8.0, tiles 10.7, 8.9 and 11.3 by size; 200,000 x 256
-//     x 256: 28.2, 50.2, 41.6, 41.5; 281 tiles of 18,000 x 100 x 256: 7.1, tiles
-//     8.8; 375 of 24,000 x 2 x 100 x 256: 9.5 and 12.8; 282 of 36,000 x 256 x 128:
-//     8.2 and 8.8; slower at most by 8%, 422 of 27,000 x 256 x 256: 9.2 and 8.6;
-//     but 250 of 16,000 x 256 x 256: 7.9 and 6.3);
+//     (30,000 x 100 x 256: 8.2, tiles of 256, 128 and 64 11.3, 8.8 and 11.2;
+//     200,000 x 256 x 256: 25.8, 38.6, 36.1, 46.4; 281 tiles of 18,000 x 100 x
+//     256: 7.4, 10.3, 7.7, 9.0; 375 of 24,000 x 2 x 100 x 256: 9.6, 13.2, 10.0,
+//     13.2; slower by 6% at most, 282 of 36,000 x 256 x 128: 8.2, 10.5, 7.9, 9.1,
+//     422 of 27,000 x 256 x 256: 9.2, 11.1, 8.7, 10.7; but 250 of 16,000 x 256 x
+//     256: 8.0, 10.2, 7.3, 7.0);
 //   - else 256 x 256 tiles if there are three for every four CUs (8,192 x 4,096
-//     x 4,096: 82, in 128 x 128 96, in 64 x 64 141; but 8,000 x 1,024 x 1,024,
-//     128 of them: 18.4, 14.4, 18.2);
-//   - 128 x 128 if there are three for two CUs (2,000 x 4,096 x 4,096: 28.9,
-//     in 64 x 64 46.5; but 1,000 x 256 x 4,096, 256 of them: 7.5 and 6.6);
+//     x 4,096: 85, in 128 x 128 100, in 64 x 64 141; but 8,000 x 1,024 x 1,024,
+//     128 of them: 18.2, 14.1, 17.9);
+//   - 128 x 128 if there are three for two CUs (2,000 x 4,096 x 4,096: 29.0,
+//     in 64 x 64 45.7; but 1,000 x 256 x 4,096, 256 of them: 7.6 and 7.0);
 //   - 64 x 64.
 template <int OUT>
 void dispatch(const MxLinearArgs& p, hipStream_t s) {
@@ -562,9 +564,9 @@ void dispatch(const MxLinearArgs& p, hipStream_t s) {
 
 hipError_t launch_mx_linear(const MxLinearArgs& p, int out, hipStream_t s) {
   // past the caches if large and written by whole 64-byte pieces: rows of such,
-  // or rows that a wave has whole (59,048 x 2 x 32 x 2,272 bf16: 69.4 us, plain
-  // 72.6; x 2,304 61.6, 68.1; 300,000 x 2 x 100 x 47 fp32 25.6, 29.4; but 2,273 168
-  // and 103, 200,000 x 256 x 240 bf16 39.0 and 35.4, 100,000 x 100 x 100 fp32 16.3
+  // or rows that a wave has whole (59,048 x 2 x 32 x 2,304 bf16: 59.1 us, plain
+  // 65.2; x 2,272 70.8, 70.4; 300,000 x 2 x 100 x 47 fp32 25.2, 30.9; but 2,273 170
+  // and 104, 200,000 x 256 x 240 bf16 39.1 and 33.4, 100,000 x 100 x 100 fp32 16.6
   // and 12.5)
   const int64_t row = p.d_out * (out == kMxOutBf16 ? 2 : 4);
   const bool stream = p.n_cap * row >= kStreamBytes && (row % 64 == 0 || p.d_out <= 64);

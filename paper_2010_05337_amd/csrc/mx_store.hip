@@ -175,9 +175,10 @@ __global__ __launch_bounds__(256) void k_mx_claim(const int32_t* ids, const int3
 // A lane writes 16 bytes of a row (E values), so that a group's stores are one
 // contiguous piece (346,000 rows of 100 fp32, plain stores: 55 us, 69 where four
 // lanes' 64 bytes lay 128 apart).  U rows of a group in flight, their ids asked
-// for together (one by one 47.7 us, so 43.0; U = 2 47.5, 8 45.1; with streaming
-// stores 33.0); every load unconditional from a clamped address (row 0 for a
-// group without a row or with an id outside the table).
+// for together (plain stores, one by one 47.7 us, so 43.0; U = 2 47.5, 8 45.1;
+// streaming stores, U = 2 31.7, 4 33.2, 8 33.9); every load unconditional from a
+// clamped address (row 0 for a group without a row or with an id outside the
+// table).
 template <typename T, int BITS, int G, int U, bool STREAM>
 __global__ __launch_bounds__(256) void k_mx_read(MxReadArgs a) {
   constexpr int E = 16 / sizeof(T), kBytes = E * BITS / 8;
