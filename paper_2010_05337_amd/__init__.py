@@ -796,7 +796,8 @@ def mx_mean(block, table: torch.Tensor, dim: int, bits: int, dtype: torch.dtype 
     """The mean of every destination's neighbours' rows, straight from a
     microscaled store (0 for a destination without any).  `block` is (indptr,
     ids): int32 row offsets and the neighbours' records, or a Blocks (block
-    0's destinations, at their capacity, and sampled vertices)."""
+    0's destinations, at their capacity, and sampled vertices).  A neighbour
+    outside the table is read as record 0 and not reported."""
     dev = _current_device(table, "table")
     table_rows, stride = _records(table, dim, bits, "table")
     if isinstance(block, Blocks):
