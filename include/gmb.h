@@ -598,6 +598,163 @@ int gmb_sage_backward_distill(const gmb_blocks* blocks, const void* x, const gmb
                               void* ws, size_t ws_bytes, float* table, int64_t num_nodes, float emb_lr,
                               void* stream);
 
+/* ---- dropout, norm and loss of a residual model ------------------------- */
+
+/* Rows of `dim` contiguous elements, row i at data + i * stride elements
+ * (stride >= dim; no alignment beyond the element's own). */
+typedef struct {
+  void* data;
+  int64_t stride;
+} gmb_rows;
+
+/* A dropout whose mask is never stored: it is drawn again wherever it is
+ * needed, in the backward for instance.  Which elements are dropped is a
+ * function of the seed, the row's key, the layer, the column and *step:
+ * Philox4x32-10 keyed by (lo32(seed), hi32(seed)) with counter (key, 2^31 +
+ * layer, column / 8, *step); columns 8 c .. 8 c + 7 take the low and high
+ * halves of its words x0 .. x3 in order, and an element is dropped where its
+ * 16 bits are below t = round(65536 p).  (The sampler's counters hold a layer
+ * below 2^31 in their second word: one seed serves both.)  Dropped elements
+ * become 0, whatever they hold; the others are multiplied by 65536 / (65536 -
+ * t) in fp32.
+ *   p      0 .. 1
+ *   layer  0 .. 2^31 - 1: masks of different layers are independent
+ *   step   device uint32 or NULL (0), read by the kernels: a captured graph
+ *          whose step moves draws another mask at every replay. */
+typedef struct {
+  uint64_t seed;
+  float p;
+  int32_t layer;
+  const uint32_t* step;
+} gmb_dropout;
+
+/* out[i, :] = [residual[i, :] +] dropout(x[i, :]) for i < n, where n = *n_dev
+ * clamped to n_cap, or n_cap when n_dev is NULL; rows at i >= n are not
+ * written.  Row i's key is ids[i] (a vertex: the same mask wherever it stands
+ * in a batch), or i when ids is NULL.  fp32 sums, rounded once to `dtype`.  The
+ * backward is the same call on the gradient (without residual).
+ *   x, residual, out  rows of `dtype`; residual may be NULL; out may be x or
+ *                     residual (the same address and stride), not overlap
+ *                     them otherwise
+ *   ids               device int32[n_cap] or NULL
+ *   dim               1 .. 65536; n_cap 0 .. 2^31 - 1 */
+int gmb_dropout_rows(const gmb_rows* x, const gmb_rows* residual, const gmb_dropout* drop, const int32_t* ids,
+                     const int32_t* n_dev, int64_t n_cap, int32_t dim, int32_t dtype, const gmb_rows* out,
+                     void* stream);
+
+/* The root-mean-square norm of a sum, for rows i < n as above:
+ *   r = [residual +] x, x dropped out first with `drop` (NULL: not),
+ *   y = weight r / sqrt(mean(r^2) + eps),
+ * with r rounded to `dtype` before it is normed (what `sum` holds is what y is
+ * the norm of, and what gmb_rms_norm_backward takes); statistics fp32.
+ *   weight  device fp32 [dim] or NULL (ones)
+ *   eps     > 0
+ *   sum     rows of `dtype` for r, or NULL; may be x or residual
+ *   format  0: out is rows of `dtype` (out may be x or residual if sum is
+ *           not); GMB_MXFP4 or GMB_MXFP8: out is records (a table of
+ *           gmb_mx_quantise: 16-byte aligned, its stride in bytes, a multiple
+ *           of 16), quantised from fp32. */
+int gmb_rms_norm(const gmb_rows* x, const gmb_rows* residual, const gmb_dropout* drop, const int32_t* ids,
+                 const int32_t* n_dev, int64_t n_cap, int32_t dim, int32_t dtype, const float* weight, float eps,
+                 const gmb_rows* sum, int32_t format, const gmb_rows* out, void* stream);
+
+/* Bytes of workspace gmb_rms_norm_backward needs for d_weight (0 for bad
+ * arguments). */
+size_t gmb_rms_norm_workspace_bytes(int64_t n_cap, int32_t dim);
+
+/* The gradients of gmb_rms_norm with format 0, for rows i < n as above:
+ * with s = 1 / sqrt(mean(r^2) + eps),
+ *   dr = carry + s (weight dy - r s^2 mean(weight dy r)),
+ * the gradient of the residual; that of x is dropout(dr); that of the weight
+ * the sum over the rows of dy r s, in a fixed order (no atomics).
+ *   dy, r        the gradient of y, and the sum (x itself if nothing was added)
+ *   carry        the gradient that reaches r from elsewhere, or NULL
+ *   d_residual   rows or NULL; may be dy, r or carry
+ *   dx           rows or NULL; the same, and not d_residual
+ *   d_weight     device fp32 [dim] or NULL (0 if there are no rows)
+ *   ws           >= gmb_rms_norm_workspace_bytes() bytes, 256-byte aligned
+ *                (NULL without d_weight). */
+int gmb_rms_norm_backward(const gmb_rows* dy, const gmb_rows* r, const gmb_rows* carry, const gmb_dropout* drop,
+                          const int32_t* ids, const int32_t* n_dev, int64_t n_cap, int32_t dim, int32_t dtype,
+                          const float* weight, float eps, const gmb_rows* d_residual, const gmb_rows* dx,
+                          float* d_weight, void* ws, size_t ws_bytes, void* stream);
+
+/* A linear head over many classes (every vertex may be one: W is the
+ * embedding table then): logits z = x W^T + bias.
+ *   x       device [rows, d] of `dtype` at x_stride elements (>= d)
+ *   w       device, element j of class c at c * w_row_stride + j *
+ *           w_col_stride elements of `dtype` (strides >= 0): rows [classes][d],
+ *           or the columns of a [d][classes] matrix
+ *   bias    device fp32 [classes] or NULL (-inf: a class that cannot be)
+ *   labels  device int32 [rows]; a row whose label is outside [0, classes)
+ *           has no loss and no gradient, whatever x holds there
+ *   rows 0 .. 2^22, d 1 .. 65536, classes 1 .. 2^27 */
+typedef struct {
+  const void* x;
+  int64_t x_stride;
+  const void* w;
+  int64_t w_row_stride, w_col_stride;
+  const float* bias;
+  const int32_t* labels;
+  int64_t rows;
+  int32_t d, classes, dtype, reserved;
+} gmb_linear_head;
+
+/* Its gradients, each NULL if it is not wanted, apart from the inputs:
+ *   dx    device [rows, d] of the head's dtype
+ *   dw    device [classes, d] of the head's dtype, or with `turned` [d, classes]
+ *   bias  device fp32 [classes] */
+typedef struct {
+  void* dx;
+  void* dw;
+  float* dbias;
+  int32_t turned, reserved;
+} gmb_linear_grads;
+
+/* Bytes of workspace gmb_linear_loss needs (0 for bad arguments); of the
+ * pointers of `grads` (NULL: the loss alone) only NULL or not counts, of w its
+ * alignment.  It grows with rows (d + classes / 16) and, with gradients, by 256
+ * MB at most (more from 262,144 rows on) and the sums that are split; the
+ * logits are never stored. */
+size_t gmb_linear_loss_workspace_bytes(const gmb_linear_head* head, const gmb_linear_grads* grads);
+
+/* The mean over the rows (those without a label count as 0) of -log
+ * softmax(z)_label, and its gradients.  A row whose logits are all -inf has
+ * neither.  x and W are finite; with a NaN or an infinity among them the loss
+ * is NaN, or the row of that x.  bf16: exact products, fp32 sums and statistics,
+ * softmax(z) - onehot rounded to bf16 before its products.  fp32: every operand
+ * is cut into two fp16 parts at a power-of-two scale (x by rows for the
+ * logits; W, and x for dw, as a whole), a product is three of the four part
+ * products; the error is of the order of an fp32 sum's beside the operand's
+ * largest value (elements below 2^-16 of it lose bits, below 2^-39 of it are
+ * lost; so are gradients of a logit below 2^-39).
+ * Nothing is added by atomics: the same bits every time.  The mean is summed in
+ * 64 bits.
+ *   loss  device fp32 scalar
+ *   ws    device workspace, 256-byte aligned. */
+int gmb_linear_loss(const gmb_linear_head* head, const gmb_linear_grads* grads, float* loss, void* ws,
+                    size_t ws_bytes, void* stream);
+
+/* ---- a model trained with dropout, from a gradient at its outputs -------- */
+
+/* gmb_sage_forward (feats NULL), or gmb_sage_forward_fused (feats the table, x
+ * its x_dst), with `drop` on every hidden output: layer l < L-1's rows, after
+ * the ReLU, are dropped out in place with layer drop->layer + l, keyed by their
+ * vertices.  (Without it: evaluation.) */
+int gmb_sage_forward_dropout(const gmb_blocks* blocks, void* x, const void* feats, int64_t num_nodes,
+                             const gmb_sage_weights* weights, const gmb_dropout* drop, float* logits, void* ws,
+                             size_t ws_bytes, uint32_t* status, void* stream);
+
+/* gmb_sage_backward (table NULL), or gmb_sage_backward_embedding, from the
+ * gradient at the model's outputs instead of a loss: d_logits device fp32
+ * [num_seeds, dims[L]] (a loss of the caller's own, or layers behind the
+ * model).  `drop`: as in the forward, or NULL.  If a bounded wait on the device
+ * runs out, the first entry of d_bias[0] is NaN. */
+int gmb_sage_backward_from(const gmb_blocks* blocks, const void* x, const gmb_sage_weights* weights,
+                           const float* d_logits, const gmb_dropout* drop, const void* fwd_ws, size_t fwd_ws_bytes,
+                           const gmb_sage_grads* grads, void* ws, size_t ws_bytes, float* table, int64_t num_nodes,
+                           float emb_lr, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -18,6 +18,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -40,6 +41,8 @@ EXPORTS = (
     "gmb_mx_row_bytes", "gmb_mx_quantise", "gmb_mx_gather", "gmb_mx_mean", "gmb_mx_linear",
     "gmb_mx_forward_workspace_bytes", "gmb_mx_forward_offset", "gmb_sage_forward_mx",
     "gmb_distill_workspace_bytes", "gmb_distill_loss", "gmb_sage_backward_distill",
+    "gmb_dropout_rows", "gmb_rms_norm", "gmb_rms_norm_workspace_bytes", "gmb_rms_norm_backward",
+    "gmb_linear_loss_workspace_bytes", "gmb_linear_loss", "gmb_sage_forward_dropout", "gmb_sage_backward_from",
 )
 
 
@@ -98,6 +101,26 @@ class MxWeightsStruct(ctypes.Structure):
 class TeacherStruct(ctypes.Structure):
     _fields_ = [("logits", ctypes.c_void_p), ("classes", ctypes.c_void_p), ("top", ctypes.c_int32),
                 ("alpha", ctypes.c_float), ("temperature", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class RowsStruct(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride", ctypes.c_int64)]
+
+
+class DropoutStruct(ctypes.Structure):
+    _fields_ = [("seed", ctypes.c_uint64), ("p", ctypes.c_float), ("layer", ctypes.c_int32), ("step", ctypes.c_void_p)]
+
+
+class LinearHeadStruct(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("x_stride", ctypes.c_int64), ("w", ctypes.c_void_p),
+                ("w_row_stride", ctypes.c_int64), ("w_col_stride", ctypes.c_int64), ("bias", ctypes.c_void_p),
+                ("labels", ctypes.c_void_p), ("rows", ctypes.c_int64), ("d", ctypes.c_int32),
+                ("classes", ctypes.c_int32), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class LinearGradsStruct(ctypes.Structure):
+    _fields_ = [("dx", ctypes.c_void_p), ("dw", ctypes.c_void_p), ("dbias", ctypes.c_void_p),
+                ("turned", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 _lib = None
@@ -195,6 +218,27 @@ def lib() -> ctypes.CDLL:
         L.gmb_sage_backward_distill.argtypes = [ctypes.POINTER(BlocksStruct), vp, ctypes.POINTER(WeightsStruct), vp,
                                                 ctypes.POINTER(TeacherStruct), vp, vp, sz,
                                                 ctypes.POINTER(GradsStruct), vp, vp, sz, vp, i64, f32, vp]
+        rows, drop = ctypes.POINTER(RowsStruct), ctypes.POINTER(DropoutStruct)
+        L.gmb_dropout_rows.restype = ctypes.c_int
+        L.gmb_dropout_rows.argtypes = [rows, rows, drop, vp, vp, i64, i32, i32, rows, vp]
+        L.gmb_rms_norm.restype = ctypes.c_int
+        L.gmb_rms_norm.argtypes = [rows, rows, drop, vp, vp, i64, i32, i32, vp, f32, rows, i32, rows, vp]
+        L.gmb_rms_norm_workspace_bytes.restype = sz
+        L.gmb_rms_norm_workspace_bytes.argtypes = [i64, i32]
+        L.gmb_rms_norm_backward.restype = ctypes.c_int
+        L.gmb_rms_norm_backward.argtypes = [rows, rows, rows, drop, vp, vp, i64, i32, i32, vp, f32, rows, rows, vp, vp,
+                                            sz, vp]
+        head, grads = ctypes.POINTER(LinearHeadStruct), ctypes.POINTER(LinearGradsStruct)
+        L.gmb_linear_loss_workspace_bytes.restype = sz
+        L.gmb_linear_loss_workspace_bytes.argtypes = [head, grads]
+        L.gmb_linear_loss.restype = ctypes.c_int
+        L.gmb_linear_loss.argtypes = [head, grads, vp, vp, sz, vp]
+        L.gmb_sage_forward_dropout.restype = ctypes.c_int
+        L.gmb_sage_forward_dropout.argtypes = [ctypes.POINTER(BlocksStruct), vp, vp, i64,
+                                               ctypes.POINTER(WeightsStruct), drop, vp, vp, sz, vp, vp]
+        L.gmb_sage_backward_from.restype = ctypes.c_int
+        L.gmb_sage_backward_from.argtypes = [ctypes.POINTER(BlocksStruct), vp, ctypes.POINTER(WeightsStruct), vp, drop,
+                                             vp, sz, ctypes.POINTER(GradsStruct), vp, sz, vp, i64, f32, vp]
         _lib = L
     return _lib
 
@@ -463,10 +507,12 @@ def _with_forward_workspace(call, blocks: Blocks, weights: SageWeights, workspac
 
 def sage_forward(blocks: Blocks, feats: torch.Tensor, weights: SageWeights,
                  workspace: torch.Tensor | None = None, logits: torch.Tensor | None = None,
-                 return_hidden: bool = False):
+                 return_hidden: bool = False, dropout: "Dropout | None" = None):
     """GraphSAGE-mean forward over the blocks; feats holds the gathered input
     rows of block 0's sources.  Returns logits [num_seeds, C] float32 (and,
-    with return_hidden, the hidden activations cut to their row counts)."""
+    with return_hidden, the hidden activations cut to their row counts).
+    `dropout` drops out the hidden activations, layer l's with layer
+    dropout.layer + l, keyed by vertex (train with sage_backward_from)."""
     _require_cuda(feats, "feats")
     if feats.dtype != weights.torch_dtype:
         raise TypeError("feats and weights must have the same dtype")
@@ -478,6 +524,10 @@ def sage_forward(blocks: Blocks, feats: torch.Tensor, weights: SageWeights,
     L, stream = lib(), _stream_handle()
 
     def call(ws):
+        if dropout is not None:
+            return L.gmb_sage_forward_dropout(ctypes.byref(blocks.struct), feats.data_ptr(), None, 0,
+                                              ctypes.byref(weights.struct), dropout.struct, logits.data_ptr(),
+                                              ws.data_ptr(), ws.numel(), None, stream)
         return L.gmb_sage_forward(ctypes.byref(blocks.struct), feats.data_ptr(), ctypes.byref(weights.struct),
                                   logits.data_ptr(), ws.data_ptr(), ws.numel(), stream)
 
@@ -508,12 +558,14 @@ def dst_capacity(blocks: Blocks) -> int:
 
 def sage_forward_fused(blocks: Blocks, feats: torch.Tensor, weights: SageWeights,
                        x_dst: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
-                       logits: torch.Tensor | None = None, return_hidden: bool = False):
+                       logits: torch.Tensor | None = None, return_hidden: bool = False,
+                       dropout: "Dropout | None" = None):
     """The forward with the feature pull folded into layer 0: `feats` is the
     whole feature table [num_nodes, dims[0]]; block 0's destination rows are
     gathered into x_dst ([dst capacity, dims[0]]), the layer-0 mean reads
     the table directly.  Returns (logits, x_dst) (and the hidden
-    activations with return_hidden); x_dst serves as `x` of sage_backward."""
+    activations with return_hidden); x_dst serves as `x` of sage_backward.
+    `dropout` as in sage_forward."""
     _require_cuda(feats, "feats")
     if feats.dtype != weights.torch_dtype:
         raise TypeError("feats and weights must have the same dtype")
@@ -530,6 +582,10 @@ def sage_forward_fused(blocks: Blocks, feats: torch.Tensor, weights: SageWeights
     L, stream, status = lib(), _stream_handle(), blocks.csr.status_word
 
     def call(ws):
+        if dropout is not None:
+            return L.gmb_sage_forward_dropout(ctypes.byref(blocks.struct), x_dst.data_ptr(), feats.data_ptr(),
+                                              feats.shape[0], ctypes.byref(weights.struct), dropout.struct,
+                                              logits.data_ptr(), ws.data_ptr(), ws.numel(), status, stream)
         return L.gmb_sage_forward_fused(ctypes.byref(blocks.struct), feats.data_ptr(), feats.shape[0],
                                         x_dst.data_ptr(), ctypes.byref(weights.struct), logits.data_ptr(),
                                         ws.data_ptr(), ws.numel(), status, stream)
@@ -619,6 +675,43 @@ def sage_backward(blocks: Blocks, feats: torch.Tensor, weights: SageWeights, log
         _check(lib().gmb_sage_backward_embedding(*common, ctypes.c_void_p(embedding.data_ptr()),
                                                  embedding.shape[0], float(emb_lr), _stream_handle()))
     return grads, loss
+
+
+def sage_backward_from(blocks: Blocks, feats: torch.Tensor, weights: SageWeights, d_logits: torch.Tensor,
+                       fwd_workspace: torch.Tensor, grads: SageGrads | None = None,
+                       workspace: torch.Tensor | None = None, embedding: torch.Tensor | None = None,
+                       emb_lr: float = 0.0, dropout: "Dropout | None" = None) -> SageGrads:
+    """The backward of sage_forward (or its fused form) from the gradient at
+    the model's outputs, float32 [num_seeds, C]: of a loss of your own or of
+    layers behind the model.  `dropout` is the forward's; the others are
+    sage_backward's."""
+    dev = _current_device(d_logits, "d_logits")
+    if d_logits.dtype is not torch.float32 or d_logits.dim() != 2 or not d_logits.is_contiguous() \
+            or d_logits.shape[0] < blocks.num_seeds or d_logits.shape[1] != weights.dims[-1]:
+        raise ValueError("d_logits must be a contiguous float32 [num_seeds, C] tensor")
+    _same_device(feats, dev, "feats")
+    table = (None, 0, 0.0)
+    if embedding is not None:
+        _same_device(embedding, dev, "embedding")
+        if embedding.dtype != torch.float32 or embedding.dim() != 2 or embedding.shape[1] != weights.dims[0] \
+                or not embedding.is_contiguous():
+            raise ValueError("embedding must be a contiguous float32 [num_nodes, dims[0]] tensor")
+        need = backward_embedding_workspace_bytes(blocks, weights)
+        table = (embedding.data_ptr(), embedding.shape[0], float(emb_lr))
+    else:
+        need = backward_workspace_bytes(blocks, weights)
+    if need == 0:
+        _check(-1)
+    if workspace is None or workspace.numel() < need or workspace.data_ptr() % 256:
+        _, workspace = _aligned_bytes(need, feats.device)
+    if grads is None:
+        grads = SageGrads(weights)
+    _check(lib().gmb_sage_backward_from(ctypes.byref(blocks.struct), feats.data_ptr(), ctypes.byref(weights.struct),
+                                        d_logits.data_ptr() or feats.data_ptr(),
+                                        None if dropout is None else dropout.struct, fwd_workspace.data_ptr(),
+                                        fwd_workspace.numel(), ctypes.byref(grads.struct), workspace.data_ptr(),
+                                        workspace.numel(), *table, _stream_handle()))
+    return grads
 
 
 def sgd_update(weights: SageWeights, grads: SageGrads, lr: float):
@@ -1027,3 +1120,258 @@ def distill_loss(logits: torch.Tensor, teacher_logits: torch.Tensor, teacher_cla
     if code:
         _check(code)
     return loss, grad
+
+
+# ---------------------------------------------------------------- dropout, norm and loss of a residual model
+
+class Dropout:
+    """A dropout of probability p whose mask is never stored: which elements
+    are dropped is a function of `seed`, the row's key, `layer`, the column and
+    `step` (gmb.h), so that the backward draws it again.  `step` is a device
+    int32 tensor of one element (or None: 0) that the kernels read: moved
+    between replays, it gives a captured step other masks."""
+
+    def __init__(self, p: float, seed: int, layer: int = 0, step: torch.Tensor | None = None):
+        if not 0.0 <= p <= 1.0:
+            raise ValueError("p must lie in 0 .. 1")
+        if not 0 <= layer < 1 << 31:
+            raise ValueError("layer must lie in 0 .. 2^31 - 1")
+        if step is not None:
+            _current_device(step, "step")
+            if step.dtype is not torch.int32 or step.numel() != 1:
+                raise TypeError("step must be an int32 tensor of one element")
+        self.p, self.seed, self.layer, self.step = p, seed, layer, step
+        self.struct = DropoutStruct(seed & 0xFFFFFFFFFFFFFFFF, p, layer, None if step is None else step.data_ptr())
+
+
+def _row_struct(t, rows: int, dim: int, dtype, dev: int, name: str) -> RowsStruct:
+    """A [rows, dim] tensor of `dtype` with contiguous rows at any stride."""
+    _same_device(t, dev, name)
+    if t.dim() != 2 or t.shape[1] != dim or t.shape[0] != rows or t.dtype is not dtype:
+        raise ValueError(f"{name} must be a [{rows}, {dim}] {dtype} tensor")
+    stride, inner = t.stride()
+    if (inner != 1 and dim > 1) or (stride < dim and rows > 1):
+        raise ValueError(f"{name} must have contiguous rows that do not overlap")
+    return RowsStruct(t.data_ptr(), stride if rows > 1 else dim)
+
+
+def _row_input(x, name: str):
+    """(device, dtype code, rows, dim, struct) of the tensor that the others of a call go by."""
+    dev = _current_device(x, name)
+    if x.dim() != 2:
+        raise ValueError(f"{name} must be [rows, dim]")
+    code = _dtype_code(x.dtype)
+    rows, dim = x.shape
+    return dev, code, rows, dim, _row_struct(x, rows, dim, x.dtype, dev, name)
+
+
+def _drop_struct(drop, dev: int):
+    if not isinstance(drop, Dropout):
+        raise TypeError("dropout must be a Dropout")
+    if drop.step is not None:
+        _same_device(drop.step, dev, "the dropout's step")
+    return drop.struct
+
+
+def _row_keys(ids, count, rows: int, dev: int):
+    """The pointers of the rows' keys and of their number on the device."""
+    if ids is not None and _int32(ids, dev, "ids") != rows:
+        raise ValueError("ids must have one entry per row")
+    if count is not None and _int32(count, dev, "count") != 1:
+        raise ValueError("count must have one element")
+    return None if ids is None else ids.data_ptr(), None if count is None else count.data_ptr()
+
+
+def dropout(x: torch.Tensor, drop: Dropout, ids: torch.Tensor | None = None, residual: torch.Tensor | None = None,
+            out: torch.Tensor | None = None, count: torch.Tensor | None = None) -> torch.Tensor:
+    """[residual +] x with elements dropped and the others scaled, float32 or
+    bfloat16 [rows, dim] with contiguous rows at any stride.  Row i's key is
+    ids[i] (int32: a vertex has the same mask wherever it stands), or i.  The
+    backward is the same call on the gradient.  With `count` (device int32 of
+    one element) only the first rows are read and written.  `out` may be x or
+    residual."""
+    dev, code, rows, dim, a = _row_input(x, "x")
+    d = _drop_struct(drop, dev)
+    keys, n_dev = _row_keys(ids, count, rows, dev)
+    b = None if residual is None else _row_struct(residual, rows, dim, x.dtype, dev, "residual")
+    if out is None:
+        out = x.new_empty((rows, dim))
+    o = _row_struct(out, rows, dim, x.dtype, dev, "out")
+    if rows:
+        code = lib().gmb_dropout_rows(a, b, d, keys, n_dev, rows, dim, code, o, _stream_handle())
+        if code:
+            _check(code)
+    return out
+
+
+def _norm_weight(weight, dim: int, dev: int):
+    if weight is None:
+        return None
+    _same_device(weight, dev, "weight")
+    if weight.dtype is not torch.float32 or weight.dim() != 1 or weight.shape[0] != dim or not weight.is_contiguous():
+        raise ValueError("weight must be a contiguous float32 [dim] tensor")
+    return weight.data_ptr()
+
+
+def rms_norm(x: torch.Tensor, weight: torch.Tensor | None, eps: float = 1e-6, residual: torch.Tensor | None = None,
+             dropout: Dropout | None = None, bits: int | None = None, ids: torch.Tensor | None = None,
+             out: torch.Tensor | None = None, sum_out: torch.Tensor | None = None,
+             count: torch.Tensor | None = None):
+    """The root-mean-square norm of r = [residual +] x (x dropped out first with
+    `dropout`, rows keyed as in gmb.dropout): returns (y, r), y = weight r /
+    sqrt(mean(r^2) + eps).  y has x's dtype, or, with `bits` (MXFP4 or MXFP8),
+    is a table of records like mx_quantise's.  r is rounded to x's dtype before
+    it is normed; it is x itself if nothing is added or dropped.  `count` as in
+    gmb.dropout; `sum_out` may be x or residual."""
+    dev, code, rows, dim, a = _row_input(x, "x")
+    keys, n_dev = _row_keys(ids, count, rows, dev)
+    b = None if residual is None else _row_struct(residual, rows, dim, x.dtype, dev, "residual")
+    drop = None if dropout is None else _drop_struct(dropout, dev)
+    g = _norm_weight(weight, dim, dev)
+    r, total = x, None
+    if sum_out is not None or residual is not None or dropout is not None:
+        r = x.new_empty((rows, dim)) if sum_out is None else sum_out
+        total = _row_struct(r, rows, dim, x.dtype, dev, "sum_out")
+    if bits is None:
+        if out is None:
+            out = x.new_empty((rows, dim))
+        o = _row_struct(out, rows, dim, x.dtype, dev, "out")
+    else:
+        if out is None:
+            out = x.new_empty((rows, mx_row_bytes(dim, bits)), dtype=torch.uint8)
+        else:
+            _same_device(out, dev, "out")
+        have, stride = _records(out, dim, bits, "out")
+        if have < rows:
+            raise ValueError("out has fewer rows than x")
+        o = RowsStruct(out.data_ptr(), stride)
+    if rows:
+        code = lib().gmb_rms_norm(a, b, drop, keys, n_dev, rows, dim, code, g, eps, total, bits or 0, o,
+                                  _stream_handle())
+        if code:
+            _check(code)
+    return out, r
+
+
+class NormGrads(NamedTuple):
+    """Gradients of rms_norm's x, residual and weight (without dropout x's and
+    the residual's are one tensor)."""
+    x: torch.Tensor
+    residual: torch.Tensor
+    weight: torch.Tensor | None
+
+
+def _workspace(workspace, need: int, like: torch.Tensor, dev: int) -> torch.Tensor:
+    """`workspace` if it holds `need` bytes at an aligned address, or a new one."""
+    if workspace is not None:
+        _same_device(workspace, dev, "workspace")
+        if workspace.dtype is torch.uint8 and workspace.numel() >= need and workspace.data_ptr() % 256 == 0:
+            return workspace
+    workspace = like.new_empty(need, dtype=torch.uint8)
+    if workspace.data_ptr() % 256:   # (torch's own blocks are aligned)
+        _, workspace = _aligned_bytes(need, like.device)
+    return workspace
+
+
+def rms_norm_backward(dy: torch.Tensor, r: torch.Tensor, weight: torch.Tensor | None, eps: float = 1e-6,
+                      carry: torch.Tensor | None = None, dropout: Dropout | None = None,
+                      ids: torch.Tensor | None = None, count: torch.Tensor | None = None,
+                      workspace: torch.Tensor | None = None) -> NormGrads:
+    """The gradients of rms_norm from dy, that of y, and r, the sum that it
+    returned (both of x's dtype).  `carry` is the gradient that reaches r from
+    elsewhere (the residual stream); `dropout`, `ids` and `count` are the
+    forward's.  The weight's gradient is float32 (None without a weight), summed
+    in a fixed order."""
+    dev, code, rows, dim, a = _row_input(r, "r")
+    b = _row_struct(dy, rows, dim, r.dtype, dev, "dy")
+    keys, n_dev = _row_keys(ids, count, rows, dev)
+    c = None if carry is None else _row_struct(carry, rows, dim, r.dtype, dev, "carry")
+    drop = None if dropout is None else _drop_struct(dropout, dev)
+    g = _norm_weight(weight, dim, dev)
+    d_residual = r.new_empty((rows, dim))
+    to = RowsStruct(d_residual.data_ptr(), dim)
+    dx, to_x = d_residual, None
+    if drop is not None:
+        dx = r.new_empty((rows, dim))
+        to_x = RowsStruct(dx.data_ptr(), dim)
+    dw = dw_ptr = ws = None
+    need = 0
+    if weight is not None:
+        dw = torch.empty_like(weight)
+        dw_ptr = dw.data_ptr()
+        need = lib().gmb_rms_norm_workspace_bytes(rows, dim)
+        if need == 0:
+            _check(-1)
+        workspace = _workspace(workspace, need, r, dev)
+        ws, need = workspace.data_ptr(), workspace.numel()
+    code = lib().gmb_rms_norm_backward(b, a, c, drop, keys, n_dev, rows, dim, code, g, eps, to, to_x, dw_ptr, ws, need,
+                                       _stream_handle())
+    if code:
+        _check(code)
+    return NormGrads(dx, d_residual, dw)
+
+
+class LinearGrads(NamedTuple):
+    """Gradients of linear_loss (None where they were not asked for)."""
+    x: torch.Tensor | None
+    w: torch.Tensor | None
+    bias: torch.Tensor | None
+
+
+def linear_loss(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, bias: torch.Tensor | None = None,
+                grad=True, loss: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """The mean over the rows of the softmax cross-entropy of x W^T + bias
+    against `labels` (int32; a row whose label is no class, -1 for instance,
+    counts as 0), and its gradients, without the logits ever being stored.  x
+    is float32 or bfloat16 [rows, d] with contiguous rows, w [classes, d] of the
+    same dtype with any non-negative strides: an embedding table, or matrix.t()
+    of a [d, classes] matrix; bias float32 [classes].  Returns (loss,
+    LinearGrads): the loss float32 of one element, the gradients of x and w of
+    their dtype (w's laid out like w), the bias's float32.  `grad` is True,
+    False, or the names of the gradients wanted ("x", "w", "bias")."""
+    dev, code, rows, d, a = _row_input(x, "x")
+    _same_device(w, dev, "w")
+    if w.dim() != 2 or w.shape[1] != d or w.dtype is not x.dtype:
+        raise ValueError(f"w must be a [classes, {d}] {x.dtype} tensor")
+    classes = w.shape[0]
+    if _int32(labels, dev, "labels") != rows:
+        raise ValueError("labels must have one entry per row")
+    if bias is not None:
+        _same_device(bias, dev, "bias")
+        if bias.dtype is not torch.float32 or bias.dim() != 1 or bias.shape[0] != classes or not bias.is_contiguous():
+            raise ValueError("bias must be a contiguous float32 [classes] tensor")
+    if grad is True or grad is False:
+        want_x = want_w = want_bias = grad
+    else:
+        grad = set(grad)
+        if grad - {"x", "w", "bias"}:
+            raise ValueError("grad names x, w and bias")
+        want_x, want_w, want_bias = "x" in grad, "w" in grad, "bias" in grad
+    row_stride, col_stride = w.stride()
+    turned = row_stride == 1 and col_stride >= classes and d > 1 and classes > 1
+    dx = x.new_empty((rows, d)) if want_x else None
+    dw = None
+    if want_w:
+        dw = w.new_empty((d, classes)).t() if turned else w.new_empty((classes, d))
+    db = bias.new_empty(classes) if want_bias and bias is not None else None
+    if loss is None:
+        loss = x.new_empty(1, dtype=torch.float32)
+    else:
+        _same_device(loss, dev, "loss")
+        if loss.dtype != torch.float32 or loss.numel() != 1:
+            raise ValueError("loss must be a 1-element float32 tensor")
+    head = LinearHeadStruct(a.data, a.stride, w.data_ptr(), row_stride, col_stride,
+                            None if bias is None else bias.data_ptr(), labels.data_ptr(), rows, d, classes, code, 0)
+    grads = None
+    if dx is not None or dw is not None or db is not None:
+        grads = LinearGradsStruct(None if dx is None else dx.data_ptr(), None if dw is None else dw.data_ptr(),
+                                  None if db is None else db.data_ptr(), 1 if turned else 0, 0)
+    L = lib()
+    need = L.gmb_linear_loss_workspace_bytes(head, grads)
+    if need == 0:
+        _check(-1)
+    workspace = _workspace(workspace, need, x, dev)
+    code = L.gmb_linear_loss(head, grads, loss.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_handle())
+    if code:
+        _check(code)
+    return loss, LinearGrads(dx, dw, db)

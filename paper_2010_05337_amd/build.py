@@ -15,7 +15,7 @@ CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libgmb.so")
 SOURCES = ["api.hip", "sample.hip", "gather.hip", "sage.hip", "sage_bwd.hip", "mx_store.hip", "mx_linear.hip", "distill.hip",
-           "api_mx.hip"]
+           "api_mx.hip", "rows.hip", "linear_loss.hip", "api_head.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",

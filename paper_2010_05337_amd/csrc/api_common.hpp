@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "gmb.h"
+#include "head_kernels.hpp"
 
 namespace gmb {
 
@@ -31,5 +32,9 @@ int abi_backward_from(const LossLaunch& how, const gmb_blocks* blocks, const voi
                       const gmb_sage_weights* weights, const float* logits, const void* fwd_ws, size_t fwd_ws_bytes,
                       const gmb_sage_grads* grads, float* loss, void* ws, size_t ws_bytes, float* table,
                       int64_t num_nodes, float emb_lr, void* stream);
+
+// A dropout: refused, or as the kernels take it (NULL: nothing is dropped).
+int abi_check_dropout(const gmb_dropout* d);
+DropArgs abi_drop_args(const gmb_dropout* d, const int32_t* ids);
 
 }  // namespace gmb

@@ -1,0 +1,527 @@
+// Row operators of a residual model on gfx950: dropout whose mask is drawn
+// again wherever it is needed, and the root-mean-square norm of a sum with
+// its backward.
+//
+// A row is cut into pieces of eight columns, which share one Philox block
+// (eight times 16 bits).  A row belongs to LANES neighbouring threads, lane o
+// has the pieces o, o + LANES, ...
+#include "head_kernels.hpp"
+#include "mx.hpp"
+#include "mx_kernels.hpp"
+#include "philox.hpp"
+
+#include <type_traits>
+
+namespace gmb {
+
+namespace {
+
+constexpr int kPiece = 8;           // columns
+
+__device__ __forceinline__ int64_t count_rows(const int32_t* n_dev, int64_t n_cap) {
+  if (!n_dev) return n_cap;
+  const int64_t m = load_size(n_dev);
+  return m < 0 ? 0 : (m < n_cap ? m : n_cap);
+}
+
+// Piece `o` of a row of `dim` columns; columns past dim are 0.
+template <typename T>
+__device__ __forceinline__ void load_piece(const void* data, int64_t at, int o, int dim, float (&v)[kPiece]) {
+  const T* p = static_cast<const T*>(data) + at + o * kPiece;
+  const int left = dim - o * kPiece;
+  if constexpr (sizeof(T) == 4) {
+    if (left >= kPiece) {
+      float w[kPiece];
+      mx_get<16>(w, p);
+      mx_get<16>(w + 4, p + 4);
+#pragma unroll
+      for (int i = 0; i < kPiece; ++i) v[i] = w[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPiece; ++i) v[i] = i < left ? p[i] : 0.f;
+    }
+  } else {
+    if (left >= kPiece) {
+      uint32_t w[4];
+      mx_get<16>(w, p);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPiece; ++i) v[i] = i < left ? bf16_to_f32(p[i]) : 0.f;
+    }
+  }
+}
+
+// What a value is in T, as fp32.
+template <typename T>
+__device__ __forceinline__ void round_piece(float (&v)[kPiece]) {
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int i = 0; i < kPiece / 2; ++i) {
+      const uint32_t w = mx_bf16x2_bits(v[2 * i], v[2 * i + 1]);
+      v[2 * i] = __uint_as_float(w << 16);
+      v[2 * i + 1] = __uint_as_float(w & 0xFFFF0000u);
+    }
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void store_piece(void* data, int64_t at, int o, int dim, const float (&v)[kPiece]) {
+  T* p = static_cast<T*>(data) + at + o * kPiece;
+  const int left = dim - o * kPiece;
+  if constexpr (sizeof(T) == 4) {
+    if (left >= kPiece) {
+      mx_put<16, false>(p, v);
+      mx_put<16, false>(p + 4, v + 4);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPiece; ++i)
+        if (i < left) p[i] = v[i];
+    }
+  } else {
+    mx_store<false>(p, v, left);
+  }
+}
+
+// Dropped elements become 0, whatever they hold; the others are scaled.
+__device__ __forceinline__ void drop_piece(const DropArgs& d, uint32_t step, uint32_t key, int o, float (&v)[kPiece]) {
+  // (the sampler's counters have a layer below 2^31 there)
+  const Philox4 x = philox4x32_10(key, 0x80000000u | d.layer, static_cast<uint32_t>(o), step, d.k0, d.k1);
+#pragma unroll
+  for (int i = 0; i < kPiece; ++i) {
+    const uint32_t u = (x.w[i / 2] >> (16 * (i & 1))) & 0xFFFFu;
+    v[i] = u < d.below ? 0.f : v[i] * d.scale;
+  }
+}
+__device__ __forceinline__ uint32_t row_key(const DropArgs& d, int64_t row) {
+  return static_cast<uint32_t>(d.ids ? d.ids[row] : static_cast<int32_t>(row));
+}
+
+// ---- dropout --------------------------------------------------------------
+
+template <typename T, int LANES>
+__global__ __launch_bounds__(256) void k_dropout(DropoutArgs p) {
+  constexpr int ROWS = 256 / LANES;
+  const int64_t n = count_rows(p.n_dev, p.n_cap);
+  const int lane = threadIdx.x % LANES, pieces = (p.dim + kPiece - 1) / kPiece;
+  const uint32_t step = p.drop.step ? *p.drop.step : 0u;
+  for (int64_t row = static_cast<int64_t>(blockIdx.x) * ROWS + threadIdx.x / LANES; row < n;
+       row += static_cast<int64_t>(gridDim.x) * ROWS) {
+    const uint32_t key = row_key(p.drop, row);
+    for (int o = lane; o < pieces; o += LANES) {
+      float v[kPiece];
+      load_piece<T>(p.x.data, row * p.x.stride, o, p.dim, v);
+      if (p.drop.below) drop_piece(p.drop, step, key, o, v);
+      if (p.residual.data) {
+        float r[kPiece];
+        load_piece<T>(p.residual.data, row * p.residual.stride, o, p.dim, r);
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i) v[i] += r[i];
+      }
+      store_piece<T>(p.out.data, row * p.out.stride, o, p.dim, v);
+    }
+  }
+}
+
+// ---- norm -----------------------------------------------------------------
+
+// The sum of a value over the LANES threads of a row (every one gets it).
+// Past a wave the waves' sums meet in LDS, in a fixed order.
+template <int LANES, int N>
+__device__ __forceinline__ void row_sum(float (&v)[N], float* lds) {
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+#pragma unroll
+    for (int o = 1; o < (LANES < 64 ? LANES : 64); o <<= 1) v[k] += __shfl_xor(v[k], o, 64);
+  if constexpr (LANES > 64) {
+    constexpr int WAVES = LANES / 64;
+    __syncthreads();                // the last row's reads
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) lds[(threadIdx.x >> 6) * N + k] = v[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      float s = 0.f;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) s += lds[w * N + k];
+      v[k] = s;
+    }
+  }
+}
+
+// rsqrt of the mean square: 1 / sqrt is rounded to within an ulp or two; one
+// step of Newton's from v_rsq_f32's result.
+__device__ __forceinline__ float inverse_root(float x) {
+  const float y = __builtin_amdgcn_rsqf(x);
+  const float e = fmaf(-x * y, y, 1.f);
+  return x < 3.0e38f ? fmaf(0.5f * y, e, y) : y;
+}
+
+// Block (LANES > 256: LANES) threads; OC pieces of the row a thread.
+template <int LANES>
+struct NormBlock {
+  static constexpr int kThreads = LANES > 256 ? LANES : 256;
+  static constexpr int kRows = kThreads / LANES;
+};
+
+// Piece `o` of the sum, as it is stored.
+template <typename T>
+__device__ __forceinline__ void load_sum(const NormArgs& p, int64_t row, int o, uint32_t step, uint32_t key,
+                                         float (&v)[kPiece]) {
+  load_piece<T>(p.x.data, row * p.x.stride, o, p.dim, v);
+  if (p.drop.below) drop_piece(p.drop, step, key, o, v);
+  if (p.residual.data) {
+    float r[kPiece];
+    load_piece<T>(p.residual.data, row * p.residual.stride, o, p.dim, r);
+#pragma unroll
+    for (int i = 0; i < kPiece; ++i) v[i] += r[i];
+  }
+  round_piece<T>(v);
+}
+
+// Piece `o` of the norm from the sum's; every lane takes part.
+template <typename T, int BITS>
+__device__ __forceinline__ void store_norm(const NormArgs& p, bool in, int64_t row, int o, int pieces, float inv,
+                                           float (&v)[kPiece]) {
+  if (in && o < pieces) {
+    float g[kPiece];
+    if (p.weight) {
+      load_piece<float>(p.weight, 0, o, p.dim, g);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPiece; ++i) g[i] = 1.f;
+    }
+#pragma unroll
+    for (int i = 0; i < kPiece; ++i) v[i] = v[i] * inv * g[i];
+    if constexpr (BITS == 0) store_piece<T>(p.out.data, row * p.out.stride, o, p.dim, v);
+  }
+  if constexpr (BITS != 0) {
+    // four neighbouring lanes have a block of 32 columns
+    const uint32_t code = mx_scale_code<BITS>(mx_lanes_max<4>(mx_top(v)));
+    const int blocks = (p.dim + kMxBlock - 1) / kMxBlock, block = o / 4;
+    if (in && block < blocks) {
+      uint32_t w[BITS / 4];
+      mx_pack<BITS>(v, code, w);
+      uint8_t* rec = static_cast<uint8_t*>(p.out.data) + row * p.out.stride;
+      __builtin_memcpy(rec + o * BITS, w, BITS);
+      if (o % 4 == 0) rec[blocks * 4 * BITS + block] = static_cast<uint8_t>(code);
+      if (block == blocks - 1)
+        for (int b = blocks * (4 * BITS + 1) + o % 4; b < p.record; b += 4) rec[b] = 0;
+    }
+  }
+}
+
+// HELD: the row stays in registers between its sum and its norm; else it is
+// read again (from the stored sum where there is one).
+template <typename T, int LANES, int OC, bool HELD, int BITS>
+__global__ __launch_bounds__(NormBlock<LANES>::kThreads) void k_rms_norm(NormArgs p) {
+  constexpr int ROWS = NormBlock<LANES>::kRows;
+  __shared__ float lds[LANES > 64 ? LANES / 64 : 1];
+  const int64_t n = count_rows(p.n_dev, p.n_cap);
+  const int lane = threadIdx.x % LANES, pieces = (p.dim + kPiece - 1) / kPiece;
+  const uint32_t step = p.drop.step ? *p.drop.step : 0u;
+  const float by = 1.f / static_cast<float>(p.dim);
+  // (the loop's bound is the workgroup's: all its threads meet at row_sum's barriers)
+  for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * ROWS; row0 < n;
+       row0 += static_cast<int64_t>(gridDim.x) * ROWS) {
+    const int64_t row = row0 + threadIdx.x / LANES;
+    const bool in = row < n;
+    const uint32_t key = in && p.drop.below ? row_key(p.drop, row) : 0u;
+    float v[HELD ? OC : 1][kPiece];
+    float ss[1] = {0.f};
+#pragma unroll HELD ? OC : 1
+    for (int k = 0; k < OC; ++k) {
+      const int o = lane + k * LANES, at = HELD ? k : 0;
+      if (in && o < pieces) {
+        load_sum<T>(p, row, o, step, key, v[at]);
+        if (p.sum.data) store_piece<T>(p.sum.data, row * p.sum.stride, o, p.dim, v[at]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i) v[at][i] = 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < kPiece; ++i) ss[0] = fmaf(v[at][i], v[at][i], ss[0]);
+    }
+    row_sum<LANES>(ss, lds);
+    const float inv = inverse_root(fmaf(ss[0], by, p.eps));
+#pragma unroll HELD ? OC : 1
+    for (int k = 0; k < OC; ++k) {
+      const int o = lane + k * LANES, at = HELD ? k : 0;
+      if constexpr (!HELD) {
+        if (in && o < pieces) {
+          if (p.sum.data) load_piece<T>(p.sum.data, row * p.sum.stride, o, p.dim, v[0]);
+          else load_sum<T>(p, row, o, step, key, v[0]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < kPiece; ++i) v[0][i] = 0.f;
+        }
+      }
+      store_norm<T, BITS>(p, in, row, o, pieces, inv, v[at]);
+    }
+  }
+}
+
+// With s = 1 / sqrt(mean r^2 + eps): dr = carry + s (g dy - r s^2 mean(g dy r)),
+// and d_weight = the sum over the rows of dy r s: a thread's rows in its
+// registers, the rows of a workgroup in LDS, the workgroups' sums one after
+// the other (k_join_parts): no atomics, the same bits every time.
+// HELD as above (else dy, r and g are read twice).
+template <typename T, int LANES, int OC, bool HELD>
+__global__ __launch_bounds__(NormBlock<LANES>::kThreads) void k_rms_norm_back(NormBackArgs p) {
+  constexpr int ROWS = NormBlock<LANES>::kRows, KEPT = HELD ? OC : 1;
+  __shared__ float lds[2 * (LANES > 64 ? LANES / 64 : 1)];
+  const int64_t n = count_rows(p.n_dev, p.n_cap);
+  const int lane = threadIdx.x % LANES, pieces = (p.dim + kPiece - 1) / kPiece;
+  const uint32_t step = p.drop.step ? *p.drop.step : 0u;
+  const float by = 1.f / static_cast<float>(p.dim);
+  float g[KEPT][kPiece], dw[OC][kPiece];
+  auto load_weight = [&](int o, float (&w)[kPiece]) {
+#pragma unroll
+    for (int i = 0; i < kPiece; ++i) w[i] = 1.f;
+    if (p.weight && o < pieces) load_piece<float>(p.weight, 0, o, p.dim, w);
+  };
+#pragma unroll
+  for (int k = 0; k < OC; ++k) {
+#pragma unroll
+    for (int i = 0; i < kPiece; ++i) dw[k][i] = 0.f;
+    if constexpr (HELD) load_weight(lane + k * LANES, g[k]);
+  }
+  for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * ROWS; row0 < n;
+       row0 += static_cast<int64_t>(gridDim.x) * ROWS) {
+    const int64_t row = row0 + threadIdx.x / LANES;
+    const bool in = row < n;
+    float r[KEPT][kPiece], dy[KEPT][kPiece];
+    float s[2] = {0.f, 0.f};        // r^2, g dy r
+    auto load = [&](int o, float (&a)[kPiece], float (&b)[kPiece]) {
+      if (in && o < pieces) {
+        load_piece<T>(p.r.data, row * p.r.stride, o, p.dim, a);
+        load_piece<T>(p.dy.data, row * p.dy.stride, o, p.dim, b);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i) a[i] = b[i] = 0.f;
+      }
+    };
+#pragma unroll HELD ? OC : 1
+    for (int k = 0; k < OC; ++k) {
+      const int o = lane + k * LANES, at = HELD ? k : 0;
+      load(o, r[at], dy[at]);
+      if constexpr (!HELD) load_weight(o, g[0]);
+#pragma unroll
+      for (int i = 0; i < kPiece; ++i) {
+        s[0] = fmaf(r[at][i], r[at][i], s[0]);
+        s[1] = fmaf(g[at][i] * dy[at][i], r[at][i], s[1]);
+      }
+    }
+    row_sum<LANES>(s, lds);
+    const float inv = inverse_root(fmaf(s[0], by, p.eps));
+    const float along = s[1] * by * inv * inv;
+    const uint32_t key = in && p.drop.below ? row_key(p.drop, row) : 0u;
+#pragma unroll
+    for (int k = 0; k < OC; ++k) {
+      const int o = lane + k * LANES, at = HELD ? k : 0;
+      if (!in || o >= pieces) continue;
+      if constexpr (!HELD) {
+        load(o, r[0], dy[0]);
+        load_weight(o, g[0]);
+      }
+      float d[kPiece];
+#pragma unroll
+      for (int i = 0; i < kPiece; ++i) {
+        dw[k][i] = fmaf(dy[at][i], r[at][i] * inv, dw[k][i]);
+        d[i] = inv * (g[at][i] * dy[at][i] - r[at][i] * along);
+      }
+      if (p.carry.data) {
+        float c[kPiece];
+        load_piece<T>(p.carry.data, row * p.carry.stride, o, p.dim, c);
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i) d[i] += c[i];
+      }
+      if (p.d_residual.data) store_piece<T>(p.d_residual.data, row * p.d_residual.stride, o, p.dim, d);
+      if (p.dx.data) {
+        if (p.drop.below) drop_piece(p.drop, step, key, o, d);
+        store_piece<T>(p.dx.data, row * p.dx.stride, o, p.dim, d);
+      }
+    }
+  }
+  if (!p.partial) return;
+  if constexpr (ROWS > 1) {
+    __shared__ float rows[ROWS][LANES * OC * kPiece];
+#pragma unroll
+    for (int k = 0; k < OC; ++k)
+#pragma unroll
+      for (int i = 0; i < kPiece; ++i) rows[threadIdx.x / LANES][(lane + k * LANES) * kPiece + i] = dw[k][i];
+    __syncthreads();
+    for (int c = threadIdx.x; c < p.dim; c += NormBlock<LANES>::kThreads) {
+      float t = 0.f;
+#pragma unroll
+      for (int w = 0; w < ROWS; ++w) t += rows[w][c];
+      p.partial[static_cast<int64_t>(blockIdx.x) * p.dim + c] = t;
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < OC; ++k)
+      if (lane + k * LANES < pieces)
+        store_piece<float>(p.partial, static_cast<int64_t>(blockIdx.x) * p.dim, lane + k * LANES, p.dim, dw[k]);
+  }
+}
+
+// out[c] = the sum over the parts of partial[part][c], in a fixed order: a
+// workgroup has 32 columns, each thread every eighth part.
+__global__ __launch_bounds__(256) void k_join_parts(const float* partial, int parts, int dim, float* out) {
+  __shared__ float lds[8][32];
+  const int col = threadIdx.x & 31, first = threadIdx.x >> 5;
+  const int c = blockIdx.x * 32 + col;
+  float t = 0.f;
+  if (c < dim)
+    for (int q = first; q < parts; q += 8) t += partial[static_cast<int64_t>(q) * dim + c];
+  lds[first][col] = t;
+  __syncthreads();
+  if (first == 0 && c < dim) {
+#pragma unroll
+    for (int w = 1; w < 8; ++w) t += lds[w][col];
+    out[c] = t;
+  }
+}
+
+// ---- the gradients of the layers below a dropout --------------------------
+
+__global__ __launch_bounds__(256) void k_scale(ScaleArgs a) {
+  const int t = blockIdx.y;
+  const int64_t n = a.n[t];
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n;
+       i += static_cast<int64_t>(gridDim.x) * 256)
+    a.w[t][i] *= a.by[t];
+}
+
+__global__ __launch_bounds__(256) void k_given_gradient(const float* from, int64_t rows, int cols, float* dz, int ldz,
+                                                        int32_t* clear, int64_t clear_n) {
+  const int64_t first = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  const int64_t step = static_cast<int64_t>(gridDim.x) * 256;
+  for (int64_t i = first; i < rows * ldz; i += step) {
+    const int64_t row = i / ldz;
+    const int c = static_cast<int>(i - row * ldz);
+    dz[i] = c < cols ? from[row * cols + c] : 0.f;
+  }
+  for (int64_t i = first; i < clear_n; i += step) clear[i] = 0;
+}
+
+// ---- dispatch -------------------------------------------------------------
+
+// Workgroups: as many as the rows need, at most `most`.
+unsigned grid_for(int64_t n, int rows, int64_t most) {
+  const int64_t need = (n + rows - 1) / rows;
+  return static_cast<unsigned>(need < most ? need : most);
+}
+
+constexpr int64_t kRowGrid = 16 * kComputeUnits;
+
+template <typename T>
+void dropout_as(const DropoutArgs& a, hipStream_t s) {
+  const int pieces = (a.dim + kPiece - 1) / kPiece;
+  auto run = [&](auto lanes) {
+    constexpr int LANES = decltype(lanes)::value;
+    hipLaunchKernelGGL((k_dropout<T, LANES>), dim3(grid_for(a.n_cap, 256 / LANES, kRowGrid)), dim3(256), 0, s, a);
+  };
+  if (pieces <= 4) run(std::integral_constant<int, 4>{});
+  else if (pieces <= 16) run(std::integral_constant<int, 16>{});
+  else if (pieces <= 32) run(std::integral_constant<int, 32>{});
+  else if (pieces <= 64) run(std::integral_constant<int, 64>{});
+  else run(std::integral_constant<int, 256>{});
+}
+
+// LANES threads and OC pieces a thread for rows of `dim` columns (at most
+// 65,536): calls f with
+// the shape.
+template <int LANES, int OC, bool HELD = true>
+struct NormShape {
+  static constexpr int kLanes = LANES, kOc = OC;
+  static constexpr bool kHeld = HELD;
+};
+template <typename F>
+void norm_shape(int dim, F&& f) {
+  const int pieces = (dim + kPiece - 1) / kPiece;
+  if (pieces <= 4) f(NormShape<4, 1>{});
+  else if (pieces <= 16) f(NormShape<16, 1>{});
+  else if (pieces <= 32) f(NormShape<32, 1>{});
+  else if (pieces <= 64) f(NormShape<64, 1>{});
+  else if (pieces <= 128) f(NormShape<64, 2>{});
+  else if (pieces <= 256) f(NormShape<256, 1>{});
+  else if (pieces <= 512) f(NormShape<256, 2>{});
+  else if (pieces <= 1024) f(NormShape<256, 4>{});
+  else if (pieces <= 2048) f(NormShape<1024, 2, false>{});
+  else if (pieces <= 4096) f(NormShape<1024, 4, false>{});
+  else f(NormShape<1024, 8, false>{});
+}
+
+constexpr int64_t kNormBackGrid = 4 * kComputeUnits;
+
+}  // namespace
+
+hipError_t launch_dropout(const DropoutArgs& a, int bf16, hipStream_t s) {
+  bf16 ? dropout_as<uint16_t>(a, s) : dropout_as<float>(a, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_rms_norm(const NormArgs& a, int bf16, int bits, hipStream_t s) {
+  norm_shape(a.dim, [&](auto shape) {
+    using S = decltype(shape);
+    using B = NormBlock<S::kLanes>;
+    const dim3 grid(grid_for(a.n_cap, B::kRows, kRowGrid)), block(B::kThreads);
+    auto run = [&](auto t) {
+      using T = decltype(t);
+      if (bits == 0) hipLaunchKernelGGL((k_rms_norm<T, S::kLanes, S::kOc, S::kHeld, 0>), grid, block, 0, s, a);
+      else if (bits == 4) hipLaunchKernelGGL((k_rms_norm<T, S::kLanes, S::kOc, S::kHeld, 4>), grid, block, 0, s, a);
+      else hipLaunchKernelGGL((k_rms_norm<T, S::kLanes, S::kOc, S::kHeld, 8>), grid, block, 0, s, a);
+    };
+    bf16 ? run(uint16_t{}) : run(float{});
+  });
+  return hipGetLastError();
+}
+
+int norm_back_parts(int64_t n_cap, int dim) {
+  int parts = 1;
+  norm_shape(dim, [&](auto shape) {
+    parts = static_cast<int>(grid_for(n_cap, NormBlock<decltype(shape)::kLanes>::kRows, kNormBackGrid));
+  });
+  return parts;
+}
+
+hipError_t launch_rms_norm_backward(const NormBackArgs& a, int bf16, hipStream_t s) {
+  NormBackArgs p = a;
+  if (!p.d_weight) p.partial = nullptr;
+  const int parts = norm_back_parts(p.n_cap, p.dim);
+  norm_shape(p.dim, [&](auto shape) {
+    using S = decltype(shape);
+    using B = NormBlock<S::kLanes>;
+    if (bf16) hipLaunchKernelGGL((k_rms_norm_back<uint16_t, S::kLanes, S::kOc, S::kHeld>), dim3(parts), dim3(B::kThreads), 0, s, p);
+    else hipLaunchKernelGGL((k_rms_norm_back<float, S::kLanes, S::kOc, S::kHeld>), dim3(parts), dim3(B::kThreads), 0, s, p);
+  });
+  if (p.d_weight)
+    hipLaunchKernelGGL(k_join_parts, dim3(static_cast<unsigned>((p.dim + 31) / 32)), dim3(256), 0, s, p.partial, parts,
+                       p.dim, p.d_weight);
+  return hipGetLastError();
+}
+
+hipError_t launch_given_gradient(const float* from, int64_t rows, int cols, float* dz, int ldz, int32_t* clear,
+                                 int64_t clear_n, hipStream_t s) {
+  const int64_t work = rows * ldz > clear_n ? rows * ldz : clear_n;
+  hipLaunchKernelGGL(k_given_gradient, dim3(grid_for(work, 1024, 4 * kComputeUnits)), dim3(256), 0, s, from, rows,
+                     cols, dz, ldz, clear, clear_n);
+  return hipGetLastError();
+}
+
+hipError_t launch_scale(const ScaleArgs& a, hipStream_t s) {
+  int64_t most = 0;
+  for (int t = 0; t < a.count; ++t) most = a.n[t] > most ? a.n[t] : most;
+  if (a.count == 0 || most == 0) return hipSuccess;
+  hipLaunchKernelGGL(k_scale, dim3(grid_for(most, 1024, kComputeUnits), static_cast<unsigned>(a.count)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace gmb

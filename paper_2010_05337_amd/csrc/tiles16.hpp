@@ -1,0 +1,198 @@
+// Tiles of a product of 16-bit operands on gfx950: acc[m][n] = sum over k of
+// A(m, k) B(n, k) with v_mfma_f32_16x16x32, both sides brought through LDS
+// straight from memory, stage by stage.
+//
+// An operand lies in memory in one of two ways and is read from LDS to match:
+//   kByRow   rows of A (or B), each contiguous along k: a lane takes the eight
+//            k of its row at once
+//   kByK     rows of k, each contiguous along m (or n): ds_read_b64_tr_b16
+//            hands a lane four k of its column
+// so none is ever transposed in memory.
+//
+// kBf16: elements are bf16, a stage is 64 of k.  kSplit: a value v is two fp16,
+// hi = v rounded and lo = v - hi rounded, with v scaled by a power of two so
+// that the largest is in [2^14, 2^15): what is lost is below 2^-22 |v| + 2^-25.
+// Rows hold 32 hi, 32 lo, 32 hi, ... (a 128-byte piece has both parts of 32
+// values), a stage is 32 of k, and a product is hi hi + hi lo + lo hi: three
+// instructions where cutting into three bf16 takes six, both at fp32's error.
+#pragma once
+
+#include "common.hpp"
+
+namespace gmb {
+
+typedef float t16_f32x4 __attribute__((ext_vector_type(4)));
+typedef short t16_i16x4 __attribute__((ext_vector_type(4)));
+typedef short t16_i16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 t16_bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 t16_f16x8 __attribute__((ext_vector_type(8)));
+
+enum T16Type { kBf16, kSplit };
+enum T16Form { kByRow, kByK };
+
+// One side of a product.  kByRow: `rows` rows of `ld` 16-bit elements, the
+// tile's first row `first`; kByK: `rows` rows of k, `cols` values wide (a
+// multiple of 64), the tile's first column `first`.  Rows and columns past the
+// end are read as some that there are: of rows and columns nothing is stored,
+// of k one of the two sides must hold zeros.
+struct T16Side {
+  const uint16_t* data;
+  int64_t ld;
+  int64_t rows;
+  int cols;
+  int64_t first;
+};
+
+template <int TM, int TN>
+constexpr int t16_stage_bytes() { return (TM + TN) * 128; }
+
+// 16 bytes a lane from global memory to LDS, at l + 16 lane.
+__device__ __forceinline__ void t16_load_lds(const void* g, void* l) {
+  typedef const __attribute__((address_space(1))) void* gp;
+  typedef __attribute__((address_space(3))) void* lp;
+  __builtin_amdgcn_global_load_lds((gp)g, (lp)l, 16, 0, 0);
+}
+
+// What brings a side's tile of T rows (or columns) into LDS.  LDS holds T x 128
+// bytes a stage: kByRow T rows of eight 16-byte pieces, piece q at q ^ (row / 2
+// % 8); kByK 64 rows of T columns (kSplit: the hi parts of 32 of k, then the lo
+// parts), pairs of pieces exchanged by t16_turn.  Both spread the rows that are
+// read together over the banks.
+__device__ __forceinline__ int t16_turn(int krow) { return (krow & 3) | ((krow >> 3) & 1) << 2; }
+
+template <T16Type TYPE, T16Form FORM, int T, int WAVES>
+struct T16Loader {
+  static constexpr int LOADS = T * 8 / (64 * WAVES);
+  static_assert(LOADS * 64 * WAVES == T * 8, "a stage is whole loads");
+  static constexpr int KROWS = TYPE == kSplit ? 32 : 64;
+  static constexpr int P = T / 8;           // pieces of a row of k
+  const char* base[LOADS];                  // kByRow: the row's address; kByK: the column's in row 0
+  int krow[LOADS];
+  int64_t ld_bytes, rows;
+
+  __device__ __forceinline__ void init(const T16Side& s, int wave, int lane) {
+    ld_bytes = s.ld * 2;
+    rows = s.rows;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int q = (i * WAVES + wave) * 64 + lane;
+      if constexpr (FORM == kByRow) {
+        const int row = q / 8, piece = (q % 8) ^ ((row >> 1) & 7);
+        const int64_t at = s.first + row < s.rows ? s.first + row : s.rows - 1;
+        base[i] = reinterpret_cast<const char*>(s.data) + at * ld_bytes + piece * 16;
+      } else {
+        const int row = q / P, slot = q % P;
+        const int chunk = (slot >> 1) ^ (t16_turn(row) & (P / 2 - 1));
+        int64_t col = s.first + (chunk * 2 + (slot & 1)) * 8;
+        if (col >= s.cols) col = 0;
+        krow[i] = TYPE == kSplit ? row & 31 : row;
+        const int64_t in_row = TYPE == kSplit ? (col / 32) * 128 + (row >> 5) * 64 + (col % 32) * 2 : col * 2;
+        base[i] = reinterpret_cast<const char*>(s.data) + in_row;
+      }
+    }
+  }
+  // stage k into the side's half of an LDS stage
+  __device__ __forceinline__ void fetch(int64_t k, char* lds, int wave) const {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      char* to = lds + (i * WAVES + wave) * 1024;
+      if constexpr (FORM == kByRow) {
+        t16_load_lds(base[i] + k * 128, to);
+      } else {
+        const int64_t row = k * KROWS + krow[i];
+        t16_load_lds(base[i] + (row < rows ? row : rows - 1) * ld_bytes, to);
+      }
+    }
+  }
+};
+
+// The operand of 16 rows (or columns) from `at` on in an LDS stage, for the
+// stage's s-th 32 (kSplit: s = 0 the hi parts, 1 the lo parts).
+template <T16Form FORM, int T>
+__device__ __forceinline__ t16_i16x8 t16_operand(const char* lds, int at, int s, int lane) {
+  const int r = lane & 15, g = lane >> 4;
+  if constexpr (FORM == kByRow) {
+    return *reinterpret_cast<const t16_i16x8*>(lds + (at + r) * 128 + ((4 * s + g) ^ ((r >> 1) & 7)) * 16);
+  } else {
+    typedef __attribute__((address_space(3))) t16_i16x4* lp;
+    const int chunk = (at / 16) ^ (((r >> 2) | (g & 1) << 2) & (T / 16 - 1));
+    const char* p = lds + (32 * s + 8 * g + (r >> 2)) * (2 * T) + chunk * 32 + (r & 3) * 8;
+    const t16_i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)p);
+    const t16_i16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(p + 4 * (2 * T)));
+    return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+}
+
+template <T16Type TYPE>
+__device__ __forceinline__ t16_f32x4 t16_mfma(t16_i16x8 a, t16_i16x8 b, t16_f32x4 c) {
+  if constexpr (TYPE == kBf16)
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(t16_bf16x8, a), __builtin_bit_cast(t16_bf16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(t16_f16x8, a), __builtin_bit_cast(t16_f16x8, b), c, 0, 0, 0);
+}
+
+// A workgroup of WM x WN waves, a wave RT x CT tiles of 16 x 16: its rows of A
+// from 16 RT wm on, of B from 16 CT wn on.  Register e of lane (g, r) of
+// acc[i][j] is row 16 i + 4 g + e of A, row 16 j + r of B.
+template <T16Type TYPE, T16Form FA, T16Form FB, int TM, int TN, int WM, int WN>
+struct T16Tile {
+  static constexpr int WAVES = WM * WN, RT = TM / (16 * WM), CT = TN / (16 * WN);
+  static constexpr int kStage = t16_stage_bytes<TM, TN>();
+
+  // acc += the stages first .. last - 1 of k; lds: two stages.  Every wave of
+  // the workgroup calls it with the same stages.
+  static __device__ __forceinline__ void run(const T16Side& a, const T16Side& b, int64_t first, int64_t last, char* lds,
+                                             t16_f32x4 (&acc)[RT][CT]) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
+    T16Loader<TYPE, FA, TM, WAVES> la;
+    T16Loader<TYPE, FB, TN, WAVES> lb;
+    la.init(a, wave, lane);
+    lb.init(b, wave, lane);
+    auto fetch = [&](int64_t k) {
+      char* to = lds + ((k - first) & 1) * kStage;
+      la.fetch(k, to, wave);
+      lb.fetch(k, to + TM * 128, wave);
+    };
+    if (first < last) fetch(first);
+    __syncthreads();
+    for (int64_t k = first; k < last; ++k) {
+      const char* at = lds + ((k - first) & 1) * kStage;
+      if (k + 1 < last) fetch(k + 1);
+      if constexpr (TYPE == kBf16) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          t16_i16x8 qa[RT], qb[CT];
+#pragma unroll
+          for (int j = 0; j < CT; ++j) qb[j] = t16_operand<FB, TN>(at + TM * 128, 16 * (CT * wn + j), s, lane);
+#pragma unroll
+          for (int i = 0; i < RT; ++i) qa[i] = t16_operand<FA, TM>(at, 16 * (RT * wm + i), s, lane);
+#pragma unroll
+          for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int j = 0; j < CT; ++j) acc[i][j] = t16_mfma<TYPE>(qa[i], qb[j], acc[i][j]);
+        }
+      } else {
+        t16_i16x8 bh[CT], bl[CT];
+#pragma unroll
+        for (int j = 0; j < CT; ++j) {
+          bh[j] = t16_operand<FB, TN>(at + TM * 128, 16 * (CT * wn + j), 0, lane);
+          bl[j] = t16_operand<FB, TN>(at + TM * 128, 16 * (CT * wn + j), 1, lane);
+        }
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+          const t16_i16x8 ah = t16_operand<FA, TM>(at, 16 * (RT * wm + i), 0, lane);
+          const t16_i16x8 al = t16_operand<FA, TM>(at, 16 * (RT * wm + i), 1, lane);
+#pragma unroll
+          for (int j = 0; j < CT; ++j) acc[i][j] = t16_mfma<TYPE>(al, bh[j], acc[i][j]);
+#pragma unroll
+          for (int j = 0; j < CT; ++j) acc[i][j] = t16_mfma<TYPE>(ah, bl[j], acc[i][j]);
+#pragma unroll
+          for (int j = 0; j < CT; ++j) acc[i][j] = t16_mfma<TYPE>(ah, bh[j], acc[i][j]);
+        }
+      }
+      __syncthreads();              // stage k is read, stage k + 1 has arrived
+    }
+  }
+};
+
+}  // namespace gmb
