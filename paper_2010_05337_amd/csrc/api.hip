@@ -520,11 +520,11 @@ int check_forward(const gmb_blocks* blocks, const gmb_sage_weights* weights, con
 
 // The layers in order.  Layer 0's linear reads its destination rows from
 // x_self; its mean reads the rows mean_rows[mean_ids[e]] (the gathered
-// input and the local ids, or the feature table and the global ids).  drop:
-// the dropout of the hidden outputs, or NULL.
+// input and the local ids, or the feature table and the global ids).  then:
+// what is done to the hidden outputs, or NULL.
 int run_forward(const gmb_blocks* blocks, const void* x_self, const int32_t* mean_ids, const void* mean_rows,
                 int64_t mean_max_id, const gmb_sage_weights* weights, float* logits, const ForwardPlan& p,
-                void* ws, hipStream_t s, const gmb_dropout* drop = nullptr) {
+                void* ws, hipStream_t s, const gmb::HiddenLaunch* then = nullptr) {
   const int L = weights->num_layers;
   const int bf16 = weights->dtype == GMB_BF16;
   char* base = static_cast<char*>(ws);
@@ -545,17 +545,9 @@ int run_forward(const gmb_blocks* blocks, const void* x_self, const int32_t* mea
                                 weights->bias[l], d_in, d_out, bf16, last ? 0 : 1,
                                 (last || !bf16) ? 1 : 0, h_out, bk.cap_dst, s);
     if (e != hipSuccess) return hip_fail(e, "linear launch");
-    if (drop && !last) {
-      gmb::DropoutArgs a{};
-      a.x = {h_out, d_out};
-      a.out = {h_out, d_out};
-      a.drop = gmb::abi_drop_args(drop, bk.src_ids);   // (the first sources are the destinations)
-      a.drop.layer += static_cast<uint32_t>(l);
-      a.n_dev = bk.sizes + gmb::kNDst;
-      a.n_cap = bk.cap_dst;
-      a.dim = d_out;
-      e = gmb::launch_dropout(a, bf16, s);
-      if (e != hipSuccess) return hip_fail(e, "dropout launch");
+    if (then && !last) {
+      e = then->launch(then->what, l, bk, h_out, d_out, bf16, s);
+      if (e != hipSuccess) return hip_fail(e, "hidden output launch");
     }
     h_in = h_out;
   }
@@ -753,30 +745,6 @@ int gmb_sage_forward_fused(const gmb_blocks* blocks, const void* feats, int64_t 
                                     x_dst, status, s);
   if (e != hipSuccess) return hip_fail(e, "gather launch");
   return run_forward(blocks, x_dst, b0.nbr, feats, num_nodes, weights, logits, p, ws, s);
-}
-
-int gmb_sage_forward_dropout(const gmb_blocks* blocks, void* x, const void* feats, int64_t num_nodes,
-                             const gmb_sage_weights* weights, const gmb_dropout* drop, float* logits, void* ws,
-                             size_t ws_bytes, uint32_t* status, void* stream) {
-  ForwardPlan p;
-  int st = check_forward(blocks, weights, logits, ws, ws_bytes, &p);
-  if (st == GMB_OK) st = gmb::abi_check_dropout(drop);
-  if (st != GMB_OK) return st;
-  if (drop->layer > kMaxInt32 - GMB_MAX_LAYERS) return fail(GMB_EINVAL, "layer=%d leaves no room for the model's", drop->layer);
-  if (feats && (num_nodes < 1 || num_nodes > kMaxInt32))
-    return fail(GMB_EINVAL, "num_nodes=%lld outside 1..2^31-1", static_cast<long long>(num_nodes));
-  if (blocks->num_seeds == 0) return ok();   // an empty batch: no rows anywhere
-  if (!x) return fail(GMB_EINVAL, "x is NULL");
-  const hipStream_t s = as_stream(stream);
-  const gmb_block& b0 = blocks->blk[0];
-  if (feats) {
-    const int64_t row_bytes = static_cast<int64_t>(weights->dims[0]) * (weights->dtype == GMB_BF16 ? 2 : 4);
-    hipError_t e = gmb::launch_gather(b0.src_ids, b0.sizes + gmb::kNDst, b0.cap_dst, feats, num_nodes, row_bytes, x,
-                                      status, s);
-    if (e != hipSuccess) return hip_fail(e, "gather launch");
-  }
-  return run_forward(blocks, x, feats ? b0.nbr : b0.indices, feats ? feats : x,
-                     feats ? num_nodes : std::max<int64_t>(b0.cap_src, 1), weights, logits, p, ws, s, drop);
 }
 
 }  // extern "C"
@@ -1073,18 +1041,6 @@ int run_backward(const gmb_blocks* blocks, const void* x, const gmb_sage_weights
   return ok();
 }
 
-// The "loss" of gmb_sage_backward_from: the gradient that the caller has.
-struct GivenGradient {
-  const float* d_logits;
-  int64_t rows;
-  int cols;
-};
-hipError_t given_gradient(const void* what, float* dz, int ldz, float*, int32_t* clear, int64_t clear_n,
-                          hipStream_t s) {
-  const GivenGradient& g = *static_cast<const GivenGradient*>(what);
-  return gmb::launch_given_gradient(g.d_logits, g.rows, g.cols, dz, ldz, clear, clear_n, s);
-}
-
 }  // namespace
 
 extern "C" {
@@ -1182,50 +1138,6 @@ int gmb_sgd_update_bf16(const gmb_sage_weights* weights, const gmb_sage_weights*
   return ok();
 }
 
-int gmb_sage_backward_from(const gmb_blocks* blocks, const void* x, const gmb_sage_weights* weights,
-                           const float* d_logits, const gmb_dropout* drop, const void* fwd_ws, size_t fwd_ws_bytes,
-                           const gmb_sage_grads* grads, void* ws, size_t ws_bytes, float* table, int64_t num_nodes,
-                           float emb_lr, void* stream) {
-  int st = check_blocks(blocks);
-  if (st == GMB_OK && drop) st = gmb::abi_check_dropout(drop);
-  if (st != GMB_OK) return st;
-  if (!weights) return fail(GMB_EINVAL, "weights is NULL");
-  if (weights->num_layers != blocks->num_layers)
-    return fail(GMB_EINVAL, "weights have %d layers, blocks %d", weights->num_layers, blocks->num_layers);
-  if (table) {
-    if (num_nodes < 1 || num_nodes > kMaxInt32)
-      return fail(GMB_EINVAL, "num_nodes=%lld outside 1..2^31-1", static_cast<long long>(num_nodes));
-    if (reinterpret_cast<uintptr_t>(table) % 16) return fail(GMB_EINVAL, "table must be 16-byte aligned");
-  }
-  // A dropped hidden value is 0, so the backward's mask (outputs above 0) stops
-  // its gradient already; what passes lacks the dropout's factor once for every
-  // hidden layer above, which a layer's gradients (and the embeddings' step)
-  // take at the end: they are linear in it.
-  const int L = weights->num_layers;
-  const gmb::DropArgs d = gmb::abi_drop_args(drop, nullptr);
-  gmb::ScaleArgs a{};
-  float by = 1.f;
-  for (int l = L - 2; l >= 0 && d.below > 0 && blocks->num_seeds > 0; --l) {
-    by *= d.scale;
-    if (!grads || !grads->d_self[l] || !grads->d_neigh[l] || !grads->d_bias[l]) break;   // (refused below)
-    const int64_t n = static_cast<int64_t>(weights->dims[l]) * weights->dims[l + 1];
-    float* const w[] = {grads->d_self[l], grads->d_neigh[l], grads->d_bias[l]};
-    for (int i = 0; i < 3; ++i) {
-      a.w[a.count] = w[i];
-      a.n[a.count] = i < 2 ? n : weights->dims[l + 1];
-      a.by[a.count++] = by;
-    }
-  }
-  const GivenGradient given{d_logits, blocks->num_seeds, weights->dims[L]};
-  const gmb::LossLaunch how{given_gradient, &given};
-  st = run_backward(blocks, x, weights, d_logits, nullptr, fwd_ws, fwd_ws_bytes, grads, nullptr, ws, ws_bytes, table,
-                    num_nodes, emb_lr * by, stream, &how);
-  if (st != GMB_OK || a.count == 0) return st;
-  const hipError_t e = gmb::launch_scale(a, as_stream(stream));
-  if (e != hipSuccess) return hip_fail(e, "scale launch");
-  return ok();
-}
-
 }  // extern "C"
 
 namespace gmb {
@@ -1240,6 +1152,28 @@ int abi_fail(int status, const char* fmt, ...) {
 }
 
 int abi_check_blocks(const gmb_blocks* b) { return check_blocks(b); }
+
+int abi_forward_with(const HiddenLaunch& then, const gmb_blocks* blocks, void* x, const void* feats, int64_t num_nodes,
+                     const gmb_sage_weights* weights, float* logits, void* ws, size_t ws_bytes, uint32_t* status,
+                     void* stream) {
+  ForwardPlan p;
+  int st = check_forward(blocks, weights, logits, ws, ws_bytes, &p);
+  if (st != GMB_OK) return st;
+  if (feats && (num_nodes < 1 || num_nodes > kMaxInt32))
+    return fail(GMB_EINVAL, "num_nodes=%lld outside 1..2^31-1", static_cast<long long>(num_nodes));
+  if (blocks->num_seeds == 0) return ok();   // an empty batch: no rows anywhere
+  if (!x) return fail(GMB_EINVAL, "x is NULL");
+  const hipStream_t s = as_stream(stream);
+  const gmb_block& b0 = blocks->blk[0];
+  if (feats) {
+    const int64_t row_bytes = static_cast<int64_t>(weights->dims[0]) * (weights->dtype == GMB_BF16 ? 2 : 4);
+    hipError_t e = gmb::launch_gather(b0.src_ids, b0.sizes + gmb::kNDst, b0.cap_dst, feats, num_nodes, row_bytes, x,
+                                      status, s);
+    if (e != hipSuccess) return hip_fail(e, "gather launch");
+  }
+  return run_forward(blocks, x, feats ? b0.nbr : b0.indices, feats ? feats : x,
+                     feats ? num_nodes : std::max<int64_t>(b0.cap_src, 1), weights, logits, p, ws, s, &then);
+}
 
 int abi_backward_from(const LossLaunch& how, const gmb_blocks* blocks, const void* x,
                       const gmb_sage_weights* weights, const float* logits, const void* fwd_ws, size_t fwd_ws_bytes,

@@ -6,7 +6,6 @@
 #include <stdint.h>
 
 #include "gmb.h"
-#include "head_kernels.hpp"
 
 namespace gmb {
 
@@ -33,8 +32,18 @@ int abi_backward_from(const LossLaunch& how, const gmb_blocks* blocks, const voi
                       const gmb_sage_grads* grads, float* loss, void* ws, size_t ws_bytes, float* table,
                       int64_t num_nodes, float emb_lr, void* stream);
 
-// A dropout: refused, or as the kernels take it (NULL: nothing is dropped).
-int abi_check_dropout(const gmb_dropout* d);
-DropArgs abi_drop_args(const gmb_dropout* d, const int32_t* ids);
+// What is done to a hidden layer's output `rows` (the first *blk.sizes[0] of
+// blk.cap_dst rows of `dim`) before the next layer reads it.
+struct HiddenLaunch {
+  hipError_t (*launch)(const void* what, int layer, const gmb_block& blk, void* rows, int dim, int bf16,
+                       hipStream_t s);
+  const void* what;
+};
+
+// gmb_sage_forward (feats NULL) or gmb_sage_forward_fused (x: its x_dst) with
+// that.
+int abi_forward_with(const HiddenLaunch& then, const gmb_blocks* blocks, void* x, const void* feats, int64_t num_nodes,
+                     const gmb_sage_weights* weights, float* logits, void* ws, size_t ws_bytes, uint32_t* status,
+                     void* stream);
 
 }  // namespace gmb

@@ -95,22 +95,19 @@ gmb::LinearLossArgs head_args(const gmb_linear_head* h, const gmb_linear_grads* 
   return a;
 }
 
-}  // namespace
-
-namespace gmb {
-
-int abi_check_dropout(const gmb_dropout* d) {
+int check_dropout(const gmb_dropout* d) {
   if (!d) return abi_fail(GMB_EINVAL, "dropout is NULL");
   if (!(d->p >= 0.f && d->p <= 1.f)) return abi_fail(GMB_EINVAL, "p=%g outside 0..1", static_cast<double>(d->p));
   if (d->layer < 0) return abi_fail(GMB_EINVAL, "layer=%d is negative", d->layer);
   return GMB_OK;
 }
 
-DropArgs abi_drop_args(const gmb_dropout* d, const int32_t* ids) {
-  DropArgs a{};
+// As the kernels take it (NULL: nothing is dropped).
+gmb::DropArgs drop_args(const gmb_dropout* d, const int32_t* ids) {
+  gmb::DropArgs a{};
   if (!d) return a;
-  a.below = drop_below(d->p);
-  a.scale = drop_scale(a.below);
+  a.below = gmb::drop_below(d->p);
+  a.scale = gmb::drop_scale(a.below);
   a.k0 = static_cast<uint32_t>(d->seed);
   a.k1 = static_cast<uint32_t>(d->seed >> 32);
   a.layer = static_cast<uint32_t>(d->layer);
@@ -119,7 +116,33 @@ DropArgs abi_drop_args(const gmb_dropout* d, const int32_t* ids) {
   return a;
 }
 
-}  // namespace gmb
+// The dropout of layer `layer`'s output, in place, by vertex.
+hipError_t drop_hidden(const void* what, int layer, const gmb_block& blk, void* rows, int dim, int bf16,
+                       hipStream_t s) {
+  gmb::DropoutArgs a{};
+  a.x = {rows, dim};
+  a.out = {rows, dim};
+  a.drop = drop_args(static_cast<const gmb_dropout*>(what), blk.src_ids);   // (the first sources are the destinations)
+  a.drop.layer += static_cast<uint32_t>(layer);
+  a.n_dev = blk.sizes + gmb::kNDst;
+  a.n_cap = blk.cap_dst;
+  a.dim = dim;
+  return gmb::launch_dropout(a, bf16, s);
+}
+
+// The "loss" of gmb_sage_backward_from: the gradient that the caller has.
+struct GivenGradient {
+  const float* d_logits;
+  int64_t rows;
+  int cols;
+};
+hipError_t given_gradient(const void* what, float* dz, int ldz, float*, int32_t* clear, int64_t clear_n,
+                          hipStream_t s) {
+  const GivenGradient& g = *static_cast<const GivenGradient*>(what);
+  return gmb::launch_given_gradient(g.d_logits, g.rows, g.cols, dz, ldz, clear, clear_n, s);
+}
+
+}  // namespace
 
 extern "C" {
 
@@ -128,7 +151,7 @@ int gmb_dropout_rows(const gmb_rows* x, const gmb_rows* residual, const gmb_drop
                      void* stream) {
   int st = check_shape(n_cap, dim);
   if (st == GMB_OK) st = check_dtype(dtype);
-  if (st == GMB_OK) st = gmb::abi_check_dropout(drop);
+  if (st == GMB_OK) st = check_dropout(drop);
   if (st != GMB_OK) return st;
   if (n_cap == 0) return GMB_OK;
   st = check_rows(x, dim, true, "x");
@@ -141,7 +164,7 @@ int gmb_dropout_rows(const gmb_rows* x, const gmb_rows* residual, const gmb_drop
   a.x = rows_in(x);
   a.residual = rows_in(residual);
   a.out = rows_out(out);
-  a.drop = gmb::abi_drop_args(drop, ids);
+  a.drop = drop_args(drop, ids);
   a.n_dev = n_dev;
   a.n_cap = n_cap;
   a.dim = dim;
@@ -156,7 +179,7 @@ int gmb_rms_norm(const gmb_rows* x, const gmb_rows* residual, const gmb_dropout*
   int st = check_shape(n_cap, dim);
   if (st == GMB_OK) st = check_dtype(dtype);
   if (st == GMB_OK) st = check_eps(eps);
-  if (st == GMB_OK && drop) st = gmb::abi_check_dropout(drop);
+  if (st == GMB_OK && drop) st = check_dropout(drop);
   if (st != GMB_OK) return st;
   if (format != 0 && format != GMB_MXFP4 && format != GMB_MXFP8) return abi_fail(GMB_EINVAL, "format=%d unknown", format);
   if (n_cap == 0) return GMB_OK;
@@ -185,7 +208,7 @@ int gmb_rms_norm(const gmb_rows* x, const gmb_rows* residual, const gmb_dropout*
   if (sum && sum->data == out->data) return abi_fail(GMB_EINVAL, "sum and out are the same rows");
   a.x = rows_in(x);
   a.residual = rows_in(residual);
-  a.drop = gmb::abi_drop_args(drop, ids);
+  a.drop = drop_args(drop, ids);
   a.n_dev = n_dev;
   a.n_cap = n_cap;
   a.dim = dim;
@@ -210,7 +233,7 @@ int gmb_rms_norm_backward(const gmb_rows* dy, const gmb_rows* r, const gmb_rows*
   int st = check_shape(n_cap, dim);
   if (st == GMB_OK) st = check_dtype(dtype);
   if (st == GMB_OK) st = check_eps(eps);
-  if (st == GMB_OK && drop) st = gmb::abi_check_dropout(drop);
+  if (st == GMB_OK && drop) st = check_dropout(drop);
   if (st != GMB_OK) return st;
   if (n_cap == 0) {   // a sum over no rows
     if (!d_weight) return GMB_OK;
@@ -246,7 +269,7 @@ int gmb_rms_norm_backward(const gmb_rows* dy, const gmb_rows* r, const gmb_rows*
   a.dy = rows_in(dy);
   a.r = rows_in(r);
   a.carry = rows_in(carry);
-  a.drop = gmb::abi_drop_args(drop, ids);
+  a.drop = drop_args(drop, ids);
   a.n_dev = n_dev;
   a.n_cap = n_cap;
   a.dim = dim;
@@ -301,6 +324,61 @@ int gmb_linear_loss(const gmb_linear_head* head, const gmb_linear_grads* grads, 
   }
   const hipError_t e = gmb::launch_linear_loss(a, bf16, as_stream(stream));
   if (e != hipSuccess) return hip_fail(e, "linear loss launch");
+  return GMB_OK;
+}
+
+int gmb_sage_forward_dropout(const gmb_blocks* blocks, void* x, const void* feats, int64_t num_nodes,
+                             const gmb_sage_weights* weights, const gmb_dropout* drop, float* logits, void* ws,
+                             size_t ws_bytes, uint32_t* status, void* stream) {
+  const int st = check_dropout(drop);
+  if (st != GMB_OK) return st;
+  if (drop->layer > kMaxInt32 - GMB_MAX_LAYERS)
+    return abi_fail(GMB_EINVAL, "layer=%d leaves no room for the model's", drop->layer);
+  return gmb::abi_forward_with({drop_hidden, drop}, blocks, x, feats, num_nodes, weights, logits, ws, ws_bytes, status,
+                               stream);
+}
+
+int gmb_sage_backward_from(const gmb_blocks* blocks, const void* x, const gmb_sage_weights* weights,
+                           const float* d_logits, const gmb_dropout* drop, const void* fwd_ws, size_t fwd_ws_bytes,
+                           const gmb_sage_grads* grads, void* ws, size_t ws_bytes, float* table, int64_t num_nodes,
+                           float emb_lr, void* stream) {
+  int st = gmb::abi_check_blocks(blocks);
+  if (st == GMB_OK && drop) st = check_dropout(drop);
+  if (st != GMB_OK) return st;
+  if (!weights) return abi_fail(GMB_EINVAL, "weights is NULL");
+  if (weights->num_layers != blocks->num_layers)
+    return abi_fail(GMB_EINVAL, "weights have %d layers, blocks %d", weights->num_layers, blocks->num_layers);
+  if (table) {
+    if (num_nodes < 1 || num_nodes > kMaxInt32)
+      return abi_fail(GMB_EINVAL, "num_nodes=%lld outside 1..2^31-1", static_cast<long long>(num_nodes));
+    if (reinterpret_cast<uintptr_t>(table) % 16) return abi_fail(GMB_EINVAL, "table must be 16-byte aligned");
+  }
+  // A dropped hidden value is 0, so the backward's mask (outputs above 0) stops
+  // its gradient already; what passes lacks the dropout's factor once for every
+  // hidden layer above, which a layer's gradients (and the embeddings' step)
+  // take at the end: they are linear in it.
+  const int L = weights->num_layers;
+  const gmb::DropArgs d = drop_args(drop, nullptr);
+  gmb::ScaleArgs a{};
+  float by = 1.f;
+  for (int l = L - 2; l >= 0 && d.below > 0 && blocks->num_seeds > 0; --l) {
+    by *= d.scale;
+    if (!grads || !grads->d_self[l] || !grads->d_neigh[l] || !grads->d_bias[l]) break;   // (refused below)
+    const int64_t n = static_cast<int64_t>(weights->dims[l]) * weights->dims[l + 1];
+    float* const w[] = {grads->d_self[l], grads->d_neigh[l], grads->d_bias[l]};
+    for (int i = 0; i < 3; ++i) {
+      a.w[a.count] = w[i];
+      a.n[a.count] = i < 2 ? n : weights->dims[l + 1];
+      a.by[a.count++] = by;
+    }
+  }
+  const GivenGradient given{d_logits, blocks->num_seeds, weights->dims[L]};
+  const gmb::LossLaunch how{given_gradient, &given};
+  st = gmb::abi_backward_from(how, blocks, x, weights, d_logits, fwd_ws, fwd_ws_bytes, grads, nullptr, ws, ws_bytes,
+                              table, num_nodes, emb_lr * by, stream);
+  if (st != GMB_OK || a.count == 0) return st;
+  const hipError_t e = gmb::launch_scale(a, as_stream(stream));
+  if (e != hipSuccess) return hip_fail(e, "scale launch");
   return GMB_OK;
 }
 
