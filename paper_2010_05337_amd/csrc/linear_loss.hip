@@ -4,13 +4,13 @@
 //
 //   k_amax, k_lay_out   x, and W where it cannot be read as it lies, as 16-bit
 //                       rows padded with zeros; rows without a label as zeros
-//   k_logits (stats)    a tile of logits in registers: every row's maximum and
-//                       sum of exponentials over the tile's classes, its label's
-//                       logit
-//   k_join_rows         the tiles of a row: lse, the loss term
-//   k_logits (grad)     the logits again, a piece of the classes at a time: G
+//   k_logits (kStats)   tiles of logits in registers: every row's maximum and
+//                       sum of exponentials over a chunk of the classes, its
+//                       label's logit
+//   k_logits (kGrad)    the chunks of a row joined, the logits again, a piece of
+//                       the classes at a time: G; few classes (kBoth): at once
 //   k_products          dx += G W and dW = G^T x of the piece
-//   k_join              sums that were split
+//   k_finish            sums that were split; the mean
 //
 // The logits are computed twice (8 n C d operations in all where keeping them
 // would take 6) and never stored; G is, in 16 bits (kSplit: two times 16), for
@@ -151,12 +151,17 @@ __device__ __forceinline__ void put_split(uint16_t* row, int c, const float (&v)
 
 // A 64 x 64 tile of the source through LDS, read along whichever of its
 // directions is contiguous, written as rows.
+// (The first `first` workgroups lay out x, the others W.)
 template <T16Type TYPE, typename T>
-__global__ __launch_bounds__(256) void k_lay_out(LayOutArgs p) {
+__global__ __launch_bounds__(256) void k_lay_out(LayOutArgs x, LayOutArgs w, int64_t first) {
   __shared__ float tile[64][65];
   __shared__ uint32_t top_of[4];
-  const int64_t r0 = static_cast<int64_t>(blockIdx.x) * 64;
-  const int c0 = blockIdx.y * 64;
+  const bool of_x = static_cast<int64_t>(blockIdx.x) < first;
+  const LayOutArgs& p = of_x ? x : w;
+  const int64_t id = of_x ? blockIdx.x : blockIdx.x - first;
+  const int across = p.out_cols / 64;
+  const int64_t r0 = id / across * 64;
+  const int c0 = static_cast<int>(id % across) * 64;
   const T* src = static_cast<const T*>(p.src);
   const int fast = threadIdx.x & 63, slow = threadIdx.x >> 6;
   const bool along_rows = p.col == 1 || p.row != 1;   // neighbouring threads: neighbouring columns
@@ -184,7 +189,7 @@ __global__ __launch_bounds__(256) void k_lay_out(LayOutArgs p) {
     __syncthreads();
     for (int w = 0; w < 4; ++w) top = top_of[w] > top ? top_of[w] : top;
     scale = split_scale(top);
-    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.all_inverse = inverse_of_power(scale);
+    if (id == 0 && threadIdx.x == 0) *p.all_inverse = inverse_of_power(scale);
   } else {
     __syncthreads();
   }
@@ -198,13 +203,13 @@ __global__ __launch_bounds__(256) void k_lay_out(LayOutArgs p) {
 #pragma unroll
     for (int q = 0; q < 8; ++q) v[q] = tile[i][j + q];
     put_split<TYPE>(p.by_all + row * ld, c0 + j, v, scale);
-    const bool first = blockIdx.y == 0 && j == 0;
+    const bool lead = c0 == 0 && j == 0;
     if (TYPE == kSplit && p.by_row) {
       const float s = split_scale(row < p.rows ? p.row_top[row] : 0u);
       put_split<TYPE>(p.by_row + row * ld, c0 + j, v, s);
-      if (first) p.row_inverse[row] = inverse_of_power(s);
+      if (lead) p.row_inverse[row] = inverse_of_power(s);
     }
-    if (first && p.labels)
+    if (lead && p.labels)
       p.kept_labels[row] = row < p.rows && has_label(p.labels, row, p.classes) ? p.labels[row] : -1;
   }
 }
@@ -213,21 +218,22 @@ __global__ __launch_bounds__(256) void k_lay_out(LayOutArgs p) {
 
 struct LogitsArgs {
   T16Side w, x;                    // W's rows: A, those of x: B (`first` is set by the kernel)
-  int64_t stages;
-  int m_tiles, n_tiles;            // classes, rows
-  int c0;                          // the first class
+  int stages;
+  int c0, m_tiles, n_tiles;        // the first class, tiles of classes from it on, of rows
+  int chunks;                      // workgroups of a row tile
   int classes;
   const float* bias;               // or NULL
   const float* row_inverse;        // kSplit
   const float* w_inverse;          // kSplit: one word
   const int32_t* labels;           // [padded rows], -1 for none
-  int64_t pad_rows;
-  float2* stats;                   // [m_tiles][pad_rows]: maximum, sum of exponentials
-  float* label_logit;              // [pad_rows]
-  const float2* rows;              // [pad_rows]: maximum, 1 / sum
-  uint16_t* g;                     // [pad_rows][ldg]
+  int64_t rows, pad_rows;
+  float2* stats;                   // [stat_chunks][pad_rows]: maximum, sum of exponentials, in powers of two
+  int stat_chunks;
+  float* label_logit;              // [pad_rows], times log2(e)
+  float* loss_rows;                // [rows], or NULL
+  uint16_t* g;                     // [pad_rows][ldg], or NULL
   int64_t ldg;
-  float* db;                       // [n_tiles][ld_db] at the piece's first class, or NULL
+  float* db;                       // [n_tiles][ld_db] from the first class on, or NULL
   int64_t ld_db;
 };
 
@@ -246,190 +252,326 @@ __device__ __forceinline__ float sum16(float v) {
   return v;
 }
 
-enum LogitsMode { kStats, kGrad };
+// A maximum and the sum of 2^(u - maximum) of some of a row's u = z log2(e),
+// joined with others'.  -inf: nothing yet.  A NaN among the u makes the sum NaN.
+__device__ __forceinline__ void join_stats(float& top, float& sum, float t, float s) {
+  const float m = fmaxf(top, t), base = m == -INFINITY ? 0.f : m;
+  sum = sum * exp2_fast(top - base) + s * exp2_fast(t - base);
+  top = m;
+}
+__device__ __forceinline__ float row_lse(float top, float sum) { return top + log2f(sum); }
+// Every logit is -inf (a sum that is no number has a NaN among them).
+__device__ __forceinline__ bool row_empty(float top, float sum) { return top == -INFINITY && sum == 0.f; }
+constexpr float kLn2 = 0.6931471805599453f;
+
+// kStats: a row's statistics over a chunk of the classes.  kGrad: G of the
+// classes' piece, from the statistics of all chunks.  kBoth: at most TM classes:
+// statistics and G at once.
+enum LogitsMode { kStats, kGrad, kBoth };
+
+template <int TM, int TN, int WM, int WN>
+struct LogitsLds {
+  static constexpr int kStages = 2 * t16_stage_bytes<TM, TN>();
+  static constexpr int kRows = kStages;                        // [2][WM][TN]: statistics; lse, label; [TN]: its logit
+  static constexpr int kClasses = kRows + (2 * WM + 1) * TN * 4;   // [WN][TM]: sums of G
+  static constexpr int kBytes = kClasses + WN * TM * 4;
+};
 
 template <T16Type TYPE, LogitsMode MODE, int TM, int TN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
-  using Tile = T16Tile<TYPE, kByRow, kByRow, TM, TN, WM, WN>;
-  constexpr int RT = Tile::RT, CT = Tile::CT;
-  __shared__ __attribute__((aligned(1024))) char lds[2 * Tile::kStage];
-  const int64_t id = xcd_id(static_cast<int64_t>(p.m_tiles) * p.n_tiles);
+  using Tile = T16Tile<TYPE, kByRow, kByRow, TM, TN, WM, WN, true>;
+  using Lds = LogitsLds<TM, TN, WM, WN>;
+  constexpr int RT = Tile::RT, CT = Tile::CT, THREADS = 64 * WM * WN;
+  static_assert(RT % 2 == 0, "classes are dealt to pairs of tiles");
+  __shared__ __attribute__((aligned(1024))) char lds[Lds::kBytes];
+  float* row_a = reinterpret_cast<float*>(lds + Lds::kRows);
+  float* row_b = row_a + WM * TN;
+  float* row_label = row_b + WM * TN;
+  const int64_t id = xcd_id(static_cast<int64_t>(p.n_tiles) * p.chunks);
   if (id < 0) return;
-  // eight row tiles wide, so that an L2 holds what neighbours share
-  const int band = static_cast<int>(id / (8 * static_cast<int64_t>(p.m_tiles)));
-  const int64_t in_band = id - static_cast<int64_t>(band) * 8 * p.m_tiles;
-  const int width = p.n_tiles - 8 * band < 8 ? p.n_tiles - 8 * band : 8;
-  const int nt = 8 * band + static_cast<int>(in_band % width), mt = static_cast<int>(in_band / width);
+  const int nt = static_cast<int>(id % p.n_tiles), chunk = static_cast<int>(id / p.n_tiles);
+  const int t0 = static_cast<int>(static_cast<int64_t>(p.m_tiles) * chunk / p.chunks);
+  const int t1 = static_cast<int>(static_cast<int64_t>(p.m_tiles) * (chunk + 1) / p.chunks);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, r = lane & 15;
   const int wm = wave / WN, wn = wave % WN;
+  const int64_t tile_row = static_cast<int64_t>(nt) * TN, row0 = tile_row + 16 * CT * wn + r;
+  typename Tile::LoadA la;
+  typename Tile::LoadB lb;
   T16Side a = p.w, b = p.x;
-  a.first = p.c0 + static_cast<int64_t>(mt) * TM;
-  b.first = static_cast<int64_t>(nt) * TN;
-  t16_f32x4 acc[RT][CT];
+  b.first = tile_row;
+  lb.init(b, wave, lane);
+  auto at_tile = [&](int t) {
+    a.first = p.c0 + static_cast<int64_t>(t) * TM;
+    la.init(a, wave, lane);
+  };
+  at_tile(t0);
+  if (t0 < t1) {
+    la.fetch(0, lds, wave);
+    lb.fetch(0, lds + TM * 128, wave);
+  }
+  // the rows' labels, scales and, for G, statistics
+  float scale[CT];
+  int label[CT];
 #pragma unroll
-  for (int i = 0; i < RT; ++i)
-#pragma unroll
-    for (int j = 0; j < CT; ++j) acc[i][j] = t16_f32x4{0.f, 0.f, 0.f, 0.f};
-  Tile::run(a, b, 0, p.stages, lds, acc);
-
-  // logits: class c0 + c(i) + e, row row(j)
-  const int cw = mt * TM + 16 * RT * wm + 4 * g;      // of the piece
-  const int64_t row0 = static_cast<int64_t>(nt) * TN + 16 * CT * wn + r;
-  float by[CT];
-#pragma unroll
-  for (int j = 0; j < CT; ++j) by[j] = TYPE == kSplit ? p.row_inverse[row0 + 16 * j] * *p.w_inverse : 1.f;
-#pragma unroll
-  for (int i = 0; i < RT; ++i)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int c = p.c0 + cw + 16 * i + e;
-      const bool in = c < p.classes;
-      const float bias = in && p.bias ? p.bias[c] : 0.f;
-#pragma unroll
-      for (int j = 0; j < CT; ++j)
-        acc[i][j][e] = in ? (TYPE == kSplit ? fmaf(acc[i][j][e], by[j], bias) : acc[i][j][e] + bias) : -INFINITY;
+  for (int j = 0; j < CT; ++j) {
+    scale[j] = kLog2e;
+    if constexpr (TYPE == kSplit) scale[j] *= p.row_inverse[row0 + 16 * j] * *p.w_inverse;
+    label[j] = p.labels[row0 + 16 * j];
+  }
+  float lse[CT];
+  if constexpr (MODE == kGrad) {
+    constexpr int PARTS = THREADS / TN > 0 ? THREADS / TN : 1;
+    static_assert(PARTS * TN <= THREADS || PARTS == 1, "");
+    float* part = reinterpret_cast<float*>(lds + Tile::kStage);      // (the second stage is still empty)
+    for (int q = threadIdx.x; q < PARTS * TN; q += THREADS) {
+      const int row = q % TN;
+      float top = -INFINITY, sum = 0.f;
+#pragma unroll 8
+      for (int c = q / TN; c < p.stat_chunks; c += PARTS) {
+        const float2 s = p.stats[c * p.pad_rows + tile_row + row];
+        join_stats(top, sum, s.x, s.y);
+      }
+      part[2 * q] = top;
+      part[2 * q + 1] = sum;
     }
-  if constexpr (MODE == kStats) {
-    float* top_of = reinterpret_cast<float*>(lds);               // [WM][TN]
-    float* sum_of = top_of + WM * TN;
+    __syncthreads();
+    for (int row = threadIdx.x; row < TN; row += THREADS) {
+      float top = part[2 * row], sum = part[2 * row + 1];
+#pragma unroll
+      for (int w = 1; w < PARTS; ++w) join_stats(top, sum, part[2 * (w * TN + row)], part[2 * (w * TN + row) + 1]);
+      const float l = row_lse(top, sum);
+      const bool on = p.labels[tile_row + row] >= 0 && !row_empty(top, sum);
+      row_a[row] = l;
+      row_b[row] = on ? 1.f : 0.f;
+      if (p.loss_rows && chunk == 0 && tile_row + row < p.rows)
+        p.loss_rows[tile_row + row] = on ? (l - p.label_logit[tile_row + row]) * kLn2 : 0.f;
+    }
+    __syncthreads();
 #pragma unroll
     for (int j = 0; j < CT; ++j) {
-      float top = -INFINITY;
-      const int y = p.labels[row0 + 16 * j] - p.c0 - cw;
+      const int q = 16 * (CT * wn + j) + r;
+      lse[j] = row_a[q];
+      if (row_b[q] == 0.f) label[j] = -1;
+    }
+  }
+  float top[CT], sum[CT];
 #pragma unroll
-      for (int i = 0; i < RT; ++i)
+  for (int j = 0; j < CT; ++j) {
+    top[j] = -INFINITY;
+    sum[j] = 0.f;
+  }
+  __syncthreads();
+  int at = 0;
+  for (int t = t0; t < t1; ++t) {
+    t16_f32x4 acc[RT][CT];
+    Tile::clear(acc);
+    for (int k = 0; k < p.stages; ++k) {
+      const bool last = k + 1 == p.stages;
+      // the next stage, across tiles: it is on its way while this tile's end is computed
+      if (last) at_tile(t + 1);
+      Tile::step(la, lb, last ? 0 : k + 1, !last || t + 1 < t1, lds + at * Tile::kStage, lds + (1 - at) * Tile::kStage,
+                 wave, lane, acc);
+      at = 1 - at;
+      if (!last || MODE != kStats) __syncthreads();
+    }
+    // u = z log2(e); register e of tile i: class c0 + 32 (i / 2) + 4 (i % 2) + e
+    const int cw = t * TM + 16 * RT * wm + 8 * g;       // of the piece
+    const int c0 = p.c0 + cw, whole = p.c0 + t * TM + TM <= p.classes;
+    if (p.bias) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float z = acc[i][j][e];
-          top = z > top || z != z ? z : top;
-          if (y == 16 * i + e) p.label_logit[row0 + 16 * j] = z;
+      for (int i = 0; i < RT; i += 2) {
+        float bias[8];
+        const int c = c0 + 16 * i;
+        if (whole) {
+          mx_get<16>(bias, p.bias + c);
+          mx_get<16>(bias + 4, p.bias + c + 4);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) bias[e] = c + e < p.classes ? p.bias[c + e] : 0.f;
         }
-      // (a NaN stays one: the row's loss is NaN then)
-      for (int o = 16; o < 64; o <<= 1) {
-        const float t = __shfl_xor(top, o, 64);
-        top = t > top || t != t ? t : top;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          bias[e] *= kLog2e;
+#pragma unroll
+          for (int j = 0; j < CT; ++j) acc[i + e / 4][j][e % 4] = fmaf(acc[i + e / 4][j][e % 4], scale[j], bias[e]);
+        }
       }
-      float sum = 0.f;
-      const float base = top == -INFINITY ? 0.f : top;
+    } else {
 #pragma unroll
       for (int i = 0; i < RT; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum += exp2_fast((acc[i][j][e] - base) * kLog2e);
-      for (int o = 16; o < 64; o <<= 1) sum += __shfl_xor(sum, o, 64);
+        for (int j = 0; j < CT; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][j][e] *= scale[j];
+    }
+    if (!whole) {
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (c0 + 16 * (i & ~1) + 4 * (i & 1) + e >= p.classes) {
+#pragma unroll
+            for (int j = 0; j < CT; ++j) acc[i][j][e] = -INFINITY;
+          }
+    }
+    if constexpr (MODE != kGrad) {
+#pragma unroll
+      for (int j = 0; j < CT; ++j) {
+        float most = top[j];
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) most = fmaxf(most, acc[i][j][e]);
+        const float base = most == -INFINITY ? 0.f : most;
+        float s = sum[j] * exp2_fast(top[j] - base);
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s += exp2_fast(acc[i][j][e] - base);
+        top[j] = most;
+        sum[j] = s;
+        // the label's logit, where it is one of this lane's
+        const int y = label[j] - c0;
+        if (y >= 0 && y < 16 * RT && (y & 31) < 8) {
+#pragma unroll
+          for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (y == 16 * (i & ~1) + 4 * (i & 1) + e) {
+                if constexpr (MODE == kBoth) row_label[16 * (CT * wn + j) + r] = acc[i][j][e];
+                else p.label_logit[row0 + 16 * j] = acc[i][j][e];
+              }
+        }
+      }
+    }
+    if constexpr (MODE == kBoth) {
+      // all classes are here: the lanes' and waves' statistics joined
+#pragma unroll
+      for (int j = 0; j < CT; ++j) {
+        for (int o = 16; o < 64; o <<= 1) join_stats(top[j], sum[j], __shfl_xor(top[j], o, 64), __shfl_xor(sum[j], o, 64));
+        if (g == 0) {
+          row_a[wm * TN + 16 * (CT * wn + j) + r] = top[j];
+          row_b[wm * TN + 16 * (CT * wn + j) + r] = sum[j];
+        }
+      }
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < CT; ++j) {
+        const int q = 16 * (CT * wn + j) + r;
+        float m = row_a[q], s = row_b[q];
+#pragma unroll
+        for (int w = 1; w < WM; ++w) join_stats(m, s, row_a[w * TN + q], row_b[w * TN + q]);
+        lse[j] = row_lse(m, s);
+        if (row_empty(m, s)) label[j] = -1;
+        if (wm == 0 && g == 0 && row0 + 16 * j < p.rows)
+          p.loss_rows[row0 + 16 * j] = label[j] >= 0 ? (lse[j] - row_label[q]) * kLn2 : 0.f;
+      }
+      if (!p.g) return;
+    }
+    if constexpr (MODE != kStats) {
+      float db[RT][4];
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) db[i][e] = 0.f;
+#pragma unroll
+      for (int j = 0; j < CT; ++j) {
+        const bool on = label[j] >= 0;
+        const int y = label[j] - c0;
+        const bool mine = y >= 0 && y < 16 * RT && (y & 31) < 8;
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float q = exp2_fast(acc[i][j][e] - lse[j]);
+            acc[i][j][e] = on ? q : 0.f;
+          }
+        if (mine) {
+#pragma unroll
+          for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (y == 16 * (i & ~1) + 4 * (i & 1) + e) acc[i][j][e] -= 1.f;
+        }
+        uint16_t* to = p.g + (row0 + 16 * j) * p.ldg;
+#pragma unroll
+        for (int i = 0; i < RT; i += 2) {
+          float v[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = acc[i + e / 4][j][e % 4];
+          put_split<TYPE>(to, cw + 16 * i, v, kGradScale);
+        }
+        if (p.db) {
+#pragma unroll
+          for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) db[i][e] += acc[i][j][e];
+        }
+      }
+      if (p.db) {
+        float* part = reinterpret_cast<float*>(lds + Lds::kClasses);
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float s = sum16(db[i][e]);
+            if (r == 0) part[wn * TM + 16 * RT * wm + 16 * (i & ~1) + 8 * g + 4 * (i & 1) + e] = s;
+          }
+        __syncthreads();
+        for (int q = threadIdx.x; q < TM; q += THREADS) {
+          float s = 0.f;
+#pragma unroll
+          for (int w = 0; w < WN; ++w) s += part[w * TM + q];
+          if (p.c0 + t * TM + q < p.classes) p.db[static_cast<int64_t>(nt) * p.ld_db + t * TM + q] = s;
+        }
+        __syncthreads();                                // (the next tile's sums)
+      }
+    } else {
+      __syncthreads();                                  // the next tile's first stage has arrived
+    }
+  }
+  if constexpr (MODE == kStats) {
+#pragma unroll
+    for (int j = 0; j < CT; ++j) {
+      for (int o = 16; o < 64; o <<= 1) join_stats(top[j], sum[j], __shfl_xor(top[j], o, 64), __shfl_xor(sum[j], o, 64));
       if (g == 0) {
-        top_of[wm * TN + 16 * (CT * wn + j) + r] = top;
-        sum_of[wm * TN + 16 * (CT * wn + j) + r] = sum;
+        row_a[wm * TN + 16 * (CT * wn + j) + r] = top[j];
+        row_b[wm * TN + 16 * (CT * wn + j) + r] = sum[j];
       }
     }
     __syncthreads();
-    for (int q = threadIdx.x; q < TN; q += 64 * WM * WN) {
-      float top = top_of[q];
+    for (int q = threadIdx.x; q < TN; q += THREADS) {
+      float m = row_a[q], s = row_b[q];
 #pragma unroll
-      for (int w = 1; w < WM; ++w) {
-        const float t = top_of[w * TN + q];
-        top = t > top || t != t ? t : top;
-      }
-      const float base = top == -INFINITY ? 0.f : top;
-      float sum = 0.f;
-#pragma unroll
-      for (int w = 0; w < WM; ++w) sum += sum_of[w * TN + q] * exp2_fast((top_of[w * TN + q] - base) * kLog2e);
-      p.stats[static_cast<int64_t>(mt) * p.pad_rows + static_cast<int64_t>(nt) * TN + q] = make_float2(top, sum);
-    }
-  } else {
-    float db[RT][4];
-#pragma unroll
-    for (int i = 0; i < RT; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) db[i][e] = 0.f;
-#pragma unroll
-    for (int j = 0; j < CT; ++j) {
-      const int64_t row = row0 + 16 * j;
-      const int32_t y = p.labels[row];
-      const float2 of = p.rows[row];
-#pragma unroll
-      for (int i = 0; i < RT; ++i) {
-        float v[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int c = p.c0 + cw + 16 * i + e;
-          const float q = exp2_fast((acc[i][j][e] - of.x) * kLog2e) * of.y;
-          v[e] = y < 0 ? 0.f : (c == y ? q - 1.f : q);
-          db[i][e] += v[e];
-        }
-        const int64_t at = row * p.ldg;
-        const int col = cw + 16 * i;
-        if constexpr (TYPE == kBf16) {
-          const uint32_t w[2] = {mx_bf16x2_bits(v[0], v[1]), mx_bf16x2_bits(v[2], v[3])};
-          mx_put<8, false>(p.g + at + col, w);
-        } else {
-          uint16_t hi[4], lo[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float x = v[e] * kGradScale;
-            const _Float16 h = static_cast<_Float16>(x);
-            const _Float16 l = static_cast<_Float16>(x - static_cast<float>(h));
-            hi[e] = __builtin_bit_cast(uint16_t, h);
-            lo[e] = __builtin_bit_cast(uint16_t, l);
-          }
-          uint16_t* to = p.g + at + (col / 32) * 64 + col % 32;
-          mx_put<8, false>(to, hi);
-          mx_put<8, false>(to + 32, lo);
-        }
-      }
-    }
-    if (p.db) {
-      float* part = reinterpret_cast<float*>(lds);               // [WN][TM]
-#pragma unroll
-      for (int i = 0; i < RT; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float t = sum16(db[i][e]);
-          if (r == 0) part[wn * TM + 16 * (RT * wm + i) + 4 * g + e] = t;
-        }
-      __syncthreads();
-      for (int q = threadIdx.x; q < TM; q += 64 * WM * WN) {
-        float t = 0.f;
-#pragma unroll
-        for (int w = 0; w < WN; ++w) t += part[w * TM + q];
-        if (p.c0 + mt * TM + q < p.classes) p.db[static_cast<int64_t>(nt) * p.ld_db + mt * TM + q] = t;
-      }
+      for (int w = 1; w < WM; ++w) join_stats(m, s, row_a[w * TN + q], row_b[w * TN + q]);
+      p.stats[chunk * p.pad_rows + tile_row + q] = make_float2(m, s);
     }
   }
 }
 
-// ---- the rows' statistics -------------------------------------------------
+// ---- the rows' losses, where no gradient is wanted --------------------------
 
-struct JoinRowsArgs {
-  const float2* stats;             // [tiles][pad_rows]
-  int tiles;
-  int64_t rows, pad_rows;
-  int32_t* labels;                 // a row whose logits are all -inf loses its label
-  const float* label_logit;
-  float2* out;                     // [pad_rows]
-  float* loss_rows;                // [rows]
-};
-
-// 32 rows a workgroup, the tiles of a row dealt to eight threads.
-__global__ __launch_bounds__(256) void k_join_rows(JoinRowsArgs p) {
-  __shared__ float2 lds[8][32];
-  const int q = threadIdx.x & 31, part = threadIdx.x >> 5;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * 32 + q;
+// As k_logits (kGrad) joins them, so that the loss alone has the same bits: the
+// chunks of a row dealt to PARTS threads.
+template <int PARTS>
+__global__ __launch_bounds__(256) void k_join_rows(const float2* stats, int chunks, int64_t rows, int64_t pad_rows,
+                                                   const int32_t* labels, const float* label_logit, float* loss_rows) {
+  constexpr int ROWS = 256 / PARTS;
+  __shared__ float2 lds[PARTS][ROWS];
+  const int q = threadIdx.x % ROWS, part = threadIdx.x / ROWS;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * ROWS + q;
   float top = -INFINITY, sum = 0.f;
-  auto add = [&](float2 s) {
-    const float m = s.x > top || s.x != s.x ? s.x : top;
-    const float base = m == -INFINITY ? 0.f : m;
-    sum = sum * exp2_fast((top - base) * kLog2e) + s.y * exp2_fast((s.x - base) * kLog2e);
-    top = m;
-  };
-  for (int t = part; t < p.tiles; t += 8) add(p.stats[static_cast<int64_t>(t) * p.pad_rows + row]);
+#pragma unroll 8
+  for (int c = part; c < chunks; c += PARTS) {
+    const float2 s = stats[c * pad_rows + row];
+    join_stats(top, sum, s.x, s.y);
+  }
   lds[part][q] = make_float2(top, sum);
   __syncthreads();
-  if (part) return;
-  for (int w = 1; w < 8; ++w) add(lds[w][q]);
-  const bool on = p.labels[row] >= 0 && top != -INFINITY;
-  if (!on) p.labels[row] = -1;
-  p.out[row] = make_float2(top, 1.f / sum);
-  if (row < p.rows) p.loss_rows[row] = on ? (top - p.label_logit[row]) + logf(sum) : 0.f;
+  if (part || row >= rows) return;
+#pragma unroll
+  for (int w = 1; w < PARTS; ++w) join_stats(top, sum, lds[w][q].x, lds[w][q].y);
+  loss_rows[row] = labels[row] >= 0 && !row_empty(top, sum) ? (row_lse(top, sum) - label_logit[row]) * kLn2 : 0.f;
 }
 
 // ---- products -------------------------------------------------------------
@@ -443,8 +585,8 @@ struct Product {
   int64_t ld;
   float factor;                    // result = sum factor inverse
   const float* inverse;            // or NULL
-  float* slab;                     // [splits][n][ld_slab]
-  int64_t ld_slab;
+  float* slab;                     // row i of split q at q part + i ld_slab
+  int64_t ld_slab, part;
   int more;                        // add to what the slab holds
 };
 
@@ -484,10 +626,7 @@ __device__ __forceinline__ void product_tile(const Product& p, int64_t id, char*
   a.first = static_cast<int64_t>(mt) * TM;
   b.first = static_cast<int64_t>(nt) * TN;
   t16_f32x4 acc[RT][CT];
-#pragma unroll
-  for (int i = 0; i < RT; ++i)
-#pragma unroll
-    for (int j = 0; j < CT; ++j) acc[i][j] = t16_f32x4{0.f, 0.f, 0.f, 0.f};
+  Tile::clear(acc);
   Tile::run(a, b, p.stages * split / p.splits, p.stages * (split + 1) / p.splits, lds, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, r = lane & 15;
   const int wm = wave / WN, wn = wave % WN;
@@ -506,7 +645,7 @@ __device__ __forceinline__ void product_tile(const Product& p, int64_t id, char*
         v = v * p.factor * inverse;   // (their product alone may be no normal number)
         put_four<TYPE == kBf16>(p.out, row * p.ld + col, v, p.m - col);
       } else {
-        float* to = p.slab + (split * p.n + row) * p.ld_slab + col;
+        float* to = p.slab + split * p.part + row * p.ld_slab + col;
         t16_f32x4 had = {0.f, 0.f, 0.f, 0.f};
         if (p.more) mx_get<16>(&had, to);
         v += had;
@@ -529,28 +668,39 @@ __global__ __launch_bounds__(64 * WM * WN) void k_products(Product dx, Product d
   else product_tile<TYPE, kByK, kByK, TM, TN, WM, WN>(dw, id - of_dx, lds);
 }
 
+// ---- sums that were split, and the mean ------------------------------------
+
 struct JoinArgs {
   const float* slab;               // [parts][rows][ld_slab]
   int parts;
   int64_t rows, cols, ld_slab;
   float factor;
-  const float* inverse;
+  const float* inverse;            // or NULL
   void* out;
   int64_t ld;
+  int blocks;                      // workgroups of the launch that have it
+};
+struct FinishArgs {
+  JoinArgs dx, dw, db;
+  const float* loss_rows;
+  int64_t rows;
+  float* loss;
 };
 
 // out = factor inverse times the sum of the parts, in a fixed order.
 template <bool BF16>
-__global__ __launch_bounds__(256) void k_join(JoinArgs p) {
+__device__ __forceinline__ void join_parts(const JoinArgs& p, int block) {
   const int64_t fours = (p.cols + 3) / 4, all = p.rows * fours;
   const float inverse = p.inverse ? *p.inverse : 1.f;
-  for (int64_t q = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; q < all;
-       q += static_cast<int64_t>(gridDim.x) * 256) {
+  for (int64_t q = static_cast<int64_t>(block) * 256 + threadIdx.x; q < all; q += static_cast<int64_t>(p.blocks) * 256) {
     const int64_t row = q / fours, col = (q - row * fours) * 4;
     t16_f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    const float* from = p.slab + row * p.ld_slab + col;
+    const int64_t step = p.rows * p.ld_slab;
+#pragma unroll 4
     for (int s = 0; s < p.parts; ++s) {
       t16_f32x4 x;
-      mx_get<16>(&x, p.slab + (s * p.rows + row) * p.ld_slab + col);
+      mx_get<16>(&x, from + s * step);
       v += x;
     }
     v = v * p.factor * inverse;
@@ -558,26 +708,53 @@ __global__ __launch_bounds__(256) void k_join(JoinArgs p) {
   }
 }
 
+// The last workgroup adds the rows' losses, in 64 bits and a fixed order; the
+// others join sums.
+template <bool BF16>
+__global__ __launch_bounds__(256) void k_finish(FinishArgs p) {
+  int block = blockIdx.x;
+  if (block < p.dx.blocks) return join_parts<BF16>(p.dx, block);
+  block -= p.dx.blocks;
+  if (block < p.dw.blocks) return join_parts<BF16>(p.dw, block);
+  block -= p.dw.blocks;
+  if (block < p.db.blocks) return join_parts<false>(p.db, block);
+  __shared__ double lds[4];
+  double s = 0.0;
+#pragma unroll 8
+  for (int64_t i = threadIdx.x; i < p.rows; i += 256) s += p.loss_rows[i];
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) s += __shfl_xor(s, o, 64);
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) *p.loss = static_cast<float>((((lds[0] + lds[1]) + lds[2]) + lds[3]) / static_cast<double>(p.rows));
+}
+
 // ---- plan -----------------------------------------------------------------
 
-constexpr int kTile = 128;
+// Tiles of a product: 256 x 256 (four waves of 128 x 128, one workgroup a CU) or
+// 64 x 64.
+constexpr int kLarge = 256, kSmall = 64;
 // G of a piece of the classes.
 constexpr int64_t kGradBytes = int64_t{256} << 20;
 constexpr int kMostTops = 1024;
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+int64_t tiles_of(int64_t x, int tile) { return (x + tile - 1) / tile; }
 
 struct Plan {
   int es;                          // 16-bit words of a value
-  int64_t pad_rows, pad_d;
-  bool copy_w;
+  int64_t pad_rows, pad_d, pad_classes;
+  bool copy_w, grad, both;         // both: statistics and G in one launch
   int64_t piece, pieces;           // classes of a piece (a multiple of kPadRows)
-  int m_tiles, n_tiles;            // classes (of all), rows
-  int dx_splits, dw_splits;
+  int tile;                        // of the logits
+  int chunks, piece_chunks;        // workgroups of a row tile, for the statistics and for G
+  int product_tile, dx_splits, dw_splits;
   bool dx_slab;
   int64_t ld_dw;                   // the contiguous extent of dw, padded to four
+  int64_t dw_rows, dw_cols;
   // offsets
-  size_t x_all, x_row, w, row_top, tops, row_inverse, inverses, labels, stats, label_logit, rows, loss_rows, g, db, dx_sums, dw_sums, total;
+  size_t x_all, x_row, w, row_top, tops, row_inverse, inverses, labels, stats, label_logit, loss_rows, g, db, dx_sums,
+      dw_sums, total;
 };
 
 Plan plan(const LinearLossArgs& a, int bf16) {
@@ -585,29 +762,49 @@ Plan plan(const LinearLossArgs& a, int bf16) {
   p.es = bf16 ? 1 : 2;
   p.pad_rows = round_up(a.rows, kPadRows);
   p.pad_d = round_up(a.d, kPadCols);
+  p.pad_classes = round_up(a.classes, kPadRows);
   // bf16 weights are read as they lie if their rows are whole stages
   p.copy_w = !(bf16 && a.w_col == 1 && a.d % kPadCols == 0 && a.w_row % 8 == 0 &&
                reinterpret_cast<uintptr_t>(a.w) % 16 == 0);
-  const int64_t pad_classes = round_up(a.classes, kPadRows);
-  const bool grad = a.dx || a.dw || a.db;
+  p.grad = a.dx || a.dw || a.db;
   int64_t piece = kGradBytes / (p.pad_rows * 2 * p.es) / kPadRows * kPadRows;
-  piece = piece < kPadRows ? kPadRows : (piece > pad_classes ? pad_classes : piece);
-  p.pieces = (pad_classes + piece - 1) / piece;
-  p.piece = round_up((pad_classes + p.pieces - 1) / p.pieces, kPadRows);
-  p.pieces = (pad_classes + p.piece - 1) / p.piece;
-  p.m_tiles = static_cast<int>((a.classes + kTile - 1) / kTile);
-  p.n_tiles = static_cast<int>(p.pad_rows / kTile);
-  auto splits = [&](int64_t tiles, int64_t stages) {
-    int64_t s = (2 * kComputeUnits + tiles - 1) / tiles;
-    const int64_t most = stages / 4;
-    s = s > most ? most : s;
-    return static_cast<int>(s < 1 ? 1 : s);
+  piece = piece < kPadRows ? kPadRows : (piece > p.pad_classes ? p.pad_classes : piece);
+  p.pieces = tiles_of(p.pad_classes, piece);
+  p.piece = round_up(tiles_of(p.pad_classes, p.pieces), kPadRows);
+  p.pieces = tiles_of(p.pad_classes, p.piece);
+  p.tile = tiles_of(a.rows, kLarge) * tiles_of(a.classes, kLarge) >= kComputeUnits / 2 ? kLarge : kSmall;
+  p.both = a.classes <= kSmall;
+  if (p.both) p.tile = kSmall;
+  // workgroups of a row tile: one for each CU (two for small tiles) where the
+  // classes' tiles allow
+  auto chunks = [&](int64_t classes) {
+    const int64_t n = tiles_of(a.rows, p.tile), m = tiles_of(classes, p.tile);
+    const int64_t want = (p.tile == kLarge ? 1 : 2) * kComputeUnits / n;
+    return static_cast<int>(want < 1 ? 1 : (want > m ? m : want));
   };
-  const int64_t d_tiles = (a.d + kTile - 1) / kTile, k = 64 / p.es;
-  p.dx_splits = splits(d_tiles * ((a.rows + kTile - 1) / kTile), p.piece / k);
-  p.dx_slab = p.dx_splits > 1 || p.pieces > 1;
-  p.dw_splits = splits(d_tiles * (p.piece / kTile), p.pad_rows / k);
-  p.ld_dw = round_up(a.turned ? a.classes : a.d, 4);
+  p.chunks = chunks(a.classes);
+  p.piece_chunks = chunks(p.piece < a.classes ? p.piece : a.classes);
+  const int64_t k = 64 / p.es;
+  p.dw_rows = a.turned ? a.d : a.classes;
+  p.dw_cols = a.turned ? a.classes : a.d;
+  p.ld_dw = round_up(p.dw_cols, 4);
+  {
+    const int64_t have = p.piece < a.classes ? p.piece : a.classes;
+    const int64_t dx = tiles_of(a.d, kLarge) * tiles_of(a.rows, kLarge), dw = tiles_of(a.d, kLarge) * tiles_of(have, kLarge);
+    const bool large = (dx * have / k + dw * a.rows / k) / 8 >= kComputeUnits / 2;
+    p.product_tile = large ? kLarge : kSmall;
+    const int64_t each = (large ? 1 : 2) * kComputeUnits / 2;
+    auto splits = [&](int64_t tiles, int64_t stages) {
+      int64_t s = (each + tiles - 1) / tiles;
+      const int64_t most = stages / 4;
+      s = s > most ? most : s;
+      return static_cast<int>(s < 1 ? 1 : s);
+    };
+    const int tile = p.product_tile;
+    p.dx_splits = splits(tiles_of(a.d, tile) * tiles_of(a.rows, tile), tiles_of(have, k));
+    p.dw_splits = splits(tiles_of(a.d, tile) * tiles_of(have, tile), tiles_of(a.rows, k));
+    p.dx_slab = p.dx_splits > 1 || p.pieces > 1;
+  }
   size_t at = 0;
   auto take = [&](int64_t bytes) {
     const size_t here = at;
@@ -623,15 +820,14 @@ Plan plan(const LinearLossArgs& a, int bf16) {
   p.row_inverse = bf16 ? 0 : take(p.pad_rows * 4);
   p.inverses = bf16 ? 0 : take(8);
   p.labels = take(p.pad_rows * 4);
-  p.stats = take(p.m_tiles * p.pad_rows * 8);
-  p.label_logit = take(p.pad_rows * 4);
-  p.rows = take(p.pad_rows * 8);
+  p.stats = p.both ? 0 : take(p.chunks * p.pad_rows * 8);
+  p.label_logit = p.both ? 0 : take(p.pad_rows * 4);
   p.loss_rows = take(p.pad_rows * 4);
-  if (grad) {
+  if (p.grad) {
     p.g = take(p.pad_rows * p.piece * 2 * p.es);
-    p.db = a.db ? take(static_cast<int64_t>(p.n_tiles) * pad_classes * 4) : 0;
+    p.db = a.db ? take(tiles_of(a.rows, p.tile) * p.pad_classes * 4) : 0;
     p.dx_sums = a.dx && p.dx_slab ? take(p.dx_splits * a.rows * round_up(a.d, 4) * 4) : 0;
-    p.dw_sums = a.dw && p.dw_splits > 1 ? take(p.dw_splits * (a.turned ? a.d * p.ld_dw : p.piece * p.ld_dw) * 4) : 0;
+    p.dw_sums = a.dw && p.dw_splits > 1 ? take(p.dw_splits * p.dw_rows * p.ld_dw * 4) : 0;
   }
   p.total = at;
   return p;
@@ -639,20 +835,32 @@ Plan plan(const LinearLossArgs& a, int bf16) {
 
 unsigned grid8(int64_t tiles) { return static_cast<unsigned>((tiles + 7) / 8 * 8); }
 
+template <T16Type TYPE, LogitsMode MODE>
+void launch_logits(const LogitsArgs& g, int tile, hipStream_t s) {
+  const dim3 grid(grid8(static_cast<int64_t>(g.n_tiles) * g.chunks));
+  if constexpr (MODE != kBoth) {
+    if (tile == kLarge) {
+      hipLaunchKernelGGL((k_logits<TYPE, MODE, kLarge, kLarge, 2, 4>), grid, dim3(512), 0, s, g);
+      return;
+    }
+  }
+  hipLaunchKernelGGL((k_logits<TYPE, MODE, kSmall, kSmall, 2, 2>), grid, dim3(256), 0, s, g);
+}
+
 template <T16Type TYPE, typename T>
 hipError_t run(const LinearLossArgs& a, hipStream_t s) {
   constexpr bool kLo = TYPE == kBf16;
   const Plan p = plan(a, kLo);
-  char* ws = a.ws;
-  auto at = [&](size_t off) { return ws + off; };
+  auto at = [&](size_t off) { return a.ws + off; };
+  auto floats = [&](size_t off) { return reinterpret_cast<float*>(a.ws + off); };
   uint16_t* x_all = reinterpret_cast<uint16_t*>(at(p.x_all));
   uint16_t* x_row = reinterpret_cast<uint16_t*>(at(p.x_row));
   int32_t* labels = reinterpret_cast<int32_t*>(at(p.labels));
-  float* inverses = kLo ? nullptr : reinterpret_cast<float*>(at(p.inverses));
+  float* inverses = kLo ? nullptr : floats(p.inverses);
   uint32_t* tops = kLo ? nullptr : reinterpret_cast<uint32_t*>(at(p.tops));
-  const bool w_rows = a.w_col == 1 || a.w_row != 1;    // W's rows are contiguous (or nothing is)
   int x_blocks = 0, w_blocks = 0;
   if constexpr (!kLo) {
+    const bool w_rows = a.w_col == 1 || a.w_row != 1;    // W's rows are contiguous (or nothing is)
     AmaxArgs m{};
     m.x = static_cast<const float*>(a.x);
     m.x_stride = a.x_stride;
@@ -673,11 +881,7 @@ hipError_t run(const LinearLossArgs& a, hipStream_t s) {
     m.w_blocks = w_blocks = blocks(m.w_rows);
     hipLaunchKernelGGL(k_amax, dim3(static_cast<unsigned>(x_blocks + w_blocks)), dim3(256), 0, s, m);
   }
-  auto lay_out = [&](const LayOutArgs& l) {
-    const dim3 grid(static_cast<unsigned>((l.out_rows + 63) / 64), static_cast<unsigned>(l.out_cols / 64));
-    hipLaunchKernelGGL((k_lay_out<TYPE, T>), grid, dim3(256), 0, s, l);
-  };
-  LayOutArgs l{};
+  LayOutArgs l{}, lw{};
   l.src = a.x;
   l.row = a.x_stride;
   l.col = 1;
@@ -694,13 +898,13 @@ hipError_t run(const LinearLossArgs& a, hipStream_t s) {
     l.row_top = reinterpret_cast<const uint32_t*>(at(p.row_top));
     l.tops = tops;
     l.top_count = x_blocks;
-    l.row_inverse = reinterpret_cast<float*>(at(p.row_inverse));
+    l.row_inverse = floats(p.row_inverse);
     l.all_inverse = inverses;
   }
-  lay_out(l);
   T16Side w{static_cast<const uint16_t*>(a.w), a.w_row, a.classes, static_cast<int>(p.pad_d), 0};
+  const int64_t across = p.pad_d / 64, x_tiles = p.pad_rows / 64 * across;
+  int64_t w_tiles = 0;
   if (p.copy_w) {
-    LayOutArgs lw{};
     lw.src = a.w;
     lw.row = a.w_row;
     lw.col = a.w_col;
@@ -713,73 +917,60 @@ hipError_t run(const LinearLossArgs& a, hipStream_t s) {
       lw.top_count = w_blocks;
       lw.all_inverse = inverses + 1;
     }
-    lay_out(lw);
+    w_tiles = tiles_of(a.classes, 64) * across;
     w.data = lw.by_all;
     w.ld = p.pad_d * p.es;
   }
+  // (a launch's threads fit 31 bits)
+  const int64_t most_tiles = kLaunchThreads / 512;
+  hipLaunchKernelGGL((k_lay_out<TYPE, T>), dim3(static_cast<unsigned>(x_tiles + w_tiles)), dim3(256), 0, s, l, lw, x_tiles);
   const T16Side x_by_row{x_row, p.pad_d * p.es, p.pad_rows, static_cast<int>(p.pad_d), 0};
   const T16Side x_by_all{x_all, p.pad_d * p.es, p.pad_rows, static_cast<int>(p.pad_d), 0};
   const int64_t k = 64 / p.es;                          // of a stage
   LogitsArgs g{};
   g.w = w;
   g.x = x_by_row;
-  g.stages = p.pad_d / k;
-  g.m_tiles = p.m_tiles;
-  g.n_tiles = p.n_tiles;
+  g.stages = static_cast<int>(p.pad_d / k);
+  g.m_tiles = static_cast<int>(tiles_of(a.classes, p.tile));
+  g.n_tiles = static_cast<int>(tiles_of(a.rows, p.tile));
+  g.chunks = p.chunks;
   g.classes = a.classes;
   g.bias = a.bias;
-  g.row_inverse = kLo ? nullptr : reinterpret_cast<const float*>(at(p.row_inverse));
+  g.row_inverse = kLo ? nullptr : floats(p.row_inverse);
   g.w_inverse = kLo ? nullptr : inverses + 1;
   g.labels = labels;
+  g.rows = a.rows;
   g.pad_rows = p.pad_rows;
   g.stats = reinterpret_cast<float2*>(at(p.stats));
-  g.label_logit = reinterpret_cast<float*>(at(p.label_logit));
-  g.rows = reinterpret_cast<const float2*>(at(p.rows));
-  // (a launch's threads fit 31 bits)
-  const int most = static_cast<int>((kLaunchThreads / 1024) / g.n_tiles);
-  for (int t = 0; t < p.m_tiles; t += most) {
-    g.c0 = t * kTile;
-    g.m_tiles = p.m_tiles - t < most ? p.m_tiles - t : most;
-    g.stats = reinterpret_cast<float2*>(at(p.stats)) + t * p.pad_rows;
-    hipLaunchKernelGGL((k_logits<TYPE, kStats, kTile, kTile, 2, 2>),
-                       dim3(grid8(static_cast<int64_t>(g.m_tiles) * g.n_tiles)), dim3(256), 0, s, g);
-  }
-  JoinRowsArgs j{};
-  j.stats = reinterpret_cast<const float2*>(at(p.stats));
-  j.tiles = p.m_tiles;
-  j.rows = a.rows;
-  j.pad_rows = p.pad_rows;
-  j.labels = labels;
-  j.label_logit = g.label_logit;
-  j.out = reinterpret_cast<float2*>(at(p.rows));
-  j.loss_rows = reinterpret_cast<float*>(at(p.loss_rows));
-  hipLaunchKernelGGL(k_join_rows, dim3(static_cast<unsigned>(p.pad_rows / 32)), dim3(256), 0, s, j);
-  const hipError_t e = launch_loss_mean(j.loss_rows, a.rows, a.loss, s);
-  if (e != hipSuccess || (!a.dx && !a.dw && !a.db)) return e;
-
-  const float mean = static_cast<float>((kLo ? 1.0 : 1.0 / kGradScale) / static_cast<double>(a.rows));
-  auto join = [&](const float* slab, int parts, int64_t rows, int64_t cols, int64_t ld_slab, float factor,
-                  const float* inverse, void* out, int64_t ld, bool lo) {
-    JoinArgs q{slab, parts, rows, cols, ld_slab, factor, inverse, out, ld};
-    const int64_t need = (rows * ((cols + 3) / 4) + 255) / 256;
-    const dim3 grid(static_cast<unsigned>(need < 8 * kComputeUnits ? need : 8 * kComputeUnits));
-    if (lo) hipLaunchKernelGGL(k_join<true>, grid, dim3(256), 0, s, q);
-    else hipLaunchKernelGGL(k_join<false>, grid, dim3(256), 0, s, q);
-  };
-  const int64_t pad_classes = round_up(a.classes, kPadRows), ld_dx = round_up(a.d, 4);
-  g.g = reinterpret_cast<uint16_t*>(at(p.g));
+  g.stat_chunks = p.chunks;
+  g.label_logit = floats(p.label_logit);
+  g.loss_rows = floats(p.loss_rows);
+  g.g = p.grad ? reinterpret_cast<uint16_t*>(at(p.g)) : nullptr;
   g.ldg = p.piece * p.es;
-  g.ld_db = pad_classes;
-  const int d_tiles = (a.d + kTile - 1) / kTile;
-  for (int64_t c0 = 0; c0 < a.classes; c0 += p.piece) {
+  g.ld_db = p.pad_classes;
+  if (!p.both) {
+    launch_logits<TYPE, kStats>(g, p.tile, s);
+    if (!p.grad) {
+      const auto join = p.tile == kLarge ? k_join_rows<2> : k_join_rows<4>;
+      hipLaunchKernelGGL(join, dim3(static_cast<unsigned>(p.pad_rows / (p.tile == kLarge ? 128 : 64))), dim3(256), 0, s,
+                         g.stats, p.chunks, a.rows, p.pad_rows, labels, g.label_logit, g.loss_rows);
+    }
+  }
+  const float mean = static_cast<float>((kLo ? 1.0 : 1.0 / kGradScale) / static_cast<double>(a.rows));
+  const int64_t ld_dx = round_up(a.d, 4);
+  for (int64_t c0 = 0; c0 < a.classes && (p.grad || p.both); c0 += p.piece) {
     const int64_t left = a.classes - c0, have = left < p.piece ? left : p.piece;
     g.c0 = static_cast<int>(c0);
-    g.m_tiles = static_cast<int>(round_up(have, kPadRows) / kTile);   // G's padding is written too
-    g.db = a.db ? reinterpret_cast<float*>(at(p.db)) + c0 : nullptr;
-    hipLaunchKernelGGL((k_logits<TYPE, kGrad, kTile, kTile, 2, 2>),
-                       dim3(grid8(static_cast<int64_t>(g.m_tiles) * g.n_tiles)), dim3(256), 0, s, g);
+    // (so G's padding is written as far as a stage of dx's product reads)
+    g.m_tiles = static_cast<int>(tiles_of(have, p.tile));
+    g.chunks = p.piece_chunks < g.m_tiles ? p.piece_chunks : g.m_tiles;
+    g.db = a.db ? floats(p.db) + c0 : nullptr;
+    if (p.both) launch_logits<TYPE, kBoth>(g, p.tile, s);
+    else launch_logits<TYPE, kGrad>(g, p.tile, s);
+    g.loss_rows = nullptr;
     if (!a.dx && !a.dw) continue;
-    const T16Side grad{g.g, g.ldg, p.pad_rows, static_cast<int>(p.piece), 0};
+    const T16Side grad{g.g, g.ldg, round_up(a.rows, p.tile), static_cast<int>(p.piece), 0};
+    const int tile = p.product_tile;
     Product dx{}, dw{};
     if (a.dx) {
       dx.a = w;
@@ -788,48 +979,62 @@ hipError_t run(const LinearLossArgs& a, hipStream_t s) {
       dx.b = grad;
       dx.m = a.d;
       dx.n = a.rows;
-      dx.m_tiles = d_tiles;
-      dx.n_tiles = static_cast<int>((a.rows + kTile - 1) / kTile);
+      dx.m_tiles = static_cast<int>(tiles_of(a.d, tile));
+      dx.n_tiles = static_cast<int>(tiles_of(a.rows, tile));
       dx.splits = p.dx_splits;
-      dx.stages = (have + k - 1) / k;
+      dx.stages = tiles_of(have, k);
       dx.factor = mean;
       dx.inverse = kLo ? nullptr : inverses + 1;
       dx.out = p.dx_slab ? nullptr : a.dx;
       dx.ld = a.d;
-      dx.slab = reinterpret_cast<float*>(at(p.dx_sums));
+      dx.slab = floats(p.dx_sums);
       dx.ld_slab = ld_dx;
       dx.more = c0 > 0;
     }
     if (a.dw) {
+      const int64_t skip = a.turned ? c0 : c0 * a.d;
       dw.a = a.turned ? grad : x_by_all;
       dw.b = a.turned ? x_by_all : grad;
+      dw.a.rows = dw.b.rows = grad.rows;
       dw.m = a.turned ? have : a.d;
       dw.n = a.turned ? a.d : have;
-      dw.m_tiles = static_cast<int>((dw.m + kTile - 1) / kTile);
-      dw.n_tiles = static_cast<int>((dw.n + kTile - 1) / kTile);
+      dw.m_tiles = static_cast<int>(tiles_of(dw.m, tile));
+      dw.n_tiles = static_cast<int>(tiles_of(dw.n, tile));
       dw.splits = p.dw_splits;
-      dw.stages = (a.rows + k - 1) / k;
+      dw.stages = tiles_of(a.rows, k);
       dw.factor = mean;
       dw.inverse = kLo ? nullptr : inverses;
-      const int64_t skip = a.turned ? c0 : c0 * a.d;
       dw.out = p.dw_splits > 1 ? nullptr : static_cast<T*>(a.dw) + skip;
-      dw.ld = a.turned ? a.classes : a.d;
-      dw.slab = reinterpret_cast<float*>(at(p.dw_sums));
+      dw.ld = p.dw_cols;
+      dw.slab = floats(p.dw_sums) + (a.turned ? c0 : c0 * p.ld_dw);
       dw.ld_slab = p.ld_dw;
+      dw.part = p.dw_rows * p.ld_dw;
     }
+    dx.part = dx.n * dx.ld_slab;
     const int64_t tiles = static_cast<int64_t>(dx.m_tiles) * dx.n_tiles * dx.splits +
                           static_cast<int64_t>(dw.m_tiles) * dw.n_tiles * dw.splits;
-    hipLaunchKernelGGL((k_products<TYPE, kTile, kTile, 2, 2>), dim3(grid8(tiles)), dim3(256), 0, s, dx, dw);
-    if (a.dw && p.dw_splits > 1)
-      join(dw.slab, dw.splits, dw.n, dw.m, dw.ld_slab, mean, dw.inverse,
-           static_cast<T*>(a.dw) + (a.turned ? c0 : c0 * a.d), dw.ld, kLo);
+    if (tiles > most_tiles) return hipErrorInvalidConfiguration;
+    if (tile == kLarge) hipLaunchKernelGGL((k_products<TYPE, kLarge, kLarge, 2, 4>), dim3(grid8(tiles)), dim3(512), 0, s, dx, dw);
+    else hipLaunchKernelGGL((k_products<TYPE, kSmall, kSmall, 2, 2>), dim3(grid8(tiles)), dim3(256), 0, s, dx, dw);
   }
+  FinishArgs f{};
+  auto join = [&](size_t slab, int parts, int64_t rows, int64_t cols, int64_t ld_slab, float factor, const float* inverse,
+                  void* out) {
+    const int64_t need = (rows * ((cols + 3) / 4) + 255) / 256;
+    return JoinArgs{floats(slab), parts, rows, cols, ld_slab, factor, inverse, out, cols,
+                    static_cast<int>(need < 8 * kComputeUnits ? need : 8 * kComputeUnits)};
+  };
   if (a.dx && p.dx_slab)
-    join(reinterpret_cast<const float*>(at(p.dx_sums)), p.dx_splits, a.rows, a.d, ld_dx, mean,
-         kLo ? nullptr : inverses + 1, a.dx, a.d, kLo);
+    f.dx = join(p.dx_sums, p.dx_splits, a.rows, a.d, ld_dx, mean, kLo ? nullptr : inverses + 1, a.dx);
+  if (a.dw && p.dw_splits > 1)
+    f.dw = join(p.dw_sums, p.dw_splits, p.dw_rows, p.dw_cols, p.ld_dw, mean, kLo ? nullptr : inverses, a.dw);
   if (a.db)
-    join(reinterpret_cast<const float*>(at(p.db)), p.n_tiles, 1, a.classes, pad_classes,
-         static_cast<float>(1.0 / static_cast<double>(a.rows)), nullptr, a.db, a.classes, false);
+    f.db = join(p.db, g.n_tiles, 1, a.classes, p.pad_classes, static_cast<float>(1.0 / static_cast<double>(a.rows)),
+                nullptr, a.db);
+  f.loss_rows = floats(p.loss_rows);
+  f.rows = a.rows;
+  f.loss = a.loss;
+  hipLaunchKernelGGL(k_finish<kLo>, dim3(static_cast<unsigned>(f.dx.blocks + f.dw.blocks + f.db.blocks + 1)), dim3(256), 0, s, f);
   return hipGetLastError();
 }
 

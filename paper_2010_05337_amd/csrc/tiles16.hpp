@@ -60,7 +60,10 @@ __device__ __forceinline__ void t16_load_lds(const void* g, void* l) {
 // read together over the banks.
 __device__ __forceinline__ int t16_turn(int krow) { return (krow & 3) | ((krow >> 3) & 1) << 2; }
 
-template <T16Type TYPE, T16Form FORM, int T, int WAVES>
+// DEAL (kByRow): LDS row 16 i + 4 g + e holds the tile's row 32 (i / 2) + 8 g + 4
+// (i % 2) + e, so that the registers of a lane's two neighbouring 16-row tiles
+// are eight rows in order.
+template <T16Type TYPE, T16Form FORM, int T, int WAVES, bool DEAL = false>
 struct T16Loader {
   static constexpr int LOADS = T * 8 / (64 * WAVES);
   static_assert(LOADS * 64 * WAVES == T * 8, "a stage is whole loads");
@@ -78,7 +81,8 @@ struct T16Loader {
       const int q = (i * WAVES + wave) * 64 + lane;
       if constexpr (FORM == kByRow) {
         const int row = q / 8, piece = (q % 8) ^ ((row >> 1) & 7);
-        const int64_t at = s.first + row < s.rows ? s.first + row : s.rows - 1;
+        const int of = DEAL ? (row & ~31) + (row & 12) * 2 + ((row >> 4) & 1) * 4 + (row & 3) : row;
+        const int64_t at = s.first + of < s.rows ? s.first + of : s.rows - 1;
         base[i] = reinterpret_cast<const char*>(s.data) + at * ld_bytes + piece * 16;
       } else {
         const int row = q / P, slot = q % P;
@@ -133,64 +137,85 @@ __device__ __forceinline__ t16_f32x4 t16_mfma(t16_i16x8 a, t16_i16x8 b, t16_f32x
 
 // A workgroup of WM x WN waves, a wave RT x CT tiles of 16 x 16: its rows of A
 // from 16 RT wm on, of B from 16 CT wn on.  Register e of lane (g, r) of
-// acc[i][j] is row 16 i + 4 g + e of A, row 16 j + r of B.
-template <T16Type TYPE, T16Form FA, T16Form FB, int TM, int TN, int WM, int WN>
+// acc[i][j] is row 16 i + 4 g + e of A (with DEAL, of LDS), row 16 j + r of B.
+template <T16Type TYPE, T16Form FA, T16Form FB, int TM, int TN, int WM, int WN, bool DEAL = false>
 struct T16Tile {
   static constexpr int WAVES = WM * WN, RT = TM / (16 * WM), CT = TN / (16 * WN);
   static constexpr int kStage = t16_stage_bytes<TM, TN>();
+  using LoadA = T16Loader<TYPE, FA, TM, WAVES, DEAL>;
+  using LoadB = T16Loader<TYPE, FB, TN, WAVES>;
+
+  static __device__ __forceinline__ void clear(t16_f32x4 (&acc)[RT][CT]) {
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+      for (int j = 0; j < CT; ++j) acc[i][j] = t16_f32x4{0.f, 0.f, 0.f, 0.f};
+  }
 
   // acc += the stages first .. last - 1 of k; lds: two stages.  Every wave of
   // the workgroup calls it with the same stages.
   static __device__ __forceinline__ void run(const T16Side& a, const T16Side& b, int64_t first, int64_t last, char* lds,
                                              t16_f32x4 (&acc)[RT][CT]) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
-    T16Loader<TYPE, FA, TM, WAVES> la;
-    T16Loader<TYPE, FB, TN, WAVES> lb;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    LoadA la;
+    LoadB lb;
     la.init(a, wave, lane);
     lb.init(b, wave, lane);
-    auto fetch = [&](int64_t k) {
-      char* to = lds + ((k - first) & 1) * kStage;
-      la.fetch(k, to, wave);
-      lb.fetch(k, to + TM * 128, wave);
-    };
-    if (first < last) fetch(first);
+    if (first < last) {
+      la.fetch(first, lds, wave);
+      lb.fetch(first, lds + TM * 128, wave);
+    }
     __syncthreads();
     for (int64_t k = first; k < last; ++k) {
-      const char* at = lds + ((k - first) & 1) * kStage;
-      if (k + 1 < last) fetch(k + 1);
-      if constexpr (TYPE == kBf16) {
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          t16_i16x8 qa[RT], qb[CT];
-#pragma unroll
-          for (int j = 0; j < CT; ++j) qb[j] = t16_operand<FB, TN>(at + TM * 128, 16 * (CT * wn + j), s, lane);
-#pragma unroll
-          for (int i = 0; i < RT; ++i) qa[i] = t16_operand<FA, TM>(at, 16 * (RT * wm + i), s, lane);
-#pragma unroll
-          for (int i = 0; i < RT; ++i)
-#pragma unroll
-            for (int j = 0; j < CT; ++j) acc[i][j] = t16_mfma<TYPE>(qa[i], qb[j], acc[i][j]);
-        }
-      } else {
-        t16_i16x8 bh[CT], bl[CT];
-#pragma unroll
-        for (int j = 0; j < CT; ++j) {
-          bh[j] = t16_operand<FB, TN>(at + TM * 128, 16 * (CT * wn + j), 0, lane);
-          bl[j] = t16_operand<FB, TN>(at + TM * 128, 16 * (CT * wn + j), 1, lane);
-        }
-#pragma unroll
-        for (int i = 0; i < RT; ++i) {
-          const t16_i16x8 ah = t16_operand<FA, TM>(at, 16 * (RT * wm + i), 0, lane);
-          const t16_i16x8 al = t16_operand<FA, TM>(at, 16 * (RT * wm + i), 1, lane);
-#pragma unroll
-          for (int j = 0; j < CT; ++j) acc[i][j] = t16_mfma<TYPE>(al, bh[j], acc[i][j]);
-#pragma unroll
-          for (int j = 0; j < CT; ++j) acc[i][j] = t16_mfma<TYPE>(ah, bl[j], acc[i][j]);
-#pragma unroll
-          for (int j = 0; j < CT; ++j) acc[i][j] = t16_mfma<TYPE>(ah, bh[j], acc[i][j]);
-        }
-      }
+      const int64_t at = (k - first) & 1;
+      step(la, lb, k + 1, k + 1 < last, lds + at * kStage, lds + (1 - at) * kStage, wave, lane, acc);
       __syncthreads();              // stage k is read, stage k + 1 has arrived
+    }
+  }
+
+  // acc += the stage that lies at `now`, while (with `more`) stage k comes to
+  // `next`.
+  // (The two are apart, and said to be: else the compiler lets the transposing
+  // reads of `now` wait for the loads into `next`.)
+  static __device__ __forceinline__ void step(const LoadA& la, const LoadB& lb, int64_t k, bool more,
+                                              const char* __restrict__ now, char* __restrict__ next, int wave, int lane,
+                                              t16_f32x4 (&acc)[RT][CT]) {
+    const int wm = wave / WN, wn = wave % WN;
+    if (more) {
+      la.fetch(k, next, wave);
+      lb.fetch(k, next + TM * 128, wave);
+    }
+    if constexpr (TYPE == kBf16) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        t16_i16x8 qa[RT], qb[CT];
+#pragma unroll
+        for (int j = 0; j < CT; ++j) qb[j] = t16_operand<FB, TN>(now + TM * 128, 16 * (CT * wn + j), s, lane);
+#pragma unroll
+        for (int i = 0; i < RT; ++i) qa[i] = t16_operand<FA, TM>(now, 16 * (RT * wm + i), s, lane);
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+          for (int j = 0; j < CT; ++j) acc[i][j] = t16_mfma<TYPE>(qa[i], qb[j], acc[i][j]);
+      }
+    } else {
+      t16_i16x8 bh[CT], bl[CT];
+#pragma unroll
+      for (int j = 0; j < CT; ++j) {
+        bh[j] = t16_operand<FB, TN>(now + TM * 128, 16 * (CT * wn + j), 0, lane);
+        bl[j] = t16_operand<FB, TN>(now + TM * 128, 16 * (CT * wn + j), 1, lane);
+      }
+#pragma unroll
+      for (int i = 0; i < RT; ++i) {
+        const t16_i16x8 ah = t16_operand<FA, TM>(now, 16 * (RT * wm + i), 0, lane);
+        const t16_i16x8 al = t16_operand<FA, TM>(now, 16 * (RT * wm + i), 1, lane);
+#pragma unroll
+        for (int j = 0; j < CT; ++j) acc[i][j] = t16_mfma<TYPE>(al, bh[j], acc[i][j]);
+#pragma unroll
+        for (int j = 0; j < CT; ++j) acc[i][j] = t16_mfma<TYPE>(ah, bl[j], acc[i][j]);
+#pragma unroll
+        for (int j = 0; j < CT; ++j) acc[i][j] = t16_mfma<TYPE>(ah, bh[j], acc[i][j]);
+      }
     }
   }
 };
