@@ -289,7 +289,12 @@ __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
   float* row_label = row_b + WM * TN;
   const int64_t id = xcd_id(static_cast<int64_t>(p.n_tiles) * p.chunks);
   if (id < 0) return;
-  const int nt = static_cast<int>(id % p.n_tiles), chunk = static_cast<int>(id / p.n_tiles);
+  // bands of eight row tiles: what an XCD's workgroups read together is few tiles
+  // of x and few chunks of W
+  const int band = static_cast<int>(id / (8 * static_cast<int64_t>(p.chunks)));
+  const int in_band = static_cast<int>(id - static_cast<int64_t>(band) * 8 * p.chunks);
+  const int width = p.n_tiles - 8 * band < 8 ? p.n_tiles - 8 * band : 8;
+  const int nt = 8 * band + in_band % width, chunk = in_band / width;
   const int t0 = static_cast<int>(static_cast<int64_t>(p.m_tiles) * chunk / p.chunks);
   const int t1 = static_cast<int>(static_cast<int64_t>(p.m_tiles) * (chunk + 1) / p.chunks);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, r = lane & 15;
@@ -300,14 +305,11 @@ __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
   T16Side a = p.w, b = p.x;
   b.first = tile_row;
   lb.init(b, wave, lane);
-  auto at_tile = [&](int t) {
-    a.first = p.c0 + static_cast<int64_t>(t) * TM;
-    la.init(a, wave, lane);
-  };
-  at_tile(t0);
+  a.first = p.c0 + static_cast<int64_t>(t0) * TM;
+  la.init(a, wave, lane);
   if (t0 < t1) {
-    la.fetch(0, lds, wave);
-    lb.fetch(0, lds + TM * 128, wave);
+    la.fetch(0, lds);
+    lb.fetch(0, lds + TM * 128);
   }
   // the rows' labels, scales and, for G, statistics
   float scale[CT];
@@ -368,51 +370,34 @@ __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
     for (int k = 0; k < p.stages; ++k) {
       const bool last = k + 1 == p.stages;
       // the next stage, across tiles: it is on its way while this tile's end is computed
-      if (last) at_tile(t + 1);
+      if (last) la.advance();
       Tile::step(la, lb, last ? 0 : k + 1, !last || t + 1 < t1, lds + at * Tile::kStage, lds + (1 - at) * Tile::kStage,
                  wave, lane, acc);
       at = 1 - at;
       if (!last || MODE != kStats) __syncthreads();
     }
-    // u = z log2(e); register e of tile i: class c0 + 32 (i / 2) + 4 (i % 2) + e
+    // u = z log2(e), in place; the registers of tiles i and i + 1 (i even) are
+    // classes c0 + 16 i .. + 7, -inf past the last class
     const int cw = t * TM + 16 * RT * wm + 8 * g;       // of the piece
-    const int c0 = p.c0 + cw, whole = p.c0 + t * TM + TM <= p.classes;
-    if (p.bias) {
+    const int c0 = p.c0 + cw;
+    const bool whole = p.c0 + t * TM + TM <= p.classes;
 #pragma unroll
-      for (int i = 0; i < RT; i += 2) {
-        float bias[8];
-        const int c = c0 + 16 * i;
-        if (whole) {
-          mx_get<16>(bias, p.bias + c);
-          mx_get<16>(bias + 4, p.bias + c + 4);
-        } else {
+    for (int i = 0; i < RT; i += 2) {
+      float bias[8] = {};
+      const int c = c0 + 16 * i;
+      if (p.bias && whole) {
+        mx_get<16>(bias, p.bias + c);
+        mx_get<16>(bias + 4, p.bias + c + 4);
+      } else if (!whole) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) bias[e] = c + e < p.classes ? p.bias[c + e] : 0.f;
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          bias[e] *= kLog2e;
-#pragma unroll
-          for (int j = 0; j < CT; ++j) acc[i + e / 4][j][e % 4] = fmaf(acc[i + e / 4][j][e % 4], scale[j], bias[e]);
-        }
+        for (int e = 0; e < 8; ++e) bias[e] = c + e >= p.classes ? -INFINITY : (p.bias ? p.bias[c + e] : 0.f);
       }
-    } else {
 #pragma unroll
-      for (int i = 0; i < RT; ++i)
+      for (int e = 0; e < 8; ++e) {
+        bias[e] *= kLog2e;
 #pragma unroll
-        for (int j = 0; j < CT; ++j)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[i][j][e] *= scale[j];
-    }
-    if (!whole) {
-#pragma unroll
-      for (int i = 0; i < RT; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (c0 + 16 * (i & ~1) + 4 * (i & 1) + e >= p.classes) {
-#pragma unroll
-            for (int j = 0; j < CT; ++j) acc[i][j][e] = -INFINITY;
-          }
+        for (int j = 0; j < CT; ++j) acc[i + e / 4][j][e % 4] = fmaf(acc[i + e / 4][j][e % 4], scale[j], bias[e]);
+      }
     }
     if constexpr (MODE != kGrad) {
 #pragma unroll
@@ -433,14 +418,13 @@ __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
         // the label's logit, where it is one of this lane's
         const int y = label[j] - c0;
         if (y >= 0 && y < 16 * RT && (y & 31) < 8) {
+          float z = 0.f;
 #pragma unroll
           for (int i = 0; i < RT; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (y == 16 * (i & ~1) + 4 * (i & 1) + e) {
-                if constexpr (MODE == kBoth) row_label[16 * (CT * wn + j) + r] = acc[i][j][e];
-                else p.label_logit[row0 + 16 * j] = acc[i][j][e];
-              }
+            for (int e = 0; e < 4; ++e) z = y == 16 * (i & ~1) + 4 * (i & 1) + e ? acc[i][j][e] : z;
+          if constexpr (MODE == kBoth) row_label[16 * (CT * wn + j) + r] = z;
+          else p.label_logit[row0 + 16 * j] = z;
         }
       }
     }
@@ -469,54 +453,36 @@ __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
       if (!p.g) return;
     }
     if constexpr (MODE != kStats) {
-      float db[RT][4];
+      float* part = reinterpret_cast<float*>(lds + Lds::kClasses);
 #pragma unroll
-      for (int i = 0; i < RT; ++i)
+      for (int i = 0; i < RT; i += 2) {
+        float db[8] = {};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) db[i][e] = 0.f;
-#pragma unroll
-      for (int j = 0; j < CT; ++j) {
-        const bool on = label[j] >= 0;
-        const int y = label[j] - c0;
-        const bool mine = y >= 0 && y < 16 * RT && (y & 31) < 8;
-#pragma unroll
-        for (int i = 0; i < RT; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float q = exp2_fast(acc[i][j][e] - lse[j]);
-            acc[i][j][e] = on ? q : 0.f;
-          }
-        if (mine) {
-#pragma unroll
-          for (int i = 0; i < RT; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (y == 16 * (i & ~1) + 4 * (i & 1) + e) acc[i][j][e] -= 1.f;
-        }
-        uint16_t* to = p.g + (row0 + 16 * j) * p.ldg;
-#pragma unroll
-        for (int i = 0; i < RT; i += 2) {
+        for (int j = 0; j < CT; ++j) {
           float v[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = acc[i + e / 4][j][e % 4];
-          put_split<TYPE>(to, cw + 16 * i, v, kGradScale);
+          for (int e = 0; e < 8; ++e) {
+            const float q = exp2_fast(acc[i + e / 4][j][e % 4] - lse[j]);
+            v[e] = label[j] >= 0 ? q : 0.f;
+          }
+          const int y = label[j] - c0 - 16 * i;
+          if (y >= 0 && y < 8) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] -= y == e ? 1.f : 0.f;
+          }
+          put_split<TYPE>(p.g + (row0 + 16 * j) * p.ldg, cw + 16 * i, v, kGradScale);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) db[e] += v[e];
         }
         if (p.db) {
 #pragma unroll
-          for (int i = 0; i < RT; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) db[i][e] += acc[i][j][e];
+          for (int e = 0; e < 8; ++e) {
+            const float s = sum16(db[e]);
+            if (r == 0) part[wn * TM + 16 * RT * wm + 16 * i + 8 * g + e] = s;
+          }
         }
       }
       if (p.db) {
-        float* part = reinterpret_cast<float*>(lds + Lds::kClasses);
-#pragma unroll
-        for (int i = 0; i < RT; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float s = sum16(db[i][e]);
-            if (r == 0) part[wn * TM + 16 * RT * wm + 16 * (i & ~1) + 8 * g + 4 * (i & 1) + e] = s;
-          }
         __syncthreads();
         for (int q = threadIdx.x; q < TM; q += THREADS) {
           float s = 0.f;
@@ -590,6 +556,10 @@ struct Product {
   int more;                        // add to what the slab holds
 };
 
+__host__ __device__ inline int64_t product_tiles(const Product& p) {
+  return static_cast<int64_t>(p.m_tiles) * p.n_tiles * p.splits;
+}
+
 // Four contiguous values of a row, `left` of them.
 template <bool BF16>
 __device__ __forceinline__ void put_four(void* out, int64_t at, t16_f32x4 v, int64_t left) {
@@ -660,12 +630,17 @@ __device__ __forceinline__ void product_tile(const Product& p, int64_t id, char*
 template <T16Type TYPE, int TM, int TN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void k_products(Product dx, Product dw) {
   __shared__ __attribute__((aligned(1024))) char lds[2 * t16_stage_bytes<TM, TN>()];
-  const int64_t of_dx = static_cast<int64_t>(dx.m_tiles) * dx.n_tiles * dx.splits;
-  const int64_t of_dw = static_cast<int64_t>(dw.m_tiles) * dw.n_tiles * dw.splits;
-  const int64_t id = xcd_id(of_dx + of_dw);
-  if (id < 0) return;
-  if (id < of_dx) product_tile<TYPE, kByK, kByRow, TM, TN, WM, WN>(dx, id, lds);
-  else product_tile<TYPE, kByK, kByK, TM, TN, WM, WN>(dw, id - of_dx, lds);
+  // workgroup ids go round the eight XCDs: each has an eighth of either product
+  const int64_t of_dx = product_tiles(dx), of_dw = product_tiles(dw);
+  const int64_t dx_each = (of_dx + 7) / 8, dw_each = (of_dw + 7) / 8, xcd = blockIdx.x & 7;
+  int64_t id = blockIdx.x >> 3;
+  if (id < dx_each) {
+    id += xcd * dx_each;
+    if (id < of_dx) product_tile<TYPE, kByK, kByRow, TM, TN, WM, WN>(dx, id, lds);
+  } else if (id < dx_each + dw_each) {
+    id += xcd * dw_each - dx_each;
+    if (id < of_dw) product_tile<TYPE, kByK, kByK, TM, TN, WM, WN>(dw, id, lds);
+  }
 }
 
 // ---- sums that were split, and the mean ------------------------------------
@@ -764,7 +739,7 @@ Plan plan(const LinearLossArgs& a, int bf16) {
   p.pad_d = round_up(a.d, kPadCols);
   p.pad_classes = round_up(a.classes, kPadRows);
   // bf16 weights are read as they lie if their rows are whole stages
-  p.copy_w = !(bf16 && a.w_col == 1 && a.d % kPadCols == 0 && a.w_row % 8 == 0 &&
+  p.copy_w = !(bf16 && a.w_col == 1 && a.d % kPadCols == 0 && a.w_row % 8 == 0 && a.w_row * 2 <= kT16MostBytes &&
                reinterpret_cast<uintptr_t>(a.w) % 16 == 0);
   p.grad = a.dx || a.dw || a.db;
   int64_t piece = kGradBytes / (p.pad_rows * 2 * p.es) / kPadRows * kPadRows;
@@ -1011,8 +986,7 @@ hipError_t run(const LinearLossArgs& a, hipStream_t s) {
       dw.part = p.dw_rows * p.ld_dw;
     }
     dx.part = dx.n * dx.ld_slab;
-    const int64_t tiles = static_cast<int64_t>(dx.m_tiles) * dx.n_tiles * dx.splits +
-                          static_cast<int64_t>(dw.m_tiles) * dw.n_tiles * dw.splits;
+    const int64_t tiles = round_up(product_tiles(dx), 8) + round_up(product_tiles(dw), 8);
     if (tiles > most_tiles) return hipErrorInvalidConfiguration;
     if (tile == kLarge) hipLaunchKernelGGL((k_products<TYPE, kLarge, kLarge, 2, 4>), dim3(grid8(tiles)), dim3(512), 0, s, dx, dw);
     else hipLaunchKernelGGL((k_products<TYPE, kSmall, kSmall, 2, 2>), dim3(grid8(tiles)), dim3(256), 0, s, dx, dw);

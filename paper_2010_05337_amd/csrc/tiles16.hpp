@@ -58,54 +58,91 @@ __device__ __forceinline__ void t16_load_lds(const void* g, void* l) {
 // % 8); kByK 64 rows of T columns (kSplit: the hi parts of 32 of k, then the lo
 // parts), pairs of pieces exchanged by t16_turn.  Both spread the rows that are
 // read together over the banks.
-__device__ __forceinline__ int t16_turn(int krow) { return (krow & 3) | ((krow >> 3) & 1) << 2; }
-
+//
+// An address is a part that the whole wave has (scalar registers) and a lane's
+// offset of 32 bits, the same for every tile and stage but those at the end
+// (64-bit addresses of eight loads took 16 registers more, which spilled): a
+// side's rows are at most 2^31 / 256 bytes apart.
+//
 // DEAL (kByRow): LDS row 16 i + 4 g + e holds the tile's row 32 (i / 2) + 8 g + 4
 // (i % 2) + e, so that the registers of a lane's two neighbouring 16-row tiles
 // are eight rows in order.
+constexpr int64_t kT16MostBytes = (int64_t{1} << 31) / 256;
+__device__ __forceinline__ int t16_turn(int krow) { return (krow & 3) | ((krow >> 3) & 1) << 2; }
+
 template <T16Type TYPE, T16Form FORM, int T, int WAVES, bool DEAL = false>
 struct T16Loader {
   static constexpr int LOADS = T * 8 / (64 * WAVES);
   static_assert(LOADS * 64 * WAVES == T * 8, "a stage is whole loads");
   static constexpr int KROWS = TYPE == kSplit ? 32 : 64;
   static constexpr int P = T / 8;           // pieces of a row of k
-  const char* base[LOADS];                  // kByRow: the row's address; kByK: the column's in row 0
-  int krow[LOADS];
-  int64_t ld_bytes, rows;
+  const char* base;                         // the tile's first row, or its first row of k
+  uint32_t off[LOADS];
+  uint32_t ld_bytes;
+  int64_t rows;                             // kByRow: from the tile's first on; kByK: of k
+  int wave, lane;
 
-  __device__ __forceinline__ void init(const T16Side& s, int wave, int lane) {
-    ld_bytes = s.ld * 2;
-    rows = s.rows;
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const int q = (i * WAVES + wave) * 64 + lane;
-      if constexpr (FORM == kByRow) {
-        const int row = q / 8, piece = (q % 8) ^ ((row >> 1) & 7);
-        const int of = DEAL ? (row & ~31) + (row & 12) * 2 + ((row >> 4) & 1) * 4 + (row & 3) : row;
-        const int64_t at = s.first + of < s.rows ? s.first + of : s.rows - 1;
-        base[i] = reinterpret_cast<const char*>(s.data) + at * ld_bytes + piece * 16;
-      } else {
-        const int row = q / P, slot = q % P;
-        const int chunk = (slot >> 1) ^ (t16_turn(row) & (P / 2 - 1));
-        int64_t col = s.first + (chunk * 2 + (slot & 1)) * 8;
-        if (col >= s.cols) col = 0;
-        krow[i] = TYPE == kSplit ? row & 31 : row;
-        const int64_t in_row = TYPE == kSplit ? (col / 32) * 128 + (row >> 5) * 64 + (col % 32) * 2 : col * 2;
-        base[i] = reinterpret_cast<const char*>(s.data) + in_row;
-      }
+  // Load i's row (kByRow) or row of k in a stage, and the offset in it.
+  __device__ __forceinline__ int row_of(int i) const {
+    const int q = (i * WAVES + wave) * 64 + lane;
+    if constexpr (FORM == kByRow) {
+      const int row = q / 8;
+      return DEAL ? (row & ~31) + (row & 12) * 2 + ((row >> 4) & 1) * 4 + (row & 3) : row;
+    } else {
+      const int row = q / P;
+      return TYPE == kSplit ? row & 31 : row;
     }
   }
-  // stage k into the side's half of an LDS stage
-  __device__ __forceinline__ void fetch(int64_t k, char* lds, int wave) const {
+  __device__ __forceinline__ uint32_t in_row(int i, const T16Side& s) const {
+    const int q = (i * WAVES + wave) * 64 + lane;
+    if constexpr (FORM == kByRow) {
+      return ((q % 8) ^ ((q >> 4) & 7)) * 16;
+    } else {
+      const int row = q / P, slot = q % P;
+      const int chunk = (slot >> 1) ^ (t16_turn(row) & (P / 2 - 1));
+      int64_t col = s.first + (chunk * 2 + (slot & 1)) * 8;
+      if (col >= s.cols) col = 0;
+      return static_cast<uint32_t>(TYPE == kSplit ? (col / 32) * 128 + (row >> 5) * 64 + (col % 32) * 2 : col * 2);
+    }
+  }
+  __device__ __forceinline__ void init(const T16Side& s, int wave_, int lane_) {
+    wave = wave_;
+    lane = lane_;
+    ld_bytes = static_cast<uint32_t>(s.ld * 2);
+    rows = FORM == kByRow ? s.rows - s.first : s.rows;
+    base = reinterpret_cast<const char*>(s.data) + (FORM == kByRow ? s.first * s.ld * 2 : 0);
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) off[i] = row_of(i) * ld_bytes + in_row(i, s);
+    if (FORM == kByRow && rows < T) clamp();
+  }
+  // kByRow: rows past the end
+  __device__ __forceinline__ void clamp() {
+    const int last = rows < 1 ? 0 : static_cast<int>(rows) - 1;
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      char* to = lds + (i * WAVES + wave) * 1024;
-      if constexpr (FORM == kByRow) {
-        t16_load_lds(base[i] + k * 128, to);
-      } else {
-        const int64_t row = k * KROWS + krow[i];
-        t16_load_lds(base[i] + (row < rows ? row : rows - 1) * ld_bytes, to);
+      const int row = row_of(i);
+      if (row > last) off[i] -= (row - last) * ld_bytes;
+    }
+  }
+  // kByRow: the next T rows (only forwards; past the end nothing may be fetched)
+  __device__ __forceinline__ void advance() {
+    base += static_cast<int64_t>(T) * ld_bytes;
+    rows -= T;
+    if (rows < T && rows > 0) clamp();
+  }
+  // stage k into the side's half of an LDS stage
+  __device__ __forceinline__ void fetch(int64_t k, char* lds) const {
+    const char* from = base + k * (FORM == kByRow ? 128 : static_cast<int64_t>(KROWS) * ld_bytes);
+    if (FORM == kByK && (k + 1) * KROWS > rows) {
+      const int last = static_cast<int>(rows - 1 - k * KROWS);    // (of this stage: 0 at least)
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int row = row_of(i);
+        t16_load_lds(from + (row > last ? off[i] - (row - last) * ld_bytes : off[i]), lds + (i * WAVES + wave) * 1024);
       }
+    } else {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) t16_load_lds(from + off[i], lds + (i * WAVES + wave) * 1024);
     }
   }
 };
@@ -162,8 +199,8 @@ struct T16Tile {
     la.init(a, wave, lane);
     lb.init(b, wave, lane);
     if (first < last) {
-      la.fetch(first, lds, wave);
-      lb.fetch(first, lds + TM * 128, wave);
+      la.fetch(first, lds);
+      lb.fetch(first, lds + TM * 128);
     }
     __syncthreads();
     for (int64_t k = first; k < last; ++k) {
@@ -182,11 +219,13 @@ struct T16Tile {
                                               t16_f32x4 (&acc)[RT][CT]) {
     const int wm = wave / WN, wn = wave % WN;
     if (more) {
-      la.fetch(k, next, wave);
-      lb.fetch(k, next + TM * 128, wave);
+      la.fetch(k, next);
+      lb.fetch(k, next + TM * 128);
     }
     if constexpr (TYPE == kBf16) {
-#pragma unroll
+      // (unrolled, the operands of both halves would be held at once: with large
+      // tiles that spills)
+#pragma unroll RT * CT >= 32 ? 1 : 2
       for (int s = 0; s < 2; ++s) {
         t16_i16x8 qa[RT], qb[CT];
 #pragma unroll
