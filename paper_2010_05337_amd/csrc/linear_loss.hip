@@ -20,6 +20,8 @@
 #include "mx_kernels.hpp"
 #include "tiles16.hpp"
 
+#include <algorithm>
+
 namespace gmb {
 
 namespace {
@@ -61,12 +63,14 @@ struct AmaxArgs {
   const float* w;                  // w_rows rows of w_cols values, w_col apart
   int64_t w_stride, w_col, w_rows;
   int w_cols;
+  int64_t w_all;                   // values in all if they lie one behind the other, or 0
   uint32_t* w_top;                 // [w_blocks]
   int x_blocks, w_blocks;
 };
 
 // The largest finite magnitudes: of every row of x and of all of them (a word a
-// workgroup), and of W (a word a workgroup).
+// workgroup), and of W (a word a workgroup).  A wave has a row (W, if its rows
+// lie one behind the other: a piece of the whole), 16 bytes a lane.
 __global__ __launch_bounds__(256) void k_amax(AmaxArgs p) {
   __shared__ uint32_t lds[4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -75,14 +79,31 @@ __global__ __launch_bounds__(256) void k_amax(AmaxArgs p) {
   const float* data = of_x ? p.x : p.w;
   const int64_t rows = of_x ? p.rows : p.w_rows, stride = of_x ? p.x_stride : p.w_stride;
   const int64_t col = of_x ? 1 : p.w_col;
-  const int cols = of_x ? p.d : p.w_cols;
   uint32_t all = 0;
   for (int64_t row = static_cast<int64_t>(block) * 4 + wave; row < rows; row += static_cast<int64_t>(blocks) * 4) {
     uint32_t top = 0;
+    int cols = of_x ? p.d : p.w_cols;
+    if (!of_x && p.w_all && p.w_all - row * stride < cols) cols = static_cast<int>(p.w_all - row * stride);
     if (!of_x || has_label(p.labels, row, p.classes)) {
-      for (int c = lane; c < cols; c += 64) {
-        const uint32_t u = finite_bits(data[row * stride + c * col]);
-        top = u > top ? u : top;
+      const float* from = data + row * stride;
+      int c = 4 * lane;
+      if (col == 1) {
+#pragma unroll 4
+        for (; c + 4 <= cols; c += 256) {
+          float v[4];
+          mx_get<16>(v, from + c);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t u = finite_bits(v[i]);
+            top = u > top ? u : top;
+          }
+        }
+      }
+      for (; c < cols; c += 256) {
+        for (int i = 0; i < 4 && c + i < cols; ++i) {
+          const uint32_t u = finite_bits(from[(c + i) * col]);
+          top = u > top ? u : top;
+        }
       }
     }
     if (of_x) {
@@ -149,9 +170,9 @@ __device__ __forceinline__ void put_split(uint16_t* row, int c, const float (&v)
   }
 }
 
-// A 64 x 64 tile of the source through LDS, read along whichever of its
-// directions is contiguous, written as rows.
-// (The first `first` workgroups lay out x, the others W.)
+// A 64 x 64 tile of the source: rows with contiguous columns eight values a
+// thread; else through LDS, read along the direction that is contiguous.  (The
+// first `first` workgroups lay out x, the others W.)
 template <T16Type TYPE, typename T>
 __global__ __launch_bounds__(256) void k_lay_out(LayOutArgs x, LayOutArgs w, int64_t first) {
   __shared__ float tile[64][65];
@@ -163,18 +184,58 @@ __global__ __launch_bounds__(256) void k_lay_out(LayOutArgs x, LayOutArgs w, int
   const int64_t r0 = id / across * 64;
   const int c0 = static_cast<int>(id % across) * 64;
   const T* src = static_cast<const T*>(p.src);
-  const int fast = threadIdx.x & 63, slow = threadIdx.x >> 6;
-  const bool along_rows = p.col == 1 || p.row != 1;   // neighbouring threads: neighbouring columns
-#pragma unroll 4
-  for (int k = 0; k < 16; ++k) {
-    const int i = along_rows ? 4 * k + slow : fast, j = along_rows ? fast : 4 * k + slow;
-    float v = 0.f;
-    if (r0 + i < p.rows && c0 + j < p.cols && (!p.labels || has_label(p.labels, r0 + i, p.classes))) {
-      const T x = src[(r0 + i) * p.row + (c0 + j) * p.col];
-      if constexpr (sizeof(T) == 4) v = x;
-      else v = bf16_to_f32(x);
+  const bool direct = p.col == 1;
+  float v[2][8];
+  bool on[2];
+  if (direct) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int64_t row = r0 + 32 * k + (threadIdx.x >> 3);
+      const int c = c0 + (threadIdx.x & 7) * 8, left = p.cols - c;
+      on[k] = row < p.rows && (!p.labels || has_label(p.labels, row, p.classes));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[k][i] = 0.f;
+      if (row >= p.rows || left <= 0) continue;     // (a row without a label is read and thrown away)
+      const T* from = src + row * p.row + c;
+      if constexpr (sizeof(T) == 4) {
+        if (left >= 8) {
+          mx_get<16>(v[k], from);
+          mx_get<16>(v[k] + 4, from + 4);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 7; ++i)
+            if (i < left) v[k][i] = from[i];
+        }
+      } else {
+        if (left >= 8) {
+          uint32_t q[4];
+          mx_get<16>(q, from);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            v[k][2 * i] = __uint_as_float(q[i] << 16);
+            v[k][2 * i + 1] = __uint_as_float(q[i] & 0xFFFF0000u);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 7; ++i)
+            if (i < left) v[k][i] = bf16_to_f32(from[i]);
+        }
+      }
     }
-    tile[i][j] = v;
+  } else {
+    const int fast = threadIdx.x & 63, slow = threadIdx.x >> 6;
+    const bool along_rows = p.row != 1;                // neighbouring threads: neighbouring columns
+#pragma unroll 4
+    for (int k = 0; k < 16; ++k) {
+      const int i = along_rows ? 4 * k + slow : fast, j = along_rows ? fast : 4 * k + slow;
+      float z = 0.f;
+      if (r0 + i < p.rows && c0 + j < p.cols) {
+        const T q = src[(r0 + i) * p.row + (c0 + j) * p.col];
+        if constexpr (sizeof(T) == 4) z = q;
+        else z = bf16_to_f32(q);
+      }
+      tile[i][j] = z;
+    }
   }
   float scale = 1.f;
   if constexpr (TYPE == kSplit) {
@@ -187,10 +248,10 @@ __global__ __launch_bounds__(256) void k_lay_out(LayOutArgs x, LayOutArgs w, int
     }
     if ((threadIdx.x & 63) == 0) top_of[threadIdx.x >> 6] = top;
     __syncthreads();
-    for (int w = 0; w < 4; ++w) top = top_of[w] > top ? top_of[w] : top;
+    for (int w4 = 0; w4 < 4; ++w4) top = top_of[w4] > top ? top_of[w4] : top;
     scale = split_scale(top);
     if (id == 0 && threadIdx.x == 0) *p.all_inverse = inverse_of_power(scale);
-  } else {
+  } else if (!direct) {
     __syncthreads();
   }
   const int64_t ld = TYPE == kSplit ? 2 * static_cast<int64_t>(p.out_cols) : p.out_cols;
@@ -199,18 +260,21 @@ __global__ __launch_bounds__(256) void k_lay_out(LayOutArgs x, LayOutArgs w, int
     const int i = 32 * k + (threadIdx.x >> 3), j = (threadIdx.x & 7) * 8;
     const int64_t row = r0 + i;
     if (row >= p.out_rows) continue;
-    float v[8];
+    if (!direct) {
+      on[k] = true;                                    // (W: no labels)
 #pragma unroll
-    for (int q = 0; q < 8; ++q) v[q] = tile[i][j + q];
-    put_split<TYPE>(p.by_all + row * ld, c0 + j, v, scale);
+      for (int q = 0; q < 8; ++q) v[k][q] = tile[i][j + q];
+    }
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[k][q] = on[k] ? v[k][q] : 0.f;
+    put_split<TYPE>(p.by_all + row * ld, c0 + j, v[k], scale);
     const bool lead = c0 == 0 && j == 0;
     if (TYPE == kSplit && p.by_row) {
       const float s = split_scale(row < p.rows ? p.row_top[row] : 0u);
-      put_split<TYPE>(p.by_row + row * ld, c0 + j, v, s);
+      put_split<TYPE>(p.by_row + row * ld, c0 + j, v[k], s);
       if (lead) p.row_inverse[row] = inverse_of_power(s);
     }
-    if (lead && p.labels)
-      p.kept_labels[row] = row < p.rows && has_label(p.labels, row, p.classes) ? p.labels[row] : -1;
+    if (lead && p.labels) p.kept_labels[row] = on[k] ? p.labels[row] : -1;
   }
 }
 
@@ -768,16 +832,44 @@ Plan plan(const LinearLossArgs& a, int bf16) {
     const int64_t dx = tiles_of(a.d, kLarge) * tiles_of(a.rows, kLarge), dw = tiles_of(a.d, kLarge) * tiles_of(have, kLarge);
     const bool large = (dx * have / k + dw * a.rows / k) / 8 >= kComputeUnits / 2;
     p.product_tile = large ? kLarge : kSmall;
-    const int64_t each = (large ? 1 : 2) * kComputeUnits / 2;
-    auto splits = [&](int64_t tiles, int64_t stages) {
-      int64_t s = (each + tiles - 1) / tiles;
-      const int64_t most = stages / 4;
-      s = s > most ? most : s;
-      return static_cast<int>(s < 1 ? 1 : s);
-    };
     const int tile = p.product_tile;
-    p.dx_splits = splits(tiles_of(a.d, tile) * tiles_of(a.rows, tile), tiles_of(have, k));
-    p.dw_splits = splits(tiles_of(a.d, tile) * tiles_of(have, tile), tiles_of(a.rows, k));
+    const int64_t dx_stages = tiles_of(have, k), dw_stages = tiles_of(a.rows, k);
+    const int64_t dx_tiles = a.dx ? tiles_of(a.d, tile) * tiles_of(a.rows, tile) : 0;
+    const int64_t dw_tiles = a.dw ? tiles_of(a.d, tile) * tiles_of(have, tile) : 0;
+    const int64_t slots = (large ? 1 : 4) * kComputeUnits / 8;   // of an XCD
+    auto most_splits = [](int64_t stages) { return stages < 8 ? int64_t{1} : stages / 4; };
+    // The numbers of splits that let an XCD's workgroups end soonest.  Its tiles:
+    // an eighth of dx's first, each `long_` stages, then dw's; done in t if what
+    // fits until then is enough.  A tile of sums that were split is stored (worth
+    // `slab` stages there) and joined (1 / 20 of a stage of the whole GPU).
+    const int64_t slab = large ? 12 : 3;
+    double best = -1.0;
+    p.dx_splits = p.dw_splits = 1;
+    for (int sw = 1; sw <= 64 && sw <= most_splits(dw_stages) && dw_tiles * (sw / 2) < 8 * slots; sw *= 2) {
+      const int64_t short_ = tiles_of(dw_stages, sw) + (sw > 1 ? slab : 0), shorts = tiles_of(dw_tiles * sw, 8);
+      for (int sx = 1; sx <= 64 && sx <= most_splits(dx_stages) && dx_tiles * (sx - 1) < 8 * slots; sx += sx < 8 ? 1 : sx / 4) {
+        const bool sums = sx > 1 || p.pieces > 1;
+        const int64_t long_ = tiles_of(dx_stages, sx) + (sums ? slab : 0), longs = tiles_of(dx_tiles * sx, 8);
+        const int64_t rounds = longs / slots, more = longs % slots;
+        auto fits = [&](int64_t t) {
+          const int64_t a0 = t - rounds * long_, a1 = a0 - long_;
+          if (a0 < 0 || (more && a1 < 0)) return false;
+          return (slots - more) * (a0 / short_) + (more ? more * (a1 / short_) : 0) >= shorts;
+        };
+        int64_t lo = (rounds + (more ? 1 : 0)) * long_, hi = lo + (shorts / slots + 2) * short_;
+        while (lo < hi) {
+          const int64_t mid = (lo + hi) / 2;
+          if (fits(mid)) hi = mid;
+          else lo = mid + 1;
+        }
+        const double cost = static_cast<double>(lo) + ((sw > 1 ? dw_tiles * sw : 0) + (sx > 1 ? dx_tiles * sx : 0)) / 20.0;
+        if (best < 0 || cost < best) {
+          best = cost;
+          p.dx_splits = sx;
+          p.dw_splits = sw;
+        }
+      }
+    }
     p.dx_slab = p.dx_splits > 1 || p.pieces > 1;
   }
   size_t at = 0;
@@ -851,6 +943,14 @@ hipError_t run(const LinearLossArgs& a, hipStream_t s) {
     m.w_rows = w_rows ? a.classes : a.d;
     m.w_cols = w_rows ? a.d : a.classes;
     m.w_top = tops + kMostTops;
+    if (m.w_col == 1 && m.w_stride == m.w_cols) {
+      // one behind the other: in rows of 1,024 values, and the rest as one more
+      const int64_t all = m.w_rows * m.w_cols;
+      m.w_cols = static_cast<int>(all < 1024 ? all : 1024);
+      m.w_stride = m.w_cols;
+      m.w_rows = tiles_of(all, m.w_cols);
+      m.w_all = all;
+    }
     auto blocks = [](int64_t rows) { return static_cast<int>(rows < 4 * kMostTops ? (rows + 3) / 4 : kMostTops); };
     m.x_blocks = x_blocks = blocks(a.rows);
     m.w_blocks = w_blocks = blocks(m.w_rows);
