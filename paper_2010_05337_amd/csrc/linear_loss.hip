@@ -282,7 +282,7 @@ __global__ __launch_bounds__(256) void k_lay_out(LayOutArgs x, LayOutArgs w, int
 
 struct LogitsArgs {
   T16Side w, x;                    // W's rows: A, those of x: B (`first` is set by the kernel)
-  int stages;
+  int d_values;                    // of a row, with the padding
   int c0, m_tiles, n_tiles;        // the first class, tiles of classes from it on, of rows
   int chunks;                      // workgroups of a row tile
   int classes;
@@ -333,9 +333,15 @@ constexpr float kLn2 = 0.6931471805599453f;
 // statistics and G at once.
 enum LogitsMode { kStats, kGrad, kBoth };
 
+// Stages in LDS.  256 x 256: two of 64 elements, 128 KB (bf16, four of 32: 535 us
+// for 494, statistics of 8,192 x 1,024 x 32,768).  64 x 64: four for logits, whose
+// sums are short (1,000 x 256 x 47 fp32: 9.0 us, two 11.1), two for products,
+// which have more code than time (6.5 us, four 12.2).
+constexpr int logits_stages(int tm) { return tm > 64 ? 2 : 4; }
+
 template <int TM, int TN, int WM, int WN>
 struct LogitsLds {
-  static constexpr int kStages = 2 * t16_stage_bytes<TM, TN>();
+  static constexpr int kStages = logits_stages(TM) * t16_stage_bytes<TM, TN, 64>();
   static constexpr int kRows = kStages;                        // [2][WM][TN]: statistics; lse, label; [TN]: its logit
   static constexpr int kClasses = kRows + (2 * WM + 1) * TN * 4;   // [WN][TM]: sums of G
   static constexpr int kBytes = kClasses + WN * TM * 4;
@@ -343,8 +349,9 @@ struct LogitsLds {
 
 template <T16Type TYPE, LogitsMode MODE, int TM, int TN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
-  using Tile = T16Tile<TYPE, kByRow, kByRow, TM, TN, WM, WN, true>;
+  using Tile = T16Tile<TYPE, kByRow, kByRow, TM, TN, WM, WN, logits_stages(TM), 64, true>;
   using Lds = LogitsLds<TM, TN, WM, WN>;
+  constexpr int NST = Tile::STAGES;
   constexpr int RT = Tile::RT, CT = Tile::CT, THREADS = 64 * WM * WN;
   static_assert(RT % 2 == 0, "classes are dealt to pairs of tiles");
   __shared__ __attribute__((aligned(1024))) char lds[Lds::kBytes];
@@ -371,10 +378,23 @@ __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
   lb.init(b, wave, lane);
   a.first = p.c0 + static_cast<int64_t>(t0) * TM;
   la.init(a, wave, lane);
-  if (t0 < t1) {
-    la.fetch(0, lds);
-    lb.fetch(0, lds + TM * 128);
-  }
+  // the stages of all tiles, one after the other: `left` are to be fetched, the
+  // next one is stage `next` of its tile (la's)
+  const int stages = p.d_values / Tile::K;
+  int left = (t1 - t0) * stages, next = 0, rest = left;   // rest: to be used
+  auto fetched = [&] {
+    --left;
+    if (++next == stages) {
+      next = 0;
+      la.advance();
+    }
+  };
+#pragma unroll
+  for (int s = 0; s < NST - 1; ++s)
+    if (left > 0) {
+      Tile::fetch(la, lb, next, lds + s * Tile::kStage);
+      fetched();
+    }
   // the rows' labels, scales and, for G, statistics
   float scale[CT];
   int label[CT];
@@ -388,7 +408,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
   if constexpr (MODE == kGrad) {
     constexpr int PARTS = THREADS / TN > 0 ? THREADS / TN : 1;
     static_assert(PARTS * TN <= THREADS || PARTS == 1, "");
-    float* part = reinterpret_cast<float*>(lds + Tile::kStage);      // (the second stage is still empty)
+    float* part = reinterpret_cast<float*>(lds + (NST - 1) * Tile::kStage);   // (the last stage is still empty)
     for (int q = threadIdx.x; q < PARTS * TN; q += THREADS) {
       const int row = q % TN;
       float top = -INFINITY, sum = 0.f;
@@ -431,14 +451,13 @@ __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
   for (int t = t0; t < t1; ++t) {
     t16_f32x4 acc[RT][CT];
     Tile::clear(acc);
-    for (int k = 0; k < p.stages; ++k) {
-      const bool last = k + 1 == p.stages;
-      // the next stage, across tiles: it is on its way while this tile's end is computed
-      if (last) la.advance();
-      Tile::step(la, lb, last ? 0 : k + 1, !last || t + 1 < t1, lds + at * Tile::kStage, lds + (1 - at) * Tile::kStage,
-                 wave, lane, acc);
-      at = 1 - at;
-      if (!last || MODE != kStats) __syncthreads();
+    for (int k = 0; k < stages; ++k) {
+      Tile::wait(--rest >= NST - 2);
+      const int to = at == 0 ? NST - 1 : at - 1;
+      const bool more = left > 0;
+      Tile::step(la, lb, next, more, lds + at * Tile::kStage, lds + to * Tile::kStage, wave, lane, acc);
+      if (more) fetched();
+      at = at == NST - 1 ? 0 : at + 1;
     }
     // u = z log2(e), in place; the registers of tiles i and i + 1 (i even) are
     // classes c0 + 16 i .. + 7, -inf past the last class
@@ -554,10 +573,8 @@ __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
           for (int w = 0; w < WN; ++w) s += part[w * TM + q];
           if (p.c0 + t * TM + q < p.classes) p.db[static_cast<int64_t>(nt) * p.ld_db + t * TM + q] = s;
         }
-        __syncthreads();                                // (the next tile's sums)
+        // (the next tile's sums come behind the barriers of its stages)
       }
-    } else {
-      __syncthreads();                                  // the next tile's first stage has arrived
     }
   }
   if constexpr (MODE == kStats) {
@@ -610,7 +627,7 @@ struct Product {
   T16Side a, b;                    // `first` is set by the kernel
   int64_t m, n;                    // out: n rows of m contiguous values
   int m_tiles, n_tiles, splits;
-  int64_t stages;                  // of k
+  int64_t k;
   void* out;                       // the result, or NULL: sums go to `slab`
   int64_t ld;
   float factor;                    // result = sum factor inverse
@@ -651,7 +668,7 @@ __device__ __forceinline__ void put_four(void* out, int64_t at, t16_f32x4 v, int
 
 template <T16Type TYPE, T16Form FA, T16Form FB, int TM, int TN, int WM, int WN>
 __device__ __forceinline__ void product_tile(const Product& p, int64_t id, char* lds) {
-  using Tile = T16Tile<TYPE, FA, FB, TM, TN, WM, WN>;
+  using Tile = T16Tile<TYPE, FA, FB, TM, TN, WM, WN, 2, 64>;
   constexpr int RT = Tile::RT, CT = Tile::CT;
   const int mt = static_cast<int>(id % p.m_tiles);
   const int64_t rest = id / p.m_tiles;
@@ -661,7 +678,8 @@ __device__ __forceinline__ void product_tile(const Product& p, int64_t id, char*
   b.first = static_cast<int64_t>(nt) * TN;
   t16_f32x4 acc[RT][CT];
   Tile::clear(acc);
-  Tile::run(a, b, p.stages * split / p.splits, p.stages * (split + 1) / p.splits, lds, acc);
+  const int64_t stages = (p.k + Tile::K - 1) / Tile::K;
+  Tile::run(a, b, stages * split / p.splits, stages * (split + 1) / p.splits, lds, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, r = lane & 15;
   const int wm = wave / WN, wn = wave % WN;
   const int64_t m0 = a.first + 16 * RT * wm + 4 * g, n0 = b.first + 16 * CT * wn + r;
@@ -693,7 +711,7 @@ __device__ __forceinline__ void product_tile(const Product& p, int64_t id, char*
 // those of W (A: x, B: G) or, turned, those of W's transpose (A: G, B: x).
 template <T16Type TYPE, int TM, int TN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void k_products(Product dx, Product dw) {
-  __shared__ __attribute__((aligned(1024))) char lds[2 * t16_stage_bytes<TM, TN>()];
+  __shared__ __attribute__((aligned(1024))) char lds[2 * t16_stage_bytes<TM, TN, 64>()];
   // workgroup ids go round the eight XCDs: each has an eighth of either product
   const int64_t of_dx = product_tiles(dx), of_dw = product_tiles(dw);
   const int64_t dx_each = (of_dx + 7) / 8, dw_each = (of_dw + 7) / 8, xcd = blockIdx.x & 7;
@@ -1001,11 +1019,10 @@ hipError_t run(const LinearLossArgs& a, hipStream_t s) {
   hipLaunchKernelGGL((k_lay_out<TYPE, T>), dim3(static_cast<unsigned>(x_tiles + w_tiles)), dim3(256), 0, s, l, lw, x_tiles);
   const T16Side x_by_row{x_row, p.pad_d * p.es, p.pad_rows, static_cast<int>(p.pad_d), 0};
   const T16Side x_by_all{x_all, p.pad_d * p.es, p.pad_rows, static_cast<int>(p.pad_d), 0};
-  const int64_t k = 64 / p.es;                          // of a stage
   LogitsArgs g{};
   g.w = w;
   g.x = x_by_row;
-  g.stages = static_cast<int>(p.pad_d / k);
+  g.d_values = static_cast<int>(p.pad_d);
   g.m_tiles = static_cast<int>(tiles_of(a.classes, p.tile));
   g.n_tiles = static_cast<int>(tiles_of(a.rows, p.tile));
   g.chunks = p.chunks;
@@ -1057,7 +1074,7 @@ hipError_t run(const LinearLossArgs& a, hipStream_t s) {
       dx.m_tiles = static_cast<int>(tiles_of(a.d, tile));
       dx.n_tiles = static_cast<int>(tiles_of(a.rows, tile));
       dx.splits = p.dx_splits;
-      dx.stages = tiles_of(have, k);
+      dx.k = have;
       dx.factor = mean;
       dx.inverse = kLo ? nullptr : inverses + 1;
       dx.out = p.dx_slab ? nullptr : a.dx;
@@ -1076,7 +1093,7 @@ hipError_t run(const LinearLossArgs& a, hipStream_t s) {
       dw.m_tiles = static_cast<int>(tiles_of(dw.m, tile));
       dw.n_tiles = static_cast<int>(tiles_of(dw.n, tile));
       dw.splits = p.dw_splits;
-      dw.stages = tiles_of(a.rows, k);
+      dw.k = a.rows;
       dw.factor = mean;
       dw.inverse = kLo ? nullptr : inverses;
       dw.out = p.dw_splits > 1 ? nullptr : static_cast<T*>(a.dw) + skip;

@@ -43,8 +43,9 @@ struct T16Side {
   int64_t first;
 };
 
-template <int TM, int TN>
-constexpr int t16_stage_bytes() { return (TM + TN) * 128; }
+// A stage of KS 16-bit elements of either side's rows.
+template <int TM, int TN, int KS>
+constexpr int t16_stage_bytes() { return (TM + TN) * KS * 2; }
 
 // 16 bytes a lane from global memory to LDS, at l + 16 lane.
 __device__ __forceinline__ void t16_load_lds(const void* g, void* l) {
@@ -53,11 +54,18 @@ __device__ __forceinline__ void t16_load_lds(const void* g, void* l) {
   __builtin_amdgcn_global_load_lds((gp)g, (lp)l, 16, 0, 0);
 }
 
-// What brings a side's tile of T rows (or columns) into LDS.  LDS holds T x 128
-// bytes a stage: kByRow T rows of eight 16-byte pieces, piece q at q ^ (row / 2
-// % 8); kByK 64 rows of T columns (kSplit: the hi parts of 32 of k, then the lo
-// parts), pairs of pieces exchanged by t16_turn.  Both spread the rows that are
-// read together over the banks.
+// Waits until at most N of this wave's loads are still on their way, and for the
+// workgroup.  (Loads and stores end in the order they were issued.)
+template <int N>
+__device__ __forceinline__ void t16_wait() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N < 63 ? N : 63) : "memory");
+}
+
+// What brings a side's tile of T rows (or columns) into LDS.  LDS holds T x KS
+// elements a stage (KS 64, or for bf16 32): kByRow T rows of KS / 8 16-byte
+// pieces, piece q at q ^ t16_spread(row); kByK KS rows of T columns (kSplit: the
+// hi parts of 32 of k, then the lo parts), pairs of pieces exchanged by t16_turn.
+// Both spread the rows that are read together over the banks.
 //
 // An address is a part that the whole wave has (scalar registers) and a lane's
 // offset of 32 bits, the same for every tile and stage but those at the end
@@ -70,11 +78,16 @@ __device__ __forceinline__ void t16_load_lds(const void* g, void* l) {
 constexpr int64_t kT16MostBytes = (int64_t{1} << 31) / 256;
 __device__ __forceinline__ int t16_turn(int krow) { return (krow & 3) | ((krow >> 3) & 1) << 2; }
 
-template <T16Type TYPE, T16Form FORM, int T, int WAVES, bool DEAL = false>
+template <int KS>
+__device__ __forceinline__ int t16_spread(int row) { return KS == 64 ? (row >> 1) & 7 : (row >> 2) & 3; }
+
+template <T16Type TYPE, T16Form FORM, int T, int WAVES, int KS, bool DEAL = false>
 struct T16Loader {
-  static constexpr int LOADS = T * 8 / (64 * WAVES);
-  static_assert(LOADS * 64 * WAVES == T * 8, "a stage is whole loads");
-  static constexpr int KROWS = TYPE == kSplit ? 32 : 64;
+  static constexpr int PIECES = KS / 8;     // of a row
+  static constexpr int LOADS = T * PIECES / (64 * WAVES);
+  static_assert(LOADS * 64 * WAVES == T * PIECES, "a stage is whole loads");
+  static_assert(KS == 64 || (KS == 32 && TYPE == kBf16), "a stage has whole products");
+  static constexpr int KROWS = TYPE == kSplit ? 32 : KS;
   static constexpr int P = T / 8;           // pieces of a row of k
   const char* base;                         // the tile's first row, or its first row of k
   uint32_t off[LOADS];
@@ -86,7 +99,7 @@ struct T16Loader {
   __device__ __forceinline__ int row_of(int i) const {
     const int q = (i * WAVES + wave) * 64 + lane;
     if constexpr (FORM == kByRow) {
-      const int row = q / 8;
+      const int row = q / PIECES;
       return DEAL ? (row & ~31) + (row & 12) * 2 + ((row >> 4) & 1) * 4 + (row & 3) : row;
     } else {
       const int row = q / P;
@@ -96,7 +109,7 @@ struct T16Loader {
   __device__ __forceinline__ uint32_t in_row(int i, const T16Side& s) const {
     const int q = (i * WAVES + wave) * 64 + lane;
     if constexpr (FORM == kByRow) {
-      return ((q % 8) ^ ((q >> 4) & 7)) * 16;
+      return ((q % PIECES) ^ t16_spread<KS>(q / PIECES)) * 16;
     } else {
       const int row = q / P, slot = q % P;
       const int chunk = (slot >> 1) ^ (t16_turn(row) & (P / 2 - 1));
@@ -132,7 +145,7 @@ struct T16Loader {
   }
   // stage k into the side's half of an LDS stage
   __device__ __forceinline__ void fetch(int64_t k, char* lds) const {
-    const char* from = base + k * (FORM == kByRow ? 128 : static_cast<int64_t>(KROWS) * ld_bytes);
+    const char* from = base + k * (FORM == kByRow ? KS * 2 : static_cast<int64_t>(KROWS) * ld_bytes);
     if (FORM == kByK && (k + 1) * KROWS > rows) {
       const int last = static_cast<int>(rows - 1 - k * KROWS);    // (of this stage: 0 at least)
 #pragma unroll
@@ -149,11 +162,11 @@ struct T16Loader {
 
 // The operand of 16 rows (or columns) from `at` on in an LDS stage, for the
 // stage's s-th 32 (kSplit: s = 0 the hi parts, 1 the lo parts).
-template <T16Form FORM, int T>
+template <T16Form FORM, int T, int KS>
 __device__ __forceinline__ t16_i16x8 t16_operand(const char* lds, int at, int s, int lane) {
   const int r = lane & 15, g = lane >> 4;
   if constexpr (FORM == kByRow) {
-    return *reinterpret_cast<const t16_i16x8*>(lds + (at + r) * 128 + ((4 * s + g) ^ ((r >> 1) & 7)) * 16);
+    return *reinterpret_cast<const t16_i16x8*>(lds + (at + r) * (KS * 2) + ((4 * s + g) ^ t16_spread<KS>(r)) * 16);
   } else {
     typedef __attribute__((address_space(3))) t16_i16x4* lp;
     const int chunk = (at / 16) ^ (((r >> 2) | (g & 1) << 2) & (T / 16 - 1));
@@ -175,12 +188,15 @@ __device__ __forceinline__ t16_f32x4 t16_mfma(t16_i16x8 a, t16_i16x8 b, t16_f32x
 // A workgroup of WM x WN waves, a wave RT x CT tiles of 16 x 16: its rows of A
 // from 16 RT wm on, of B from 16 CT wn on.  Register e of lane (g, r) of
 // acc[i][j] is row 16 i + 4 g + e of A (with DEAL, of LDS), row 16 j + r of B.
-template <T16Type TYPE, T16Form FA, T16Form FB, int TM, int TN, int WM, int WN, bool DEAL = false>
+// LDS holds NST stages: NST - 1 are on their way or waiting while one is used.
+template <T16Type TYPE, T16Form FA, T16Form FB, int TM, int TN, int WM, int WN, int NST, int KS, bool DEAL = false>
 struct T16Tile {
-  static constexpr int WAVES = WM * WN, RT = TM / (16 * WM), CT = TN / (16 * WN);
-  static constexpr int kStage = t16_stage_bytes<TM, TN>();
-  using LoadA = T16Loader<TYPE, FA, TM, WAVES, DEAL>;
-  using LoadB = T16Loader<TYPE, FB, TN, WAVES>;
+  static constexpr int WAVES = WM * WN, RT = TM / (16 * WM), CT = TN / (16 * WN), STAGES = NST;
+  static constexpr int kStage = t16_stage_bytes<TM, TN, KS>();
+  static constexpr int K = TYPE == kSplit ? KS / 2 : KS;      // values of a stage
+  using LoadA = T16Loader<TYPE, FA, TM, WAVES, KS, DEAL>;
+  using LoadB = T16Loader<TYPE, FB, TN, WAVES, KS>;
+  static constexpr int LOADS = LoadA::LOADS + LoadB::LOADS;
 
   static __device__ __forceinline__ void clear(t16_f32x4 (&acc)[RT][CT]) {
 #pragma unroll
@@ -189,8 +205,22 @@ struct T16Tile {
       for (int j = 0; j < CT; ++j) acc[i][j] = t16_f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  // acc += the stages first .. last - 1 of k; lds: two stages.  Every wave of
-  // the workgroup calls it with the same stages.
+  static __device__ __forceinline__ void fetch(const LoadA& la, const LoadB& lb, int64_t k, char* to) {
+    la.fetch(k, to);
+    lb.fetch(k, to + TM * KS * 2);
+  }
+
+  // The oldest stage has arrived, for every wave, and the one before it is read:
+  // `full`: NST - 1 stages were asked for since that one; `later`: at least that
+  // many stores were made after its loads.
+  template <int LATER = 0>
+  static __device__ __forceinline__ void wait(bool full) {
+    if (NST > 2 && full) t16_wait<(NST - 2) * LOADS + LATER>();
+    else t16_wait<NST == 2 ? LATER : 0>();
+  }
+
+  // acc += the stages first .. last - 1 of k; lds: NST stages.  Every wave of the
+  // workgroup calls it with the same stages.
   static __device__ __forceinline__ void run(const T16Side& a, const T16Side& b, int64_t first, int64_t last, char* lds,
                                              t16_f32x4 (&acc)[RT][CT]) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -198,40 +228,38 @@ struct T16Tile {
     LoadB lb;
     la.init(a, wave, lane);
     lb.init(b, wave, lane);
-    if (first < last) {
-      la.fetch(first, lds);
-      lb.fetch(first, lds + TM * 128);
+#pragma unroll
+    for (int s = 0; s < NST - 1; ++s)
+      if (first + s < last) fetch(la, lb, first + s, lds + s * kStage);
+    int at = 0;
+    for (int64_t k = first; k < last; ++k) {
+      wait(k + NST - 2 < last);
+      const int to = at == 0 ? NST - 1 : at - 1;
+      step(la, lb, k + NST - 1, k + NST - 1 < last, lds + at * kStage, lds + to * kStage, wave, lane, acc);
+      at = at == NST - 1 ? 0 : at + 1;
     }
     __syncthreads();
-    for (int64_t k = first; k < last; ++k) {
-      const int64_t at = (k - first) & 1;
-      step(la, lb, k + 1, k + 1 < last, lds + at * kStage, lds + (1 - at) * kStage, wave, lane, acc);
-      __syncthreads();              // stage k is read, stage k + 1 has arrived
-    }
   }
 
   // acc += the stage that lies at `now`, while (with `more`) stage k comes to
-  // `next`.
-  // (The two are apart, and said to be: else the compiler lets the transposing
-  // reads of `now` wait for the loads into `next`.)
+  // `next`.  (The two are apart, and said to be: else the compiler lets the
+  // transposing reads of `now` wait for the loads into `next`.)
   static __device__ __forceinline__ void step(const LoadA& la, const LoadB& lb, int64_t k, bool more,
                                               const char* __restrict__ now, char* __restrict__ next, int wave, int lane,
                                               t16_f32x4 (&acc)[RT][CT]) {
     const int wm = wave / WN, wn = wave % WN;
-    if (more) {
-      la.fetch(k, next);
-      lb.fetch(k, next + TM * 128);
-    }
+    if (more) fetch(la, lb, k, next);
+    const char* now_b = now + TM * KS * 2;
     if constexpr (TYPE == kBf16) {
       // (unrolled, the operands of both halves would be held at once: with large
       // tiles that spills)
 #pragma unroll RT * CT >= 32 ? 1 : 2
-      for (int s = 0; s < 2; ++s) {
+      for (int s = 0; s < KS / 32; ++s) {
         t16_i16x8 qa[RT], qb[CT];
 #pragma unroll
-        for (int j = 0; j < CT; ++j) qb[j] = t16_operand<FB, TN>(now + TM * 128, 16 * (CT * wn + j), s, lane);
+        for (int j = 0; j < CT; ++j) qb[j] = t16_operand<FB, TN, KS>(now_b, 16 * (CT * wn + j), s, lane);
 #pragma unroll
-        for (int i = 0; i < RT; ++i) qa[i] = t16_operand<FA, TM>(now, 16 * (RT * wm + i), s, lane);
+        for (int i = 0; i < RT; ++i) qa[i] = t16_operand<FA, TM, KS>(now, 16 * (RT * wm + i), s, lane);
 #pragma unroll
         for (int i = 0; i < RT; ++i)
 #pragma unroll
@@ -241,13 +269,13 @@ struct T16Tile {
       t16_i16x8 bh[CT], bl[CT];
 #pragma unroll
       for (int j = 0; j < CT; ++j) {
-        bh[j] = t16_operand<FB, TN>(now + TM * 128, 16 * (CT * wn + j), 0, lane);
-        bl[j] = t16_operand<FB, TN>(now + TM * 128, 16 * (CT * wn + j), 1, lane);
+        bh[j] = t16_operand<FB, TN, KS>(now_b, 16 * (CT * wn + j), 0, lane);
+        bl[j] = t16_operand<FB, TN, KS>(now_b, 16 * (CT * wn + j), 1, lane);
       }
 #pragma unroll
       for (int i = 0; i < RT; ++i) {
-        const t16_i16x8 ah = t16_operand<FA, TM>(now, 16 * (RT * wm + i), 0, lane);
-        const t16_i16x8 al = t16_operand<FA, TM>(now, 16 * (RT * wm + i), 1, lane);
+        const t16_i16x8 ah = t16_operand<FA, TM, KS>(now, 16 * (RT * wm + i), 0, lane);
+        const t16_i16x8 al = t16_operand<FA, TM, KS>(now, 16 * (RT * wm + i), 1, lane);
 #pragma unroll
         for (int j = 0; j < CT; ++j) acc[i][j] = t16_mfma<TYPE>(al, bh[j], acc[i][j]);
 #pragma unroll
