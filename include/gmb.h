@@ -713,8 +713,8 @@ typedef struct {
 
 /* Bytes of workspace gmb_linear_loss needs (0 for bad arguments); of the
  * pointers of `grads` (NULL: the loss alone) only NULL or not counts, of w its
- * alignment.  It grows with rows (d + classes / 16) and, with gradients, by 256
- * MB at most (more from 262,144 rows on) and the sums that are split; the
+ * alignment.  It grows with rows (d + classes / 16) and, with gradients, by 384
+ * MB at most (more from 393,216 rows on) and the sums that are split; the
  * logits are never stored. */
 size_t gmb_linear_loss_workspace_bytes(const gmb_linear_head* head, const gmb_linear_grads* grads);
 

@@ -744,24 +744,54 @@ struct FinishArgs {
   float* loss;
 };
 
+// Parts from which on a workgroup has 16 times four columns and 16 threads share
+// the parts of each (63 parts of 47 x 256: one thread for all, 16 us; 16, 4).
+constexpr int kManyParts = 8;
+constexpr int join_columns(int parts) { return parts > kManyParts ? 16 : 256; }   // fours of a workgroup
+
 // out = factor inverse times the sum of the parts, in a fixed order.
 template <bool BF16>
 __device__ __forceinline__ void join_parts(const JoinArgs& p, int block) {
   const int64_t fours = (p.cols + 3) / 4, all = p.rows * fours;
   const float inverse = p.inverse ? *p.inverse : 1.f;
+  const int64_t step = p.rows * p.ld_slab;
+  if (p.parts > kManyParts) {
+    __shared__ t16_f32x4 lds[16][16];
+    const int q0 = threadIdx.x & 15, mine = threadIdx.x >> 4;
+    for (int64_t first = static_cast<int64_t>(block) * 16; first < all; first += static_cast<int64_t>(p.blocks) * 16) {
+      const int64_t q = first + q0, row = q / fours, col = (q - row * fours) * 4;
+      t16_f32x4 v = {0.f, 0.f, 0.f, 0.f};
+      if (q < all) {
+        const float* from = p.slab + row * p.ld_slab + col;
+#pragma unroll 8
+        for (int s = mine; s < p.parts; s += 16) {
+          t16_f32x4 x;
+          mx_get<16>(&x, from + s * step);
+          v += x;
+        }
+      }
+      __syncthreads();              // the last turn's reads
+      lds[mine][q0] = v;
+      __syncthreads();
+      if (mine == 0 && q < all) {
+#pragma unroll
+        for (int w = 1; w < 16; ++w) v += lds[w][q0];
+        put_four<BF16>(p.out, row * p.ld + col, v * p.factor * inverse, p.cols - col);
+      }
+    }
+    return;
+  }
   for (int64_t q = static_cast<int64_t>(block) * 256 + threadIdx.x; q < all; q += static_cast<int64_t>(p.blocks) * 256) {
     const int64_t row = q / fours, col = (q - row * fours) * 4;
     t16_f32x4 v = {0.f, 0.f, 0.f, 0.f};
     const float* from = p.slab + row * p.ld_slab + col;
-    const int64_t step = p.rows * p.ld_slab;
 #pragma unroll 4
     for (int s = 0; s < p.parts; ++s) {
       t16_f32x4 x;
       mx_get<16>(&x, from + s * step);
       v += x;
     }
-    v = v * p.factor * inverse;
-    put_four<BF16>(p.out, row * p.ld + col, v, p.cols - col);
+    put_four<BF16>(p.out, row * p.ld + col, v * p.factor * inverse, p.cols - col);
   }
 }
 
@@ -786,13 +816,234 @@ __global__ __launch_bounds__(256) void k_finish(FinishArgs p) {
   if (threadIdx.x == 0) *p.loss = static_cast<float>((((lds[0] + lds[1]) + lds[2]) + lds[3]) / static_cast<double>(p.rows));
 }
 
+// ---- small heads ----------------------------------------------------------
+
+// W whole in LDS, in fp32: v_mfma_f32_16x16x4_f32 (exact products, fp32 sums) on
+// what is read once, with its own strides and type: no rows are laid out, nothing
+// is cut, and G never leaves the workgroup, which has sixteen rows.  LDS rows are a multiple of four words
+// that is odd in fours apart: sixteen rows' reads of four words, and four rows'
+// of sixteen, fall on different banks.  (1,000 x 256 x 47 fp32 through k_logits
+// and k_products: 29 us of kernels in five launches, here 17 in two.)
+constexpr int kSmallClasses = 256, kSmallCells = 16384, kSmallD = 1024;
+constexpr int64_t kSmallRows = 16 * kComputeUnits;
+
+struct SmallArgs {
+  const void* x;
+  int64_t x_stride;
+  const void* w;
+  int64_t w_row, w_col;
+  const float* bias;               // or NULL
+  const int32_t* labels;
+  int rows, d, classes;
+  float mean;                      // 1 / rows
+  float* loss_rows;
+  int grad;                        // whether G is wanted
+  void* dx;                        // or NULL
+  float* dw;                       // a part a workgroup: [classes][ld_dw], turned [d][ld_dw], or NULL
+  int64_t ld_dw, part_dw;
+  int turned;
+  float* db;                       // a part a workgroup, ld_db apart, or NULL
+  int64_t ld_db;
+};
+
+template <typename T>
+__device__ __forceinline__ float as_float(T v) {
+  if constexpr (sizeof(T) == 4) return v;
+  else return bf16_to_f32(v);
+}
+template <typename T>
+__device__ __forceinline__ t16_f32x4 get_four(const T* p) {
+  t16_f32x4 v;
+  if constexpr (sizeof(T) == 4) {
+    mx_get<16>(&v, p);
+  } else {
+    uint32_t q[2];
+    mx_get<8>(q, p);
+    v = t16_f32x4{__uint_as_float(q[0] << 16), __uint_as_float(q[0] & 0xFFFF0000u), __uint_as_float(q[1] << 16),
+                  __uint_as_float(q[1] & 0xFFFF0000u)};
+  }
+  return v;
+}
+
+constexpr int kSmallThreads = 1024;
+
+// rows x cols values, element (i, j) at i row + j (N = 4: j in fours, whole ones) or
+// any j (N = 1), zeros behind them up to pad_rows x pad_cols, through put(i, j,
+// value): every thread of the workgroup, four loads on their way at a time, none
+// behind a branch (what is past the end is read where there is something, and left
+// out).
+template <int N, typename T, typename F>
+__device__ __forceinline__ void bring(const T* from, int64_t row, int64_t col, int rows, int cols, int pad_rows,
+                                      int pad_cols, F&& put) {
+  const int across = pad_cols / N;
+  int i = threadIdx.x / across, j = threadIdx.x - i * across;
+  const int step_i = kSmallThreads / across, step_j = kSmallThreads - step_i * across;
+#pragma unroll 1
+  while (i < pad_rows) {
+    t16_f32x4 v[4];
+    int at_i[4], at_j[4];
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      const bool in = i < rows && N * j < cols;
+      const T* p = from + (in ? i * row + N * j * col : 0);
+      if constexpr (N == 4) v[m] = get_four<T>(p);
+      else v[m][0] = as_float(*p);
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[m][e] = in ? v[m][e] : 0.f;
+      at_i[m] = i;
+      at_j[m] = j;
+      i += step_i;
+      j += step_j;
+      if (j >= across) {
+        j -= across;
+        ++i;
+      }
+    }
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+      if (at_i[m] < pad_rows) put(at_i[m], N * at_j[m], v[m]);
+  }
+}
+
+__device__ __forceinline__ t16_f32x4 mfma4(float a, float b, t16_f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
+}
+
+template <typename T>
+__global__ __launch_bounds__(kSmallThreads) void k_small_head(SmallArgs p) {
+  constexpr int kWords = (kSmallCells + 4 * kSmallClasses) + 16 * (kSmallD + 4) + 16 * (kSmallClasses + 4);
+  __shared__ __attribute__((aligned(16))) float lds[kWords];
+  __shared__ float lb[kSmallClasses], row_top[16][16], row_sum[16][16], row_label[16];
+  __shared__ int32_t row_y[16];
+  const int ct = (p.classes + 15) / 16, dt = (p.d + 15) / 16;
+  const int sd = 16 * dt + 4, sc = 16 * ct + 4;
+  float* lw = lds;                                       // [16 ct][sd]
+  float* lx = lw + 16 * ct * sd;                         // [16][sd]
+  float* lg = lx + 16 * sd;                              // [16][sc]
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = lane >> 4, r = lane & 15;
+  const int64_t row0 = 16 * static_cast<int64_t>(blockIdx.x);
+  const int rows = p.rows - row0 < 16 ? static_cast<int>(p.rows - row0) : 16;
+  if (threadIdx.x < 16) {
+    const int32_t y = static_cast<int>(threadIdx.x) < rows ? p.labels[row0 + threadIdx.x] : -1;
+    row_y[threadIdx.x] = y >= 0 && y < p.classes ? y : -1;
+  }
+  // the biases, times log2(e); -inf for no class
+  if (const int c = threadIdx.x; c < 16 * ct)
+    lb[c] = c < p.classes ? (p.bias ? p.bias[c] * kLog2e : 0.f) : -INFINITY;
+  // W, zeros around it, read along the direction that is contiguous
+  const T* w = static_cast<const T*>(p.w);
+  if (p.w_col == 1 && p.d % 4 == 0)
+    bring<4>(w, p.w_row, 1, p.classes, p.d, 16 * ct, 16 * dt,
+             [&](int c, int j, const t16_f32x4& v) { *reinterpret_cast<t16_f32x4*>(lw + c * sd + j) = v; });
+  else if (p.w_col == 1 || p.w_row != 1)
+    bring<1>(w, p.w_row, p.w_col, p.classes, p.d, 16 * ct, 16 * dt,
+             [&](int c, int j, const t16_f32x4& v) { lw[c * sd + j] = v[0]; });
+  else
+    bring<1>(w, p.w_col, 1, p.d, p.classes, 16 * dt, 16 * ct,
+             [&](int j, int c, const t16_f32x4& v) { lw[c * sd + j] = v[0]; });
+  __syncthreads();                                       // the labels
+  // (a row without a label is read, and left out)
+  const T* x = static_cast<const T*>(p.x) + row0 * p.x_stride;
+  auto keep = [&](int i, const t16_f32x4& v) { return row_y[i] >= 0 ? v : t16_f32x4{0.f, 0.f, 0.f, 0.f}; };
+  if (p.d % 4 == 0)
+    bring<4>(x, p.x_stride, 1, rows, p.d, 16, 16 * dt,
+             [&](int i, int j, const t16_f32x4& v) { *reinterpret_cast<t16_f32x4*>(lx + i * sd + j) = keep(i, v); });
+  else
+    bring<1>(x, p.x_stride, 1, rows, p.d, 16, 16 * dt,
+             [&](int i, int j, const t16_f32x4& v) { lx[i * sd + j] = keep(i, v)[0]; });
+  __syncthreads();
+  // logits: wave i has class tile i; a step of sixteen of d is four instructions,
+  // lane group g having d 4 g .. 4 g + 3 of them
+  t16_f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  const int y = row_y[r], c0 = 16 * wave + 4 * g;
+  if (wave < ct) {
+#pragma unroll 2
+    for (int k = 0; k < dt; ++k) {
+      const t16_f32x4 b = *reinterpret_cast<const t16_f32x4*>(lx + r * sd + 16 * k + 4 * g);
+      const t16_f32x4 a = *reinterpret_cast<const t16_f32x4*>(lw + (16 * wave + r) * sd + 16 * k + 4 * g);
+#pragma unroll
+      for (int s = 0; s < 4; ++s) acc = mfma4(a[s], b[s], acc);
+    }
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      acc[e] = fmaf(acc[e], kLog2e, lb[c0 + e]);
+      if (c0 + e == y) row_label[r] = acc[e];
+      top = fmaxf(top, acc[e]);
+    }
+    const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum += exp2_fast(acc[e] - base);
+    for (int o = 16; o < 64; o <<= 1) join_stats(top, sum, __shfl_xor(top, o, 64), __shfl_xor(sum, o, 64));
+    if (g == 0) {
+      row_top[wave][r] = top;
+      row_sum[wave][r] = sum;
+    }
+  }
+  __syncthreads();
+  float top = row_top[0][r], sum = row_sum[0][r];
+  for (int v = 1; v < ct; ++v) join_stats(top, sum, row_top[v][r], row_sum[v][r]);
+  const float lse = row_lse(top, sum);
+  const bool on = y >= 0 && !row_empty(top, sum);
+  if (wave == 0 && g == 0 && r < rows) p.loss_rows[row0 + r] = on ? (lse - row_label[r]) * kLn2 : 0.f;
+  if (!p.grad) return;
+  if (wave < ct) {
+    t16_f32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float q = exp2_fast(acc[e] - lse);
+      v[e] = on ? (c0 + e == y ? q - 1.f : q) : 0.f;
+    }
+    *reinterpret_cast<t16_f32x4*>(lg + r * sc + c0) = v;
+  }
+  __syncthreads();
+  if (p.db && static_cast<int>(threadIdx.x) < p.classes) {
+    float s = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < 16; ++i) s += lg[i * sc + threadIdx.x];
+    p.db[blockIdx.x * p.ld_db + threadIdx.x] = s;
+  }
+  if (p.dx) {
+    for (int q = wave; q < dt; q += 16) {
+      t16_f32x4 v = {0.f, 0.f, 0.f, 0.f};
+      for (int k = 0; k < ct; ++k) {
+        const t16_f32x4 b = *reinterpret_cast<const t16_f32x4*>(lg + r * sc + 16 * k + 4 * g);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) v = mfma4(lw[(16 * k + 4 * g + s) * sd + 16 * q + r], b[s], v);
+      }
+      const int col = 16 * q + 4 * g;
+      if (r < rows && col < p.d) put_four<sizeof(T) == 2>(p.dx, (row0 + r) * p.d + col, v * p.mean, p.d - col);
+    }
+  }
+  if (p.dw) {
+    float* part = p.dw + blockIdx.x * p.part_dw;
+    for (int q = wave; q < ct * dt; q += 16) {
+      const int tc = q / dt, tj = q - tc * dt;
+      t16_f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const float a = lx[(4 * g + s) * sd + 16 * tj + r], b = lg[(4 * g + s) * sc + 16 * tc + r];
+        v = p.turned ? mfma4(b, a, v) : mfma4(a, b, v);
+      }
+      // (the part's rows are whole fours)
+      const int row = (p.turned ? 16 * tj : 16 * tc) + r, col = (p.turned ? 16 * tc : 16 * tj) + 4 * g;
+      if (row < (p.turned ? p.d : p.classes) && col < p.ld_dw) mx_put<16, false>(part + row * p.ld_dw + col, &v);
+    }
+  }
+}
+
 // ---- plan -----------------------------------------------------------------
 
 // Tiles of a product: 256 x 256 (four waves of 128 x 128, one workgroup a CU) or
 // 64 x 64.
 constexpr int kLarge = 256, kSmall = 64;
-// G of a piece of the classes.
-constexpr int64_t kGradBytes = int64_t{256} << 20;
+// G of a piece of the classes: less costs launches whose tiles do not fill the GPU
+// and sums that are stored in between (4,000 x 256 x 100,000 bf16 at 64, 128, 256, 512
+// and 1,024 MB: 1,455, 1,241, 1,150, 1,133, 1,122 us; 4,000 x 256 x 20,011 fp32, 331
+// MB in one piece: 636, 595, 593, 559, 560; 8,192 x 1,024 x 32,768 bf16: 2,128, 1,956,
+// 1,978, 2,038, 2,032), more only memory.
+constexpr int64_t kGradBytes = int64_t{384} << 20;
 constexpr int kMostTops = 1024;
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
@@ -802,6 +1053,7 @@ struct Plan {
   int es;                          // 16-bit words of a value
   int64_t pad_rows, pad_d, pad_classes;
   bool copy_w, grad, both;         // both: statistics and G in one launch
+  int small;                       // workgroups of a small head, or 0
   int64_t piece, pieces;           // classes of a piece (a multiple of kPadRows)
   int tile;                        // of the logits
   int chunks, piece_chunks;        // workgroups of a row tile, for the statistics and for G
@@ -824,6 +1076,24 @@ Plan plan(const LinearLossArgs& a, int bf16) {
   p.copy_w = !(bf16 && a.w_col == 1 && a.d % kPadCols == 0 && a.w_row % 8 == 0 && a.w_row * 2 <= kT16MostBytes &&
                reinterpret_cast<uintptr_t>(a.w) % 16 == 0);
   p.grad = a.dx || a.dw || a.db;
+  p.dw_rows = a.turned ? a.d : a.classes;
+  p.dw_cols = a.turned ? a.classes : a.d;
+  p.ld_dw = round_up(p.dw_cols, 4);
+  size_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const size_t here = at;
+    at += static_cast<size_t>(round_up(bytes, 256));
+    return here;
+  };
+  if (round_up(a.classes, 16) * round_up(a.d, 16) <= kSmallCells && a.classes <= kSmallClasses && a.d <= kSmallD &&
+      a.rows <= kSmallRows) {
+    p.small = static_cast<int>(tiles_of(a.rows, 16));
+    p.loss_rows = take(a.rows * 4);
+    p.db = a.db ? take(p.small * round_up(a.classes, 4) * 4) : 0;
+    p.dw_sums = a.dw ? take(p.small * p.dw_rows * p.ld_dw * 4) : 0;
+    p.total = at;
+    return p;
+  }
   int64_t piece = kGradBytes / (p.pad_rows * 2 * p.es) / kPadRows * kPadRows;
   piece = piece < kPadRows ? kPadRows : (piece > p.pad_classes ? p.pad_classes : piece);
   p.pieces = tiles_of(p.pad_classes, piece);
@@ -842,9 +1112,6 @@ Plan plan(const LinearLossArgs& a, int bf16) {
   p.chunks = chunks(a.classes);
   p.piece_chunks = chunks(p.piece < a.classes ? p.piece : a.classes);
   const int64_t k = 64 / p.es;
-  p.dw_rows = a.turned ? a.d : a.classes;
-  p.dw_cols = a.turned ? a.classes : a.d;
-  p.ld_dw = round_up(p.dw_cols, 4);
   {
     const int64_t have = p.piece < a.classes ? p.piece : a.classes;
     const int64_t dx = tiles_of(a.d, kLarge) * tiles_of(a.rows, kLarge), dw = tiles_of(a.d, kLarge) * tiles_of(have, kLarge);
@@ -890,12 +1157,6 @@ Plan plan(const LinearLossArgs& a, int bf16) {
     }
     p.dx_slab = p.dx_splits > 1 || p.pieces > 1;
   }
-  size_t at = 0;
-  auto take = [&](int64_t bytes) {
-    const size_t here = at;
-    at += static_cast<size_t>(round_up(bytes, 256));
-    return here;
-  };
   const int64_t x_bytes = p.pad_rows * p.pad_d * 2 * p.es;
   p.x_all = take(x_bytes);
   p.x_row = bf16 ? p.x_all : take(x_bytes);
@@ -932,10 +1193,60 @@ void launch_logits(const LogitsArgs& g, int tile, hipStream_t s) {
   hipLaunchKernelGGL((k_logits<TYPE, MODE, kSmall, kSmall, 2, 2>), grid, dim3(256), 0, s, g);
 }
 
+JoinArgs join_of(const float* slab, int parts, int64_t rows, int64_t cols, int64_t ld_slab, float factor,
+                 const float* inverse, void* out) {
+  const int64_t need = tiles_of(rows * tiles_of(cols, 4), join_columns(parts));
+  return JoinArgs{slab, parts, rows, cols, ld_slab, factor, inverse, out, cols,
+                  static_cast<int>(need < 8 * kComputeUnits ? need : 8 * kComputeUnits)};
+}
+
+template <bool BF16>
+hipError_t finish(FinishArgs f, const LinearLossArgs& a, const float* loss_rows, hipStream_t s) {
+  f.loss_rows = loss_rows;
+  f.rows = a.rows;
+  f.loss = a.loss;
+  hipLaunchKernelGGL(k_finish<BF16>, dim3(static_cast<unsigned>(f.dx.blocks + f.dw.blocks + f.db.blocks + 1)), dim3(256), 0,
+                     s, f);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t run_small(const LinearLossArgs& a, const Plan& p, hipStream_t s) {
+  auto floats = [&](size_t off) { return reinterpret_cast<float*>(a.ws + off); };
+  const float mean = static_cast<float>(1.0 / static_cast<double>(a.rows));
+  SmallArgs m{};
+  m.x = a.x;
+  m.x_stride = a.x_stride;
+  m.w = a.w;
+  m.w_row = a.w_row;
+  m.w_col = a.w_col;
+  m.bias = a.bias;
+  m.labels = a.labels;
+  m.rows = static_cast<int>(a.rows);
+  m.d = a.d;
+  m.classes = a.classes;
+  m.mean = mean;
+  m.loss_rows = floats(p.loss_rows);
+  m.grad = p.grad;
+  m.dx = a.dx;
+  m.dw = a.dw ? floats(p.dw_sums) : nullptr;
+  m.ld_dw = p.ld_dw;
+  m.part_dw = p.dw_rows * p.ld_dw;
+  m.turned = a.turned;
+  m.db = a.db ? floats(p.db) : nullptr;
+  m.ld_db = round_up(a.classes, 4);
+  hipLaunchKernelGGL(k_small_head<T>, dim3(static_cast<unsigned>(p.small)), dim3(kSmallThreads), 0, s, m);
+  FinishArgs f{};
+  if (a.dw) f.dw = join_of(m.dw, p.small, p.dw_rows, p.dw_cols, p.ld_dw, mean, nullptr, a.dw);
+  if (a.db) f.db = join_of(m.db, p.small, 1, a.classes, m.ld_db, mean, nullptr, a.db);
+  return finish<sizeof(T) == 2>(f, a, m.loss_rows, s);
+}
+
 template <T16Type TYPE, typename T>
 hipError_t run(const LinearLossArgs& a, hipStream_t s) {
   constexpr bool kLo = TYPE == kBf16;
   const Plan p = plan(a, kLo);
+  if (p.small) return run_small<T>(a, p, s);
   auto at = [&](size_t off) { return a.ws + off; };
   auto floats = [&](size_t off) { return reinterpret_cast<float*>(a.ws + off); };
   uint16_t* x_all = reinterpret_cast<uint16_t*>(at(p.x_all));
@@ -1109,24 +1420,14 @@ hipError_t run(const LinearLossArgs& a, hipStream_t s) {
     else hipLaunchKernelGGL((k_products<TYPE, kSmall, kSmall, 2, 2>), dim3(grid8(tiles)), dim3(256), 0, s, dx, dw);
   }
   FinishArgs f{};
-  auto join = [&](size_t slab, int parts, int64_t rows, int64_t cols, int64_t ld_slab, float factor, const float* inverse,
-                  void* out) {
-    const int64_t need = (rows * ((cols + 3) / 4) + 255) / 256;
-    return JoinArgs{floats(slab), parts, rows, cols, ld_slab, factor, inverse, out, cols,
-                    static_cast<int>(need < 8 * kComputeUnits ? need : 8 * kComputeUnits)};
-  };
-  if (a.dx && p.dx_slab)
-    f.dx = join(p.dx_sums, p.dx_splits, a.rows, a.d, ld_dx, mean, kLo ? nullptr : inverses + 1, a.dx);
+  const float* w_inverse = kLo ? nullptr : inverses + 1;
+  if (a.dx && p.dx_slab) f.dx = join_of(floats(p.dx_sums), p.dx_splits, a.rows, a.d, ld_dx, mean, w_inverse, a.dx);
   if (a.dw && p.dw_splits > 1)
-    f.dw = join(p.dw_sums, p.dw_splits, p.dw_rows, p.dw_cols, p.ld_dw, mean, kLo ? nullptr : inverses, a.dw);
+    f.dw = join_of(floats(p.dw_sums), p.dw_splits, p.dw_rows, p.dw_cols, p.ld_dw, mean, inverses, a.dw);
   if (a.db)
-    f.db = join(p.db, g.n_tiles, 1, a.classes, p.pad_classes, static_cast<float>(1.0 / static_cast<double>(a.rows)),
-                nullptr, a.db);
-  f.loss_rows = floats(p.loss_rows);
-  f.rows = a.rows;
-  f.loss = a.loss;
-  hipLaunchKernelGGL(k_finish<kLo>, dim3(static_cast<unsigned>(f.dx.blocks + f.dw.blocks + f.db.blocks + 1)), dim3(256), 0, s, f);
-  return hipGetLastError();
+    f.db = join_of(floats(p.db), g.n_tiles, 1, a.classes, p.pad_classes,
+                   static_cast<float>(1.0 / static_cast<double>(a.rows)), nullptr, a.db);
+  return finish<kLo>(f, a, floats(p.loss_rows), s);
 }
 
 __global__ __launch_bounds__(256) void k_zero(uint16_t* p, int64_t n) {

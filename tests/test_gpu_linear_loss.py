@@ -95,10 +95,13 @@ def check(x, w, y, b, got, grads):
         near(grads.bias, db, (eg_sum.sum(0) + (n + 8) * U * g.abs().sum(0)) / n * 1.01 + 2 * U * db.abs(), "dbias")
 
 
-# rows, columns and classes around tiles (128), stages (32, 64) and their padding
+# a head that fits LDS, one in small tiles, one in large ones
+HEADS = [(60, 40, 200), (60, 140, 1000), (2100, 64, 5000)]
+# rows, columns and classes around tiles (64, 256), stages (32, 64) and their padding
 SIZES = [(1, 1, 1), (1, 5, 2), (3, 16, 8), (64, 16, 47), (5, 64, 127), (127, 33, 128), (128, 100, 129), (129, 128, 256), (200, 63, 257),
          (300, 65, 47), (1000, 256, 47), (257, 300, 1000), (1, 256, 5000), (40, 129, 5003), (513, 7, 640), (31, 700, 300),
-         (1500, 48, 172), (2, 2048, 33)]
+         (1500, 48, 172), (2, 2048, 33), (4096, 16, 40), (4097, 16, 40), (50, 1024, 16), (50, 1025, 16), (33, 64, 256),
+         (33, 64, 257), (2048, 96, 5000)]
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
@@ -147,9 +150,10 @@ def test_gradients_asked_for_one_by_one(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
-def test_rows_without_a_label(dtype):
+@pytest.mark.parametrize("size", HEADS + [(140, 70, 300)], ids=str)
+def test_rows_without_a_label(size, dtype):
     """Whatever stands in them, and labels of any value outside the classes."""
-    n, d, classes = 140, 70, 300
+    n, d, classes = size
     x, w, y, b = problem(n, d, classes, dtype, 4, none=0.0)
     off = torch.arange(n, device="cuda") % 3 == 1
     y[off] = torch.where(torch.arange(int(off.sum()), device="cuda") % 2 == 0, classes, -(1 << 31)).int()
@@ -168,10 +172,11 @@ def test_rows_without_a_label(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
-def test_classes_that_cannot_be(dtype):
-    x, w, y, b = problem(60, 40, 200, dtype, 5, none=0.0)
+@pytest.mark.parametrize("size", HEADS, ids=str)
+def test_classes_that_cannot_be(size, dtype):
+    x, w, y, b = problem(*size, dtype, 5, none=0.0)
     b[::2] = -math.inf
-    y = torch.randint(0, 100, (60,), device="cuda", dtype=torch.int32) * 2 + 1
+    y = torch.randint(0, size[2] // 2, (size[0],), device="cuda", dtype=torch.int32) * 2 + 1
     loss, g = gmb.linear_loss(x, w, y, bias=b)
     check(x, w, y, b, loss, g)
     assert not g.w[::2].any() and not g.bias[::2].any()
@@ -184,27 +189,29 @@ def test_classes_that_cannot_be(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
-def test_not_numbers_stay_in_their_rows(dtype):
-    x, w, y, b = problem(40, 64, 150, dtype, 6, none=0.0)
+@pytest.mark.parametrize("size", HEADS, ids=str)
+def test_not_numbers_stay_in_their_rows(size, dtype):
+    x, w, y, b = problem(*size, dtype, 6, none=0.0)
     want, wg = gmb.linear_loss(x, w, y, bias=b)
     bad = x.clone()
     bad[7, 3] = float("nan")
     loss, g = gmb.linear_loss(bad, w, y, bias=b)
     assert math.isnan(loss.item()) and bool(g.x[7].isnan().all())
-    keep = torch.arange(40, device="cuda") != 7
+    keep = torch.arange(size[0], device="cuda") != 7
     assert torch.equal(g.x[keep], wg.x[keep])
     w[5, 5] = float("inf")
     assert not math.isfinite(gmb.linear_loss(x, w, y, bias=b)[0].item())
 
 
-def test_sizes_of_values():
+@pytest.mark.parametrize("size", HEADS, ids=str)
+def test_sizes_of_values(size):
     """fp32 operands far from one, rows and weights of very different sizes."""
     for sx, sw in [(1e-12, 1e12), (1e15, 1e-16), (1e-30, 1e29), (1e-40, 1.0)]:
-        x, w, y, b = problem(70, 50, 200, torch.float32, 7)
+        x, w, y, b = problem(*size, torch.float32, 7)
         x, w = x * sx, w * sw
         loss, g = gmb.linear_loss(x, w, y, bias=b)
         check(x, w, y, b, loss, g)
-    x, w, y, b = problem(70, 50, 200, torch.float32, 8)
+    x, w, y, b = problem(*size, torch.float32, 8)
     x[::7] *= 1e-6
     x[1::7] *= 20
     loss, g = gmb.linear_loss(x, w, y, bias=b)
@@ -213,10 +220,10 @@ def test_sizes_of_values():
     check(torch.zeros_like(x), torch.zeros_like(w), y, None, loss, g)
 
 
-@pytest.mark.parametrize("dtype, size", [(torch.bfloat16, (9000, 24, 20000)), (torch.float32, (5000, 40, 16001)),
-                                         (torch.bfloat16, (200, 8, 600_000)), (torch.float32, (20_000, 16, 47))], ids=str)
+@pytest.mark.parametrize("dtype, size", [(torch.bfloat16, (9000, 24, 30000)), (torch.float32, (5000, 40, 24001)),
+                                         (torch.bfloat16, (200, 8, 900_000)), (torch.float32, (20_000, 16, 47))], ids=str)
 def test_in_pieces(dtype, size):
-    """More than 256 MB of gradients of logits: the classes in pieces, sums that are split."""
+    """More than 384 MB of gradients of logits: the classes in pieces, sums that are split."""
     x, w, y, b = problem(*size, dtype, 9)
     loss, g = gmb.linear_loss(x, w, y, bias=b)
     check(x, w, y, b, loss, g)
@@ -227,7 +234,11 @@ def test_in_pieces(dtype, size):
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
 def test_the_same_bits_every_time(dtype):
-    x, w, y, b = problem(300, 200, 3000, dtype, 10)
+    for size in HEADS + [(300, 200, 3000)]:
+        same_bits(*problem(*size, dtype, 10))
+
+
+def same_bits(x, w, y, b):
     first, g = gmb.linear_loss(x, w, y, bias=b)
     for _ in range(3):
         loss, h = gmb.linear_loss(x, w, y, bias=b)
