@@ -1144,11 +1144,15 @@ class Dropout:
         self.struct = DropoutStruct(seed & 0xFFFFFFFFFFFFFFFF, p, layer, None if step is None else step.data_ptr())
 
 
-def _row_struct(t, rows: int, dim: int, dtype, dev: int, name: str) -> RowsStruct:
-    """A [rows, dim] tensor of `dtype` with contiguous rows at any stride."""
-    _same_device(t, dev, name)
-    if t.dim() != 2 or t.shape[1] != dim or t.shape[0] != rows or t.dtype is not dtype:
-        raise ValueError(f"{name} must be a [{rows}, {dim}] {dtype} tensor")
+def _row_struct(t, shape, dtype, dev: int, name: str) -> RowsStruct:
+    """A tensor of that shape [rows, dim] and dtype with contiguous rows at any stride."""
+    if not isinstance(t, torch.Tensor) or t.get_device() != dev:
+        _current_device(t, name)
+    if t.shape != shape or t.dtype is not dtype:
+        raise ValueError(f"{name} must be a [{shape[0]}, {shape[1]}] {dtype} tensor")
+    rows, dim = shape
+    if t.is_contiguous():
+        return RowsStruct(t.data_ptr(), dim)
     stride, inner = t.stride()
     if (inner != 1 and dim > 1) or (stride < dim and rows > 1):
         raise ValueError(f"{name} must have contiguous rows that do not overlap")
@@ -1156,13 +1160,17 @@ def _row_struct(t, rows: int, dim: int, dtype, dev: int, name: str) -> RowsStruc
 
 
 def _row_input(x, name: str):
-    """(device, dtype code, rows, dim, struct) of the tensor that the others of a call go by."""
+    """(device, dtype code, shape, struct) of the tensor that the others of a call go by."""
     dev = _current_device(x, name)
-    if x.dim() != 2:
+    shape = x.shape
+    if len(shape) != 2:
         raise ValueError(f"{name} must be [rows, dim]")
-    code = _dtype_code(x.dtype)
-    rows, dim = x.shape
-    return dev, code, rows, dim, _row_struct(x, rows, dim, x.dtype, dev, name)
+    return dev, _dtype_code(x.dtype), shape, _row_struct(x, shape, x.dtype, dev, name)
+
+
+def _row_like(x: torch.Tensor) -> torch.Tensor:
+    """A new contiguous tensor like x."""
+    return torch.empty_like(x) if x.is_contiguous() else x.new_empty(x.shape)
 
 
 def _drop_struct(drop, dev: int):
@@ -1175,6 +1183,8 @@ def _drop_struct(drop, dev: int):
 
 def _row_keys(ids, count, rows: int, dev: int):
     """The pointers of the rows' keys and of their number on the device."""
+    if ids is None and count is None:
+        return None, None
     if ids is not None and _int32(ids, dev, "ids") != rows:
         raise ValueError("ids must have one entry per row")
     if count is not None and _int32(count, dev, "count") != 1:
@@ -1190,13 +1200,16 @@ def dropout(x: torch.Tensor, drop: Dropout, ids: torch.Tensor | None = None, res
     backward is the same call on the gradient.  With `count` (device int32 of
     one element) only the first rows are read and written.  `out` may be x or
     residual."""
-    dev, code, rows, dim, a = _row_input(x, "x")
+    dev, code, shape, a = _row_input(x, "x")
+    rows, dim = shape
     d = _drop_struct(drop, dev)
     keys, n_dev = _row_keys(ids, count, rows, dev)
-    b = None if residual is None else _row_struct(residual, rows, dim, x.dtype, dev, "residual")
+    b = None if residual is None else _row_struct(residual, shape, x.dtype, dev, "residual")
     if out is None:
-        out = x.new_empty((rows, dim))
-    o = _row_struct(out, rows, dim, x.dtype, dev, "out")
+        out = _row_like(x)
+        o = RowsStruct(out.data_ptr(), dim)
+    else:
+        o = _row_struct(out, shape, x.dtype, dev, "out")
     if rows:
         code = lib().gmb_dropout_rows(a, b, d, keys, n_dev, rows, dim, code, o, _stream_handle())
         if code:
@@ -1223,24 +1236,32 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor | None, eps: float = 1e-6, re
     is a table of records like mx_quantise's.  r is rounded to x's dtype before
     it is normed; it is x itself if nothing is added or dropped.  `count` as in
     gmb.dropout; `sum_out` may be x or residual."""
-    dev, code, rows, dim, a = _row_input(x, "x")
+    dev, code, shape, a = _row_input(x, "x")
+    rows, dim = shape
     keys, n_dev = _row_keys(ids, count, rows, dev)
-    b = None if residual is None else _row_struct(residual, rows, dim, x.dtype, dev, "residual")
+    b = None if residual is None else _row_struct(residual, shape, x.dtype, dev, "residual")
     drop = None if dropout is None else _drop_struct(dropout, dev)
     g = _norm_weight(weight, dim, dev)
     r, total = x, None
     if sum_out is not None or residual is not None or dropout is not None:
-        r = x.new_empty((rows, dim)) if sum_out is None else sum_out
-        total = _row_struct(r, rows, dim, x.dtype, dev, "sum_out")
+        if sum_out is None:
+            r = _row_like(x)
+            total = RowsStruct(r.data_ptr(), dim)
+        else:
+            r = sum_out
+            total = _row_struct(r, shape, x.dtype, dev, "sum_out")
     if bits is None:
         if out is None:
-            out = x.new_empty((rows, dim))
-        o = _row_struct(out, rows, dim, x.dtype, dev, "out")
-    else:
-        if out is None:
-            out = x.new_empty((rows, mx_row_bytes(dim, bits)), dtype=torch.uint8)
+            out = _row_like(x)
+            o = RowsStruct(out.data_ptr(), dim)
         else:
-            _same_device(out, dev, "out")
+            o = _row_struct(out, shape, x.dtype, dev, "out")
+    elif out is None:
+        stride = mx_row_bytes(dim, bits)
+        out = x.new_empty((rows, stride), dtype=torch.uint8)
+        o = RowsStruct(out.data_ptr(), stride)
+    else:
+        _same_device(out, dev, "out")
         have, stride = _records(out, dim, bits, "out")
         if have < rows:
             raise ValueError("out has fewer rows than x")
@@ -1282,17 +1303,18 @@ def rms_norm_backward(dy: torch.Tensor, r: torch.Tensor, weight: torch.Tensor | 
     elsewhere (the residual stream); `dropout`, `ids` and `count` are the
     forward's.  The weight's gradient is float32 (None without a weight), summed
     in a fixed order."""
-    dev, code, rows, dim, a = _row_input(r, "r")
-    b = _row_struct(dy, rows, dim, r.dtype, dev, "dy")
+    dev, code, shape, a = _row_input(r, "r")
+    rows, dim = shape
+    b = _row_struct(dy, shape, r.dtype, dev, "dy")
     keys, n_dev = _row_keys(ids, count, rows, dev)
-    c = None if carry is None else _row_struct(carry, rows, dim, r.dtype, dev, "carry")
+    c = None if carry is None else _row_struct(carry, shape, r.dtype, dev, "carry")
     drop = None if dropout is None else _drop_struct(dropout, dev)
     g = _norm_weight(weight, dim, dev)
-    d_residual = r.new_empty((rows, dim))
+    d_residual = _row_like(r)
     to = RowsStruct(d_residual.data_ptr(), dim)
     dx, to_x = d_residual, None
     if drop is not None:
-        dx = r.new_empty((rows, dim))
+        dx = _row_like(r)
         to_x = RowsStruct(dx.data_ptr(), dim)
     dw = dw_ptr = ws = None
     need = 0
@@ -1329,7 +1351,8 @@ def linear_loss(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, bias: to
     LinearGrads): the loss float32 of one element, the gradients of x and w of
     their dtype (w's laid out like w), the bias's float32.  `grad` is True,
     False, or the names of the gradients wanted ("x", "w", "bias")."""
-    dev, code, rows, d, a = _row_input(x, "x")
+    dev, code, shape, a = _row_input(x, "x")
+    rows, d = shape
     _same_device(w, dev, "w")
     if w.dim() != 2 or w.shape[1] != d or w.dtype is not x.dtype:
         raise ValueError(f"w must be a [classes, {d}] {x.dtype} tensor")
@@ -1349,11 +1372,11 @@ def linear_loss(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, bias: to
         want_x, want_w, want_bias = "x" in grad, "w" in grad, "bias" in grad
     row_stride, col_stride = w.stride()
     turned = row_stride == 1 and col_stride >= classes and d > 1 and classes > 1
-    dx = x.new_empty((rows, d)) if want_x else None
+    dx = _row_like(x) if want_x else None
     dw = None
     if want_w:
-        dw = w.new_empty((d, classes)).t() if turned else w.new_empty((classes, d))
-    db = bias.new_empty(classes) if want_bias and bias is not None else None
+        dw = w.new_empty((d, classes)).t() if turned else _row_like(w)
+    db = torch.empty_like(bias) if want_bias and bias is not None else None
     if loss is None:
         loss = x.new_empty(1, dtype=torch.float32)
     else:
