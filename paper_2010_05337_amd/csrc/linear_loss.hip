@@ -602,7 +602,8 @@ __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
 // chunks of a row dealt to PARTS threads.
 template <int PARTS>
 __global__ __launch_bounds__(256) void k_join_rows(const float2* stats, int chunks, int64_t rows, int64_t pad_rows,
-                                                   const int32_t* labels, const float* label_logit, float* loss_rows) {
+                                                   const int32_t* labels, const float* label_logit, float* loss_rows,
+                                                   int classes) {
   constexpr int ROWS = 256 / PARTS;
   __shared__ float2 lds[PARTS][ROWS];
   const int q = threadIdx.x % ROWS, part = threadIdx.x / ROWS;
@@ -618,7 +619,7 @@ __global__ __launch_bounds__(256) void k_join_rows(const float2* stats, int chun
   if (part || row >= rows) return;
 #pragma unroll
   for (int w = 1; w < PARTS; ++w) join_stats(top, sum, lds[w][q].x, lds[w][q].y);
-  loss_rows[row] = labels[row] >= 0 && !row_empty(top, sum) ? (row_lse(top, sum) - label_logit[row]) * kLn2 : 0.f;
+  loss_rows[row] = has_label(labels, row, classes) && !row_empty(top, sum) ? (row_lse(top, sum) - label_logit[row]) * kLn2 : 0.f;
 }
 
 // ---- products -------------------------------------------------------------
@@ -816,34 +817,49 @@ __global__ __launch_bounds__(256) void k_finish(FinishArgs p) {
   if (threadIdx.x == 0) *p.loss = static_cast<float>((((lds[0] + lds[1]) + lds[2]) + lds[3]) / static_cast<double>(p.rows));
 }
 
-// ---- small heads ----------------------------------------------------------
+// ---- few rows, small heads -------------------------------------------------
 
-// W whole in LDS, in fp32: v_mfma_f32_16x16x4_f32 (exact products, fp32 sums) on
-// what is read once, with its own strides and type: no rows are laid out, nothing
-// is cut, and G never leaves the workgroup, which has sixteen rows.  LDS rows are a multiple of four words
-// that is odd in fours apart: sixteen rows' reads of four words, and four rows'
-// of sixteen, fall on different banks.  (1,000 x 256 x 47 fp32 through k_logits
-// and k_products: 29 us of kernels in five launches, here 17 in two.)
-constexpr int kSmallClasses = 256, kSmallCells = 16384, kSmallD = 1024;
-constexpr int64_t kSmallRows = 16 * kComputeUnits;
+// v_mfma_f32_16x16x4_f32 (exact products, fp32 sums) on W as it lies, with its own
+// strides and type, read once a pass: no rows are laid out, nothing is cut, and G
+// never leaves the workgroup, which has sixteen rows (in LDS) and goes over tiles
+// of the classes of its chunk.  A tile has up to 16,384 values of W, sixteen a
+// thread: the next one is on its way in registers while this one is used.  LDS
+// rows are a multiple of four words that is odd in fours apart: sixteen rows'
+// reads of four words, and four rows' of sixteen, fall on different banks.  Code
+// is kept short: a launch starts with an empty instruction cache, and the first
+// form, its loops unrolled, took 22 us for 12.8.
+//   kBoth   all classes are one tile (1,000 x 256 x 47 fp32: 17 us in two launches,
+//           through k_logits and k_products 29 in five)
+//   kStats, kGrad   as in k_logits (5 x 226 x 147,879 fp32: 60 and 114 us for 134 MB read
+//           and 268 read and written)
+constexpr int kStreamThreads = 1024, kStreamWaves = 16;
+constexpr int kStreamClasses = 256, kStreamCells = 16384, kStreamD = 1024;   // a tile's classes, values; d
 
-struct SmallArgs {
+struct StreamArgs {
   const void* x;
   int64_t x_stride;
   const void* w;
   int64_t w_row, w_col;
   const float* bias;               // or NULL
   const int32_t* labels;
-  int rows, d, classes;
-  float mean;                      // 1 / rows
-  float* loss_rows;
-  int grad;                        // whether G is wanted
-  void* dx;                        // or NULL
-  float* dw;                       // a part a workgroup: [classes][ld_dw], turned [d][ld_dw], or NULL
-  int64_t ld_dw, part_dw;
+  int64_t rows;
+  int d, classes;
+  int tile;                        // classes of a tile, a multiple of 16
+  int tiles, row_blocks, chunks;
   int turned;
-  float* db;                       // a part a workgroup, ld_db apart, or NULL
-  int64_t ld_db;
+  float mean;                      // 1 / rows
+  float2* stats;                   // [chunks][16 row_blocks]
+  float* label_logit;              // [16 row_blocks]
+  float* loss_rows;                // [rows]
+  int grad;                        // kBoth: whether G is wanted
+  // Results, or (sums) parts of sums: dx's one a chunk, the others' one a row block.
+  void* dx;
+  int dx_sums;
+  int64_t ld_dx, part_dx;
+  void* dw;
+  float* db;
+  int dw_sums;
+  int64_t ld_dw, part_dw, part_db;
 };
 
 template <typename T>
@@ -865,178 +881,256 @@ __device__ __forceinline__ t16_f32x4 get_four(const T* p) {
   return v;
 }
 
-constexpr int kSmallThreads = 1024;
-
-// rows x cols values, element (i, j) at i row + j (N = 4: j in fours, whole ones) or
-// any j (N = 1), zeros behind them up to pad_rows x pad_cols, through put(i, j,
-// value): every thread of the workgroup, four loads on their way at a time, none
-// behind a branch (what is past the end is read where there is something, and left
-// out).
-template <int N, typename T, typename F>
-__device__ __forceinline__ void bring(const T* from, int64_t row, int64_t col, int rows, int cols, int pad_rows,
-                                      int pad_cols, F&& put) {
-  const int across = pad_cols / N;
-  int i = threadIdx.x / across, j = threadIdx.x - i * across;
-  const int step_i = kSmallThreads / across, step_j = kSmallThreads - step_i * across;
-#pragma unroll 1
-  while (i < pad_rows) {
-    t16_f32x4 v[4];
-    int at_i[4], at_j[4];
-#pragma unroll
-    for (int m = 0; m < 4; ++m) {
-      const bool in = i < rows && N * j < cols;
-      const T* p = from + (in ? i * row + N * j * col : 0);
-      if constexpr (N == 4) v[m] = get_four<T>(p);
-      else v[m][0] = as_float(*p);
-#pragma unroll
-      for (int e = 0; e < N; ++e) v[m][e] = in ? v[m][e] : 0.f;
-      at_i[m] = i;
-      at_j[m] = j;
-      i += step_i;
-      j += step_j;
-      if (j >= across) {
-        j -= across;
-        ++i;
-      }
-    }
-#pragma unroll
-    for (int m = 0; m < 4; ++m)
-      if (at_i[m] < pad_rows) put(at_i[m], N * at_j[m], v[m]);
-  }
-}
-
 __device__ __forceinline__ t16_f32x4 mfma4(float a, float b, t16_f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
 
-template <typename T>
-__global__ __launch_bounds__(kSmallThreads) void k_small_head(SmallArgs p) {
-  constexpr int kWords = (kSmallCells + 4 * kSmallClasses) + 16 * (kSmallD + 4) + 16 * (kSmallClasses + 4);
+// A thread's fours of a block of LDS rows [rows][4 across] (at most sixteen values
+// a thread): four m is row row[m], columns 4 at[m] .. + 3.
+struct Fours {
+  int row[4], at[4];               // row -1: none
+  // by_row: neighbouring threads have neighbouring fours; else neighbouring rows
+  __device__ __forceinline__ void init(int rows, int across, bool by_row) {
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      const int q = threadIdx.x + m * kStreamThreads;
+      const int a = q / (by_row ? across : rows), b = q - a * (by_row ? across : rows);
+      row[m] = q < rows * across ? (by_row ? a : b) : -1;
+      at[m] = by_row ? b : a;
+    }
+  }
+  // The values from element (row, column) at row r + column c; rows from `have` on
+  // and columns from `cols` on are 0.  No load is behind a branch: what is past the
+  // end is read where there is something, and left out.
+  template <typename T>
+  __device__ __forceinline__ void load(const T* from, int64_t r, int64_t c, int have, int cols, t16_f32x4 (&v)[4]) const {
+    if (c == 1 && cols % 4 == 0) {
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        const bool in = row[m] >= 0 && row[m] < have && 4 * at[m] < cols;
+        v[m] = get_four<T>(from + (in ? row[m] * r + 4 * at[m] : 0));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[m][e] = in ? v[m][e] : 0.f;
+      }
+    } else {
+#pragma unroll
+      for (int m = 0; m < 4; ++m)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const bool in = row[m] >= 0 && row[m] < have && 4 * at[m] + e < cols;
+          const float z = as_float(from[in ? row[m] * r + (4 * at[m] + e) * c : 0]);
+          v[m][e] = in ? z : 0.f;
+        }
+    }
+  }
+  __device__ __forceinline__ void store(float* lds, int stride, const t16_f32x4 (&v)[4]) const {
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+      if (row[m] >= 0) *reinterpret_cast<t16_f32x4*>(lds + row[m] * stride + 4 * at[m]) = v[m];
+  }
+};
+
+template <typename T, LogitsMode MODE>
+__global__ __launch_bounds__(kStreamThreads) void k_stream_head(StreamArgs p) {
+  constexpr int kWords = (kStreamCells + 4 * kStreamClasses) + 16 * (kStreamD + 4) + 16 * (kStreamClasses + 4);
   __shared__ __attribute__((aligned(16))) float lds[kWords];
-  __shared__ float lb[kSmallClasses], row_top[16][16], row_sum[16][16], row_label[16];
+  __shared__ float row_top[kStreamWaves][16], row_sum[kStreamWaves][16], row_label[16];
   __shared__ int32_t row_y[16];
-  const int ct = (p.classes + 15) / 16, dt = (p.d + 15) / 16;
-  const int sd = 16 * dt + 4, sc = 16 * ct + 4;
-  float* lw = lds;                                       // [16 ct][sd]
-  float* lx = lw + 16 * ct * sd;                         // [16][sd]
+  const int ct = p.tile / 16, dt = (p.d + 15) / 16;
+  const int sd = 16 * dt + 4, sc = p.tile + 4;
+  float* lw = lds;                                       // [tile][sd]
+  float* lx = lw + p.tile * sd;                          // [16][sd]
   float* lg = lx + 16 * sd;                              // [16][sc]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, r = lane & 15;
-  const int64_t row0 = 16 * static_cast<int64_t>(blockIdx.x);
+  const int block = blockIdx.x % p.row_blocks, chunk = blockIdx.x / p.row_blocks;
+  const int t0 = static_cast<int>(static_cast<int64_t>(p.tiles) * chunk / p.chunks);
+  const int t1 = static_cast<int>(static_cast<int64_t>(p.tiles) * (chunk + 1) / p.chunks);
+  const int64_t row0 = 16 * static_cast<int64_t>(block);
   const int rows = p.rows - row0 < 16 ? static_cast<int>(p.rows - row0) : 16;
+  const T* w = static_cast<const T*>(p.w);
+  Fours of_w;
+  t16_f32x4 next[4];
+  of_w.init(p.tile, 4 * dt, p.w_col == 1 || p.w_row != 1);
+  auto fetch = [&](int t) {
+    const int64_t c = static_cast<int64_t>(t) * p.tile;
+    const int have = p.classes - c < p.tile ? static_cast<int>(p.classes - c) : p.tile;
+    of_w.load(w + c * p.w_row, p.w_row, p.w_col, have, p.d, next);
+  };
+  fetch(t0);
   if (threadIdx.x < 16) {
     const int32_t y = static_cast<int>(threadIdx.x) < rows ? p.labels[row0 + threadIdx.x] : -1;
     row_y[threadIdx.x] = y >= 0 && y < p.classes ? y : -1;
   }
-  // the biases, times log2(e); -inf for no class
-  if (const int c = threadIdx.x; c < 16 * ct)
-    lb[c] = c < p.classes ? (p.bias ? p.bias[c] * kLog2e : 0.f) : -INFINITY;
-  // W, zeros around it, read along the direction that is contiguous
-  const T* w = static_cast<const T*>(p.w);
-  if (p.w_col == 1 && p.d % 4 == 0)
-    bring<4>(w, p.w_row, 1, p.classes, p.d, 16 * ct, 16 * dt,
-             [&](int c, int j, const t16_f32x4& v) { *reinterpret_cast<t16_f32x4*>(lw + c * sd + j) = v; });
-  else if (p.w_col == 1 || p.w_row != 1)
-    bring<1>(w, p.w_row, p.w_col, p.classes, p.d, 16 * ct, 16 * dt,
-             [&](int c, int j, const t16_f32x4& v) { lw[c * sd + j] = v[0]; });
-  else
-    bring<1>(w, p.w_col, 1, p.d, p.classes, 16 * dt, 16 * ct,
-             [&](int j, int c, const t16_f32x4& v) { lw[c * sd + j] = v[0]; });
-  __syncthreads();                                       // the labels
-  // (a row without a label is read, and left out)
-  const T* x = static_cast<const T*>(p.x) + row0 * p.x_stride;
-  auto keep = [&](int i, const t16_f32x4& v) { return row_y[i] >= 0 ? v : t16_f32x4{0.f, 0.f, 0.f, 0.f}; };
-  if (p.d % 4 == 0)
-    bring<4>(x, p.x_stride, 1, rows, p.d, 16, 16 * dt,
-             [&](int i, int j, const t16_f32x4& v) { *reinterpret_cast<t16_f32x4*>(lx + i * sd + j) = keep(i, v); });
-  else
-    bring<1>(x, p.x_stride, 1, rows, p.d, 16, 16 * dt,
-             [&](int i, int j, const t16_f32x4& v) { lx[i * sd + j] = keep(i, v)[0]; });
-  __syncthreads();
-  // logits: wave i has class tile i; a step of sixteen of d is four instructions,
-  // lane group g having d 4 g .. 4 g + 3 of them
-  t16_f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  const int y = row_y[r], c0 = 16 * wave + 4 * g;
-  if (wave < ct) {
-#pragma unroll 2
-    for (int k = 0; k < dt; ++k) {
-      const t16_f32x4 b = *reinterpret_cast<const t16_f32x4*>(lx + r * sd + 16 * k + 4 * g);
-      const t16_f32x4 a = *reinterpret_cast<const t16_f32x4*>(lw + (16 * wave + r) * sd + 16 * k + 4 * g);
+  {
+    Fours of_x;
+    t16_f32x4 v[4];
+    of_x.init(16, 4 * dt, true);
+    of_x.load(static_cast<const T*>(p.x) + row0 * p.x_stride, p.x_stride, 1, rows, p.d, v);
+    __syncthreads();                                     // the labels
 #pragma unroll
-      for (int s = 0; s < 4; ++s) acc = mfma4(a[s], b[s], acc);
+    for (int m = 0; m < 4; ++m)                          // (a row without a label is read, and left out)
+      if (of_x.row[m] >= 0 && row_y[of_x.row[m]] < 0) v[m] = t16_f32x4{0.f, 0.f, 0.f, 0.f};
+    of_x.store(lx, sd, v);
+  }
+  const int y = row_y[r];
+  float top = -INFINITY, sum = 0.f, lse = 0.f;
+  bool on = y >= 0;
+  if constexpr (MODE == kGrad) {
+    if (threadIdx.x < 256) {
+      const int q = threadIdx.x & 15, part = threadIdx.x >> 4;
+#pragma unroll 4
+      for (int c = part; c < p.chunks; c += 16) {
+        const float2 s = p.stats[(static_cast<int64_t>(c) * p.row_blocks + block) * 16 + q];
+        join_stats(top, sum, s.x, s.y);
+      }
+      row_top[part][q] = top;
+      row_sum[part][q] = sum;
     }
-    float top = -INFINITY, sum = 0.f;
+    __syncthreads();
+    top = row_top[0][r];
+    sum = row_sum[0][r];
+    for (int v = 1; v < 16; ++v) join_stats(top, sum, row_top[v][r], row_sum[v][r]);
+    lse = row_lse(top, sum);
+    on = on && !row_empty(top, sum);
+    if (chunk == 0 && wave == 0 && g == 0 && r < rows)
+      p.loss_rows[row0 + r] = on ? (lse - p.label_logit[row0 + r]) * kLn2 : 0.f;
+  }
+  t16_f32x4 dx[4];                                       // d tiles wave, wave + 16, ...
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      acc[e] = fmaf(acc[e], kLog2e, lb[c0 + e]);
-      if (c0 + e == y) row_label[r] = acc[e];
-      top = fmaxf(top, acc[e]);
+  for (int m = 0; m < 4; ++m) dx[m] = t16_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+  for (int t = t0; t < t1; ++t) {
+    const int c_tile = t * p.tile;
+    if (t > t0) __syncthreads();                         // the last tile is used
+    of_w.store(lw, sd, next);
+    if (t + 1 < t1) fetch(t + 1);
+    __syncthreads();
+    // logits: wave i has 16 classes of the tile; a step of sixteen of d is four
+    // instructions, lane group g having d 4 g .. 4 g + 3 of them
+    t16_f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    const int c0 = 16 * wave + 4 * g;
+    if (wave < ct) {
+      for (int k = 0; k < dt; ++k) {
+        const t16_f32x4 b = *reinterpret_cast<const t16_f32x4*>(lx + r * sd + 16 * k + 4 * g);
+        const t16_f32x4 a = *reinterpret_cast<const t16_f32x4*>(lw + (16 * wave + r) * sd + 16 * k + 4 * g);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) acc = mfma4(a[s], b[s], acc);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int c = c_tile + c0 + e;
+        const float bias = p.bias ? p.bias[c < p.classes ? c : 0] : 0.f;
+        acc[e] = c < p.classes ? fmaf(acc[e], kLog2e, bias * kLog2e) : -INFINITY;
+      }
+      if constexpr (MODE != kGrad) {
+        const float most = fmaxf(fmaxf(fmaxf(acc[0], acc[1]), fmaxf(acc[2], acc[3])), top);
+        const float base = most == -INFINITY ? 0.f : most;
+        sum *= exp2_fast(top - base);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          sum += exp2_fast(acc[e] - base);
+          if (c_tile + c0 + e == y) {
+            if constexpr (MODE == kBoth) row_label[r] = acc[e];
+            else p.label_logit[row0 + r] = acc[e];
+          }
+        }
+        top = most;
+      }
     }
-    const float base = top == -INFINITY ? 0.f : top;
+    if constexpr (MODE == kBoth) {
+      for (int o = 16; o < 64; o <<= 1) join_stats(top, sum, __shfl_xor(top, o, 64), __shfl_xor(sum, o, 64));
+      if (g == 0) {
+        row_top[wave][r] = top;
+        row_sum[wave][r] = sum;
+      }
+      __syncthreads();
+      top = row_top[0][r];
+      sum = row_sum[0][r];
+      for (int v = 1; v < ct; ++v) join_stats(top, sum, row_top[v][r], row_sum[v][r]);
+      lse = row_lse(top, sum);
+      on = on && !row_empty(top, sum);
+      if (wave == 0 && g == 0 && r < rows) p.loss_rows[row0 + r] = on ? (lse - row_label[r]) * kLn2 : 0.f;
+      if (!p.grad) return;
+    }
+    if constexpr (MODE != kStats) {
+      if (wave < ct) {
+        t16_f32x4 v;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sum += exp2_fast(acc[e] - base);
+        for (int e = 0; e < 4; ++e) {
+          const float q = exp2_fast(acc[e] - lse);
+          v[e] = on ? (c_tile + c0 + e == y ? q - 1.f : q) : 0.f;
+        }
+        *reinterpret_cast<t16_f32x4*>(lg + r * sc + c0) = v;
+      }
+      __syncthreads();
+      if (const int c = threadIdx.x; p.db && c < p.tile && c_tile + c < p.classes) {
+        float s = 0.f;
+#pragma unroll 4
+        for (int i = 0; i < 16; ++i) s += lg[i * sc + c];
+        p.db[block * p.part_db + c_tile + c] = p.dw_sums ? s : s * p.mean;
+      }
+      if (p.dx) {
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          const int q = wave + 16 * m;
+          if (q < dt) {
+            for (int k = 0; k < ct; ++k) {
+              const t16_f32x4 b = *reinterpret_cast<const t16_f32x4*>(lg + r * sc + 16 * k + 4 * g);
+#pragma unroll
+              for (int s = 0; s < 4; ++s) dx[m] = mfma4(lw[(16 * k + 4 * g + s) * sd + 16 * q + r], b[s], dx[m]);
+            }
+          }
+        }
+      }
+      if (p.dw) {
+        for (int q = wave; q < ct * dt; q += kStreamWaves) {
+          const int tc = q / dt, tj = q - tc * dt;
+          t16_f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int s = 0; s < 4; ++s) {
+            const float a = lx[(4 * g + s) * sd + 16 * tj + r], b = lg[(4 * g + s) * sc + 16 * tc + r];
+            v = p.turned ? mfma4(b, a, v) : mfma4(a, b, v);
+          }
+          // a row of the result, and four of its columns
+          const int row = p.turned ? 16 * tj + r : c_tile + 16 * tc + r;
+          const int col = p.turned ? c_tile + 16 * tc + 4 * g : 16 * tj + 4 * g;
+          const int left = (p.turned ? p.classes : p.d) - col;
+          if (row >= (p.turned ? p.d : p.classes) || left <= 0) continue;
+          const int64_t at = row * p.ld_dw + col;
+          if (p.dw_sums) mx_put<16, false>(static_cast<float*>(p.dw) + block * p.part_dw + at, &v);   // (rows of whole fours)
+          else put_four<sizeof(T) == 2>(p.dw, at, v * p.mean, left);
+        }
+      }
+    }
+  }
+  if constexpr (MODE == kStats) {
     for (int o = 16; o < 64; o <<= 1) join_stats(top, sum, __shfl_xor(top, o, 64), __shfl_xor(sum, o, 64));
     if (g == 0) {
       row_top[wave][r] = top;
       row_sum[wave][r] = sum;
     }
-  }
-  __syncthreads();
-  float top = row_top[0][r], sum = row_sum[0][r];
-  for (int v = 1; v < ct; ++v) join_stats(top, sum, row_top[v][r], row_sum[v][r]);
-  const float lse = row_lse(top, sum);
-  const bool on = y >= 0 && !row_empty(top, sum);
-  if (wave == 0 && g == 0 && r < rows) p.loss_rows[row0 + r] = on ? (lse - row_label[r]) * kLn2 : 0.f;
-  if (!p.grad) return;
-  if (wave < ct) {
-    t16_f32x4 v;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float q = exp2_fast(acc[e] - lse);
-      v[e] = on ? (c0 + e == y ? q - 1.f : q) : 0.f;
+    __syncthreads();
+    if (threadIdx.x < 16) {
+      for (int v = 1; v < ct; ++v) join_stats(top, sum, row_top[v][r], row_sum[v][r]);
+      p.stats[(static_cast<int64_t>(chunk) * p.row_blocks + block) * 16 + r] = make_float2(top, sum);
     }
-    *reinterpret_cast<t16_f32x4*>(lg + r * sc + c0) = v;
-  }
-  __syncthreads();
-  if (p.db && static_cast<int>(threadIdx.x) < p.classes) {
-    float s = 0.f;
-#pragma unroll 4
-    for (int i = 0; i < 16; ++i) s += lg[i * sc + threadIdx.x];
-    p.db[blockIdx.x * p.ld_db + threadIdx.x] = s;
-  }
-  if (p.dx) {
-    for (int q = wave; q < dt; q += 16) {
-      t16_f32x4 v = {0.f, 0.f, 0.f, 0.f};
-      for (int k = 0; k < ct; ++k) {
-        const t16_f32x4 b = *reinterpret_cast<const t16_f32x4*>(lg + r * sc + 16 * k + 4 * g);
+  } else if (p.dx && r < rows) {
 #pragma unroll
-        for (int s = 0; s < 4; ++s) v = mfma4(lw[(16 * k + 4 * g + s) * sd + 16 * q + r], b[s], v);
-      }
-      const int col = 16 * q + 4 * g;
-      if (r < rows && col < p.d) put_four<sizeof(T) == 2>(p.dx, (row0 + r) * p.d + col, v * p.mean, p.d - col);
-    }
-  }
-  if (p.dw) {
-    float* part = p.dw + blockIdx.x * p.part_dw;
-    for (int q = wave; q < ct * dt; q += 16) {
-      const int tc = q / dt, tj = q - tc * dt;
-      t16_f32x4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const float a = lx[(4 * g + s) * sd + 16 * tj + r], b = lg[(4 * g + s) * sc + 16 * tc + r];
-        v = p.turned ? mfma4(b, a, v) : mfma4(a, b, v);
-      }
-      // (the part's rows are whole fours)
-      const int row = (p.turned ? 16 * tj : 16 * tc) + r, col = (p.turned ? 16 * tc : 16 * tj) + 4 * g;
-      if (row < (p.turned ? p.d : p.classes) && col < p.ld_dw) mx_put<16, false>(part + row * p.ld_dw + col, &v);
+    for (int m = 0; m < 4; ++m) {
+      const int col = 16 * (wave + 16 * m) + 4 * g;
+      if (col >= p.d) continue;
+      const int64_t at = (row0 + r) * p.ld_dx + col;
+      if (p.dx_sums) mx_put<16, false>(static_cast<float*>(p.dx) + chunk * p.part_dx + at, &dx[m]);
+      else put_four<sizeof(T) == 2>(p.dx, at, dx[m] * p.mean, p.d - col);
     }
   }
 }
 
 // ---- plan -----------------------------------------------------------------
 
-// Tiles of a product: 256 x 256 (four waves of 128 x 128, one workgroup a CU) or
-// 64 x 64.
+// Tiles: 256 x 256 (eight waves of 128 x 64, one workgroup a CU), 64 x 64 (four of 32 x
+// 32).
 constexpr int kLarge = 256, kSmall = 64;
 // G of a piece of the classes: less costs launches whose tiles do not fill the GPU
 // and sums that are stored in between (4,000 x 256 x 100,000 bf16 at 64, 128, 256, 512
@@ -1053,7 +1147,9 @@ struct Plan {
   int es;                          // 16-bit words of a value
   int64_t pad_rows, pad_d, pad_classes;
   bool copy_w, grad, both;         // both: statistics and G in one launch
-  int small;                       // workgroups of a small head, or 0
+  // k_stream_head: row blocks (0: not taken), chunks and tiles of the classes
+  int row_blocks, stream_chunks, stream_tile, stream_tiles;
+  bool one_tile;
   int64_t piece, pieces;           // classes of a piece (a multiple of kPadRows)
   int tile;                        // of the logits
   int chunks, piece_chunks;        // workgroups of a row tile, for the statistics and for G
@@ -1065,6 +1161,98 @@ struct Plan {
   size_t x_all, x_row, w, row_top, tops, row_inverse, inverses, labels, stats, label_logit, loss_rows, g, db, dx_sums,
       dw_sums, total;
 };
+
+// Which tiles k_products takes, and how many splits of k, by when an XCD's
+// workgroups end: its tiles are an eighth of dx's first, each `long_` stages, then
+// dw's; done in t if what fits until then is enough.  A kind of tile: its edge,
+// workgroups of a CU, microseconds of a stage and of a tile of sums that is stored
+// (bf16 and kSplit alike, in stages of 64 elements).  The whole call, us, with 256 /
+// with 64, * the rule's: 784 x 631 x 4,132 fp32 150 / 111 *; 1,000 x 256 x 5,000 bf16 79 / 48
+// *; 445 x 8 x 73,341 fp32 196 / 134 *; 8,192 x 1,024 x 2,048 bf16 167 * / 195; 4,000 x 256 x
+// 20,011 fp32 583 * / 650; 4,000 x 256 x 100,000 bf16 1,079 * / 1,440.  (128 x 128, two a CU:
+// 118, 64, 150, 169, 575, 1,194.)
+struct TileKind {
+  int edge, each;
+  double stage, sums;
+};
+constexpr TileKind kTileKinds[] = {{kLarge, 1, 1.9, 20.0}, {kSmall, 4, 0.8, 3.0}};
+
+void plan_products(const LinearLossArgs& a, Plan* p) {
+  const int64_t have = p->piece < a.classes ? p->piece : a.classes, k = 64 / p->es;
+  const int64_t dx_stages = tiles_of(have, k), dw_stages = tiles_of(a.rows, k);
+  auto most_splits = [](int64_t stages) { return stages < 8 ? int64_t{1} : stages / 4; };
+  double best = -1.0;
+  for (const TileKind& kind : kTileKinds) {
+    // (tiles that are mostly padding)
+    if (kind.edge > kSmall && (a.rows <= kind.edge / 4 || a.d <= kind.edge / 4 || have <= kind.edge / 4)) continue;
+    const int64_t slots = kind.each * kComputeUnits / 8, slab = static_cast<int64_t>(kind.sums / kind.stage + 0.5);
+    const int64_t d_tiles = tiles_of(a.d, kind.edge);
+    const int64_t dx_tiles = a.dx ? d_tiles * tiles_of(a.rows, kind.edge) : 0;
+    const int64_t dw_tiles = a.dw ? d_tiles * tiles_of(have, kind.edge) : 0;
+    for (int sw = 1; sw <= 64 && sw <= most_splits(dw_stages) && dw_tiles * (sw / 2) < 8 * slots; sw *= 2) {
+      const int64_t short_ = tiles_of(dw_stages, sw) + (sw > 1 ? slab : 0), shorts = tiles_of(dw_tiles * sw, 8);
+      for (int sx = 1; sx <= 256 && sx <= most_splits(dx_stages) && dx_tiles * (sx - 1) < 8 * slots; sx += sx < 8 ? 1 : sx / 4) {
+        const bool sums = sx > 1 || p->pieces > 1;
+        const int64_t long_ = tiles_of(dx_stages, sx) + (sums ? slab : 0), longs = tiles_of(dx_tiles * sx, 8);
+        const int64_t rounds = longs / slots, more = longs % slots;
+        auto fits = [&](int64_t t) {
+          const int64_t a0 = t - rounds * long_, a1 = a0 - long_;
+          if (a0 < 0 || (more && a1 < 0)) return false;
+          return (slots - more) * (a0 / short_) + (more ? more * (a1 / short_) : 0) >= shorts;
+        };
+        int64_t lo = (rounds + (more ? 1 : 0)) * long_, hi = lo + (shorts / slots + 2) * short_;
+        while (lo < hi) {
+          const int64_t mid = (lo + hi) / 2;
+          if (fits(mid)) hi = mid;
+          else lo = mid + 1;
+        }
+        // (sums are joined by the whole GPU: 4.5 TB/s)
+        const double joined = ((sw > 1 ? dw_tiles * sw : 0) + (sx > 1 ? dx_tiles * sx : 0)) *
+                              (static_cast<double>(kind.edge) * kind.edge * 4 / 4.5e6);
+        const double cost = static_cast<double>(lo) * kind.stage + joined;
+        if (best < 0 || cost < best) {
+          best = cost;
+          p->product_tile = kind.edge;
+          p->dx_splits = sx;
+          p->dw_splits = sw;
+        }
+      }
+    }
+  }
+}
+
+// Whether k_stream_head takes it, and how (us of the whole call, with it / by
+// k_logits and k_products):
+//   - fp32, sixteen rows at most: its fp32 products (157 TFLOP/s) hide behind
+//     reading W (5 x 226 x 147,879: 178 / 268; 1 x 128 x 5,000: 25 / 30), or a short
+//     pass (1,000 x 256 x 47: 20 / 29; 300 x 32 x 2,000: 27 / 29; but 165 x 177 x 1,577,
+//     2^25.7 products: 43 / 34), its sums of dW 64 MB at most;
+//   - bf16, where nothing else need be laid out, only short passes of one tile
+//     (64 x 16 x 8: 20 / 28; but 1,000 x 128 x 172, two tiles: 32 / 28), or few rows
+//     whose W would be copied (16 x 100 x 100,000: 53 / 68; x 256 x 100,000: 101 / 82).
+constexpr int64_t kStreamWork = int64_t{1} << 25, kStreamSums = int64_t{16} << 20;
+
+bool plan_stream(const LinearLossArgs& a, int bf16, Plan* p) {
+  if (a.d > kStreamD) return false;
+  const int64_t blocks = tiles_of(a.rows, 16), pad_d = round_up(a.d, 16);
+  int64_t tile = kStreamCells / pad_d / 16 * 16;
+  tile = std::min<int64_t>(std::min<int64_t>(tile, kStreamClasses), round_up(a.classes, 16));
+  const int64_t tiles = tiles_of(a.classes, static_cast<int>(tile));
+  int64_t chunks = tiles_of(kComputeUnits, blocks);
+  chunks = std::min(chunks, tiles);
+  if (blocks > kComputeUnits) return false;
+  const bool brief = 16 * blocks * pad_d * a.classes <= kStreamWork;
+  if (blocks > 1 && (!brief || blocks * a.classes * static_cast<int64_t>(a.d) > kStreamSums)) return false;
+  if (bf16 && !(tiles == 1 && brief) &&
+      !(blocks == 1 && a.d % kPadCols != 0 && static_cast<int64_t>(a.classes) * a.d >= int64_t{1} << 20))
+    return false;
+  p->row_blocks = static_cast<int>(blocks);
+  p->stream_tile = static_cast<int>(tile);
+  p->stream_tiles = static_cast<int>(tiles);
+  p->stream_chunks = static_cast<int>(chunks);
+  p->one_tile = tiles == 1;
+  return true;
+}
 
 Plan plan(const LinearLossArgs& a, int bf16) {
   Plan p{};
@@ -1085,12 +1273,14 @@ Plan plan(const LinearLossArgs& a, int bf16) {
     at += static_cast<size_t>(round_up(bytes, 256));
     return here;
   };
-  if (round_up(a.classes, 16) * round_up(a.d, 16) <= kSmallCells && a.classes <= kSmallClasses && a.d <= kSmallD &&
-      a.rows <= kSmallRows) {
-    p.small = static_cast<int>(tiles_of(a.rows, 16));
+  if (plan_stream(a, bf16, &p)) {
+    const int64_t pad = 16 * static_cast<int64_t>(p.row_blocks);
+    p.stats = p.one_tile ? 0 : take(p.stream_chunks * pad * 8);
+    p.label_logit = p.one_tile ? 0 : take(pad * 4);
     p.loss_rows = take(a.rows * 4);
-    p.db = a.db ? take(p.small * round_up(a.classes, 4) * 4) : 0;
-    p.dw_sums = a.dw ? take(p.small * p.dw_rows * p.ld_dw * 4) : 0;
+    p.db = a.db && p.row_blocks > 1 ? take(p.row_blocks * round_up(a.classes, 4) * 4) : 0;
+    p.dw_sums = a.dw && p.row_blocks > 1 ? take(p.row_blocks * p.dw_rows * p.ld_dw * 4) : 0;
+    p.dx_sums = a.dx && p.stream_chunks > 1 ? take(p.stream_chunks * a.rows * round_up(a.d, 4) * 4) : 0;
     p.total = at;
     return p;
   }
@@ -1099,7 +1289,14 @@ Plan plan(const LinearLossArgs& a, int bf16) {
   p.pieces = tiles_of(p.pad_classes, piece);
   p.piece = round_up(tiles_of(p.pad_classes, p.pieces), kPadRows);
   p.pieces = tiles_of(p.pad_classes, p.piece);
-  p.tile = tiles_of(a.rows, kLarge) * tiles_of(a.classes, kLarge) >= kComputeUnits / 2 ? kLarge : kSmall;
+  // Large tiles of logits where there are enough, few of their rows are padding, and
+  // rows or products many (256 / 64, us of the whole call: 4,000 x 64 x 10,000 bf16 82.6 /
+  // 87.8, 8,192 x 1,024 x 2,048 164 / 201; but 300 x 100 x 50,000 75 / 66, 1,000 x 128 x
+  // 20,000 71 / 69, 784 x 631 x 4,132 fp32, 68 tiles, 155 / 112)
+  p.tile = tiles_of(a.rows, kLarge) * tiles_of(a.classes, kLarge) >= kComputeUnits / 2 &&
+                   8 * a.rows >= 7 * p.pad_rows && (a.rows > 1024 || a.d >= 256)
+               ? kLarge
+               : kSmall;
   p.both = a.classes <= kSmall;
   if (p.both) p.tile = kSmall;
   // workgroups of a row tile: one for each CU (two for small tiles) where the
@@ -1111,52 +1308,8 @@ Plan plan(const LinearLossArgs& a, int bf16) {
   };
   p.chunks = chunks(a.classes);
   p.piece_chunks = chunks(p.piece < a.classes ? p.piece : a.classes);
-  const int64_t k = 64 / p.es;
-  {
-    const int64_t have = p.piece < a.classes ? p.piece : a.classes;
-    const int64_t dx = tiles_of(a.d, kLarge) * tiles_of(a.rows, kLarge), dw = tiles_of(a.d, kLarge) * tiles_of(have, kLarge);
-    const bool large = (dx * have / k + dw * a.rows / k) / 8 >= kComputeUnits / 2;
-    p.product_tile = large ? kLarge : kSmall;
-    const int tile = p.product_tile;
-    const int64_t dx_stages = tiles_of(have, k), dw_stages = tiles_of(a.rows, k);
-    const int64_t dx_tiles = a.dx ? tiles_of(a.d, tile) * tiles_of(a.rows, tile) : 0;
-    const int64_t dw_tiles = a.dw ? tiles_of(a.d, tile) * tiles_of(have, tile) : 0;
-    const int64_t slots = (large ? 1 : 4) * kComputeUnits / 8;   // of an XCD
-    auto most_splits = [](int64_t stages) { return stages < 8 ? int64_t{1} : stages / 4; };
-    // The numbers of splits that let an XCD's workgroups end soonest.  Its tiles:
-    // an eighth of dx's first, each `long_` stages, then dw's; done in t if what
-    // fits until then is enough.  A tile of sums that were split is stored (worth
-    // `slab` stages there) and joined (1 / 20 of a stage of the whole GPU).
-    const int64_t slab = large ? 12 : 3;
-    double best = -1.0;
-    p.dx_splits = p.dw_splits = 1;
-    for (int sw = 1; sw <= 64 && sw <= most_splits(dw_stages) && dw_tiles * (sw / 2) < 8 * slots; sw *= 2) {
-      const int64_t short_ = tiles_of(dw_stages, sw) + (sw > 1 ? slab : 0), shorts = tiles_of(dw_tiles * sw, 8);
-      for (int sx = 1; sx <= 64 && sx <= most_splits(dx_stages) && dx_tiles * (sx - 1) < 8 * slots; sx += sx < 8 ? 1 : sx / 4) {
-        const bool sums = sx > 1 || p.pieces > 1;
-        const int64_t long_ = tiles_of(dx_stages, sx) + (sums ? slab : 0), longs = tiles_of(dx_tiles * sx, 8);
-        const int64_t rounds = longs / slots, more = longs % slots;
-        auto fits = [&](int64_t t) {
-          const int64_t a0 = t - rounds * long_, a1 = a0 - long_;
-          if (a0 < 0 || (more && a1 < 0)) return false;
-          return (slots - more) * (a0 / short_) + (more ? more * (a1 / short_) : 0) >= shorts;
-        };
-        int64_t lo = (rounds + (more ? 1 : 0)) * long_, hi = lo + (shorts / slots + 2) * short_;
-        while (lo < hi) {
-          const int64_t mid = (lo + hi) / 2;
-          if (fits(mid)) hi = mid;
-          else lo = mid + 1;
-        }
-        const double cost = static_cast<double>(lo) + ((sw > 1 ? dw_tiles * sw : 0) + (sx > 1 ? dx_tiles * sx : 0)) / 20.0;
-        if (best < 0 || cost < best) {
-          best = cost;
-          p.dx_splits = sx;
-          p.dw_splits = sw;
-        }
-      }
-    }
-    p.dx_slab = p.dx_splits > 1 || p.pieces > 1;
-  }
+  plan_products(a, &p);
+  p.dx_slab = p.dx_splits > 1 || p.pieces > 1;
   const int64_t x_bytes = p.pad_rows * p.pad_d * 2 * p.es;
   p.x_all = take(x_bytes);
   p.x_row = bf16 ? p.x_all : take(x_bytes);
@@ -1211,10 +1364,11 @@ hipError_t finish(FinishArgs f, const LinearLossArgs& a, const float* loss_rows,
 }
 
 template <typename T>
-hipError_t run_small(const LinearLossArgs& a, const Plan& p, hipStream_t s) {
+hipError_t run_stream(const LinearLossArgs& a, const Plan& p, hipStream_t s) {
   auto floats = [&](size_t off) { return reinterpret_cast<float*>(a.ws + off); };
   const float mean = static_cast<float>(1.0 / static_cast<double>(a.rows));
-  SmallArgs m{};
+  const int64_t ld_dx = round_up(a.d, 4);
+  StreamArgs m{};
   m.x = a.x;
   m.x_stride = a.x_stride;
   m.w = a.w;
@@ -1222,23 +1376,43 @@ hipError_t run_small(const LinearLossArgs& a, const Plan& p, hipStream_t s) {
   m.w_col = a.w_col;
   m.bias = a.bias;
   m.labels = a.labels;
-  m.rows = static_cast<int>(a.rows);
+  m.rows = a.rows;
   m.d = a.d;
   m.classes = a.classes;
+  m.tile = p.stream_tile;
+  m.tiles = p.stream_tiles;
+  m.row_blocks = p.row_blocks;
+  m.chunks = p.stream_chunks;
+  m.turned = a.turned;
   m.mean = mean;
+  m.stats = reinterpret_cast<float2*>(a.ws + p.stats);
+  m.label_logit = floats(p.label_logit);
   m.loss_rows = floats(p.loss_rows);
   m.grad = p.grad;
-  m.dx = a.dx;
-  m.dw = a.dw ? floats(p.dw_sums) : nullptr;
-  m.ld_dw = p.ld_dw;
+  m.dx_sums = p.stream_chunks > 1;
+  m.dx = a.dx && m.dx_sums ? floats(p.dx_sums) : a.dx;
+  m.ld_dx = m.dx_sums ? ld_dx : a.d;
+  m.part_dx = a.rows * ld_dx;
+  m.dw_sums = p.row_blocks > 1;
+  m.dw = a.dw && m.dw_sums ? floats(p.dw_sums) : a.dw;
+  m.db = a.db && m.dw_sums ? floats(p.db) : a.db;
+  m.ld_dw = m.dw_sums ? p.ld_dw : p.dw_cols;
   m.part_dw = p.dw_rows * p.ld_dw;
-  m.turned = a.turned;
-  m.db = a.db ? floats(p.db) : nullptr;
-  m.ld_db = round_up(a.classes, 4);
-  hipLaunchKernelGGL(k_small_head<T>, dim3(static_cast<unsigned>(p.small)), dim3(kSmallThreads), 0, s, m);
+  m.part_db = round_up(a.classes, 4);
+  const dim3 grid(static_cast<unsigned>(p.row_blocks * p.stream_chunks)), threads(kStreamThreads);
+  if (p.one_tile) {
+    hipLaunchKernelGGL((k_stream_head<T, kBoth>), grid, threads, 0, s, m);
+  } else {
+    hipLaunchKernelGGL((k_stream_head<T, kStats>), grid, threads, 0, s, m);
+    if (p.grad) hipLaunchKernelGGL((k_stream_head<T, kGrad>), grid, threads, 0, s, m);
+    else
+      hipLaunchKernelGGL(k_join_rows<16>, dim3(static_cast<unsigned>(p.row_blocks)), dim3(256), 0, s, m.stats, m.chunks,
+                         a.rows, 16 * static_cast<int64_t>(p.row_blocks), a.labels, m.label_logit, m.loss_rows, a.classes);
+  }
   FinishArgs f{};
-  if (a.dw) f.dw = join_of(m.dw, p.small, p.dw_rows, p.dw_cols, p.ld_dw, mean, nullptr, a.dw);
-  if (a.db) f.db = join_of(m.db, p.small, 1, a.classes, m.ld_db, mean, nullptr, a.db);
+  if (a.dx && m.dx_sums) f.dx = join_of(floats(p.dx_sums), m.chunks, a.rows, a.d, ld_dx, mean, nullptr, a.dx);
+  if (a.dw && m.dw_sums) f.dw = join_of(floats(p.dw_sums), m.row_blocks, p.dw_rows, p.dw_cols, p.ld_dw, mean, nullptr, a.dw);
+  if (a.db && m.dw_sums) f.db = join_of(floats(p.db), m.row_blocks, 1, a.classes, m.part_db, mean, nullptr, a.db);
   return finish<sizeof(T) == 2>(f, a, m.loss_rows, s);
 }
 
@@ -1246,7 +1420,7 @@ template <T16Type TYPE, typename T>
 hipError_t run(const LinearLossArgs& a, hipStream_t s) {
   constexpr bool kLo = TYPE == kBf16;
   const Plan p = plan(a, kLo);
-  if (p.small) return run_small<T>(a, p, s);
+  if (p.row_blocks) return run_stream<T>(a, p, s);
   auto at = [&](size_t off) { return a.ws + off; };
   auto floats = [&](size_t off) { return reinterpret_cast<float*>(a.ws + off); };
   uint16_t* x_all = reinterpret_cast<uint16_t*>(at(p.x_all));
@@ -1356,7 +1530,7 @@ hipError_t run(const LinearLossArgs& a, hipStream_t s) {
     if (!p.grad) {
       const auto join = p.tile == kLarge ? k_join_rows<2> : k_join_rows<4>;
       hipLaunchKernelGGL(join, dim3(static_cast<unsigned>(p.pad_rows / (p.tile == kLarge ? 128 : 64))), dim3(256), 0, s,
-                         g.stats, p.chunks, a.rows, p.pad_rows, labels, g.label_logit, g.loss_rows);
+                         g.stats, p.chunks, a.rows, p.pad_rows, labels, g.label_logit, g.loss_rows, a.classes);
     }
   }
   const float mean = static_cast<float>((kLo ? 1.0 : 1.0 / kGradScale) / static_cast<double>(a.rows));
