@@ -531,8 +531,8 @@ void norm_shape(int dim, F&& f) {
   else if (pieces <= 256) f(NormShape<256, 1>{});
   else if (pieces <= 512) f(NormShape<256, 2>{});
   else if (pieces <= 1024) f(NormShape<256, 4>{});
-  else if (pieces <= 2048) f(NormShape<1024, 2, false>{});
-  else if (pieces <= 4096) f(NormShape<1024, 4, false>{});
+  else if (pieces <= 2048) f(NormShape<1024, 2>{});
+  else if (pieces <= 4096) f(NormShape<1024, 4>{});
   else f(NormShape<1024, 8, false>{});
 }
 
