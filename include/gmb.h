@@ -713,21 +713,24 @@ typedef struct {
 
 /* Bytes of workspace gmb_linear_loss needs (0 for bad arguments); of the
  * pointers of `grads` (NULL: the loss alone) only NULL or not counts, of w its
- * alignment.  It grows with rows (d + classes / 16) and, with gradients, by 384
- * MB at most (more from 393,216 rows on) and the sums that are split; the
- * logits are never stored. */
+ * alignment.  It holds 16-bit copies of x and, unless it is bf16 in aligned rows
+ * of a multiple of 64 values, of W (its size, rows rounded up to 64 values), and
+ * with gradients 384 MB at most of G = softmax(z) - onehot (a piece of the
+ * classes; more from 393,216 rows on), sums of dbias (rows classes / 16 bytes)
+ * and those of dx and dw that are split.  The logits are never stored.  0 too
+ * where the three extents together are more than a launch takes. */
 size_t gmb_linear_loss_workspace_bytes(const gmb_linear_head* head, const gmb_linear_grads* grads);
 
 /* The mean over the rows (those without a label count as 0) of -log
  * softmax(z)_label, and its gradients.  A row whose logits are all -inf has
  * neither.  x and W are finite; with a NaN or an infinity among them the loss
  * is NaN, or the row of that x.  bf16: exact products, fp32 sums and statistics,
- * softmax(z) - onehot rounded to bf16 before its products.  fp32: every operand
- * is cut into two fp16 parts at a power-of-two scale (x by rows for the
- * logits; W, and x for dw, as a whole), a product is three of the four part
- * products; the error is of the order of an fp32 sum's beside the operand's
- * largest value (elements below 2^-16 of it lose bits, below 2^-39 of it are
- * lost; so are gradients of a logit below 2^-39).
+ * softmax(z) - onehot rounded to bf16 before its products.  fp32: few rows or
+ * classes by fp32 products; else every operand is cut into two fp16 parts at a
+ * power-of-two scale (x by rows for the logits; W, and x for dw, as a whole), a
+ * product is three of the four part products; the error is of the order of an
+ * fp32 sum's beside the operand's largest value (elements below 2^-16 of it lose
+ * bits, below 2^-39 of it are lost; so are gradients of a logit below 2^-39).
  * Nothing is added by atomics: the same bits every time.  The mean is summed in
  * 64 bits.
  *   loss  device fp32 scalar

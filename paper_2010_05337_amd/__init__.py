@@ -522,11 +522,12 @@ def sage_forward(blocks: Blocks, feats: torch.Tensor, weights: SageWeights,
     if logits is None:
         logits = torch.empty((max(B, 0), C), dtype=torch.float32, device=feats.device)
     L, stream = lib(), _stream_handle()
+    drop = None if dropout is None else _drop_struct(dropout, feats.get_device())
 
     def call(ws):
-        if dropout is not None:
+        if drop is not None:
             return L.gmb_sage_forward_dropout(ctypes.byref(blocks.struct), feats.data_ptr(), None, 0,
-                                              ctypes.byref(weights.struct), dropout.struct, logits.data_ptr(),
+                                              ctypes.byref(weights.struct), drop, logits.data_ptr(),
                                               ws.data_ptr(), ws.numel(), None, stream)
         return L.gmb_sage_forward(ctypes.byref(blocks.struct), feats.data_ptr(), ctypes.byref(weights.struct),
                                   logits.data_ptr(), ws.data_ptr(), ws.numel(), stream)
@@ -580,11 +581,12 @@ def sage_forward_fused(blocks: Blocks, feats: torch.Tensor, weights: SageWeights
     if logits is None:
         logits = torch.empty((max(B, 0), C), dtype=torch.float32, device=feats.device)
     L, stream, status = lib(), _stream_handle(), blocks.csr.status_word
+    drop = None if dropout is None else _drop_struct(dropout, feats.get_device())
 
     def call(ws):
-        if dropout is not None:
+        if drop is not None:
             return L.gmb_sage_forward_dropout(ctypes.byref(blocks.struct), x_dst.data_ptr(), feats.data_ptr(),
-                                              feats.shape[0], ctypes.byref(weights.struct), dropout.struct,
+                                              feats.shape[0], ctypes.byref(weights.struct), drop,
                                               logits.data_ptr(), ws.data_ptr(), ws.numel(), status, stream)
         return L.gmb_sage_forward_fused(ctypes.byref(blocks.struct), feats.data_ptr(), feats.shape[0],
                                         x_dst.data_ptr(), ctypes.byref(weights.struct), logits.data_ptr(),
@@ -708,7 +710,7 @@ def sage_backward_from(blocks: Blocks, feats: torch.Tensor, weights: SageWeights
         grads = SageGrads(weights)
     _check(lib().gmb_sage_backward_from(ctypes.byref(blocks.struct), feats.data_ptr(), ctypes.byref(weights.struct),
                                         d_logits.data_ptr() or feats.data_ptr(),
-                                        None if dropout is None else dropout.struct, fwd_workspace.data_ptr(),
+                                        None if dropout is None else _drop_struct(dropout, dev), fwd_workspace.data_ptr(),
                                         fwd_workspace.numel(), ctypes.byref(grads.struct), workspace.data_ptr(),
                                         workspace.numel(), *table, _stream_handle()))
     return grads
@@ -1234,8 +1236,9 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor | None, eps: float = 1e-6, re
     `dropout`, rows keyed as in gmb.dropout): returns (y, r), y = weight r /
     sqrt(mean(r^2) + eps).  y has x's dtype, or, with `bits` (MXFP4 or MXFP8),
     is a table of records like mx_quantise's.  r is rounded to x's dtype before
-    it is normed; it is x itself if nothing is added or dropped.  `count` as in
-    gmb.dropout; `sum_out` may be x or residual."""
+    it is normed; it is x itself if nothing is added or dropped (with out=x too:
+    then it holds y).  `count` as in gmb.dropout; `sum_out` may be x or residual,
+    so may `out` if `sum_out` is not."""
     dev, code, shape, a = _row_input(x, "x")
     rows, dim = shape
     keys, n_dev = _row_keys(ids, count, rows, dev)

@@ -319,6 +319,9 @@ int gmb_linear_loss(const gmb_linear_head* head, const gmb_linear_grads* grads, 
     if (reinterpret_cast<uintptr_t>(ws) % gmb::kAbiAlign)
       return abi_fail(GMB_EINVAL, "workspace is not 256-byte aligned");
     const size_t need = gmb_linear_loss_workspace_bytes(head, grads);
+    if (!need)
+      return abi_fail(GMB_EINVAL, "rows=%lld, d=%d and classes=%d are too many together", static_cast<long long>(a.rows),
+                      a.d, a.classes);
     if (ws_bytes < need) return abi_fail(GMB_ENOSPC, "workspace holds %zu bytes, %zu needed", ws_bytes, need);
     a.ws = static_cast<char*>(ws);
   }

@@ -1328,7 +1328,11 @@ Plan plan(const LinearLossArgs& a, int bf16) {
     p.dx_sums = a.dx && p.dx_slab ? take(p.dx_splits * a.rows * round_up(a.d, 4) * 4) : 0;
     p.dw_sums = a.dw && p.dw_splits > 1 ? take(p.dw_splits * p.dw_rows * p.ld_dw * 4) : 0;
   }
-  p.total = at;
+  // (a launch's threads fit 31 bits; else there is no plan: 0 bytes)
+  const int64_t across = p.pad_d / 64, have = p.piece < a.classes ? p.piece : a.classes, tile = p.product_tile;
+  const int64_t laid_out = (p.pad_rows / 64 + (p.copy_w ? tiles_of(a.classes, 64) : 0)) * across;
+  const int64_t products = tiles_of(a.d, tile) * (tiles_of(a.rows, tile) * p.dx_splits + tiles_of(have, tile) * p.dw_splits);
+  p.total = laid_out > kLaunchThreads / 256 || (p.grad && products + 16 > kLaunchThreads / 512) ? 0 : at;
   return p;
 }
 
@@ -1499,8 +1503,6 @@ hipError_t run(const LinearLossArgs& a, hipStream_t s) {
     w.data = lw.by_all;
     w.ld = p.pad_d * p.es;
   }
-  // (a launch's threads fit 31 bits)
-  const int64_t most_tiles = kLaunchThreads / 512;
   hipLaunchKernelGGL((k_lay_out<TYPE, T>), dim3(static_cast<unsigned>(x_tiles + w_tiles)), dim3(256), 0, s, l, lw, x_tiles);
   const T16Side x_by_row{x_row, p.pad_d * p.es, p.pad_rows, static_cast<int>(p.pad_d), 0};
   const T16Side x_by_all{x_all, p.pad_d * p.es, p.pad_rows, static_cast<int>(p.pad_d), 0};
@@ -1589,7 +1591,6 @@ hipError_t run(const LinearLossArgs& a, hipStream_t s) {
     }
     dx.part = dx.n * dx.ld_slab;
     const int64_t tiles = round_up(product_tiles(dx), 8) + round_up(product_tiles(dw), 8);
-    if (tiles > most_tiles) return hipErrorInvalidConfiguration;
     if (tile == kLarge) hipLaunchKernelGGL((k_products<TYPE, kLarge, kLarge, 2, 4>), dim3(grid8(tiles)), dim3(512), 0, s, dx, dw);
     else hipLaunchKernelGGL((k_products<TYPE, kSmall, kSmall, 2, 2>), dim3(grid8(tiles)), dim3(256), 0, s, dx, dw);
   }

@@ -145,6 +145,20 @@ def test_a_bf16_model_with_dropout(tiny, dtype):
     assert all(bool(t.isfinite().all()) for t in grads.d_self + grads.d_neigh + grads.d_bias)
 
 
+def test_dropout_is_a_dropout(tiny):
+    wl, _ = tiny
+    csr, seeds, blocks = sample(tiny)
+    w = weights((16, 32, 8), 3)
+    feats = torch.from_numpy(wl.feats).cuda()
+    x = gmb.gather_features(blocks, feats)
+    ws = torch.empty(gmb.forward_workspace_bytes(blocks, w), dtype=torch.uint8, device="cuda")
+    out = gmb.sage_forward(blocks, x, w, workspace=ws)
+    for call in [lambda: gmb.sage_forward(blocks, x, w, dropout=0.5), lambda: gmb.sage_forward_fused(blocks, feats, w, dropout=0.5),
+                 lambda: gmb.sage_backward_from(blocks, x, w, out, ws, dropout=0.5)]:
+        with pytest.raises(TypeError):
+            call()
+
+
 def head_step(blocks, x, w, ws, drop, gain, table, labels, model_drop):
     """One pass of a residual head on the model: outputs h, r = h + dropout(h turned), its norm, the loss over the table's rows."""
     h = gmb.sage_forward(blocks, x, w, workspace=ws, dropout=model_drop)

@@ -140,6 +140,44 @@ def test_layouts_and_strides(size, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("size", [(1, 65536, 3), (3, 20_000, 700), (40, 60_000, 300), (300, 5000, 1), (17, 9, 4000), (70, 1025, 4100),
+                                  (100_000, 3, 2)], ids=str)
+def test_long_rows_and_lean_heads(size, dtype):
+    x, w, y, b = problem(*size, dtype, 17)
+    loss, grads = gmb.linear_loss(x, w, y, bias=b)
+    check(x, w, y, b, loss, grads)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("size", [(40, 64, 30), (300, 128, 700)], ids=str)
+def test_weights_that_are_broadcast(size, dtype):
+    """Strides of zero: every element has a gradient of its own."""
+    n, d, classes = size
+    x, w, y, b = problem(*size, dtype, 18)
+    for wide in (w[0].expand(classes, d), w[:, :1].expand(classes, d), w[0, 0].expand(classes, d)):
+        loss, g = gmb.linear_loss(x, wide, y, bias=b)
+        check(x, wide, y, b, loss, g)
+        dense, h = gmb.linear_loss(x, wide.contiguous(), y, bias=b)
+        assert torch.equal(loss, dense) and all(torch.equal(p, q) for p, q in zip(g, h))
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+def test_two_streams_at_once(dtype):
+    problems = [problem(400, 96, 1500, dtype, 19), problem(250, 64, 900, dtype, 20)]
+    want = [gmb.linear_loss(x, w, y, bias=b) for x, w, y, b in problems]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], [[], []]
+    for _ in range(5):
+        for k, (x, w, y, b) in enumerate(problems):
+            with torch.cuda.stream(streams[k]):
+                got[k].append(gmb.linear_loss(x, w, y, bias=b))
+    torch.cuda.synchronize()
+    for k, (loss, g) in enumerate(want):
+        for mine, h in got[k]:
+            assert torch.equal(mine, loss) and all(torch.equal(p, q) for p, q in zip(g, h))
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
 def test_gradients_asked_for_one_by_one(dtype):
     x, w, y, b = problem(150, 96, 333, dtype, 3)
     loss, all_ = gmb.linear_loss(x, w, y, bias=b)

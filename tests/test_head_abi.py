@@ -128,12 +128,24 @@ def test_linear_loss_bytes_refuses(gmb, bad):
 def test_linear_loss_refuses_a_small_workspace(gmb):
     need = loss(gmb, size_only=True)
     assert need > 0 and loss(gmb, ws=P, ws_bytes=need - 1) == ENOSPC
-    more = loss(gmb, size_only=True, dx=S + (1 << 30), dw=S + (1 << 31), db=S + (3 << 30))
-    assert more > need
+    grads = dict(dx=S + (1 << 30), dw=S + (1 << 31), db=S + (3 << 30))
+    assert loss(gmb, size_only=True, **grads) >= need    # (one launch, nothing in between)
+    assert loss(gmb, size_only=True, n=2000, classes=5000, **grads) > loss(gmb, size_only=True, n=2000, classes=5000)
+
+
+@pytest.mark.parametrize("big", [
+    dict(n=1 << 22, d=65536, xs=65536, wr=65536, classes=1000, dx=S, dw=S), dict(n=100, d=65536, xs=65536, wr=65536, classes=1 << 27),
+    dict(n=1 << 22, d=65536, xs=65536, wr=65536, classes=1 << 27, dtype=1, dx=S, dw=S)], ids=str)
+def test_linear_loss_refuses_what_no_launch_takes(gmb, big):
+    # more 64 x 64 tiles than a launch has workgroups: said before anything is launched
+    assert loss(gmb, size_only=True, **big) == 0
+    apart = {k: v if k not in ("dx", "dw") else 1 << 60 for k, v in big.items()}
+    assert loss(gmb, ws=P, ws_bytes=1 << 60, **apart) == EINVAL
+    assert b"too many together" in gmb.lib().gmb_last_error()
 
 
 def test_linear_loss_workspace_is_bounded(gmb):
-    # a hundred million classes for a thousand rows: no room for the logits (200 GB), 256 MB of gradients at a time
+    # a hundred million classes for a thousand rows: no room for the logits (200 GB), 384 MB of gradients at a time
     need = loss(gmb, size_only=True, n=1000, d=128, xs=128, wr=128, classes=100_000_000, dtype=1, dx=S, dw=S)
     assert need < 8 << 30
 
