@@ -162,6 +162,27 @@ def test_weights_that_are_broadcast(size, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("size", [(3, 64, 40), (4, 2048, 700)], ids=str)
+def test_offsets_past_32_bits(size, dtype):
+    """Rows of x, and then of W's transpose or of W, 2^31 + 8 (2^23 + 8) elements apart."""
+    n, d, classes = size
+    x, w, y, b = problem(*size, dtype, 21)
+    want, wg = gmb.linear_loss(x, w, y, bias=b)
+    apart = (1 << 31) + 8
+    memory = torch.empty((n - 1) * apart + d, dtype=dtype, device="cuda")
+    far = memory.as_strided((n, d), (apart, 1))
+    far.copy_(x)
+    loss, g = gmb.linear_loss(far, w, y, bias=b)
+    assert torch.equal(loss, want) and all(torch.equal(p, q) for p, q in zip(g, wg))
+    apart = (1 << 23) + 8                            # (700 rows of it: 5.9 billion elements)
+    memory = torch.empty((classes - 1) * apart + d, dtype=dtype, device="cuda")
+    far = memory.as_strided((classes, d), (apart, 1))
+    far.copy_(w)
+    loss, g = gmb.linear_loss(x, far, y, bias=b)
+    assert torch.equal(loss, want) and all(torch.equal(p, q) for p, q in zip(g, wg))
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
 def test_two_streams_at_once(dtype):
     problems = [problem(400, 96, 1500, dtype, 19), problem(250, 64, 900, dtype, 20)]
     want = [gmb.linear_loss(x, w, y, bias=b) for x, w, y, b in problems]

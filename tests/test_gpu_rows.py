@@ -285,6 +285,23 @@ def test_more_rows_than_a_grid():
     near(got.weight, dw, 256 * U32 * (wide(x) ** 2 * s).sum(0), "weight")
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+def test_offsets_past_32_bits(dtype):
+    """Rows 2^31 + 8 elements apart: the same bits as side by side."""
+    n, dim, apart = 3, 300, (1 << 31) + 8
+    x, res, g = rows(n, dim, 30, dtype), rows(n, dim, 31, dtype), torch.rand(dim, device="cuda")
+    memory = torch.empty((n - 1) * apart + 2 * dim, dtype=dtype, device="cuda")
+    far, out = memory.as_strided((n, dim), (apart, 1)), memory.as_strided((n, dim), (apart, 1), dim)
+    far.copy_(x)
+    d = gmb.Dropout(0.5, 8)
+    assert torch.equal(gmb.dropout(far, d, residual=res, out=out), gmb.dropout(x, d, residual=res))
+    y, r = gmb.rms_norm(far, g, EPS, residual=res, dropout=d, sum_out=out)
+    y2, r2 = gmb.rms_norm(x, g, EPS, residual=res, dropout=d)
+    assert torch.equal(y, y2) and torch.equal(r, r2)
+    got, want = gmb.rms_norm_backward(far, r, g, EPS, carry=far), gmb.rms_norm_backward(x, r2, g, EPS, carry=x)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_captured_and_replayed():
     x, res, g = (rows(500, 256, 22 + i, torch.float32) for i in range(3))
     w = g[0].abs().contiguous()
