@@ -11,10 +11,14 @@
 //                       the classes at a time: G; few classes (kBoth): at once
 //   k_products          dx += G W and dW = G^T x of the piece
 //   k_finish            sums that were split; the mean
+//   k_stream_head       few rows, or few classes: all of it on W as it lies
 //
 // The logits are computed twice (8 n C d operations in all where keeping them
 // would take 6) and never stored; G is, in 16 bits (kSplit: two times 16), for
 // a piece of the classes.  Nothing is added by atomics: the same bits every time.
+// The figures below are times of kernels; a large product of the library's reaches
+// 1,210 TFLOP/s in bf16 on random values (here the power it may draw is the bound:
+// 8,192 x 1,024 x 32,768 takes it 514 us, with zeros 336).
 #include "head_kernels.hpp"
 #include "mx.hpp"
 #include "mx_kernels.hpp"
@@ -70,7 +74,8 @@ struct AmaxArgs {
 
 // The largest finite magnitudes: of every row of x and of all of them (a word a
 // workgroup), and of W (a word a workgroup).  A wave has a row (W, if its rows
-// lie one behind the other: a piece of the whole), 16 bytes a lane.
+// lie one behind the other: a piece of the whole), 16 bytes a lane.  Bound by the
+// reading: 4,000 and 20,011 rows of 256, 25 MB, 8.9 us.
 __global__ __launch_bounds__(256) void k_amax(AmaxArgs p) {
   __shared__ uint32_t lds[4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -172,7 +177,8 @@ __device__ __forceinline__ void put_split(uint16_t* row, int c, const float (&v)
 
 // A 64 x 64 tile of the source: rows with contiguous columns eight values a
 // thread; else through LDS, read along the direction that is contiguous.  (The
-// first `first` workgroups lay out x, the others W.)
+// first `first` workgroups lay out x, the others W.)  Bound by memory: 25 MB read
+// and 29 written, 11.8 us.
 template <T16Type TYPE, typename T>
 __global__ __launch_bounds__(256) void k_lay_out(LayOutArgs x, LayOutArgs w, int64_t first) {
   __shared__ float tile[64][65];
@@ -334,9 +340,10 @@ constexpr float kLn2 = 0.6931471805599453f;
 enum LogitsMode { kStats, kGrad, kBoth };
 
 // Stages in LDS.  256 x 256: two of 64 elements, 128 KB (bf16, four of 32: 535 us
-// for 494, statistics of 8,192 x 1,024 x 32,768).  64 x 64: four for logits, whose
-// sums are short (1,000 x 256 x 47 fp32: 9.0 us, two 11.1), two for products,
-// which have more code than time (6.5 us, four 12.2).
+// for 494, statistics of 8,192 x 1,024 x 32,768; 128 x 256 in three of 32, two
+// workgroups a CU: 561 for 515).  64 x 64: four for logits, whose sums are short
+// (1,000 x 256 x 47 fp32: 9.0 us, two 11.1), two for products, which have more
+// code than time (6.5 us, four 12.2).
 constexpr int logits_stages(int tm) { return tm > 64 ? 2 : 4; }
 
 template <int TM, int TN, int WM, int WN>
@@ -347,6 +354,14 @@ struct LogitsLds {
   static constexpr int kBytes = kClasses + WN * TM * 4;
 };
 
+// A workgroup has a tile of rows and goes over its chunk of the classes, tile by
+// tile, without a pause in the loads between two; a lane has eight neighbouring
+// classes of a row, so that G leaves in 16 bytes.  256 x 256: bound by the matrix
+// instructions (49 % busy: what the power allows), and where d is short by the
+// exponentials behind every tile's 4 d / 64 stages of them.  bf16, statistics and G:
+// 8,192 x 1,024 x 32,768 515 and 592 us (1,067 and 929 TFLOP/s), 4,000 x 256 x 100,000 260
+// and 374 (789 and 548); fp32 4,000 x 256 x 20,011 125 and 161 (three part products: 983
+// and 764).
 template <T16Type TYPE, LogitsMode MODE, int TM, int TN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
   using Tile = T16Tile<TYPE, kByRow, kByRow, TM, TN, WM, WN, logits_stages(TM), 64, true>;
@@ -709,7 +724,12 @@ __device__ __forceinline__ void product_tile(const Product& p, int64_t id, char*
 }
 
 // dx = G W (A: W by its rows of k, B: G by its rows), then dW = G^T x, its rows
-// those of W (A: x, B: G) or, turned, those of W's transpose (A: G, B: x).
+// those of W (A: x, B: G) or, turned, those of W's transpose (A: G, B: x).  One
+// launch, so that the ends of one fill the other's.  256 x 256: matrix instructions,
+// and G from the last-level cache (loss of 8,192 x 1,024 x 32,768 bf16: 1,021 us, 1,077
+// TFLOP/s; 4,000 x 256 x 100,000 bf16 511, 801; 4,000 x 256 x 20,011 fp32 280, 879 of part
+// products).  Four waves of 128 x 128 instead of eight, their operands read a stage
+// ahead: 535 us a piece for 531, and the logits' kernels spilled.
 template <T16Type TYPE, int TM, int TN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void k_products(Product dx, Product dw) {
   __shared__ __attribute__((aligned(1024))) char lds[2 * t16_stage_bytes<TM, TN, 64>()];
@@ -797,7 +817,7 @@ __device__ __forceinline__ void join_parts(const JoinArgs& p, int block) {
 }
 
 // The last workgroup adds the rows' losses, in 64 bits and a fixed order; the
-// others join sums.
+// others join sums, bound by reading them (4,000 x 256 x 20,011 fp32: 33 us).
 template <bool BF16>
 __global__ __launch_bounds__(256) void k_finish(FinishArgs p) {
   int block = blockIdx.x;
