@@ -357,8 +357,9 @@ struct LogitsLds {
 // A workgroup has a tile of rows and goes over its chunk of the classes, tile by
 // tile, without a pause in the loads between two; a lane has eight neighbouring
 // classes of a row, so that G leaves in 16 bytes.  256 x 256: bound by the matrix
-// instructions (49 % busy: what the power allows), and where d is short by the
-// exponentials behind every tile's 4 d / 64 stages of them.  bf16, statistics and G:
+// instructions (busy 0.49; the library's product takes as long), and where d is
+// short by the exponentials behind every tile's d / 64 stages of them.  bf16,
+// statistics and G:
 // 8,192 x 1,024 x 32,768 515 and 592 us (1,067 and 929 TFLOP/s), 4,000 x 256 x 100,000 260
 // and 374 (789 and 548); fp32 4,000 x 256 x 20,011 125 and 161 (three part products: 983
 // and 764).
