@@ -360,8 +360,8 @@ struct LogitsLds {
 // instructions (busy 0.49; the library's product takes as long), and where d is
 // short by the exponentials behind every tile's d / 64 stages of them.  bf16,
 // statistics and G:
-// 8,192 x 1,024 x 32,768 515 and 592 us (1,067 and 929 TFLOP/s), 4,000 x 256 x 100,000 260
-// and 374 (789 and 548); fp32 4,000 x 256 x 20,011 125 and 161 (three part products: 983
+// 8,192 x 1,024 x 32,768 505 and 600 us (1,088 and 916 TFLOP/s), 4,000 x 256 x 100,000 247
+// and 365 (830 and 561); fp32 4,000 x 256 x 20,011 125 and 161 (three part products: 983
 // and 764).
 template <T16Type TYPE, LogitsMode MODE, int TM, int TN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
@@ -452,7 +452,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
 #pragma unroll
     for (int j = 0; j < CT; ++j) {
       const int q = 16 * (CT * wn + j) + r;
-      lse[j] = row_a[q];
+      lse[j] = row_b[q] == 0.f ? INFINITY : row_a[q];   // (G is 0 there)
       if (row_b[q] == 0.f) label[j] = -1;
     }
   }
@@ -475,43 +475,52 @@ __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
       if (more) fetched();
       at = at == NST - 1 ? 0 : at + 1;
     }
-    // u = z log2(e), in place; the registers of tiles i and i + 1 (i even) are
-    // classes c0 + 16 i .. + 7, -inf past the last class
+    // u = z log2(e) = acc by[j], in place where there is more to it than that; the
+    // registers of tiles i and i + 1 (i even) are classes c0 + 16 i .. + 7, -inf past
+    // the last class
     const int cw = t * TM + 16 * RT * wm + 8 * g;       // of the piece
     const int c0 = p.c0 + cw;
     const bool whole = p.c0 + t * TM + TM <= p.classes;
+    float by[CT];
 #pragma unroll
-    for (int i = 0; i < RT; i += 2) {
-      float bias[8] = {};
-      const int c = c0 + 16 * i;
-      if (p.bias && whole) {
-        mx_get<16>(bias, p.bias + c);
-        mx_get<16>(bias + 4, p.bias + c + 4);
-      } else if (!whole) {
+    for (int j = 0; j < CT; ++j) by[j] = scale[j];
+    if (p.bias || !whole) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) bias[e] = c + e >= p.classes ? -INFINITY : (p.bias ? p.bias[c + e] : 0.f);
-      }
+      for (int j = 0; j < CT; ++j) by[j] = 1.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        bias[e] *= kLog2e;
+      for (int i = 0; i < RT; i += 2) {
+        float bias[8] = {};
+        const int c = c0 + 16 * i;
+        if (whole) {
+          mx_get<16>(bias, p.bias + c);
+          mx_get<16>(bias + 4, p.bias + c + 4);
+        } else {
 #pragma unroll
-        for (int j = 0; j < CT; ++j) acc[i + e / 4][j][e % 4] = fmaf(acc[i + e / 4][j][e % 4], scale[j], bias[e]);
+          for (int e = 0; e < 8; ++e) bias[e] = c + e >= p.classes ? -INFINITY : (p.bias ? p.bias[c + e] : 0.f);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          bias[e] *= kLog2e;
+#pragma unroll
+          for (int j = 0; j < CT; ++j) acc[i + e / 4][j][e % 4] = fmaf(acc[i + e / 4][j][e % 4], scale[j], bias[e]);
+        }
       }
     }
     if constexpr (MODE != kGrad) {
 #pragma unroll
       for (int j = 0; j < CT; ++j) {
-        float most = top[j];
+        float most = -INFINITY;
 #pragma unroll
         for (int i = 0; i < RT; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) most = fmaxf(most, acc[i][j][e]);
+        most = fmaxf(top[j], most * by[j]);
         const float base = most == -INFINITY ? 0.f : most;
         float s = sum[j] * exp2_fast(top[j] - base);
 #pragma unroll
         for (int i = 0; i < RT; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s += exp2_fast(acc[i][j][e] - base);
+          for (int e = 0; e < 4; ++e) s += exp2_fast(fmaf(acc[i][j][e], by[j], -base));
         top[j] = most;
         sum[j] = s;
         // the label's logit, where it is one of this lane's
@@ -522,6 +531,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
           for (int i = 0; i < RT; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) z = y == 16 * (i & ~1) + 4 * (i & 1) + e ? acc[i][j][e] : z;
+          z *= by[j];
           if constexpr (MODE == kBoth) row_label[16 * (CT * wn + j) + r] = z;
           else p.label_logit[row0 + 16 * j] = z;
         }
@@ -546,8 +556,10 @@ __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
         for (int w = 1; w < WM; ++w) join_stats(m, s, row_a[w * TN + q], row_b[w * TN + q]);
         lse[j] = row_lse(m, s);
         if (row_empty(m, s)) label[j] = -1;
+        const float of_label = lse[j];
+        if (label[j] < 0) lse[j] = INFINITY;              // (G is 0 there)
         if (wm == 0 && g == 0 && row0 + 16 * j < p.rows)
-          p.loss_rows[row0 + 16 * j] = label[j] >= 0 ? (lse[j] - row_label[q]) * kLn2 : 0.f;
+          p.loss_rows[row0 + 16 * j] = label[j] >= 0 ? (of_label - row_label[q]) * kLn2 : 0.f;
       }
       if (!p.g) return;
     }
@@ -561,8 +573,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
           float v[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const float q = exp2_fast(acc[i + e / 4][j][e % 4] - lse[j]);
-            v[e] = label[j] >= 0 ? q : 0.f;
+            v[e] = exp2_fast(fmaf(acc[i + e / 4][j][e % 4], by[j], -lse[j]));
           }
           const int y = label[j] - c0 - 16 * i;
           if (y >= 0 && y < 8) {
@@ -570,8 +581,10 @@ __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
             for (int e = 0; e < 8; ++e) v[e] -= y == e ? 1.f : 0.f;
           }
           put_split<TYPE>(p.g + (row0 + 16 * j) * p.ldg, cw + 16 * i, v, kGradScale);
+          if (p.db) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) db[e] += v[e];
+            for (int e = 0; e < 8; ++e) db[e] += v[e];
+          }
         }
         if (p.db) {
 #pragma unroll

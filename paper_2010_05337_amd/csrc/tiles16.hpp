@@ -211,12 +211,10 @@ struct T16Tile {
   }
 
   // The oldest stage has arrived, for every wave, and the one before it is read:
-  // `full`: NST - 1 stages were asked for since that one; `later`: at least that
-  // many stores were made after its loads.
-  template <int LATER = 0>
+  // `full`: NST - 1 stages were asked for since that one.
   static __device__ __forceinline__ void wait(bool full) {
-    if (NST > 2 && full) t16_wait<(NST - 2) * LOADS + LATER>();
-    else t16_wait<NST == 2 ? LATER : 0>();
+    if (NST > 2 && full) t16_wait<(NST - 2) * LOADS>();
+    else t16_wait<0>();
   }
 
   // acc += the stages first .. last - 1 of k; lds: NST stages.  Every wave of the
