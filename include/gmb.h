@@ -648,7 +648,8 @@ int gmb_dropout_rows(const gmb_rows* x, const gmb_rows* residual, const gmb_drop
  * with r rounded to `dtype` before it is normed (what `sum` holds is what y is
  * the norm of, and what gmb_rms_norm_backward takes); statistics fp32.
  *   weight  device fp32 [dim] or NULL (ones)
- *   eps     > 0
+ *   eps     a positive normal number (>= 2^-126).  A row whose squares add up
+ *           past fp32's range norms to 0
  *   sum     rows of `dtype` for r, or NULL; may be x or residual
  *   format  0: out is rows of `dtype` (out may be x or residual if sum is
  *           not); GMB_MXFP4 or GMB_MXFP8: out is records (a table of

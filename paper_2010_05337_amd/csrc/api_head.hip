@@ -53,8 +53,10 @@ int check_in_place(const gmb_rows* out, const gmb_rows* in, const char* what) {
 gmb::RowsIn rows_in(const gmb_rows* r) { return r ? gmb::RowsIn{r->data, r->stride} : gmb::RowsIn{nullptr, 0}; }
 gmb::RowsOut rows_out(const gmb_rows* r) { return r ? gmb::RowsOut{r->data, r->stride} : gmb::RowsOut{nullptr, 0}; }
 
+// (the kernels' root takes normal numbers)
 int check_eps(float eps) {
-  if (!(eps > 0.f) || eps > 3.0e38f) return abi_fail(GMB_EINVAL, "eps=%g is not positive", static_cast<double>(eps));
+  if (!(eps >= 1.17549435e-38f) || eps > 3.0e38f)
+    return abi_fail(GMB_EINVAL, "eps=%g is no positive normal number", static_cast<double>(eps));
   return GMB_OK;
 }
 

@@ -178,6 +178,18 @@ def test_norm_rows_of_zeros_and_not_numbers():
         assert torch.equal(gmb.mx_gather(None, rec, dim, 8)[1], torch.zeros(dim, device="cuda"))
 
 
+def test_norm_of_the_smallest_eps():
+    """2^-126 beside rows of zeros, and of values whose squares are 0 or no normal numbers."""
+    eps = 2.0 ** -126
+    x = torch.ones(4, 100, device="cuda") * torch.tensor([0.0, 1e-30, 1e-19, 3e-19], device="cuda")[:, None]
+    y, _ = gmb.rms_norm(x, None, eps)
+    want = head_ref.rms_norm(wide(x), torch.ones(100, dtype=torch.float64), eps)
+    # (a square below 2^-126 is off by half of 2^-149: 2^-24 of eps)
+    near(y, want, 64 * U32 * want.abs(), "norm")
+    g = gmb.rms_norm_backward(torch.full_like(x, 1e-20), x, None, eps)
+    assert bool(g.x.isfinite().all())
+
+
 def test_norm_in_place():
     for dim in (256, 5000, 40000):
         x, res, g = rows(5, dim, 12, torch.float32), rows(5, dim, 13, torch.float32), torch.rand(dim, device="cuda")

@@ -62,7 +62,7 @@ def norm(gmb, x=P, xs=100, res=False, rs=100, total=False, ts=100, out=Q, os_=10
 @pytest.mark.parametrize("bad", SHAPE + [
     dict(x=None), dict(x=False), dict(xs=99), dict(out=None), dict(out=False), dict(os_=99), dict(res=None), dict(res=R, rs=99),
     dict(total=R, ts=99), dict(total=P, ts=101), dict(res=R, total=R, ts=101), dict(total=Q), dict(out=P, os_=101),
-    dict(eps=0.0), dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")), dict(fmt=5), dict(fmt=-4),
+    dict(eps=0.0), dict(eps=1e-38), dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")), dict(fmt=5), dict(fmt=-4),
     dict(fmt=8, os_=128), dict(fmt=8, os_=143), dict(fmt=8, os_=144, out=Q + 8), dict(fmt=4, os_=64), dict(fmt=8, os_=144, out=P),
     dict(fmt=8, os_=144, res=R, out=R), dict(none=False, p=2.0), dict(none=False, layer=-3)], ids=str)
 def test_norm_refuses(gmb, bad):
@@ -87,7 +87,7 @@ def back(gmb, dy=P, dys=100, r=Q, rs=100, carry=False, cs=100, d_res=R, ds=100, 
 @pytest.mark.parametrize("bad", SHAPE + [
     dict(dy=None), dict(dy=False), dict(dys=99), dict(r=None), dict(r=False), dict(rs=99), dict(carry=None), dict(carry=S, cs=99),
     dict(d_res=None), dict(ds=99), dict(dx=None), dict(dx=S, xs=99), dict(d_res=P, ds=101), dict(d_res=Q, ds=101),
-    dict(dx=Q, xs=101), dict(dx=R), dict(carry=S, dx=S, xs=101), dict(eps=0.0), dict(none=False, p=-1.0),
+    dict(dx=Q, xs=101), dict(dx=R), dict(carry=S, dx=S, xs=101), dict(eps=0.0), dict(eps=1e-38), dict(none=False, p=-1.0),
     dict(dw=S), dict(dw=S, ws=P + 16, ws_bytes=1 << 30)], ids=str)
 def test_norm_backward_refuses(gmb, bad):
     assert back(gmb, **bad) == EINVAL
