@@ -360,9 +360,9 @@ struct LogitsLds {
 // instructions (busy 0.49; the library's product takes as long), and where d is
 // short by the exponentials behind every tile's d / 64 stages of them.  bf16,
 // statistics and G:
-// 8,192 x 1,024 x 32,768 505 and 600 us (1,088 and 916 TFLOP/s), 4,000 x 256 x 100,000 247
-// and 365 (830 and 561); fp32 4,000 x 256 x 20,011 125 and 161 (three part products: 983
-// and 764).
+// 8,192 x 1,024 x 32,768 500 and 599 us (1,099 and 918 TFLOP/s), 4,000 x 256 x 100,000 249
+// and 368 (824 and 556); fp32 4,000 x 256 x 20,011 125 and 162 (three part products: 987
+// and 759).
 template <T16Type TYPE, LogitsMode MODE, int TM, int TN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
   using Tile = T16Tile<TYPE, kByRow, kByRow, TM, TN, WM, WN, logits_stages(TM), 64, true>;
@@ -740,8 +740,8 @@ __device__ __forceinline__ void product_tile(const Product& p, int64_t id, char*
 // dx = G W (A: W by its rows of k, B: G by its rows), then dW = G^T x, its rows
 // those of W (A: x, B: G) or, turned, those of W's transpose (A: G, B: x).  One
 // launch, so that the ends of one fill the other's.  256 x 256: matrix instructions,
-// and G from the last-level cache (loss of 8,192 x 1,024 x 32,768 bf16: 1,021 us, 1,077
-// TFLOP/s; 4,000 x 256 x 100,000 bf16 511, 801; 4,000 x 256 x 20,011 fp32 280, 879 of part
+// and G from the last-level cache (loss of 8,192 x 1,024 x 32,768 bf16: 1,008 us, 1,090
+// TFLOP/s; 4,000 x 256 x 100,000 bf16 515, 795; 4,000 x 256 x 20,011 fp32 280, 879 of part
 // products).  Four waves of 128 x 128 instead of eight, their operands read a stage
 // ahead: 535 us a piece for 531, and the logits' kernels spilled.
 template <T16Type TYPE, int TM, int TN, int WM, int WN>
