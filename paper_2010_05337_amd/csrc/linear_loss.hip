@@ -324,9 +324,13 @@ __device__ __forceinline__ float sum16(float v) {
 
 // A maximum and the sum of 2^(u - maximum) of some of a row's u = z log2(e),
 // joined with others'.  -inf: nothing yet.  A NaN among the u makes the sum NaN.
-__device__ __forceinline__ void join_stats(float& top, float& sum, float t, float s) {
+// SUM is double where a chain is as long as the classes or their chunks are many:
+// 50,000 equal terms added up in fp32 round the same way one after the other (a
+// row's loss over 400,000 classes was off by 7e-5).
+template <typename SUM>
+__device__ __forceinline__ void join_stats(float& top, SUM& sum, float t, float s) {
   const float m = fmaxf(top, t), base = m == -INFINITY ? 0.f : m;
-  sum = sum * exp2_fast(top - base) + s * exp2_fast(t - base);
+  sum = sum * static_cast<SUM>(exp2_fast(top - base)) + static_cast<SUM>(s) * static_cast<SUM>(exp2_fast(t - base));
   top = m;
 }
 __device__ __forceinline__ float row_lse(float top, float sum) { return top + log2f(sum); }
@@ -427,14 +431,15 @@ __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
     float* part = reinterpret_cast<float*>(lds + (NST - 1) * Tile::kStage);   // (the last stage is still empty)
     for (int q = threadIdx.x; q < PARTS * TN; q += THREADS) {
       const int row = q % TN;
-      float top = -INFINITY, sum = 0.f;
+      float top = -INFINITY;
+      double sum = 0.0;
 #pragma unroll 8
       for (int c = q / TN; c < p.stat_chunks; c += PARTS) {
         const float2 s = p.stats[c * p.pad_rows + tile_row + row];
         join_stats(top, sum, s.x, s.y);
       }
       part[2 * q] = top;
-      part[2 * q + 1] = sum;
+      part[2 * q + 1] = static_cast<float>(sum);
     }
     __syncthreads();
     for (int row = threadIdx.x; row < TN; row += THREADS) {
@@ -456,11 +461,12 @@ __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
       if (row_b[q] == 0.f) label[j] = -1;
     }
   }
-  float top[CT], sum[CT];
+  float top[CT];
+  double long_sum[CT];              // (tiles follow one another: as many links as the chunk has)
 #pragma unroll
   for (int j = 0; j < CT; ++j) {
     top[j] = -INFINITY;
-    sum[j] = 0.f;
+    long_sum[j] = 0.0;
   }
   __syncthreads();
   int at = 0;
@@ -516,13 +522,13 @@ __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
           for (int e = 0; e < 4; ++e) most = fmaxf(most, acc[i][j][e]);
         most = fmaxf(top[j], most * by[j]);
         const float base = most == -INFINITY ? 0.f : most;
-        float s = sum[j] * exp2_fast(top[j] - base);
+        float s = 0.f;
 #pragma unroll
         for (int i = 0; i < RT; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) s += exp2_fast(fmaf(acc[i][j][e], by[j], -base));
+        long_sum[j] = long_sum[j] * static_cast<double>(exp2_fast(top[j] - base)) + static_cast<double>(s);
         top[j] = most;
-        sum[j] = s;
         // the label's logit, where it is one of this lane's
         const int y = label[j] - c0;
         if (y >= 0 && y < 16 * RT && (y & 31) < 8) {
@@ -541,10 +547,11 @@ __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
       // all classes are here: the lanes' and waves' statistics joined
 #pragma unroll
       for (int j = 0; j < CT; ++j) {
-        for (int o = 16; o < 64; o <<= 1) join_stats(top[j], sum[j], __shfl_xor(top[j], o, 64), __shfl_xor(sum[j], o, 64));
+        float sum = static_cast<float>(long_sum[j]);
+        for (int o = 16; o < 64; o <<= 1) join_stats(top[j], sum, __shfl_xor(top[j], o, 64), __shfl_xor(sum, o, 64));
         if (g == 0) {
           row_a[wm * TN + 16 * (CT * wn + j) + r] = top[j];
-          row_b[wm * TN + 16 * (CT * wn + j) + r] = sum[j];
+          row_b[wm * TN + 16 * (CT * wn + j) + r] = sum;
         }
       }
       __syncthreads();
@@ -609,10 +616,11 @@ __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
   if constexpr (MODE == kStats) {
 #pragma unroll
     for (int j = 0; j < CT; ++j) {
-      for (int o = 16; o < 64; o <<= 1) join_stats(top[j], sum[j], __shfl_xor(top[j], o, 64), __shfl_xor(sum[j], o, 64));
+      float sum = static_cast<float>(long_sum[j]);
+      for (int o = 16; o < 64; o <<= 1) join_stats(top[j], sum, __shfl_xor(top[j], o, 64), __shfl_xor(sum, o, 64));
       if (g == 0) {
         row_a[wm * TN + 16 * (CT * wn + j) + r] = top[j];
-        row_b[wm * TN + 16 * (CT * wn + j) + r] = sum[j];
+        row_b[wm * TN + 16 * (CT * wn + j) + r] = sum;
       }
     }
     __syncthreads();
@@ -637,12 +645,14 @@ __global__ __launch_bounds__(256) void k_join_rows(const float2* stats, int chun
   __shared__ float2 lds[PARTS][ROWS];
   const int q = threadIdx.x % ROWS, part = threadIdx.x / ROWS;
   const int64_t row = static_cast<int64_t>(blockIdx.x) * ROWS + q;
-  float top = -INFINITY, sum = 0.f;
+  float top = -INFINITY;
+  double long_sum = 0.0;
 #pragma unroll 8
   for (int c = part; c < chunks; c += PARTS) {
     const float2 s = stats[c * pad_rows + row];
-    join_stats(top, sum, s.x, s.y);
+    join_stats(top, long_sum, s.x, s.y);
   }
+  float sum = static_cast<float>(long_sum);
   lds[part][q] = make_float2(top, sum);
   __syncthreads();
   if (part || row >= rows) return;
@@ -1009,6 +1019,7 @@ __global__ __launch_bounds__(kStreamThreads) void k_stream_head(StreamArgs p) {
   }
   const int y = row_y[r];
   float top = -INFINITY, sum = 0.f, lse = 0.f;
+  double long_sum = 0.0;
   bool on = y >= 0;
   if constexpr (MODE == kGrad) {
     if (threadIdx.x < 256) {
@@ -1016,10 +1027,10 @@ __global__ __launch_bounds__(kStreamThreads) void k_stream_head(StreamArgs p) {
 #pragma unroll 4
       for (int c = part; c < p.chunks; c += 16) {
         const float2 s = p.stats[(static_cast<int64_t>(c) * p.row_blocks + block) * 16 + q];
-        join_stats(top, sum, s.x, s.y);
+        join_stats(top, long_sum, s.x, s.y);
       }
       row_top[part][q] = top;
-      row_sum[part][q] = sum;
+      row_sum[part][q] = static_cast<float>(long_sum);
     }
     __syncthreads();
     top = row_top[0][r];
@@ -1060,7 +1071,7 @@ __global__ __launch_bounds__(kStreamThreads) void k_stream_head(StreamArgs p) {
       if constexpr (MODE != kGrad) {
         const float most = fmaxf(fmaxf(fmaxf(acc[0], acc[1]), fmaxf(acc[2], acc[3])), top);
         const float base = most == -INFINITY ? 0.f : most;
-        sum *= exp2_fast(top - base);
+        sum = 0.f;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           sum += exp2_fast(acc[e] - base);
@@ -1069,6 +1080,9 @@ __global__ __launch_bounds__(kStreamThreads) void k_stream_head(StreamArgs p) {
             else p.label_logit[row0 + r] = acc[e];
           }
         }
+        // (kBoth has one tile; else the chunk's tiles follow one another)
+        if constexpr (MODE == kStats)
+          long_sum = long_sum * static_cast<double>(exp2_fast(top - base)) + static_cast<double>(sum);
         top = most;
       }
     }
@@ -1139,6 +1153,7 @@ __global__ __launch_bounds__(kStreamThreads) void k_stream_head(StreamArgs p) {
     }
   }
   if constexpr (MODE == kStats) {
+    sum = static_cast<float>(long_sum);
     for (int o = 16; o < 64; o <<= 1) join_stats(top, sum, __shfl_xor(top, o, 64), __shfl_xor(sum, o, 64));
     if (g == 0) {
       row_top[wave][r] = top;
