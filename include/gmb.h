@@ -715,11 +715,13 @@ typedef struct {
 /* Bytes of workspace gmb_linear_loss needs (0 for bad arguments); of the
  * pointers of `grads` (NULL: the loss alone) only NULL or not counts, of w its
  * alignment.  It holds 16-bit copies of x and, unless it is bf16 in aligned rows
- * of a multiple of 64 values, of W (its size, rows rounded up to 64 values), and
- * with gradients 384 MB at most of G = softmax(z) - onehot (a piece of the
- * classes; more from 393,216 rows on), sums of dbias (rows classes / 16 bytes)
- * and those of dx and dw that are split.  The logits are never stored.  0 too
- * where the three extents together are more than a launch takes. */
+ * of a multiple of 64 values, of W (fp32: two of x; rows rounded up to 64 values),
+ * and with gradients those of the logits, G = softmax(z) - onehot, of a piece of the
+ * classes: 384 MB at most (more from 393,216 rows on), and that piece's sums where
+ * they are split: of dw 128 MB at most, of dx 64 MB more than its own size in fp32,
+ * of dbias a 32nd of G.  Few rows or classes: none of these, 64 MB of sums at most.
+ * The logits are never stored.  0 too where the three extents together are more
+ * than a launch takes. */
 size_t gmb_linear_loss_workspace_bytes(const gmb_linear_head* head, const gmb_linear_grads* grads);
 
 /* The mean over the rows (those without a label count as 0) of -log

@@ -10,7 +10,8 @@
 //   k_logits (kGrad)    the chunks of a row joined, the logits again, a piece of
 //                       the classes at a time: G; few classes (kBoth): at once
 //   k_products          dx += G W and dW = G^T x of the piece
-//   k_finish            sums that were split; the mean
+//   k_join_piece        dW and db of a piece, where their sums were split
+//   k_finish            the same of the last piece, and dx; the mean
 //   k_stream_head       few rows, or few classes: all of it on W as it lies
 //
 // The logits are computed twice (8 n C d operations in all where keeping them
@@ -840,6 +841,16 @@ __device__ __forceinline__ void join_parts(const JoinArgs& p, int block) {
   }
 }
 
+// dW and db of a piece behind which others come: their sums' memory is one piece's
+// (for all classes it would grow with the rows, whose number makes pieces small and
+// splits many: 20 GB for 16,384 rows over 2.4M classes of 256).
+template <bool BF16>
+__global__ __launch_bounds__(256) void k_join_piece(JoinArgs dw, JoinArgs db) {
+  const int block = blockIdx.x;
+  if (block < dw.blocks) join_parts<BF16>(dw, block);
+  else join_parts<false>(db, block - dw.blocks);
+}
+
 // The last workgroup adds the rows' losses, in 64 bits and a fixed order; the
 // others join sums, bound by reading them (4,000 x 256 x 20,011 fp32: 33 us).
 template <bool BF16>
@@ -1204,8 +1215,8 @@ struct Plan {
   int chunks, piece_chunks;        // workgroups of a row tile, for the statistics and for G
   int product_tile, dx_splits, dw_splits;
   bool dx_slab;
-  int64_t ld_dw;                   // the contiguous extent of dw, padded to four
-  int64_t dw_rows, dw_cols;
+  int64_t ld_dw;                   // the contiguous extent of a piece's dw, padded to four
+  int64_t dw_rows, dw_cols;        // of a piece's dw (k_stream_head: of all of it)
   // offsets
   size_t x_all, x_row, w, row_top, tops, row_inverse, inverses, labels, stats, label_logit, loss_rows, g, db, dx_sums,
       dw_sums, total;
@@ -1338,6 +1349,9 @@ Plan plan(const LinearLossArgs& a, int bf16) {
   p.pieces = tiles_of(p.pad_classes, piece);
   p.piece = round_up(tiles_of(p.pad_classes, p.pieces), kPadRows);
   p.pieces = tiles_of(p.pad_classes, p.piece);
+  const int64_t of_piece = p.piece < a.classes ? p.piece : a.classes;
+  (a.turned ? p.dw_cols : p.dw_rows) = of_piece;
+  p.ld_dw = round_up(p.dw_cols, 4);
   // Large tiles of logits where there are enough, few of their rows are padding, and
   // rows or products many (256 / 64, us of the whole call: 4,000 x 64 x 10,000 bf16 82.6 /
   // 87.8, 8,192 x 1,024 x 2,048 164 / 201; but 300 x 100 x 50,000 75 / 66, 1,000 x 128 x
@@ -1356,7 +1370,7 @@ Plan plan(const LinearLossArgs& a, int bf16) {
     return static_cast<int>(want < 1 ? 1 : (want > m ? m : want));
   };
   p.chunks = chunks(a.classes);
-  p.piece_chunks = chunks(p.piece < a.classes ? p.piece : a.classes);
+  p.piece_chunks = chunks(of_piece);
   plan_products(a, &p);
   p.dx_slab = p.dx_splits > 1 || p.pieces > 1;
   const int64_t x_bytes = p.pad_rows * p.pad_d * 2 * p.es;
@@ -1373,14 +1387,14 @@ Plan plan(const LinearLossArgs& a, int bf16) {
   p.loss_rows = take(p.pad_rows * 4);
   if (p.grad) {
     p.g = take(p.pad_rows * p.piece * 2 * p.es);
-    p.db = a.db ? take(tiles_of(a.rows, p.tile) * p.pad_classes * 4) : 0;
+    p.db = a.db ? take(tiles_of(a.rows, p.tile) * p.piece * 4) : 0;
     p.dx_sums = a.dx && p.dx_slab ? take(p.dx_splits * a.rows * round_up(a.d, 4) * 4) : 0;
     p.dw_sums = a.dw && p.dw_splits > 1 ? take(p.dw_splits * p.dw_rows * p.ld_dw * 4) : 0;
   }
   // (a launch's threads fit 31 bits; else there is no plan: 0 bytes)
-  const int64_t across = p.pad_d / 64, have = p.piece < a.classes ? p.piece : a.classes, tile = p.product_tile;
+  const int64_t across = p.pad_d / 64, tile = p.product_tile;
   const int64_t laid_out = (p.pad_rows / 64 + (p.copy_w ? tiles_of(a.classes, 64) : 0)) * across;
-  const int64_t products = tiles_of(a.d, tile) * (tiles_of(a.rows, tile) * p.dx_splits + tiles_of(have, tile) * p.dw_splits);
+  const int64_t products = tiles_of(a.d, tile) * (tiles_of(a.rows, tile) * p.dx_splits + tiles_of(of_piece, tile) * p.dw_splits);
   p.total = laid_out > kLaunchThreads / 256 || (p.grad && products + 16 > kLaunchThreads / 512) ? 0 : at;
   return p;
 }
@@ -1400,9 +1414,9 @@ void launch_logits(const LogitsArgs& g, int tile, hipStream_t s) {
 }
 
 JoinArgs join_of(const float* slab, int parts, int64_t rows, int64_t cols, int64_t ld_slab, float factor,
-                 const float* inverse, void* out) {
+                 const float* inverse, void* out, int64_t ld) {
   const int64_t need = tiles_of(rows * tiles_of(cols, 4), join_columns(parts));
-  return JoinArgs{slab, parts, rows, cols, ld_slab, factor, inverse, out, cols,
+  return JoinArgs{slab, parts, rows, cols, ld_slab, factor, inverse, out, ld,
                   static_cast<int>(need < 8 * kComputeUnits ? need : 8 * kComputeUnits)};
 }
 
@@ -1463,9 +1477,10 @@ hipError_t run_stream(const LinearLossArgs& a, const Plan& p, hipStream_t s) {
                          a.rows, 16 * static_cast<int64_t>(p.row_blocks), a.labels, m.label_logit, m.loss_rows, a.classes);
   }
   FinishArgs f{};
-  if (a.dx && m.dx_sums) f.dx = join_of(floats(p.dx_sums), m.chunks, a.rows, a.d, ld_dx, mean, nullptr, a.dx);
-  if (a.dw && m.dw_sums) f.dw = join_of(floats(p.dw_sums), m.row_blocks, p.dw_rows, p.dw_cols, p.ld_dw, mean, nullptr, a.dw);
-  if (a.db && m.dw_sums) f.db = join_of(floats(p.db), m.row_blocks, 1, a.classes, m.part_db, mean, nullptr, a.db);
+  if (a.dx && m.dx_sums) f.dx = join_of(floats(p.dx_sums), m.chunks, a.rows, a.d, ld_dx, mean, nullptr, a.dx, a.d);
+  if (a.dw && m.dw_sums)
+    f.dw = join_of(floats(p.dw_sums), m.row_blocks, p.dw_rows, p.dw_cols, p.ld_dw, mean, nullptr, a.dw, p.dw_cols);
+  if (a.db && m.dw_sums) f.db = join_of(floats(p.db), m.row_blocks, 1, a.classes, m.part_db, mean, nullptr, a.db, a.classes);
   return finish<sizeof(T) == 2>(f, a, m.loss_rows, s);
 }
 
@@ -1575,7 +1590,7 @@ hipError_t run(const LinearLossArgs& a, hipStream_t s) {
   g.loss_rows = floats(p.loss_rows);
   g.g = p.grad ? reinterpret_cast<uint16_t*>(at(p.g)) : nullptr;
   g.ldg = p.piece * p.es;
-  g.ld_db = p.pad_classes;
+  g.ld_db = p.piece;
   if (!p.both) {
     launch_logits<TYPE, kStats>(g, p.tile, s);
     if (!p.grad) {
@@ -1585,72 +1600,78 @@ hipError_t run(const LinearLossArgs& a, hipStream_t s) {
     }
   }
   const float mean = static_cast<float>((kLo ? 1.0 : 1.0 / kGradScale) / static_cast<double>(a.rows));
+  const float mean_db = static_cast<float>(1.0 / static_cast<double>(a.rows));
   const int64_t ld_dx = round_up(a.d, 4);
+  const float* w_inverse = kLo ? nullptr : inverses + 1;
+  FinishArgs f{};
   for (int64_t c0 = 0; c0 < a.classes && (p.grad || p.both); c0 += p.piece) {
     const int64_t left = a.classes - c0, have = left < p.piece ? left : p.piece;
     g.c0 = static_cast<int>(c0);
     // (so G's padding is written as far as a stage of dx's product reads)
     g.m_tiles = static_cast<int>(tiles_of(have, p.tile));
     g.chunks = p.piece_chunks < g.m_tiles ? p.piece_chunks : g.m_tiles;
-    g.db = a.db ? floats(p.db) + c0 : nullptr;
+    g.db = a.db ? floats(p.db) : nullptr;
     if (p.both) launch_logits<TYPE, kBoth>(g, p.tile, s);
     else launch_logits<TYPE, kGrad>(g, p.tile, s);
     g.loss_rows = nullptr;
-    if (!a.dx && !a.dw) continue;
-    const T16Side grad{g.g, g.ldg, round_up(a.rows, p.tile), static_cast<int>(p.piece), 0};
-    const int tile = p.product_tile;
-    Product dx{}, dw{};
-    if (a.dx) {
-      dx.a = w;
-      dx.a.data = w.data + c0 * w.ld;
-      dx.a.rows = left;
-      dx.b = grad;
-      dx.m = a.d;
-      dx.n = a.rows;
-      dx.m_tiles = static_cast<int>(tiles_of(a.d, tile));
-      dx.n_tiles = static_cast<int>(tiles_of(a.rows, tile));
-      dx.splits = p.dx_splits;
-      dx.k = have;
-      dx.factor = mean;
-      dx.inverse = kLo ? nullptr : inverses + 1;
-      dx.out = p.dx_slab ? nullptr : a.dx;
-      dx.ld = a.d;
-      dx.slab = floats(p.dx_sums);
-      dx.ld_slab = ld_dx;
-      dx.more = c0 > 0;
+    if (a.db) f.db = join_of(floats(p.db), g.n_tiles, 1, have, p.piece, mean_db, nullptr, a.db + c0, have);
+    if (a.dx || a.dw) {
+      const T16Side grad{g.g, g.ldg, round_up(a.rows, p.tile), static_cast<int>(p.piece), 0};
+      const int tile = p.product_tile;
+      Product dx{}, dw{};
+      if (a.dx) {
+        dx.a = w;
+        dx.a.data = w.data + c0 * w.ld;
+        dx.a.rows = left;
+        dx.b = grad;
+        dx.m = a.d;
+        dx.n = a.rows;
+        dx.m_tiles = static_cast<int>(tiles_of(a.d, tile));
+        dx.n_tiles = static_cast<int>(tiles_of(a.rows, tile));
+        dx.splits = p.dx_splits;
+        dx.k = have;
+        dx.factor = mean;
+        dx.inverse = w_inverse;
+        dx.out = p.dx_slab ? nullptr : a.dx;
+        dx.ld = a.d;
+        dx.slab = floats(p.dx_sums);
+        dx.ld_slab = ld_dx;
+        dx.more = c0 > 0;
+      }
+      if (a.dw) {
+        T* out = static_cast<T*>(a.dw) + (a.turned ? c0 : c0 * a.d);
+        dw.a = a.turned ? grad : x_by_all;
+        dw.b = a.turned ? x_by_all : grad;
+        dw.a.rows = dw.b.rows = grad.rows;
+        dw.m = a.turned ? have : a.d;
+        dw.n = a.turned ? a.d : have;
+        dw.m_tiles = static_cast<int>(tiles_of(dw.m, tile));
+        dw.n_tiles = static_cast<int>(tiles_of(dw.n, tile));
+        dw.splits = p.dw_splits;
+        dw.k = a.rows;
+        dw.factor = mean;
+        dw.inverse = kLo ? nullptr : inverses;
+        dw.ld = a.turned ? a.classes : a.d;
+        dw.ld_slab = p.ld_dw;
+        dw.part = dw.n * dw.ld_slab;
+        if (p.dw_splits > 1) {
+          dw.slab = floats(p.dw_sums);
+          f.dw = join_of(dw.slab, p.dw_splits, dw.n, dw.m, p.ld_dw, mean, dw.inverse, out, dw.ld);
+        } else {
+          dw.out = out;
+        }
+      }
+      dx.part = dx.n * dx.ld_slab;
+      const int64_t tiles = round_up(product_tiles(dx), 8) + round_up(product_tiles(dw), 8);
+      if (tile == kLarge) hipLaunchKernelGGL((k_products<TYPE, kLarge, kLarge, 2, 4>), dim3(grid8(tiles)), dim3(512), 0, s, dx, dw);
+      else hipLaunchKernelGGL((k_products<TYPE, kSmall, kSmall, 2, 2>), dim3(grid8(tiles)), dim3(256), 0, s, dx, dw);
     }
-    if (a.dw) {
-      const int64_t skip = a.turned ? c0 : c0 * a.d;
-      dw.a = a.turned ? grad : x_by_all;
-      dw.b = a.turned ? x_by_all : grad;
-      dw.a.rows = dw.b.rows = grad.rows;
-      dw.m = a.turned ? have : a.d;
-      dw.n = a.turned ? a.d : have;
-      dw.m_tiles = static_cast<int>(tiles_of(dw.m, tile));
-      dw.n_tiles = static_cast<int>(tiles_of(dw.n, tile));
-      dw.splits = p.dw_splits;
-      dw.k = a.rows;
-      dw.factor = mean;
-      dw.inverse = kLo ? nullptr : inverses;
-      dw.out = p.dw_splits > 1 ? nullptr : static_cast<T*>(a.dw) + skip;
-      dw.ld = p.dw_cols;
-      dw.slab = floats(p.dw_sums) + (a.turned ? c0 : c0 * p.ld_dw);
-      dw.ld_slab = p.ld_dw;
-      dw.part = p.dw_rows * p.ld_dw;
+    if (c0 + p.piece < a.classes && f.dw.blocks + f.db.blocks > 0) {
+      hipLaunchKernelGGL(k_join_piece<kLo>, dim3(static_cast<unsigned>(f.dw.blocks + f.db.blocks)), dim3(256), 0, s, f.dw, f.db);
+      f.dw = f.db = JoinArgs{};
     }
-    dx.part = dx.n * dx.ld_slab;
-    const int64_t tiles = round_up(product_tiles(dx), 8) + round_up(product_tiles(dw), 8);
-    if (tile == kLarge) hipLaunchKernelGGL((k_products<TYPE, kLarge, kLarge, 2, 4>), dim3(grid8(tiles)), dim3(512), 0, s, dx, dw);
-    else hipLaunchKernelGGL((k_products<TYPE, kSmall, kSmall, 2, 2>), dim3(grid8(tiles)), dim3(256), 0, s, dx, dw);
   }
-  FinishArgs f{};
-  const float* w_inverse = kLo ? nullptr : inverses + 1;
-  if (a.dx && p.dx_slab) f.dx = join_of(floats(p.dx_sums), p.dx_splits, a.rows, a.d, ld_dx, mean, w_inverse, a.dx);
-  if (a.dw && p.dw_splits > 1)
-    f.dw = join_of(floats(p.dw_sums), p.dw_splits, p.dw_rows, p.dw_cols, p.ld_dw, mean, inverses, a.dw);
-  if (a.db)
-    f.db = join_of(floats(p.db), g.n_tiles, 1, a.classes, p.pad_classes,
-                   static_cast<float>(1.0 / static_cast<double>(a.rows)), nullptr, a.db);
+  if (a.dx && p.dx_slab) f.dx = join_of(floats(p.dx_sums), p.dx_splits, a.rows, a.d, ld_dx, mean, w_inverse, a.dx, a.d);
   return finish<kLo>(f, a, floats(p.loss_rows), s);
 }
 
