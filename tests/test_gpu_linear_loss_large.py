@@ -23,9 +23,11 @@ if not torch.cuda.is_available():
     pytest.skip("no GPU on this machine", allow_module_level=True)
 
 import paper_2010_05337_amd as gmb  # noqa: E402
+from test_gpu_linear_loss import check, problem  # noqa: E402
 
 U = 2.0 ** -24
 TYPES = [torch.float32, torch.bfloat16]
+GUARD = 4096
 
 
 # tiles of 256 x 256 in one chunk of the classes a row; W as it lies, in 256 chunks
@@ -56,3 +58,75 @@ def test_long_sums_of_equal_exponentials(rows, d, classes, most, dtype):
     assert err <= tol, ("dbias", err / p, tol / p)
     err = abs(float(g.bias[0].double()) - (math.exp(top) / total - int((y == 0).sum()) / rows))
     assert err <= tol / p * math.exp(top) / total + 64 * U, ("dbias of the largest", err)
+
+
+def guarded(bytes_, dtype, shape):
+    """Memory of exactly that size, and the bytes behind it."""
+    raw = torch.full((bytes_ + GUARD,), 0x5A, dtype=torch.uint8, device="cuda")
+    assert raw.data_ptr() % 256 == 0
+    return raw[:bytes_].view(dtype).view(shape), raw[bytes_:]
+
+
+def through_the_abi(x, w, y, b, turned, names="xwb"):
+    """(loss, LinearGrads) with a workspace of exactly the bytes asked for; nothing behind it or the results is written."""
+    (n, d), classes, code = x.shape, w.shape[0], gmb._dtype_code(x.dtype)
+    es = x.element_size()
+    dx, gx = guarded(n * d * es, x.dtype, (n, d)) if "x" in names else (None, None)
+    dw, gw = guarded(classes * d * es, x.dtype, (d, classes) if turned else (classes, d)) if "w" in names else (None, None)
+    db, gb = guarded(classes * 4, torch.float32, (classes,)) if "b" in names and b is not None else (None, None)
+    loss, gl = guarded(4, torch.float32, (1,))
+    head = gmb.LinearHeadStruct(x.data_ptr(), x.stride(0), w.data_ptr(), *w.stride(), None if b is None else b.data_ptr(),
+                                y.data_ptr(), n, d, classes, code, 0)
+    grads = gmb.LinearGradsStruct(*[None if t is None else t.data_ptr() for t in (dx, dw, db)], int(turned), 0)
+    need = gmb.lib().gmb_linear_loss_workspace_bytes(head, grads)
+    ws, gs = guarded(need, torch.uint8, (need,))
+    assert gmb.lib().gmb_linear_loss(head, grads, loss.data_ptr(), ws.data_ptr(), need, gmb._stream_handle()) == 0
+    for name, guard in (("dx", gx), ("dw", gw), ("dbias", gb), ("loss", gl), ("workspace", gs)):
+        assert guard is None or bool((guard == 0x5A).all()), name
+    return loss, gmb.LinearGrads(dx, dw.t() if turned and dw is not None else dw, db)
+
+
+# small heads, one tile, few rows over many classes, tiles of 64 and 256, sums that are split; and pieces of the classes
+SIZES = [(1, 1, 1), (300, 65, 47), (1000, 256, 47), (5, 100, 20_001), (16, 100, 30_001), (129, 128, 257), (1500, 48, 172),
+         (784, 63, 4133), (2100, 64, 5001), (9000, 24, 30_001), (5000, 64, 50_003)]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("size", SIZES, ids=str)
+def test_nothing_is_written_behind_the_workspace_and_the_results(size, dtype):
+    x, w, y, b = problem(*size, dtype, 31)
+    for turned in (False, True):
+        loss, g = through_the_abi(x, w, y, b, turned)
+        want, h = gmb.linear_loss(x, w, y, bias=b)
+        assert torch.equal(loss, want) and torch.equal(g.x, h.x) and torch.equal(g.bias, h.bias)
+        if not turned:
+            check(x, w, y, b, loss, g)
+            assert torch.equal(g.w, h.w)
+        else:                                      # (the product's other operand order: the same sums)
+            check(x, w, y, b, loss, g)
+
+
+@pytest.mark.parametrize("d", [64, 192])
+@pytest.mark.parametrize("bias", [False, True])
+def test_pieces_of_weights_read_as_they_lie(d, bias):
+    """bf16 rows of whole stages, at a stride past them, the classes in several pieces and the last one ragged."""
+    n, classes = 9000, 30_001
+    x, w, y, b = problem(n, d, classes, torch.bfloat16, 32, bias)
+    wide = torch.full((classes, d + 64), float("nan"), device="cuda", dtype=torch.bfloat16)
+    wide[:, :d] = w
+    view = wide[:, :d]
+    for turned in (False, True):
+        loss, g = through_the_abi(x, view, y, b, turned)
+        check(x, w, y, b, loss, g)
+        want, h = gmb.linear_loss(x, w, y, bias=b)
+        assert torch.equal(loss, want) and torch.equal(g.x, h.x)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("names", ["w", "b", "x", "wb"])
+def test_some_gradients_of_pieces(names, dtype):
+    x, w, y, b = problem(9000, 24, 30_001, dtype, 33)
+    want, h = gmb.linear_loss(x, w, y, bias=b)
+    loss, g = through_the_abi(x, w, y, b, False, names)
+    assert torch.equal(loss, want)
+    check(x, w, y, b, loss, g)
