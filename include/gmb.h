@@ -746,7 +746,10 @@ int gmb_linear_loss(const gmb_linear_head* head, const gmb_linear_grads* grads, 
 /* gmb_sage_forward (feats NULL), or gmb_sage_forward_fused (feats the table, x
  * its x_dst), with `drop` on every hidden output: layer l < L-1's rows, after
  * the ReLU, are dropped out in place with layer drop->layer + l, keyed by their
- * vertices.  (Without it: evaluation.) */
+ * vertices.  (Without it: evaluation.)  Its backward is gmb_sage_backward_from
+ * with the same `drop`: the workspace does not say that its rows were dropped out,
+ * and gmb_sage_backward, _embedding and _distill, which take no dropout, would
+ * leave out its factor in the layers below. */
 int gmb_sage_forward_dropout(const gmb_blocks* blocks, void* x, const void* feats, int64_t num_nodes,
                              const gmb_sage_weights* weights, const gmb_dropout* drop, float* logits, void* ws,
                              size_t ws_bytes, uint32_t* status, void* stream);

@@ -490,19 +490,40 @@ def forward_workspace_bytes(blocks: Blocks, weights: SageWeights) -> int:
     return lib().gmb_forward_workspace_bytes(ctypes.byref(blocks.struct), ctypes.byref(weights.struct))
 
 
-def _with_forward_workspace(call, blocks: Blocks, weights: SageWeights, workspace, device):
+def _with_forward_workspace(call, blocks: Blocks, weights: SageWeights, workspace, device, drop):
     """call(workspace), or, where none is given or the call refuses it as too
     small (before anything is enqueued), call on one allocated here; returns
-    (status, the workspace used)."""
+    (status, the workspace used).  The workspace keeps what the forward dropped
+    out with, for _check_dropped."""
+    code = ENOSPC
     if workspace is not None and workspace.numel() > 0 and workspace.data_ptr() % 256 == 0:
         code = call(workspace)
-        if code != ENOSPC:
-            return code, workspace
-    need = forward_workspace_bytes(blocks, weights)
-    if need == 0:
-        _check(-1)
-    _, workspace = _aligned_bytes(need, device)
-    return call(workspace), workspace
+    if code == ENOSPC:
+        need = forward_workspace_bytes(blocks, weights)
+        if need == 0:
+            _check(-1)
+        _, workspace = _aligned_bytes(need, device)
+        code = call(workspace)
+    if code == 0:
+        workspace.dropped = _dropped(drop)
+    return code, workspace
+
+
+def _dropped(drop) -> int:
+    """What of 65536 elements a dropout (or None) drops, as the kernels round it."""
+    return 0 if drop is None else int(65536.0 * drop.p + 0.5)
+
+
+def _check_dropped(blocks: Blocks, fwd_workspace: torch.Tensor, drop):
+    """A backward takes the probability that the forward dropped out with: without
+    it the layers below a dropout would lack its factor.  (Known where the tensor
+    is the one that the last forward was given; a copy or another view of its
+    memory does not say.)"""
+    want = _dropped(drop)
+    had = getattr(fwd_workspace, "dropped", want)
+    if had != want and blocks.num_layers > 1:
+        raise ValueError(f"fwd_workspace is of a forward with dropout p={had / 65536:g}, the backward is asked for with"
+                         f" p={want / 65536:g} (sage_backward_from takes the forward's dropout)")
 
 
 def sage_forward(blocks: Blocks, feats: torch.Tensor, weights: SageWeights,
@@ -532,7 +553,7 @@ def sage_forward(blocks: Blocks, feats: torch.Tensor, weights: SageWeights,
         return L.gmb_sage_forward(ctypes.byref(blocks.struct), feats.data_ptr(), ctypes.byref(weights.struct),
                                   logits.data_ptr(), ws.data_ptr(), ws.numel(), stream)
 
-    code, workspace = _with_forward_workspace(call, blocks, weights, workspace, feats.device)
+    code, workspace = _with_forward_workspace(call, blocks, weights, workspace, feats.device, drop)
     _check(code)
     if not return_hidden:
         return logits
@@ -592,7 +613,7 @@ def sage_forward_fused(blocks: Blocks, feats: torch.Tensor, weights: SageWeights
                                         x_dst.data_ptr(), ctypes.byref(weights.struct), logits.data_ptr(),
                                         ws.data_ptr(), ws.numel(), status, stream)
 
-    code, workspace = _with_forward_workspace(call, blocks, weights, workspace, feats.device)
+    code, workspace = _with_forward_workspace(call, blocks, weights, workspace, feats.device, drop)
     _check(code)
     if not return_hidden:
         return logits, x_dst
@@ -637,7 +658,10 @@ def sage_backward(blocks: Blocks, feats: torch.Tensor, weights: SageWeights, log
     float32 device tensor.  With `embedding` (the fp32 [num_nodes, dims[0]]
     table the layer-0 inputs were taken from) the gradient in the input
     rows is applied to the table as an SGD step of size emb_lr.  A NaN loss
-    may also mean that a bounded wait on the device ran out (gmb.h)."""
+    may also mean that a bounded wait on the device ran out (gmb.h).  A forward
+    with dropout is refused: its backward is sage_backward_from, which takes the
+    dropout (distill_loss gives the gradient at the outputs)."""
+    _check_dropped(blocks, fwd_workspace, None)
     if labels is not None or teacher is None:
         _require_cuda(labels, "labels")
         if labels.dtype != torch.int32 or labels.numel() < blocks.num_seeds:
@@ -685,8 +709,8 @@ def sage_backward_from(blocks: Blocks, feats: torch.Tensor, weights: SageWeights
                        emb_lr: float = 0.0, dropout: "Dropout | None" = None) -> SageGrads:
     """The backward of sage_forward (or its fused form) from the gradient at
     the model's outputs, float32 [num_seeds, C]: of a loss of your own or of
-    layers behind the model.  `dropout` is the forward's; the others are
-    sage_backward's."""
+    layers behind the model.  `dropout` is the forward's (another probability
+    than the forward's is refused); the others are sage_backward's."""
     dev = _current_device(d_logits, "d_logits")
     if d_logits.dtype is not torch.float32 or d_logits.dim() != 2 or not d_logits.is_contiguous() \
             or d_logits.shape[0] < blocks.num_seeds or d_logits.shape[1] != weights.dims[-1]:
@@ -704,13 +728,14 @@ def sage_backward_from(blocks: Blocks, feats: torch.Tensor, weights: SageWeights
         need = backward_workspace_bytes(blocks, weights)
     if need == 0:
         _check(-1)
+    drop = None if dropout is None else _drop_struct(dropout, dev)
+    _check_dropped(blocks, fwd_workspace, drop)
     if workspace is None or workspace.numel() < need or workspace.data_ptr() % 256:
         _, workspace = _aligned_bytes(need, feats.device)
     if grads is None:
         grads = SageGrads(weights)
     _check(lib().gmb_sage_backward_from(ctypes.byref(blocks.struct), feats.data_ptr(), ctypes.byref(weights.struct),
-                                        d_logits.data_ptr() or feats.data_ptr(),
-                                        None if dropout is None else _drop_struct(dropout, dev), fwd_workspace.data_ptr(),
+                                        d_logits.data_ptr() or feats.data_ptr(), drop, fwd_workspace.data_ptr(),
                                         fwd_workspace.numel(), ctypes.byref(grads.struct), workspace.data_ptr(),
                                         workspace.numel(), *table, _stream_handle()))
     return grads
