@@ -686,7 +686,9 @@ int gmb_rms_norm_backward(const gmb_rows* dy, const gmb_rows* r, const gmb_rows*
  *   w       device, element j of class c at c * w_row_stride + j *
  *           w_col_stride elements of `dtype` (strides >= 0): rows [classes][d],
  *           or the columns of a [d][classes] matrix
- *   bias    device fp32 [classes] or NULL (-inf: a class that cannot be)
+ *   bias    device fp32 [classes] or NULL (-inf: a class that cannot be; so is one
+ *           below -2.35e38, as logits are held times log2(e): a mask of the type's
+ *           lowest value is one of -inf)
  *   labels  device int32 [rows]; a row whose label is outside [0, classes)
  *           has no loss and no gradient, whatever x holds there
  *   rows 0 .. 2^22, d 1 .. 65536, classes 1 .. 2^27 */

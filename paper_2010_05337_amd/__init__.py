@@ -1375,7 +1375,8 @@ def linear_loss(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, bias: to
     counts as 0), and its gradients, without the logits ever being stored.  x
     is float32 or bfloat16 [rows, d] with contiguous rows, w [classes, d] of the
     same dtype with any non-negative strides: an embedding table, or matrix.t()
-    of a [d, classes] matrix; bias float32 [classes].  Returns (loss,
+    of a [d, classes] matrix; bias float32 [classes] (-inf or the type's lowest
+    value: a class that cannot be).  Returns (loss,
     LinearGrads): the loss float32 of one element, the gradients of x and w of
     their dtype (w's laid out like w), the bias's float32.  `grad` is True,
     False, or the names of the gradients wanted ("x", "w", "bias")."""

@@ -130,3 +130,18 @@ def test_some_gradients_of_pieces(names, dtype):
     loss, g = through_the_abi(x, w, y, b, False, names)
     assert torch.equal(loss, want)
     check(x, w, y, b, loss, g)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("size", [(60, 40, 200), (5, 100, 20_001), (60, 140, 1000), (2100, 64, 5000)], ids=str)
+def test_a_mask_of_the_lowest_value_is_one_of_infinities(size, dtype):
+    n, d, classes = size
+    x, w, y, b = problem(n, d, classes, dtype, 34, none=0.0)
+    lowest = torch.finfo(torch.float32).min
+    for off, label in ((slice(0, None, 2), 1), (slice(0, None, 2), 0), (slice(0, None), 1)):   # (other classes, the labels too, all)
+        y = torch.randint(0, classes // 2, (n,), device="cuda", dtype=torch.int32) * 2 + label
+        never, low = b.clone(), b.clone()
+        never[off], low[off] = -math.inf, lowest
+        want, h = gmb.linear_loss(x, w, y, bias=never)
+        loss, g = gmb.linear_loss(x, w, y, bias=low)
+        assert torch.equal(loss, want) and all(torch.equal(p, q) for p, q in zip(g, h))
