@@ -334,10 +334,16 @@ __device__ __forceinline__ void join_stats(float& top, SUM& sum, float t, float 
   sum = sum * static_cast<SUM>(exp2_fast(top - base)) + static_cast<SUM>(s) * static_cast<SUM>(exp2_fast(t - base));
   top = m;
 }
-__device__ __forceinline__ float row_lse(float top, float sum) { return top + log2f(sum); }
 // Every logit is -inf (a sum that is no number has a NaN among them).
 __device__ __forceinline__ bool row_empty(float top, float sum) { return top == -INFINITY && sum == 0.f; }
 constexpr float kLn2 = 0.6931471805599453f;
+// A row's loss and probabilities go by the distance to its maximum, 2^(u - top) /
+// sum, not to the logarithm of its sum: top + log2(sum) in 32 bits has lost what the
+// sum says where logits are far from 0 (equal ones at 1e5: probabilities 0.3% off, at
+// 1e9 all 1).
+__device__ __forceinline__ float row_loss(float top, float sum, float of_label) {
+  return ((top - of_label) + log2f(sum)) * kLn2;
+}
 
 // kStats: a row's statistics over a chunk of the classes.  kGrad: G of the
 // classes' piece, from the statistics of all chunks.  kBoth: at most TM classes:
@@ -354,7 +360,7 @@ constexpr int logits_stages(int tm) { return tm > 64 ? 2 : 4; }
 template <int TM, int TN, int WM, int WN>
 struct LogitsLds {
   static constexpr int kStages = logits_stages(TM) * t16_stage_bytes<TM, TN, 64>();
-  static constexpr int kRows = kStages;                        // [2][WM][TN]: statistics; lse, label; [TN]: its logit
+  static constexpr int kRows = kStages;                        // [2][WM][TN]: statistics; maximum, 1 / sum; [TN]: label's logit
   static constexpr int kClasses = kRows + (2 * WM + 1) * TN * 4;   // [WN][TM]: sums of G
   static constexpr int kBytes = kClasses + WN * TM * 4;
 };
@@ -425,7 +431,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
     if constexpr (TYPE == kSplit) scale[j] *= p.row_inverse[row0 + 16 * j] * *p.w_inverse;
     label[j] = p.labels[row0 + 16 * j];
   }
-  float lse[CT];
+  float base[CT], over[CT];         // G: 2^(u - base) over - onehot
   if constexpr (MODE == kGrad) {
     constexpr int PARTS = THREADS / TN > 0 ? THREADS / TN : 1;
     static_assert(PARTS * TN <= THREADS || PARTS == 1, "");
@@ -447,19 +453,19 @@ __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
       float top = part[2 * row], sum = part[2 * row + 1];
 #pragma unroll
       for (int w = 1; w < PARTS; ++w) join_stats(top, sum, part[2 * (w * TN + row)], part[2 * (w * TN + row) + 1]);
-      const float l = row_lse(top, sum);
       const bool on = p.labels[tile_row + row] >= 0 && !row_empty(top, sum);
-      row_a[row] = l;
-      row_b[row] = on ? 1.f : 0.f;
+      row_a[row] = top;
+      row_b[row] = on ? 1.f / sum : 0.f;
       if (p.loss_rows && chunk == 0 && tile_row + row < p.rows)
-        p.loss_rows[tile_row + row] = on ? (l - p.label_logit[tile_row + row]) * kLn2 : 0.f;
+        p.loss_rows[tile_row + row] = on ? row_loss(top, sum, p.label_logit[tile_row + row]) : 0.f;
     }
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < CT; ++j) {
       const int q = 16 * (CT * wn + j) + r;
-      lse[j] = row_b[q] == 0.f ? INFINITY : row_a[q];   // (G is 0 there)
-      if (row_b[q] == 0.f) label[j] = -1;
+      over[j] = row_b[q];
+      base[j] = over[j] == 0.f ? INFINITY : row_a[q];   // (G is 0 there)
+      if (over[j] == 0.f) label[j] = -1;
     }
   }
   float top[CT];
@@ -522,13 +528,13 @@ __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) most = fmaxf(most, acc[i][j][e]);
         most = fmaxf(top[j], most * by[j]);
-        const float base = most == -INFINITY ? 0.f : most;
+        const float from = most == -INFINITY ? 0.f : most;
         float s = 0.f;
 #pragma unroll
         for (int i = 0; i < RT; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s += exp2_fast(fmaf(acc[i][j][e], by[j], -base));
-        long_sum[j] = long_sum[j] * static_cast<double>(exp2_fast(top[j] - base)) + static_cast<double>(s);
+          for (int e = 0; e < 4; ++e) s += exp2_fast(fmaf(acc[i][j][e], by[j], -from));
+        long_sum[j] = long_sum[j] * static_cast<double>(exp2_fast(top[j] - from)) + static_cast<double>(s);
         top[j] = most;
         // the label's logit, where it is one of this lane's
         const int y = label[j] - c0;
@@ -562,12 +568,11 @@ __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
         float m = row_a[q], s = row_b[q];
 #pragma unroll
         for (int w = 1; w < WM; ++w) join_stats(m, s, row_a[w * TN + q], row_b[w * TN + q]);
-        lse[j] = row_lse(m, s);
         if (row_empty(m, s)) label[j] = -1;
-        const float of_label = lse[j];
-        if (label[j] < 0) lse[j] = INFINITY;              // (G is 0 there)
+        base[j] = label[j] < 0 ? INFINITY : m;            // (G is 0 there)
+        over[j] = label[j] < 0 ? 0.f : 1.f / s;
         if (wm == 0 && g == 0 && row0 + 16 * j < p.rows)
-          p.loss_rows[row0 + 16 * j] = label[j] >= 0 ? (of_label - row_label[q]) * kLn2 : 0.f;
+          p.loss_rows[row0 + 16 * j] = label[j] >= 0 ? row_loss(m, s, row_label[q]) : 0.f;
       }
       if (!p.g) return;
     }
@@ -581,7 +586,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
           float v[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            v[e] = exp2_fast(fmaf(acc[i + e / 4][j][e % 4], by[j], -lse[j]));
+            v[e] = exp2_fast(fmaf(acc[i + e / 4][j][e % 4], by[j], -base[j])) * over[j];
           }
           const int y = label[j] - c0 - 16 * i;
           if (y >= 0 && y < 8) {
@@ -659,7 +664,7 @@ __global__ __launch_bounds__(256) void k_join_rows(const float2* stats, int chun
   if (part || row >= rows) return;
 #pragma unroll
   for (int w = 1; w < PARTS; ++w) join_stats(top, sum, lds[w][q].x, lds[w][q].y);
-  loss_rows[row] = has_label(labels, row, classes) && !row_empty(top, sum) ? (row_lse(top, sum) - label_logit[row]) * kLn2 : 0.f;
+  loss_rows[row] = has_label(labels, row, classes) && !row_empty(top, sum) ? row_loss(top, sum, label_logit[row]) : 0.f;
 }
 
 // ---- products -------------------------------------------------------------
@@ -1029,7 +1034,7 @@ __global__ __launch_bounds__(kStreamThreads) void k_stream_head(StreamArgs p) {
     of_x.store(lx, sd, v);
   }
   const int y = row_y[r];
-  float top = -INFINITY, sum = 0.f, lse = 0.f;
+  float top = -INFINITY, sum = 0.f, over = 0.f;
   double long_sum = 0.0;
   bool on = y >= 0;
   if constexpr (MODE == kGrad) {
@@ -1047,10 +1052,10 @@ __global__ __launch_bounds__(kStreamThreads) void k_stream_head(StreamArgs p) {
     top = row_top[0][r];
     sum = row_sum[0][r];
     for (int v = 1; v < 16; ++v) join_stats(top, sum, row_top[v][r], row_sum[v][r]);
-    lse = row_lse(top, sum);
+    over = 1.f / sum;
     on = on && !row_empty(top, sum);
     if (chunk == 0 && wave == 0 && g == 0 && r < rows)
-      p.loss_rows[row0 + r] = on ? (lse - p.label_logit[row0 + r]) * kLn2 : 0.f;
+      p.loss_rows[row0 + r] = on ? row_loss(top, sum, p.label_logit[row0 + r]) : 0.f;
   }
   t16_f32x4 dx[4];                                       // d tiles wave, wave + 16, ...
 #pragma unroll
@@ -1107,9 +1112,9 @@ __global__ __launch_bounds__(kStreamThreads) void k_stream_head(StreamArgs p) {
       top = row_top[0][r];
       sum = row_sum[0][r];
       for (int v = 1; v < ct; ++v) join_stats(top, sum, row_top[v][r], row_sum[v][r]);
-      lse = row_lse(top, sum);
+      over = 1.f / sum;
       on = on && !row_empty(top, sum);
-      if (wave == 0 && g == 0 && r < rows) p.loss_rows[row0 + r] = on ? (lse - row_label[r]) * kLn2 : 0.f;
+      if (wave == 0 && g == 0 && r < rows) p.loss_rows[row0 + r] = on ? row_loss(top, sum, row_label[r]) : 0.f;
       if (!p.grad) return;
     }
     if constexpr (MODE != kStats) {
@@ -1117,7 +1122,7 @@ __global__ __launch_bounds__(kStreamThreads) void k_stream_head(StreamArgs p) {
         t16_f32x4 v;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float q = exp2_fast(acc[e] - lse);
+          const float q = exp2_fast(acc[e] - top) * over;
           v[e] = on ? (c_tile + c0 + e == y ? q - 1.f : q) : 0.f;
         }
         *reinterpret_cast<t16_f32x4*>(lg + r * sc + c0) = v;

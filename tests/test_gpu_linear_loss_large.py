@@ -145,3 +145,29 @@ def test_a_mask_of_the_lowest_value_is_one_of_infinities(size, dtype):
         want, h = gmb.linear_loss(x, w, y, bias=never)
         loss, g = gmb.linear_loss(x, w, y, bias=low)
         assert torch.equal(loss, want) and all(torch.equal(p, q) for p, q in zip(g, h))
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("size", [(60, 40, 20), (60, 40, 200), (5, 100, 20_001), (60, 140, 1000), (2100, 64, 5000)], ids=str)
+def test_logits_far_from_zero(size, dtype):
+    """Equal logits of any size: uniform probabilities (the bounds above; here arguments are 0)."""
+    n, d, classes = size
+    gen = torch.Generator(device="cuda").manual_seed(35)
+    x = torch.randn(n, d, device="cuda", generator=gen).to(dtype)
+    w = torch.zeros(classes, d, device="cuda", dtype=dtype)
+    w += (0.1 * torch.randn(d, device="cuda", generator=gen)).to(dtype)
+    y = (torch.arange(n, device="cuda") % 5).int()
+    count = torch.bincount(y.long(), minlength=classes).double() / n
+    for at in (1e5, -1e5, 1e9, -1e9, -1e30, 3e37, -2e38):
+        b = torch.full((classes,), at, device="cuda")
+        alone, _ = gmb.linear_loss(x, w, y, bias=b, grad=False)
+        loss, g = gmb.linear_loss(x, w, y, bias=b)
+        assert torch.equal(alone, loss)
+        err = abs(float(loss.double()) - math.log(classes))
+        assert err <= 283 * U, (at, "loss", err)
+        err = float((g.bias.double() - (1 / classes - count)).abs().max())
+        assert err <= 464 * U / classes + 64 * U * float(count.max()), (at, "dbias", err)
+        # softmax - onehot times equal rows: nothing but its roundings, those of the entries (bf16: 2^-8 of each, their
+        # magnitudes add up to 2) and of the sum of three part products a class, each addition a half-step of at most 2
+        entry = 2 / n * ((2.0 ** -8 if dtype is torch.bfloat16 else 2.0 ** -20) + 3 * (classes + 8) * U)
+        assert float(g.x.abs().max()) <= entry * float(w[0].abs().max()), (at, "dx", float(g.x.abs().max()))
