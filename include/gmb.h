@@ -667,7 +667,8 @@ size_t gmb_rms_norm_workspace_bytes(int64_t n_cap, int32_t dim);
  * with s = 1 / sqrt(mean(r^2) + eps),
  *   dr = carry + s (weight dy - r s^2 mean(weight dy r)),
  * the gradient of the residual; that of x is dropout(dr); that of the weight
- * the sum over the rows of dy r s, in a fixed order (no atomics).
+ * the sum over the rows of dy r s, in a fixed order (no atomics).  A row that
+ * normed to 0 (see eps) passes the carry alone.
  *   dy, r        the gradient of y, and the sum (x itself if nothing was added)
  *   carry        the gradient that reaches r from elsewhere, or NULL
  *   d_residual   rows or NULL; may be dy, r or carry

@@ -429,7 +429,9 @@ __global__ __launch_bounds__(NormBlock<LANES>::kThreads) void k_rms_norm_back(No
     }
     row_sum<LANES>(s, lds);
     const float inv = inverse_root(fmaf(s[0], by, p.eps));
-    const float along = s[1] * by * inv * inv;
+    // (squares past fp32's range: the row norms to 0 and nothing comes back through
+    // it, however large the other sum is; a NaN stays one through inv)
+    const float along = inv > 0.f ? s[1] * by * inv * inv : 0.f;
     const uint32_t key = in && p.drop.below ? row_key(p.drop, row) : 0u;
 #pragma unroll
     for (int k = 0; k < OC; ++k) {
