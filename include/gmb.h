@@ -730,8 +730,10 @@ size_t gmb_linear_loss_workspace_bytes(const gmb_linear_head* head, const gmb_li
 /* The mean over the rows (those without a label count as 0) of -log
  * softmax(z)_label, and its gradients.  A row whose logits are all -inf has
  * neither.  x and W are finite; with a NaN or an infinity among them the loss
- * is NaN, or the row of that x.  bf16: exact products, fp32 sums and statistics,
- * softmax(z) - onehot rounded to bf16 before its products.  fp32: few rows or
+ * is NaN, or the row of that x.  Logits are fp32; a row's sum of exponentials is
+ * 64 bits from tile to tile, its loss and probabilities go by the distance to its
+ * largest logit.  bf16: exact products, fp32 sums, softmax(z) - onehot rounded to
+ * bf16 before its products (not for dbias).  fp32: few rows or
  * classes by fp32 products; else every operand is cut into two fp16 parts at a
  * power-of-two scale (x by rows for the logits; W, and x for dw, as a whole), a
  * product is three of the four part products; the error is of the order of an
@@ -749,10 +751,11 @@ int gmb_linear_loss(const gmb_linear_head* head, const gmb_linear_grads* grads, 
 /* gmb_sage_forward (feats NULL), or gmb_sage_forward_fused (feats the table, x
  * its x_dst), with `drop` on every hidden output: layer l < L-1's rows, after
  * the ReLU, are dropped out in place with layer drop->layer + l, keyed by their
- * vertices.  (Without it: evaluation.)  Its backward is gmb_sage_backward_from
- * with the same `drop`: the workspace does not say that its rows were dropped out,
- * and gmb_sage_backward, _embedding and _distill, which take no dropout, would
- * leave out its factor in the layers below. */
+ * vertices (in a bf16 model the scaled rows are rounded once more).  (Without it:
+ * evaluation.)  Its backward is gmb_sage_backward_from with the same `drop`: the
+ * workspace does not say that its rows were dropped out, and gmb_sage_backward,
+ * _embedding and _distill, which take no dropout, would leave out its factor in
+ * the layers below. */
 int gmb_sage_forward_dropout(const gmb_blocks* blocks, void* x, const void* feats, int64_t num_nodes,
                              const gmb_sage_weights* weights, const gmb_dropout* drop, float* logits, void* ws,
                              size_t ws_bytes, uint32_t* status, void* stream);

@@ -118,7 +118,9 @@ gmb::DropArgs drop_args(const gmb_dropout* d, const int32_t* ids) {
   return a;
 }
 
-// The dropout of layer `layer`'s output, in place, by vertex.
+// The dropout of layer `layer`'s output, in place, by vertex.  (A bf16 model's rows
+// are rounded as the layer stores them and again here, half a step each: the
+// layers' kernels stay without dropout.  At p = 1/2 the factor is 2 and exact.)
 hipError_t drop_hidden(const void* what, int layer, const gmb_block& blk, void* rows, int dim, int bf16,
                        hipStream_t s) {
   gmb::DropoutArgs a{};

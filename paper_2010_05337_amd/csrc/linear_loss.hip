@@ -17,6 +17,11 @@
 // The logits are computed twice (8 n C d operations in all where keeping them
 // would take 6) and never stored; G is, in 16 bits (kSplit: two times 16), for
 // a piece of the classes.  Nothing is added by atomics: the same bits every time.
+// bf16: G is rounded to bf16 (half a step of each entry) so that its products take
+// one matrix instruction; two parts of it would take two, half as much again for
+// the whole call.  What shows is the label's entry, p - 1: dx and dw are 0.0019 of
+// their size from 64 bits where their own rounding to bf16 alone is 0.0017 (0.0010
+// of G's, in quadrature).  dbias adds G up before it is rounded.
 // The figures below are times of kernels; a large product of the library's reaches
 // 1,210 TFLOP/s in bf16 on random values (here the power it may draw is the bound:
 // 8,192 x 1,024 x 32,768 takes it 514 us, with zeros 336).
@@ -371,9 +376,9 @@ struct LogitsLds {
 // instructions (busy 0.49; the library's product takes as long), and where d is
 // short by the exponentials behind every tile's d / 64 stages of them.  bf16,
 // statistics and G:
-// 8,192 x 1,024 x 32,768 500 and 599 us (1,099 and 918 TFLOP/s), 4,000 x 256 x 100,000 249
-// and 368 (824 and 556); fp32 4,000 x 256 x 20,011 125 and 162 (three part products: 987
-// and 759).
+// 8,192 x 1,024 x 32,768 502 and 602 us (1,096 and 912 TFLOP/s), 4,000 x 256 x 100,000 250
+// and 369 (820 and 555); fp32 4,000 x 256 x 20,011 128 and 164 (three part products: 959
+// and 750).
 template <T16Type TYPE, LogitsMode MODE, int TM, int TN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void k_logits(LogitsArgs p) {
   using Tile = T16Tile<TYPE, kByRow, kByRow, TM, TN, WM, WN, logits_stages(TM), 64, true>;
@@ -756,8 +761,8 @@ __device__ __forceinline__ void product_tile(const Product& p, int64_t id, char*
 // dx = G W (A: W by its rows of k, B: G by its rows), then dW = G^T x, its rows
 // those of W (A: x, B: G) or, turned, those of W's transpose (A: G, B: x).  One
 // launch, so that the ends of one fill the other's.  256 x 256: matrix instructions,
-// and G from the last-level cache (loss of 8,192 x 1,024 x 32,768 bf16: 1,008 us, 1,090
-// TFLOP/s; 4,000 x 256 x 100,000 bf16 515, 795; 4,000 x 256 x 20,011 fp32 280, 879 of part
+// and G from the last-level cache (loss of 8,192 x 1,024 x 32,768 bf16: 1,001 us, 1,099
+// TFLOP/s; 4,000 x 256 x 100,000 bf16 509, 805; 4,000 x 256 x 20,011 fp32 279, 880 of part
 // products).  Four waves of 128 x 128 instead of eight, their operands read a stage
 // ahead: 535 us a piece for 531, and the logits' kernels spilled.
 template <T16Type TYPE, int TM, int TN, int WM, int WN>
@@ -890,8 +895,9 @@ __global__ __launch_bounds__(256) void k_finish(FinishArgs p) {
 // form, its loops unrolled, took 22 us for 12.8.
 //   kBoth   all classes are one tile (1,000 x 256 x 47 fp32: 17 us in two launches,
 //           through k_logits and k_products 29 in five)
-//   kStats, kGrad   as in k_logits (5 x 226 x 147,879 fp32: 60 and 114 us for 134 MB read
-//           and 268 read and written)
+//   kStats, kGrad   as in k_logits (5 x 226 x 147,879 fp32: 73 and 128 us traced, the
+//           call 186, for 134 MB read and 268 read and written)
+// 128 registers a thread are few: kBoth spills 17 (and 58 scalar ones), kGrad 9 (47).
 constexpr int kStreamThreads = 1024, kStreamWaves = 16;
 constexpr int kStreamClasses = 256, kStreamCells = 16384, kStreamD = 1024;   // a tile's classes, values; d
 
@@ -1289,12 +1295,12 @@ void plan_products(const LinearLossArgs& a, Plan* p) {
 // Whether k_stream_head takes it, and how (us of the whole call, with it / by
 // k_logits and k_products):
 //   - fp32, sixteen rows at most: its fp32 products (157 TFLOP/s) hide behind
-//     reading W (5 x 226 x 147,879: 178 / 268; 1 x 128 x 5,000: 25 / 30), or a short
+//     reading W (5 x 226 x 147,879: 186 / 268; 1 x 128 x 5,000: 25 / 30), or a short
 //     pass (1,000 x 256 x 47: 20 / 29; 300 x 32 x 2,000: 27 / 29; but 165 x 177 x 1,577,
 //     2^25.7 products: 43 / 34), its sums of dW 64 MB at most;
 //   - bf16, where nothing else need be laid out, only short passes of one tile
 //     (64 x 16 x 8: 20 / 28; but 1,000 x 128 x 172, two tiles: 32 / 28), or few rows
-//     whose W would be copied (16 x 100 x 100,000: 53 / 68; x 256 x 100,000: 101 / 82).
+//     whose W would be copied (16 x 100 x 100,000: 54 / 68; x 256 x 100,000: 101 / 82).
 constexpr int64_t kStreamWork = int64_t{1} << 25, kStreamSums = int64_t{16} << 20;
 
 bool plan_stream(const LinearLossArgs& a, int bf16, Plan* p) {

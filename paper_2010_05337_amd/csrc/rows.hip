@@ -355,8 +355,8 @@ __global__ __launch_bounds__(NormBlock<LANES>::kThreads) void k_rms_norm(NormArg
 
 // With s = 1 / sqrt(mean r^2 + eps): dr = carry + s (g dy - r s^2 mean(g dy r)),
 // and d_weight = the sum over the rows of dy r s: a thread's rows in its
-// registers, the rows of a workgroup in LDS, the workgroups' sums one after
-// the other (k_join_parts): no atomics, the same bits every time.
+// registers, the rows of a workgroup in LDS, the workgroups' sums in 128 chains
+// that meet in a fixed order (k_join_parts): no atomics, the same bits every time.
 // HELD: a row's dy and r, and its carry, stay in registers as they lie in memory,
 // and the next row's are on their way meanwhile (8,192 x 4,096 bf16: 63 us, 78
 // without, when the sums of d_weight took 12.3 of them); else dy, r and g are read
